@@ -382,6 +382,145 @@ enum {
 gmagnus_status_t gmagnus_bandwidth_probe(int32_t kind, void *dst, const void *src, int64_t bytes, int32_t grid,
                                          int32_t reps, void *hip_stream, double *ms);
 
+/* ---------------------------------------------------------------------------
+ * Routed expert products. A layer of experts is a sparse matrix product whose
+ * pattern a router chooses: the routing matrix R (tokens x experts, at most
+ * top_k entries a row, R[t,e] the weight of expert e for token t) says which
+ * rows meet which expert's matrix. These entry points give R from a router's
+ * logits as canonical CSR in both orders (each a matrix the calls above
+ * accept: R^T * R counts the experts used together), the products of the rows
+ * grouped by expert in 16 and in 8 bits, the sum of a token's results, and the
+ * gradients of all but the 8-bit products.
+ *
+ * They run asynchronously on hip_stream, allocate nothing and read nothing
+ * back, so they may be captured into a HIP graph. Device arrays of sizes
+ * (group_ptr, index, slot) are trusted as the routing gives them, but numbers
+ * out of range never lead to an access outside the arrays: an index outside
+ * X reads as a row of zeros, bounds are clamped to the rows there are.
+ * Sums are held in fp32; results are rounded once, to the output's type. */
+typedef enum {
+    GMAGNUS_DATA_FP32 = 0,
+    GMAGNUS_DATA_BF16 = 1,
+    GMAGNUS_DATA_FP16 = 2,
+    GMAGNUS_DATA_FP8_E4M3 = 3 /* OCP E4M3: no infinities, largest finite value 448 */
+} gmagnus_data_type_t;
+
+/* A row-major matrix, or a stack of them (one per group, stack_stride elements
+ * apart), in device memory. Columns are contiguous; row_stride >= n_cols. */
+typedef struct {
+    void *data;
+    int64_t n_rows;
+    int64_t n_cols;
+    int64_t row_stride;   /* elements */
+    int64_t stack_stride; /* elements; read for stacks only */
+    int32_t data_type;    /* gmagnus_data_type_t */
+} gmagnus_dense_t;
+
+/* The arrays of a routing matrix (device, the caller's). Row t's entries lie
+ * at row_ptr[t] .. row_ptr[t+1], experts ascending; expert e's at group_ptr[e]
+ * .. group_ptr[e+1], tokens ascending. slot maps the first order to the
+ * second. Places past the last entry hold -1 (weights: 0). */
+typedef struct {
+    int64_t *row_ptr;    /* n_tokens + 1 */
+    int32_t *expert;     /* n_tokens * top_k: columns of R */
+    float *weight;       /* n_tokens * top_k: values of R */
+    int64_t *group_ptr;  /* n_experts + 1 */
+    int32_t *token;      /* n_tokens * top_k: columns of R^T, the grouped rows' tokens */
+    int32_t *slot;       /* n_tokens * top_k: grouped row of each entry of R */
+    float *group_weight; /* n_tokens * top_k: values of R^T */
+} gmagnus_routing_t;
+
+/* Device bytes gmagnus_route needs as workspace (host-only; 0 for sizes it refuses). */
+int64_t gmagnus_route_workspace_bytes(int64_t n_tokens, int64_t n_experts, int64_t top_k);
+
+/* Chooses the top_k largest of each row of logits (n_tokens x n_experts, fp32,
+ * bf16 or fp16); of equal logits the lowest expert first. -inf and NaN are
+ * masked: never chosen, so a row may have fewer entries, or none. (The type's
+ * lowest finite value is an ordinary logit.) Weights are exp(l - max) over its
+ * sum, taken over the chosen experts (normalise = 1) or over all unmasked
+ * ones (normalise = 0).
+ * Errors: INVALID_VALUE (NULL, sizes, types, top_k not in 1..n_experts,
+ * workspace too small), UNSUPPORTED (n_experts > 1024, n_tokens * top_k >=
+ * 2^31), HIP. */
+gmagnus_status_t gmagnus_route(const gmagnus_dense_t *logits, int64_t top_k, int32_t normalise,
+                               const gmagnus_routing_t *out, void *workspace, int64_t workspace_bytes,
+                               void *hip_stream);
+
+/* Gradient of the logits from the gradient of the weights (d_weight, fp32, in
+ * the order of R's entries): with p the softmax that gave the weights,
+ * p_i * (g_i - sum_j p_j g_j), g zero where an expert was not chosen. Masked
+ * logits get zero. routing: expert, row_ptr and weight are read.
+ * Errors as gmagnus_route. */
+gmagnus_status_t gmagnus_route_backward(const gmagnus_dense_t *logits, int64_t top_k, int32_t normalise,
+                                        const gmagnus_routing_t *routing, const float *d_weight,
+                                        const gmagnus_dense_t *d_logits, void *hip_stream);
+
+/* Ragged groups of rows: group e holds the grouped rows group_ptr[e] ..
+ * group_ptr[e+1] of n_rows; grouped row r stands for row index[r] of X, or
+ * (index NULL) for row r. */
+typedef struct {
+    int64_t n_groups;
+    int64_t n_rows;           /* grouped rows the arrays have room for */
+    const int64_t *group_ptr; /* device, n_groups + 1 */
+    const int32_t *index;     /* device, n_rows, or NULL */
+} gmagnus_groups_t;
+
+/* Y[r,:] = X[index[r],:] * W_e^T for every row r of every group e, W a stack of
+ * n_groups matrices N x K; with transposed = 1, Y[r,:] = X[index[r],:] * W_e
+ * and W is a stack of K x N. Rows of Y past the last group are set to zero.
+ * X and W have one type, bf16 or fp16; Y has it too, or fp32.
+ * Errors: INVALID_VALUE (NULL, shapes, strides, types), UNSUPPORTED (n_rows
+ * or a side of a matrix >= 2^31), HIP. */
+gmagnus_status_t gmagnus_group_product(const gmagnus_groups_t *groups, const gmagnus_dense_t *X,
+                                       const gmagnus_dense_t *W, int32_t transposed, const gmagnus_dense_t *Y,
+                                       void *hip_stream);
+
+/* D_e = sum over group e's rows r of DY[r,:]^T * X[index[r],:], a stack of
+ * n_groups matrices N x K: the gradient of gmagnus_group_product's W. An empty
+ * group's is zero. DY and X have one type, bf16 or fp16; D has it too, or fp32.
+ * Errors as gmagnus_group_product. */
+gmagnus_status_t gmagnus_group_outer(const gmagnus_groups_t *groups, const gmagnus_dense_t *DY,
+                                     const gmagnus_dense_t *X, const gmagnus_dense_t *D, void *hip_stream);
+
+/* Values that share a scale along a row, and along a column of weights. */
+#define GMAGNUS_SCALE_BLOCK 128
+
+/* Q = X / scale rounded to E4M3, one scale for each block of block_rows (1 or
+ * 128) x 128 values: the block's largest magnitude / 448, at least 2^-126. X
+ * is fp32, bf16 or fp16, a matrix or a stack of n_stack; Q has its shape, and
+ * scale (fp32) ceil(n_rows / block_rows) x ceil(n_cols / 128). A NaN makes its
+ * block's scale NaN, an infinity makes it infinite.
+ * Errors: INVALID_VALUE, UNSUPPORTED, HIP. */
+gmagnus_status_t gmagnus_quantise_blocks(const gmagnus_dense_t *X, int64_t n_stack, int64_t block_rows,
+                                         const gmagnus_dense_t *Q, const gmagnus_dense_t *scale, void *hip_stream);
+
+/* gmagnus_group_product (W N x K) on E4M3 operands: X with a scale for each row
+ * and 128 columns, W with one for each 128 rows and 128 columns, as
+ * gmagnus_quantise_blocks gives them. The products of a block of 128 are
+ * summed by the matrix units and its sum scaled in fp32. Y is bf16, fp16 or fp32.
+ * One group is the plain matrix product.
+ * Errors as gmagnus_group_product. */
+gmagnus_status_t gmagnus_group_product_fp8(const gmagnus_groups_t *groups, const gmagnus_dense_t *X,
+                                           const gmagnus_dense_t *X_scale, const gmagnus_dense_t *W,
+                                           const gmagnus_dense_t *W_scale, const gmagnus_dense_t *Y, void *hip_stream);
+
+/* OUT[t,:] = sum over the entries j of row t of weight[j] * Y[slot[j],:]
+ * (weight NULL: 1). OUT has row_ptr's rows; Y and OUT have one type, fp32,
+ * bf16 or fp16. n_entries is the length of slot and weight. A slot outside Y
+ * adds nothing. Errors: INVALID_VALUE, UNSUPPORTED, HIP. */
+gmagnus_status_t gmagnus_combine(const int64_t *row_ptr, const int32_t *slot, const float *weight, int64_t n_entries,
+                                 const gmagnus_dense_t *Y, const gmagnus_dense_t *OUT, void *hip_stream);
+
+/* Gradients of gmagnus_combine: D_Y[slot[j],:] = weight[j] * D_OUT[t,:] and
+ * d_weight[j] = sum of Y[slot[j],:] * D_OUT[t,:] (fp32). Rows of D_Y past the
+ * last entry and places of d_weight past it are set to zero (the slots of a
+ * routing are a permutation of the rows before it). weight NULL means 1;
+ * d_weight (and then Y) or D_Y may be NULL where it is not wanted.
+ * Errors as gmagnus_combine. */
+gmagnus_status_t gmagnus_combine_backward(const int64_t *row_ptr, const int32_t *slot, const float *weight,
+                                          int64_t n_entries, const gmagnus_dense_t *Y, const gmagnus_dense_t *D_OUT,
+                                          const gmagnus_dense_t *D_Y, float *d_weight, void *hip_stream);
+
 /* Frees device blocks cached by the library's allocator (no plan may be alive). */
 void gmagnus_release_cache(void);
 

@@ -32,7 +32,7 @@ FLAGS = [
 ]
 
 SOURCES = ["prims.hip", "setup.hip", "expand.hip", "rowsplit.hip", "multisplit.hip", "tiles.hip", "accumulate.hip",
-           "plan.hip", "probe.hip", "static_plan.hip"]
+           "plan.hip", "probe.hip", "static_plan.hip", "route.hip", "group.hip", "group_fp8.hip"]
 
 
 def _compile(src: str) -> str:

@@ -1,0 +1,239 @@
+// Shared pieces of the dense-operand kernels (routed expert products): 16-bit
+// element types, eight elements at a time at any alignment, and the row tiles
+// of ragged groups.
+#pragma once
+
+#include "common.hpp"
+#include "host.hpp"
+
+namespace gm {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// 16 bytes at the alignment of an element (the hardware takes any address).
+template <int ALIGN>
+struct Bytes16 {
+    uint32_t v[4] __attribute__((packed, aligned(ALIGN)));
+};
+
+GM_DEV float to_f32(float x) { return x; }
+GM_DEV float to_f32(__bf16 x) { return (float)x; }
+GM_DEV float to_f32(_Float16 x) { return (float)x; }
+
+// Two values rounded to nearest even, as 32 bits.
+template <typename T>
+GM_DEV uint32_t pack2(float a, float b);
+template <>
+GM_DEV uint32_t pack2<__bf16>(float a, float b) {
+    const bf16x2 v = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, v);
+}
+template <>
+GM_DEV uint32_t pack2<_Float16>(float a, float b) {
+    const f16x2 v = {(_Float16)a, (_Float16)b};
+    return __builtin_bit_cast(uint32_t, v);
+}
+
+// 16 bytes of 16-bit elements, those from `valid` on as zeros; not read either.
+template <typename T>
+GM_DEV u32x4 load8(const T *p, int valid) {
+    u32x4 r = {0, 0, 0, 0};
+    if (valid >= 8) {
+        const Bytes16<sizeof(T)> b = *reinterpret_cast<const Bytes16<sizeof(T)> *>(p);
+        r = u32x4{b.v[0], b.v[1], b.v[2], b.v[3]};
+    } else if (valid > 0) {
+        const uint16_t *s = reinterpret_cast<const uint16_t *>(p);
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < valid) r[i >> 1] |= (uint32_t)s[i] << (16 * (i & 1));
+    }
+    return r;
+}
+
+// Eight elements as fp32, those from `valid` on zero.
+template <typename T>
+GM_DEV void load_f32x8(const T *p, int valid, float (&v)[8]) {
+    if constexpr (sizeof(T) == 4) {
+        if (valid >= 8) {
+            const Bytes16<4> b0 = reinterpret_cast<const Bytes16<4> *>(p)[0], b1 = reinterpret_cast<const Bytes16<4> *>(p)[1];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[i] = __uint_as_float(b0.v[i]);
+                v[4 + i] = __uint_as_float(b1.v[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < valid ? p[i] : 0.f;
+        }
+    } else {
+        typedef T vec __attribute__((ext_vector_type(8)));
+        const vec x = __builtin_bit_cast(vec, load8(p, valid));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)x[i];
+    }
+}
+
+GM_DEV f32x4 mfma_16x16x32(u32x4 a, u32x4 b, f32x4 c, __bf16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+GM_DEV f32x4 mfma_16x16x32(u32x4 a, u32x4 b, f32x4 c, _Float16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// Rows [begin, end) of ragged group e, clamped to the rows there are; group
+// n_groups is what lies past the last one.
+GM_DEV void group_rows(const int64_t *gp, int64_t n_groups, int64_t n_rows, int64_t e, int64_t &begin, int64_t &end) {
+    const int64_t b = gp[e], f = e < n_groups ? gp[e + 1] : n_rows;
+    begin = b < 0 ? 0 : b > n_rows ? n_rows : b;
+    end = f < begin ? begin : f > n_rows ? n_rows : f;
+}
+
+// Row tiles of at most BM rows, group after group, the rows past the last
+// group as one more. A wave counts them 64 groups at a time; all lanes get the
+// same answer.
+template <int BM>
+GM_DEV int64_t count_row_tiles(const int64_t *gp, int64_t n_groups, int64_t n_rows) {
+    const int lane = threadIdx.x & (GM_WAVE - 1);
+    int n = 0;
+    for (int64_t e = lane; e <= n_groups; e += GM_WAVE) {
+        int64_t b, f;
+        group_rows(gp, n_groups, n_rows, e, b, f);
+        n += (int)((f - b + BM - 1) / BM);
+    }
+    return wave_reduce_sum<int32_t>(n);
+}
+
+struct RowTile {
+    int64_t group;  // n_groups: rows past the last group
+    int64_t begin;  // first row
+    int rows;       // at most BM
+};
+
+// Tile t of the order above (t is below the count).
+template <int BM>
+GM_DEV RowTile find_row_tile(const int64_t *gp, int64_t n_groups, int64_t n_rows, int64_t t) {
+    const int lane = threadIdx.x & (GM_WAVE - 1);
+    int left = (int)t;
+    for (int64_t e0 = 0; e0 <= n_groups; e0 += GM_WAVE) {
+        const int64_t e = e0 + lane;
+        int64_t b = 0, f = 0;
+        if (e <= n_groups) group_rows(gp, n_groups, n_rows, e, b, f);
+        const int n = (int)((f - b + BM - 1) / BM);
+        const int upto = wave_incl_scan<int32_t>(n);
+        const uint64_t hit = ballot(upto > left);
+        if (hit) {
+            const int src = __ffsll((unsigned long long)hit) - 1;
+            const int in = left - (__builtin_amdgcn_readlane(upto, src) - __builtin_amdgcn_readlane(n, src));
+            const int64_t gb = __builtin_amdgcn_readlane((int)b, src), gf = __builtin_amdgcn_readlane((int)f, src);
+            const int64_t begin = gb + (int64_t)in * BM;
+            return RowTile{e0 + src, begin, (int)(gf - begin < BM ? gf - begin : BM)};
+        }
+        left -= __builtin_amdgcn_readlane(upto, GM_WAVE - 1);
+    }
+    return RowTile{n_groups, n_rows, 0};
+}
+
+// Upper bound of count_row_tiles on the host, which does not know the groups.
+inline int64_t row_tiles_bound(int64_t n_groups, int64_t n_rows, int bm) {
+    return n_rows / bm + (n_groups + 1 < n_rows ? n_groups + 1 : n_rows);
+}
+
+// Tile (row tile, column tile) number t: bands of 8 column tiles, row tiles
+// within a band, so that the tiles in flight on one XCD share rows and columns.
+GM_DEV void band_tile(int64_t t, int64_t n_row, int64_t n_col, int64_t &row, int64_t &col) {
+    constexpr int64_t BAND = 8;
+    const int64_t band = t / (n_row * BAND), r = t - band * n_row * BAND;
+    const int64_t w = n_col - band * BAND < BAND ? n_col - band * BAND : BAND;
+    row = r / w;
+    col = band * BAND + (r - row * w);
+}
+
+inline int data_size(int32_t type) {
+    return type == GMAGNUS_DATA_FP32 ? 4 : type == GMAGNUS_DATA_FP8_E4M3 ? 1 : 2;
+}
+
+// Common checks of a dense operand of an entry point.
+inline void check_dense(const gmagnus_dense_t *m, const char *name, int64_t n_rows, int64_t n_cols, int64_t n_stack = 1) {
+    const std::string s(name);
+    GM_REQUIRE(m != nullptr, GMAGNUS_ERROR_INVALID_VALUE, "NULL " + s);
+    GM_REQUIRE(m->data_type >= GMAGNUS_DATA_FP32 && m->data_type <= GMAGNUS_DATA_FP8_E4M3, GMAGNUS_ERROR_INVALID_VALUE,
+               "unknown data type of " + s);
+    GM_REQUIRE(m->n_rows == n_rows && m->n_cols == n_cols, GMAGNUS_ERROR_INVALID_VALUE,
+               s + " is " + std::to_string(m->n_rows) + " x " + std::to_string(m->n_cols) + ", expected " +
+                   std::to_string(n_rows) + " x " + std::to_string(n_cols));
+    GM_REQUIRE(n_rows <= 1 || m->row_stride >= n_cols, GMAGNUS_ERROR_INVALID_VALUE, "row stride of " + s + " below its columns");
+    GM_REQUIRE(n_stack <= 1 || n_rows == 0 || m->stack_stride >= 0, GMAGNUS_ERROR_INVALID_VALUE, "negative stack stride of " + s);
+    GM_REQUIRE(m->data != nullptr || n_rows == 0 || n_cols == 0 || n_stack == 0, GMAGNUS_ERROR_INVALID_VALUE,
+               "NULL data of " + s);
+    GM_REQUIRE(m->data == nullptr || (uintptr_t)m->data % data_size(m->data_type) == 0, GMAGNUS_ERROR_INVALID_VALUE,
+               "data of " + s + " is not aligned to its type");
+}
+
+// One operand of a tile.
+struct Side {
+    const void *base;      // of the tile's first element (K_ROWS: of its first column)
+    int64_t stride;        // elements between rows in memory
+    const int32_t *index;  // row numbers in memory of the rows below, or null
+    int64_t n_mem;         // rows in memory that an index may name
+    int valid;             // elements of the tile's own axis
+};
+
+// Row `r`'s address, null where its index names none.
+template <typename T>
+GM_DEV const T *row_at(const Side &s, int64_t r) {
+    if (s.index) {
+        const int64_t i = s.index[r];
+        return i < 0 || i >= s.n_mem ? nullptr : static_cast<const T *>(s.base) + i * s.stride;
+    }
+    return static_cast<const T *>(s.base) + r * s.stride;
+}
+
+// Four neighbours of an output row, as many as there are.
+template <typename OUT>
+GM_DEV void store4(OUT *p, f32x4 v, int64_t left, bool wide) {
+    if (wide && left >= 4) {
+        if constexpr (sizeof(OUT) == 4)
+            *reinterpret_cast<f32x4 *>(p) = v;
+        else
+            *reinterpret_cast<u32x2 *>(p) = u32x2{pack2<OUT>(v[0], v[1]), pack2<OUT>(v[2], v[3])};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < left) p[i] = (OUT)v[i];
+    }
+}
+
+// Rows of zeros.
+template <typename OUT>
+GM_DEV void zero_tile(OUT *out, int64_t stride, int rows, int cols) {
+    for (int r = threadIdx.x / 64; r < rows; r += blockDim.x / 64)
+        for (int c = threadIdx.x % 64; c < cols; c += 64) out[r * stride + c] = (OUT)0.f;
+}
+
+// Work groups of a launch: the kernels' loops take what exceeds this.
+constexpr int64_t MAX_GRID = 1 << 22;
+
+inline void check_groups(const gmagnus_groups_t *g) {
+    GM_REQUIRE(g != nullptr, GMAGNUS_ERROR_INVALID_VALUE, "NULL groups");
+    GM_REQUIRE(g->n_groups >= 1 && g->n_rows >= 0, GMAGNUS_ERROR_INVALID_VALUE, "groups: n_groups must be positive, n_rows not negative");
+    GM_REQUIRE(g->group_ptr != nullptr, GMAGNUS_ERROR_INVALID_VALUE, "groups: NULL group_ptr");
+    GM_REQUIRE(g->n_rows < INT32_MAX && g->n_groups < INT32_MAX, GMAGNUS_ERROR_UNSUPPORTED, "groups: more than 2^31 - 2 rows or groups");
+}
+
+inline void check_side(int64_t n, const char *what) {
+    GM_REQUIRE(n >= 1, GMAGNUS_ERROR_INVALID_VALUE, std::string(what) + " must be positive");
+    GM_REQUIRE(n < INT32_MAX, GMAGNUS_ERROR_UNSUPPORTED, std::string(what) + " beyond 2^31 - 2");
+}
+
+// 16-byte aligned rows (and matrices of a stack).
+inline bool aligned16(const void *p, int64_t stride, int64_t stack, int size) {
+    return (uintptr_t)p % 16 == 0 && stride * size % 16 == 0 && stack * size % 16 == 0;
+}
+
+}  // namespace gm

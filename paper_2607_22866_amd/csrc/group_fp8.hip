@@ -1,0 +1,333 @@
+// Matrix products grouped by ragged runs of rows on 8-bit operands (E4M3) with
+// a scale for each block of 128, and the rounding of matrices to that form.
+//   Y[r,n] = sum over blocks b of sx[r,b] * sw[n/128,b] * (sum over k in b of x[r,k] * w[n,k])
+// A step of the reduction is one block, so its sum leaves the matrix unit
+// unscaled and is scaled as it joins the fp32 result.
+#include "dense.hpp"
+
+namespace gm {
+namespace {
+
+constexpr int SB = GMAGNUS_SCALE_BLOCK;
+constexpr float FP8_MAX = 448.f;
+constexpr float SCALE_MIN = 0x1p-126f;
+
+// ----------------------------------------------------------------- quantise
+struct QuantArgs {
+    const void *x;
+    uint8_t *q;
+    float *scale;
+    int64_t n_rows, n_cols, xs, xg, qs, qg, ss, sg, n_stack;
+};
+
+// Magnitudes compare as their bits, NaN above infinity above the rest.
+GM_DEV uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+GM_DEV float block_scale(uint32_t most) {
+    const float s = __uint_as_float(most) / FP8_MAX;
+    return s < SCALE_MIN ? SCALE_MIN : s;  // (a NaN stays)
+}
+
+GM_DEV float to_range(float x, float scale) {
+    const float v = x / scale;
+    return v > FP8_MAX ? FP8_MAX : v < -FP8_MAX ? -FP8_MAX : v;
+}
+
+GM_DEV uint32_t pack_fp8(float a, float b, float c, float d) {
+    int v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
+}
+
+GM_DEV void store_fp8x8(uint8_t *p, int valid, const float (&v)[8], float scale) {
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = to_range(v[i], scale);
+    const uint32_t w[2] = {pack_fp8(r[0], r[1], r[2], r[3]), pack_fp8(r[4], r[5], r[6], r[7])};
+    if (valid >= 8) {
+        struct Bytes8 {
+            uint32_t v[2] __attribute__((packed, aligned(1)));
+        };
+        *reinterpret_cast<Bytes8 *>(p) = Bytes8{{w[0], w[1]}};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < valid) p[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+    }
+}
+
+// One scale a row and 128 columns: 16 lanes a block, eight values a lane.
+template <typename T>
+__global__ __launch_bounds__(256) void k_quantise_rows(QuantArgs a) {
+    const int64_t blocks = (a.n_cols + SB - 1) / SB, total = a.n_stack * a.n_rows * blocks;
+    const int lane = threadIdx.x & 63;
+    for (int64_t u0 = blockIdx.x * 16ll + threadIdx.x / 64 * 4; u0 < total; u0 += gridDim.x * 16ll) {
+        const int64_t u = u0 + lane / 16;
+        const int64_t row = u / blocks, b = u - row * blocks, g = row / a.n_rows, r = row - g * a.n_rows;
+        const int64_t c0 = b * SB + lane % 16 * 8;
+        const int valid = u >= total || c0 >= a.n_cols ? 0 : a.n_cols - c0 >= 8 ? 8 : (int)(a.n_cols - c0);
+        float v[8] = {};
+        if (valid > 0) load_f32x8(static_cast<const T *>(a.x) + g * a.xg + r * a.xs + c0, valid, v);
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d, 64));
+        const float s = block_scale(m);
+        if (valid > 0) store_fp8x8(a.q + g * a.qg + r * a.qs + c0, valid, v, s);
+        if (u < total && lane % 16 == 0) a.scale[g * a.sg + r * a.ss + b] = s;
+    }
+}
+
+// One scale for 128 x 128 values: a work group a block, kept in registers.
+template <typename T>
+__global__ __launch_bounds__(256) void k_quantise_tiles(QuantArgs a) {
+    __shared__ uint32_t part[4];
+    const int64_t bc = (a.n_cols + SB - 1) / SB, br = (a.n_rows + SB - 1) / SB, total = a.n_stack * br * bc;
+    for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
+        const int64_t g = u / (br * bc), t = u - g * br * bc, tr = t / bc, tc = t - tr * bc;
+        const int64_t c0 = tc * SB + threadIdx.x % 16 * 8;
+        const int cols = c0 >= a.n_cols ? 0 : a.n_cols - c0 >= 8 ? 8 : (int)(a.n_cols - c0);
+        float v[8][8];
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t r = tr * SB + i * 16 + threadIdx.x / 16;
+            load_f32x8(static_cast<const T *>(a.x) + g * a.xg + (r < a.n_rows ? r : 0) * a.xs + (cols ? c0 : 0),
+                       r < a.n_rows ? cols : 0, v[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = max(m, magnitude(v[i][j]));
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d, 64));
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x / 64] = m;
+        __syncthreads();
+        m = max(max(part[0], part[1]), max(part[2], part[3]));
+        const float s = block_scale(m);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t r = tr * SB + i * 16 + threadIdx.x / 16;
+            if (r < a.n_rows && cols > 0) store_fp8x8(a.q + g * a.qg + r * a.qs + c0, cols, v[i], s);
+        }
+        if (threadIdx.x == 0) a.scale[g * a.sg + tr * a.ss + tc] = s;
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------ product
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// 16x16x128 on E4M3 operands, block scales of one (exponent byte 127).
+GM_DEV f32x4 mfma_fp8(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b1, f32x4 c) {
+    const i32x8 a = {(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3], (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
+    const i32x8 b = {(int)b0[0], (int)b0[1], (int)b0[2], (int)b0[3], (int)b1[0], (int)b1[1], (int)b1[2], (int)b1[3]};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+}
+
+struct Fp8Args {
+    const int64_t *gp;
+    const int32_t *index;
+    int64_t n_groups, n_rows, n_x, n, k;
+    const uint8_t *x, *w;
+    const float *sx, *sw;
+    void *y;
+    int64_t xs, sxs, ws, wg, sws, swg, ys;
+    bool wide;
+    int64_t max_row_tiles;
+};
+
+// 16 bytes, those from `valid` on zero and not read.
+GM_DEV u32x4 load16(const uint8_t *p, int64_t valid) {
+    u32x4 r = {0, 0, 0, 0};
+    if (valid >= 16) {
+        const Bytes16<1> b = *reinterpret_cast<const Bytes16<1> *>(p);
+        r = u32x4{b.v[0], b.v[1], b.v[2], b.v[3]};
+    } else if (valid > 0) {
+#pragma unroll
+        for (int i = 0; i < 15; ++i)
+            if (i < valid) r[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+    }
+    return r;
+}
+
+// Any alignment: tiles of 128 x 128 staged through registers, four waves of
+// 64 x 64. LDS rows are one block of 128 bytes; chunk c of row r sits at
+// c ^ (r / 2 % 8). A lane's 32 reduction bytes are chunks g and g + 4 of its row,
+// the same for both operands (the order within a block does not matter).
+constexpr int GEN_B = 128, GEN_T = 256;
+
+template <typename OUT>
+__global__ __launch_bounds__(GEN_T) void k_group_product_fp8_any(Fp8Args a) {
+    __shared__ u32x4 lds[2 * GEN_B * 8];
+    u32x4 *lp = lds, *lq = lds + GEN_B * 8;
+    const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16, wv = threadIdx.x / 64;
+    const int p0 = wv / 2 * 64, q0 = wv % 2 * 64;
+    const int64_t n_row = min(count_row_tiles<GEN_B>(a.gp, a.n_groups, a.n_rows), a.max_row_tiles);
+    const int64_t n_col = (a.n + GEN_B - 1) / GEN_B, total = n_row * n_col;
+    for (int64_t blk = blockIdx.x; blk < total; blk += gridDim.x) {
+        int64_t tr, tc;
+        band_tile(xcd_tile(blk, total), n_row, n_col, tr, tc);
+        const RowTile t = find_row_tile<GEN_B>(a.gp, a.n_groups, a.n_rows, tr);
+        const int64_t n0 = tc * GEN_B;
+        const int cols = (int)(a.n - n0 < GEN_B ? a.n - n0 : GEN_B);
+        OUT *out = static_cast<OUT *>(a.y) + t.begin * a.ys + n0;
+        if (t.group >= a.n_groups) {
+            zero_tile(out, a.ys, t.rows, cols);
+            continue;
+        }
+        auto x_row = [&](int r) -> int64_t {  // row of X, or -1
+            if (r >= t.rows) return -1;
+            const int64_t i = a.index ? a.index[t.begin + r] : t.begin + r;
+            return i < 0 || i >= a.n_x ? -1 : i;
+        };
+        const uint8_t *pr[4], *qr[4];
+        const float *sp[4];
+        const float *sq = a.sw + t.group * a.swg + n0 / SB * a.sws;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = (threadIdx.x + i * GEN_T) / 8;
+            const int64_t xr = x_row(r), sr = x_row(p0 + 16 * i + i16);
+            pr[i] = xr < 0 ? nullptr : a.x + xr * a.xs;
+            qr[i] = r < cols ? a.w + t.group * a.wg + (n0 + r) * a.ws : nullptr;
+            sp[i] = sr < 0 ? nullptr : a.sx + sr * a.sxs;
+        }
+        f32x4 acc[4][4] = {};
+        u32x4 vp[4], vq[4];
+        auto load = [&](int64_t k0) {
+            const int64_t k = k0 + threadIdx.x % 8 * 16;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                vp[i] = pr[i] ? load16(pr[i] + k, a.k - k) : u32x4{0, 0, 0, 0};
+                vq[i] = qr[i] ? load16(qr[i] + k, a.k - k) : u32x4{0, 0, 0, 0};
+            }
+        };
+        load(0);
+        for (int64_t k0 = 0; k0 < a.k; k0 += SB) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = (threadIdx.x + i * GEN_T) / 8, at = r * 8 + ((threadIdx.x % 8) ^ (r / 2 % 8));
+                lp[at] = vp[i];
+                lq[at] = vq[i];
+            }
+            __syncthreads();
+            if (k0 + SB < a.k) load(k0 + SB);
+            float s[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] = (sp[i] ? sp[i][k0 / SB] : 0.f) * sq[k0 / SB];
+            u32x4 fp[4][2], fq[4][2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int rp = p0 + 16 * i + i16, rq = q0 + 16 * i + i16;
+                    fp[i][h] = lp[rp * 8 + ((h * 4 + g) ^ (rp / 2 % 8))];
+                    fq[i][h] = lq[rq * 8 + ((h * 4 + g) ^ (rq / 2 % 8))];
+                }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const f32x4 d = mfma_fp8(fq[j][0], fq[j][1], fp[i][0], fp[i][1], f32x4{0, 0, 0, 0});
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] += s[i] * d[e];
+                }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = p0 + 16 * i + i16;
+            if (r < t.rows)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int c = q0 + 16 * j + g * 4;
+                    store4(out + r * a.ys + c, acc[i][j], cols - c, a.wide);
+                }
+        }
+    }
+}
+
+}  // namespace
+}  // namespace gm
+
+using namespace gm;
+
+extern "C" gmagnus_status_t gmagnus_quantise_blocks(const gmagnus_dense_t *X, int64_t n_stack, int64_t block_rows,
+                                                    const gmagnus_dense_t *Q, const gmagnus_dense_t *scale,
+                                                    void *hip_stream) {
+    return guarded([&] {
+        GM_REQUIRE(X && Q && scale, GMAGNUS_ERROR_INVALID_VALUE, "NULL X, Q or scale");
+        GM_REQUIRE(block_rows == 1 || block_rows == SB, GMAGNUS_ERROR_INVALID_VALUE, "block_rows must be 1 or 128");
+        const int64_t n = X->n_rows, k = X->n_cols;
+        GM_REQUIRE(n >= 0 && n_stack >= 0, GMAGNUS_ERROR_INVALID_VALUE, "negative rows or stack");
+        check_side(k, "columns of X");
+        GM_REQUIRE(n < INT32_MAX && n_stack < INT32_MAX, GMAGNUS_ERROR_UNSUPPORTED, "rows or stack beyond 2^31 - 2");
+        check_dense(X, "X", n, k, n_stack);
+        check_dense(Q, "Q", n, k, n_stack);
+        check_dense(scale, "scale", (n + block_rows - 1) / block_rows, (k + SB - 1) / SB, n_stack);
+        GM_REQUIRE(X->data_type != GMAGNUS_DATA_FP8_E4M3 && Q->data_type == GMAGNUS_DATA_FP8_E4M3 &&
+                       scale->data_type == GMAGNUS_DATA_FP32,
+                   GMAGNUS_ERROR_INVALID_VALUE, "X must be fp32, bf16 or fp16, Q E4M3, scale fp32");
+        if (n == 0 || n_stack == 0) return;
+        const QuantArgs a{X->data, (uint8_t *)Q->data, (float *)scale->data, n, k, X->row_stride, X->stack_stride,
+                          Q->row_stride, Q->stack_stride, scale->row_stride, scale->stack_stride, n_stack};
+        hipStream_t s = (hipStream_t)hip_stream;
+        auto launch = [&](auto v) {
+            using T = decltype(v);
+            if (block_rows == 1) {
+                const int64_t units = n_stack * n * scale->n_cols;
+                hipLaunchKernelGGL(k_quantise_rows<T>, dim3(grid_for(units, 16, MAX_GRID)), dim3(256), 0, s, a);
+            } else {
+                hipLaunchKernelGGL(k_quantise_tiles<T>, dim3(grid_for(n_stack * scale->n_rows * scale->n_cols, 1, MAX_GRID)),
+                                   dim3(256), 0, s, a);
+            }
+        };
+        if (X->data_type == GMAGNUS_DATA_BF16)
+            launch(__bf16{});
+        else if (X->data_type == GMAGNUS_DATA_FP16)
+            launch(_Float16{});
+        else
+            launch(float{});
+        GM_CHECK_LAUNCH();
+    });
+}
+
+extern "C" gmagnus_status_t gmagnus_group_product_fp8(const gmagnus_groups_t *groups, const gmagnus_dense_t *X,
+                                                      const gmagnus_dense_t *X_scale, const gmagnus_dense_t *W,
+                                                      const gmagnus_dense_t *W_scale, const gmagnus_dense_t *Y,
+                                                      void *hip_stream) {
+    return guarded([&] {
+        check_groups(groups);
+        GM_REQUIRE(X && W && Y && X_scale && W_scale, GMAGNUS_ERROR_INVALID_VALUE, "NULL X, W, Y or scale");
+        const int64_t k = X->n_cols, n = Y->n_cols;
+        check_side(k, "columns of X");
+        check_side(n, "columns of Y");
+        const int64_t n_x = groups->index ? X->n_rows : groups->n_rows, kb = (k + SB - 1) / SB;
+        check_dense(X, "X", n_x, k);
+        check_dense(X_scale, "X_scale", n_x, kb);
+        check_dense(Y, "Y", groups->n_rows, n);
+        check_dense(W, "W", n, k, groups->n_groups);
+        check_dense(W_scale, "W_scale", (n + SB - 1) / SB, kb, groups->n_groups);
+        GM_REQUIRE(n_x >= 0 && n_x < INT32_MAX, GMAGNUS_ERROR_UNSUPPORTED, "rows of X beyond 2^31 - 2");
+        GM_REQUIRE(X->data_type == GMAGNUS_DATA_FP8_E4M3 && W->data_type == GMAGNUS_DATA_FP8_E4M3 &&
+                       X_scale->data_type == GMAGNUS_DATA_FP32 && W_scale->data_type == GMAGNUS_DATA_FP32 &&
+                       Y->data_type != GMAGNUS_DATA_FP8_E4M3,
+                   GMAGNUS_ERROR_INVALID_VALUE, "X and W must be E4M3, their scales fp32, Y fp32, bf16 or fp16");
+        if (groups->n_rows == 0) return;
+        const int64_t row_tiles = row_tiles_bound(groups->n_groups, groups->n_rows, GEN_B);
+        const Fp8Args a{groups->group_ptr, groups->index, groups->n_groups, groups->n_rows, n_x, n, k,
+                        (const uint8_t *)X->data, (const uint8_t *)W->data, (const float *)X_scale->data,
+                        (const float *)W_scale->data, Y->data, X->row_stride, X_scale->row_stride, W->row_stride,
+                        W->stack_stride, W_scale->row_stride, W_scale->stack_stride, Y->row_stride,
+                        aligned16(Y->data, Y->row_stride, 0, data_size(Y->data_type)), row_tiles};
+        hipStream_t s = (hipStream_t)hip_stream;
+        const int64_t tiles = row_tiles * ((n + GEN_B - 1) / GEN_B);
+        const dim3 grid((unsigned)(tiles < MAX_GRID ? tiles : MAX_GRID));
+        if (Y->data_type == GMAGNUS_DATA_BF16)
+            hipLaunchKernelGGL(k_group_product_fp8_any<__bf16>, grid, dim3(GEN_T), 0, s, a);
+        else if (Y->data_type == GMAGNUS_DATA_FP16)
+            hipLaunchKernelGGL(k_group_product_fp8_any<_Float16>, grid, dim3(GEN_T), 0, s, a);
+        else
+            hipLaunchKernelGGL(k_group_product_fp8_any<float>, grid, dim3(GEN_T), 0, s, a);
+        GM_CHECK_LAUNCH();
+    });
+}

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <new>
 #include <string>
 #include <vector>
 
@@ -34,6 +35,24 @@ void set_last_error(const std::string &msg);
     do {                                                      \
         if (!(cond)) throw ::gm::Error{(status), (msg)};      \
     } while (0)
+
+// Runs an entry point's body; what it throws becomes a status and a message.
+template <class F>
+inline gmagnus_status_t guarded(F &&f) {
+    try {
+        f();
+        return GMAGNUS_SUCCESS;
+    } catch (const Error &e) {
+        set_last_error(e.msg);
+        return e.status;
+    } catch (const std::bad_alloc &) {
+        set_last_error("host allocation failed");
+        return GMAGNUS_ERROR_OUT_OF_MEMORY;
+    } catch (...) {
+        set_last_error("unexpected exception");
+        return GMAGNUS_ERROR_HIP;
+    }
+}
 
 // Device memory for one plan. Blocks come from the user's callbacks or from
 // the library's process-wide caching allocator. free() keeps a block on the

@@ -1813,23 +1813,6 @@ void do_update_values(gmagnus_plan_s *p, const void *a_val, const void *b_val) {
     if (s != p->stream) GM_HIP(hipStreamWaitEvent(p->stream, join, 0));
 }
 
-template <class F>
-gmagnus_status_t guarded(F &&f) {
-    try {
-        f();
-        return GMAGNUS_SUCCESS;
-    } catch (const Error &e) {
-        set_last_error(e.msg);
-        return e.status;
-    } catch (const std::bad_alloc &) {
-        set_last_error("host allocation failed");
-        return GMAGNUS_ERROR_OUT_OF_MEMORY;
-    } catch (...) {
-        set_last_error("unexpected exception");
-        return GMAGNUS_ERROR_HIP;
-    }
-}
-
 }  // namespace
 
 namespace gm {

@@ -55,6 +55,25 @@ class MatrixDesc(ctypes.Structure):
                 ("index_type", ctypes.c_int32), ("value_type", ctypes.c_int32)]
 
 
+DATA_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3}
+SCALE_BLOCK = 128
+
+
+class DenseDesc(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n_rows", ctypes.c_int64), ("n_cols", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("stack_stride", ctypes.c_int64), ("data_type", ctypes.c_int32)]
+
+
+class RoutingDesc(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("row_ptr", "expert", "weight", "group_ptr", "token", "slot",
+                                               "group_weight")]
+
+
+class GroupsDesc(ctypes.Structure):
+    _fields_ = [("n_groups", ctypes.c_int64), ("n_rows", ctypes.c_int64), ("group_ptr", ctypes.c_void_p),
+                ("index", ctypes.c_void_p)]
+
+
 ALLOC_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p)
 FREE_FN = ctypes.CFUNCTYPE(None, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p)
 
@@ -112,7 +131,10 @@ EXPORTS = ["gmagnus_options_init", "gmagnus_get_params", "gmagnus_plan", "gmagnu
            "gmagnus_split_panels", "gmagnus_release_cache", "gmagnus_last_error", "gmagnus_status_string",
            "gmagnus_update_values", "gmagnus_expansion_path", "gmagnus_bandwidth_probe", "gmagnus_plan_static",
            "gmagnus_get_params_typed", "gmagnus_plan_typed", "gmagnus_spgemm_numeric_typed",
-           "gmagnus_update_values_typed", "gmagnus_row_products_typed", "gmagnus_split_panels_typed"]
+           "gmagnus_update_values_typed", "gmagnus_row_products_typed", "gmagnus_split_panels_typed",
+           "gmagnus_route_workspace_bytes", "gmagnus_route", "gmagnus_route_backward", "gmagnus_group_product",
+           "gmagnus_group_outer", "gmagnus_quantise_blocks", "gmagnus_group_product_fp8", "gmagnus_combine",
+           "gmagnus_combine_backward"]
 
 _lib = None
 
@@ -156,6 +178,18 @@ def load(path: str = LIB_PATH):
     lib.gmagnus_bandwidth_probe.argtypes = [ctypes.c_int32, P, P, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, P,
                                             ctypes.POINTER(ctypes.c_double)]
     lib.gmagnus_bandwidth_probe.restype = ctypes.c_int
+    D, G, I64, I32 = ctypes.POINTER(DenseDesc), ctypes.POINTER(GroupsDesc), ctypes.c_int64, ctypes.c_int32
+    R = ctypes.POINTER(RoutingDesc)
+    lib.gmagnus_route_workspace_bytes.argtypes = [I64, I64, I64]
+    lib.gmagnus_route_workspace_bytes.restype = ctypes.c_int64
+    lib.gmagnus_route.argtypes = [D, I64, I32, R, P, I64, P]
+    lib.gmagnus_route_backward.argtypes = [D, I64, I32, R, P, D, P]
+    lib.gmagnus_group_product.argtypes = [G, D, D, I32, D, P]
+    lib.gmagnus_group_outer.argtypes = [G, D, D, D, P]
+    lib.gmagnus_quantise_blocks.argtypes = [D, I64, I64, D, D, P]
+    lib.gmagnus_group_product_fp8.argtypes = [G, D, D, D, D, D, P]
+    lib.gmagnus_combine.argtypes = [P, P, P, I64, D, D, P]
+    lib.gmagnus_combine_backward.argtypes = [P, P, P, I64, D, D, D, P, P]
     lib.gmagnus_release_cache.argtypes = []
     lib.gmagnus_release_cache.restype = None
     lib.gmagnus_last_error.restype = ctypes.c_char_p
@@ -164,7 +198,9 @@ def load(path: str = LIB_PATH):
     for f in ("gmagnus_get_params", "gmagnus_plan", "gmagnus_plan_static", "gmagnus_spgemm_symbolic", "gmagnus_spgemm_numeric",
               "gmagnus_update_values", "gmagnus_plan_info", "gmagnus_row_products", "gmagnus_split_panels",
               "gmagnus_get_params_typed", "gmagnus_plan_typed", "gmagnus_spgemm_numeric_typed",
-              "gmagnus_update_values_typed", "gmagnus_row_products_typed", "gmagnus_split_panels_typed"):
+              "gmagnus_update_values_typed", "gmagnus_row_products_typed", "gmagnus_split_panels_typed",
+              "gmagnus_route", "gmagnus_route_backward", "gmagnus_group_product", "gmagnus_group_outer",
+              "gmagnus_quantise_blocks", "gmagnus_group_product_fp8", "gmagnus_combine", "gmagnus_combine_backward"):
         getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -414,3 +450,259 @@ def bandwidth_probe(kind: str, nbytes: int = 4 << 30, reps: int = 5, grid: int =
 
 def release_cache():
     load().gmagnus_release_cache()
+
+
+# ------------------------------------------------------------ routed expert products
+def _dense(t: torch.Tensor, device: torch.device, name: str, dims: int = 2) -> DenseDesc:
+    """Descriptor of a matrix (dims 2) or a stack of them (dims 3) whose columns are contiguous."""
+    _require_device(t, device, name)
+    if t.dim() != dims:
+        raise ValueError("%s must have %d dimensions" % (name, dims))
+    if t.dtype not in DATA_TYPES:
+        raise ValueError("%s has an unsupported type %s" % (name, t.dtype))
+    n_rows, n_cols = t.shape[-2:]
+    st = t.stride()
+    if n_cols > 1 and st[-1] != 1:
+        raise ValueError("%s must have contiguous columns" % name)
+    return DenseDesc(t.data_ptr(), n_rows, n_cols, max(st[-2], n_cols) if n_rows <= 1 else st[-2],
+                     st[0] if dims == 3 else 0, DATA_TYPES[t.dtype])
+
+
+def _array(t: torch.Tensor, device: torch.device, name: str, dtype, numel: int) -> int:
+    _require_device(t, device, name)
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() != numel:
+        raise ValueError("%s must be a contiguous %s array of %d entries" % (name, dtype, numel))
+    return t.data_ptr()
+
+
+class _Launch:
+    """The stream of a call on device tensors; arrays made inside belong to that stream, and inputs of others
+    are not reused before it has read them."""
+
+    def __init__(self, stream, t: torch.Tensor, *inputs):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise ValueError("operands must be CUDA tensors")
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError("operands are on %s, the current device is cuda:%d" % (t.device, torch.cuda.current_device()))
+        self._ctx = None
+        if stream is not None:
+            for x in (t,) + inputs:
+                if isinstance(x, torch.Tensor) and x.is_cuda:
+                    x.record_stream(stream)
+            self._ctx = torch.cuda.stream(stream)
+        self.stream = _stream(stream)
+
+    def __enter__(self):
+        if self._ctx is not None:
+            self._ctx.__enter__()
+        return self.stream
+
+    def __exit__(self, *a):
+        if self._ctx is not None:
+            self._ctx.__exit__(*a)
+
+
+def _out(out, shape, dtype, device, name):
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(out.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s" % (name, tuple(shape)))
+    return out
+
+
+@dataclass
+class Routing:
+    """The routing matrix (tokens x experts) as device arrays in both orders. Arrays
+    of entries have n_tokens * top_k places; places past the last entry hold -1
+    (weights 0)."""
+
+    n_tokens: int
+    n_experts: int
+    top_k: int
+    normalise: bool
+    row_ptr: torch.Tensor       # int64, n_tokens + 1
+    expert: torch.Tensor        # int32: a token's experts, ascending
+    weight: torch.Tensor        # float32
+    group_ptr: torch.Tensor     # int64, n_experts + 1
+    token: torch.Tensor         # int32: an expert's tokens, ascending
+    slot: torch.Tensor          # int32: grouped row of each entry
+    group_weight: torch.Tensor  # float32: the weights by grouped row
+
+    @property
+    def nnz(self) -> int:
+        """Entries (waits for the device)."""
+        return int(self.row_ptr[-1])
+
+    def matrix(self) -> DeviceCSR:
+        """The routing matrix, tokens x experts (waits for the device)."""
+        n = self.nnz
+        return DeviceCSR(self.n_tokens, self.n_experts, self.row_ptr, self.expert[:n], self.weight[:n])
+
+    def transposed(self) -> DeviceCSR:
+        """Its transpose, experts x tokens (waits for the device)."""
+        n = self.nnz
+        return DeviceCSR(self.n_experts, self.n_tokens, self.group_ptr, self.token[:n], self.group_weight[:n])
+
+    def _desc(self) -> RoutingDesc:
+        return RoutingDesc(self.row_ptr.data_ptr(), self.expert.data_ptr(), self.weight.data_ptr(),
+                           self.group_ptr.data_ptr(), self.token.data_ptr(), self.slot.data_ptr(),
+                           self.group_weight.data_ptr())
+
+
+def route(logits: torch.Tensor, top_k: int, normalise: bool = True, stream=None) -> Routing:
+    """The top_k largest logits of each token (-inf and NaN are masked; ties: the
+    lowest expert) with softmax weights over them (normalise) or over all experts."""
+    with _Launch(stream, logits) as s:
+        dev = logits.device
+        d = _dense(logits, dev, "logits")
+        t, e = logits.shape
+        lib = load()
+        n = t * top_k if top_k > 0 else 0
+        i32 = torch.empty(3, n, dtype=torch.int32, device=dev)
+        f32 = torch.empty(2, n, dtype=torch.float32, device=dev)
+        ptr = torch.empty(t + e + 2, dtype=torch.int64, device=dev)
+        nbytes = lib.gmagnus_route_workspace_bytes(t, e, top_k)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        r = Routing(t, e, top_k, bool(normalise), ptr[:t + 1], i32[0], f32[0], ptr[t + 1:], i32[1], i32[2], f32[1])
+        _check(lib.gmagnus_route(ctypes.byref(d), top_k, int(r.normalise), ctypes.byref(r._desc()), ws.data_ptr(), nbytes, s))
+        return r
+
+
+def route_backward(logits: torch.Tensor, routing: Routing, d_weight: torch.Tensor,
+                   out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Gradient of the logits from the gradient of routing.weight (float32, n_tokens * top_k)."""
+    with _Launch(stream, logits, d_weight, routing.row_ptr, routing.expert, routing.weight, out) as s:
+        dev = logits.device
+        d = _dense(logits, dev, "logits")
+        if tuple(logits.shape) != (routing.n_tokens, routing.n_experts):
+            raise ValueError("logits must have the routing's shape")
+        _require_device(routing.row_ptr, dev, "routing")
+        g = _array(d_weight, dev, "d_weight", torch.float32, routing.n_tokens * routing.top_k)
+        out = _out(out, logits.shape, logits.dtype, dev, "out")
+        o = _dense(out, dev, "out")
+        _check(load().gmagnus_route_backward(ctypes.byref(d), routing.top_k, int(routing.normalise),
+                                             ctypes.byref(routing._desc()), g, ctypes.byref(o), s))
+        return out
+
+
+def _groups(group_ptr, index, n_rows: int, device) -> GroupsDesc:
+    gp = _array(group_ptr, device, "group_ptr", torch.int64, group_ptr.numel())
+    if group_ptr.numel() < 2:
+        raise ValueError("group_ptr must have at least two entries")
+    ix = None if index is None else _array(index, device, "index", torch.int32, n_rows)
+    return GroupsDesc(group_ptr.numel() - 1, n_rows, gp, ix)
+
+
+def group_product(x: torch.Tensor, w: torch.Tensor, group_ptr: torch.Tensor, index: Optional[torch.Tensor] = None,
+                  transposed: bool = False, out_dtype=None, out: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """y[r] = x[index[r]] @ w[e].T (transposed: @ w[e]) for every row r of every
+    group e, group_ptr[e] <= r < group_ptr[e + 1]. index None: x's own rows.
+    bfloat16 or float16, sums in fp32; out_dtype: the inputs' type or float32."""
+    with _Launch(stream, x, w, group_ptr, index, out) as s:
+        dev = x.device
+        dx, dw = _dense(x, dev, "x"), _dense(w, dev, "w", 3)
+        n_rows = x.shape[0] if index is None else index.numel()
+        gd = _groups(group_ptr, index, n_rows, dev)
+        if w.shape[0] != gd.n_groups:
+            raise ValueError("w must have one matrix a group")
+        out = _out(out, (n_rows, dw.n_cols if transposed else dw.n_rows),
+                   out_dtype or x.dtype, dev, "out")
+        dy = _dense(out, dev, "out")
+        _check(load().gmagnus_group_product(ctypes.byref(gd), ctypes.byref(dx), ctypes.byref(dw), int(transposed),
+                                            ctypes.byref(dy), s))
+        return out
+
+
+def group_outer(d_y: torch.Tensor, x: torch.Tensor, group_ptr: torch.Tensor, index: Optional[torch.Tensor] = None,
+                out_dtype=None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Gradient of group_product's w: for every group e the sum of d_y[r].T @ x[index[r]] over its rows."""
+    with _Launch(stream, d_y, x, group_ptr, index, out) as s:
+        dev = d_y.device
+        ddy, dx = _dense(d_y, dev, "d_y"), _dense(x, dev, "x")
+        gd = _groups(group_ptr, index, d_y.shape[0], dev)
+        out = _out(out, (gd.n_groups, ddy.n_cols, dx.n_cols), out_dtype or x.dtype, dev, "out")
+        dd = _dense(out, dev, "out", 3)
+        _check(load().gmagnus_group_outer(ctypes.byref(gd), ctypes.byref(ddy), ctypes.byref(dx), ctypes.byref(dd), s))
+        return out
+
+
+def quantise_blocks(x: torch.Tensor, block_rows: int = 1, stream=None):
+    """(q, scale): x / scale as float8_e4m3fn, with one float32 scale for each block
+    of block_rows (1: activations, 128: weights) x 128 values. x: a matrix or a stack."""
+    with _Launch(stream, x) as s:
+        dev = x.device
+        dims = 3 if x.dim() == 3 else 2
+        dx = _dense(x, dev, "x", dims)
+        if block_rows not in (1, SCALE_BLOCK):
+            raise ValueError("block_rows must be 1 or %d" % SCALE_BLOCK)
+        q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=dev)
+        scale = torch.empty(tuple(x.shape[:-2]) + (-(-dx.n_rows // block_rows), -(-dx.n_cols // SCALE_BLOCK)),
+                            dtype=torch.float32, device=dev)
+        dq, ds = _dense(q, dev, "q", dims), _dense(scale, dev, "scale", dims)
+        _check(load().gmagnus_quantise_blocks(ctypes.byref(dx), x.shape[0] if dims == 3 else 1, block_rows,
+                                              ctypes.byref(dq), ctypes.byref(ds), s))
+        return q, scale
+
+
+def group_product_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
+                      group_ptr: torch.Tensor, index: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
+                      out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """group_product of float8_e4m3fn operands with the scales quantise_blocks gives
+    (x: block_rows 1, w: block_rows 128). One group is the plain product."""
+    with _Launch(stream, x, x_scale, w, w_scale, group_ptr, index, out) as s:
+        dev = x.device
+        dx, dxs = _dense(x, dev, "x"), _dense(x_scale, dev, "x_scale")
+        dw, dws = _dense(w, dev, "w", 3), _dense(w_scale, dev, "w_scale", 3)
+        n_rows = x.shape[0] if index is None else index.numel()
+        gd = _groups(group_ptr, index, n_rows, dev)
+        if w.shape[0] != gd.n_groups or w_scale.shape[0] != gd.n_groups:
+            raise ValueError("w and w_scale must have one matrix a group")
+        out = _out(out, (n_rows, dw.n_rows), out_dtype, dev, "out")
+        dy = _dense(out, dev, "out")
+        _check(load().gmagnus_group_product_fp8(ctypes.byref(gd), ctypes.byref(dx), ctypes.byref(dxs), ctypes.byref(dw),
+                                                ctypes.byref(dws), ctypes.byref(dy), s))
+        return out
+
+
+def _combine_args(row_ptr, slot, weight, dev):
+    rp = _array(row_ptr, dev, "row_ptr", torch.int64, row_ptr.numel())
+    if row_ptr.numel() < 1:
+        raise ValueError("row_ptr is empty")
+    n = slot.numel()
+    return rp, _array(slot, dev, "slot", torch.int32, n), \
+        None if weight is None else _array(weight, dev, "weight", torch.float32, n), n
+
+
+def combine(y: torch.Tensor, row_ptr: torch.Tensor, slot: torch.Tensor, weight: Optional[torch.Tensor] = None,
+            out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """out[t] = sum over the entries j of token t of weight[j] * y[slot[j]] (weight None: 1)."""
+    with _Launch(stream, y, row_ptr, slot, weight, out) as s:
+        dev = y.device
+        d = _dense(y, dev, "y")
+        rp, sl, w, n = _combine_args(row_ptr, slot, weight, dev)
+        out = _out(out, (row_ptr.numel() - 1, d.n_cols), y.dtype, dev, "out")
+        o = _dense(out, dev, "out")
+        _check(load().gmagnus_combine(rp, sl, w, n, ctypes.byref(d), ctypes.byref(o), s))
+        return out
+
+
+def combine_backward(y: Optional[torch.Tensor], row_ptr: torch.Tensor, slot: torch.Tensor,
+                     weight: Optional[torch.Tensor], d_out: torch.Tensor, n_rows: Optional[int] = None, stream=None):
+    """(gradient of y, gradient of weight) of combine. y None (with n_rows, the rows
+    of y): the weights' gradient is not wanted and None."""
+    with _Launch(stream, d_out, y, row_ptr, slot, weight) as s:
+        dev = d_out.device
+        do = _dense(d_out, dev, "d_out")
+        rp, sl, w, n = _combine_args(row_ptr, slot, weight, dev)
+        if row_ptr.numel() - 1 != do.n_rows:
+            raise ValueError("d_out must have a row a token")
+        if y is None and n_rows is None:
+            raise ValueError("n_rows is required without y")
+        dy = None if y is None else _dense(y, dev, "y")
+        d_y = torch.empty((n_rows if y is None else y.shape[0], do.n_cols), dtype=d_out.dtype, device=dev)
+        d_w = None if y is None else torch.empty(n, dtype=torch.float32, device=dev)
+        _check(load().gmagnus_combine_backward(rp, sl, w, n, None if dy is None else ctypes.byref(dy), ctypes.byref(do),
+                                               ctypes.byref(_dense(d_y, dev, "d_y")),
+                                               None if d_w is None else d_w.data_ptr(), s))
+        return d_y, d_w
