@@ -8,6 +8,8 @@
 // as the row number (W in the transposed product, both operands of the
 // gradient). The matrix units take Q as their row operand and P as their column
 // operand, so that a lane's four results are neighbours on the q axis.
+#include <type_traits>
+
 #include "dense.hpp"
 
 namespace gm {
@@ -150,6 +152,247 @@ GM_DEV void tile_any(const Side &p, const Side &q, int64_t n_k, OUT *out, int64_
     }
 }
 
+// ---------------------------------------------------------------- fast layout
+// Tiles brought straight from memory into LDS, 16 bytes a lane, for operands
+// whose rows are 16-byte aligned and whose contiguous axis is a multiple of 8.
+// LDS positions follow the lane order, so the swizzle is applied to what a lane
+// fetches. Two buffers: while the matrix units work on one step's tile the next
+// one is on its way.
+struct Dma {
+    const char *base;   // of the tile
+    uint32_t records;   // bytes that may be read from base (k as rows without an index: of one row)
+    int64_t stride;     // bytes between rows
+    const int32_t *index;
+    int64_t n_mem;
+    int valid;
+};
+
+constexpr uint32_t NOWHERE = 0x80000000u;  // beyond any operand's bytes: reads as zeros
+
+// Lane l's 16 bytes at base + soff + v go to LDS at `to` + 16 l; zeros where v is not
+// below `records`. An instruction without results: the compiler, which would
+// wait for it before every transposing read of LDS, counts no load, and
+// wait_and_barrier() is what waits.
+GM_DEV void load_to_lds(const char *base, uint32_t records, uint32_t v, uint32_t soff, char *to) {
+    typedef __attribute__((address_space(3))) char lds_char;
+    const uint64_t b = (uint64_t)base;
+    const u32x4 rsrc = {(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, records, 0x00027000u};
+    const uint32_t m0 = (uint32_t)(uintptr_t)(lds_char *)to;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :
+                 : "s"(m0), "v"(v), "s"(rsrc), "s"(soff)
+                 : "memory");
+}
+
+// IDX: k as rows, their numbers by an index (k contiguous: the index is read once, at init).
+template <bool KROWS, bool IDX, int B, int THREADS>
+struct Feed {
+    static constexpr int W = THREADS / 64, L = B * BK * 2 / 1024 / W;  // loads of a wave a step
+    static constexpr int PITCH = KROWS ? B * 2 : BK * 2;               // bytes of an LDS row
+    static constexpr int SLOTS = PITCH / 16, ROWS = 1024 / PITCH;      // of one load
+    uint32_t at[L];
+    int32_t ids[KROWS && IDX ? L : 1];
+
+    GM_DEV static int wave() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)); }
+    GM_DEV static int row_of(int i) { return (wave() * L + i) * ROWS + (threadIdx.x & 63) / SLOTS; }
+    // first element on the contiguous axis that this lane fetches in load i
+    GM_DEV static int elem_of(int i) {
+        const int r = row_of(i), s = (threadIdx.x & 63) % SLOTS;
+        if constexpr (KROWS) return (((s >> 1) ^ swz<true>(r)) << 1 | (s & 1)) * 8;
+        return (s ^ swz<false>(r)) * 8;
+    }
+    GM_DEV void init(const Dma &d) {
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            const int r = row_of(i), x = elem_of(i);
+            if constexpr (KROWS) {
+                at[i] = x < d.valid ? (IDX ? 0u : (uint32_t)(r * d.stride)) + x * 2 : NOWHERE;
+            } else {
+                int64_t m = r;
+                bool ok = r < d.valid;
+                if (IDX && d.index && ok) {
+                    m = d.index[r];
+                    ok = m >= 0 && m < d.n_mem;
+                }
+                at[i] = ok ? (uint32_t)(m * d.stride) + x * 2 : NOWHERE;
+            }
+        }
+    }
+    // the rows' numbers of step k0
+    GM_DEV void fetch_ids(const Dma &d, int k0, int n_k) {
+        if constexpr (KROWS && IDX) {
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                const int k = k0 + row_of(i);
+                ids[i] = k < n_k ? d.index[k] : -1;
+            }
+        }
+    }
+    // load i of step k0
+    GM_DEV void issue(const Dma &d, char *lds, int k0, int n_k, int i) {
+        const char *base = d.base;
+        uint32_t records = d.records, soff = 0, v = at[i];
+        if constexpr (KROWS && IDX) {
+            const bool ok = ids[i] >= 0 && ids[i] < (int)d.n_mem && v != NOWHERE;
+            v = ok ? v + (uint32_t)ids[i] * (uint32_t)d.stride : NOWHERE;
+        } else if constexpr (KROWS) {
+            // the rows below n_k: what lies past them reads as zeros
+            const int rows = n_k - k0 < BK ? n_k - k0 : BK;
+            base += k0 * d.stride;
+            records = (uint32_t)((rows - 1) * d.stride) + d.records;
+        } else {
+            soff = (uint32_t)k0 * 2;
+            v = elem_of(i) < n_k - k0 ? v : NOWHERE;
+        }
+        load_to_lds(base, records, v, soff, lds + (wave() * L + i) * 1024);
+    }
+};
+
+// Every wave's loads into LDS have landed and its reads are done, for all waves.
+// (Loads into LDS count as memory operations that a barrier alone does not wait
+// for.)
+GM_DEV void wait_and_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// What a wave reads of an operand's tile: its fragments from row (column) x0 on.
+template <bool KROWS, int B>
+struct Reader {
+    typedef __attribute__((address_space(3))) const char lds_char;
+    uint32_t at[KROWS ? 1 : 2];  // byte offset in a tile, for each half of the step (k contiguous)
+    GM_DEV Reader(int x0) {
+        const int lane = threadIdx.x & 63, i = lane % 16, g = lane / 16;
+        if constexpr (KROWS) {
+            // row 8g + i/4 of the step's half; unit x0/16 + t (t below 8) sits at (x0/16 + t) ^ swz
+            const int k = g * 8 + i / 4;
+            at[0] = k * (B * 2) + ((x0 / 16) ^ swz<true>(k)) * 32 + (i % 4) * 8;
+        } else {
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) at[kk] = (x0 + i) * 128 + ((kk * 4 + g) ^ swz<false>(i)) * 16;
+        }
+    }
+    // fragment t (16 rows) of half kk of the tile at `tile`
+    GM_DEV u32x4 get(const char *tile, int kk, int t) const {
+        lds_char *p = (lds_char *)tile;
+        if constexpr (KROWS) {
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            p += (at[0] ^ (uint32_t)(t * 32)) + kk * 32 * (B * 2);
+            const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p));
+            const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 4 * (B * 2))));
+            return u32x4{lo[0], lo[1], hi[0], hi[1]};
+        } else {
+            typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+            return *(lds_u32x4 *)(p + at[kk] + t * 16 * 128);
+        }
+    }
+};
+
+// A tile by WP x WQ waves. A wave's share of a step is four units of (32
+// reduction elements, half of its p rows); a unit's fragments are read from LDS
+// while the one before is multiplied. The barrier stands before a step's last
+// unit, whose fragments are in registers by then, so that the buffer can be
+// filled again and the next step's first fragments read behind it. The loads
+// into LDS are spread over two units: issued together they hold every wave up
+// at the memory pipeline while the matrix units idle.
+template <typename T, typename OUT, bool PK, bool QK, bool PI, bool QI, int BP, int BQ, int WP, int WQ>
+GM_DEV void tile_fast(const Dma &p, const Dma &q, int n_k, OUT *out, int64_t out_stride, bool wide, char *lds) {
+    constexpr int THREADS = 64 * WP * WQ, MP = BP / WP, MQ = BQ / WQ, NP = MP / 32, NQ = MQ / 16;
+    constexpr int PB = BP * BK * 2, QB = BQ * BK * 2;
+    char *lp = lds, *lq = lds + 2 * PB;
+    const int lane = threadIdx.x & 63, w = threadIdx.x / 64;
+    const int p0 = w / WQ * MP, q0 = w % WQ * MQ;
+    Feed<PK, PI, BP, THREADS> fp;
+    Feed<QK, QI, BQ, THREADS> fq;
+    fp.init(p);
+    fq.init(q);
+    const Reader<PK, BP> rp(p0);
+    const Reader<QK, BQ> rq(q0);
+    f32x4 acc[2][NP][NQ] = {};
+    u32x4 a0[NP], a1[NP], b0[NQ], b1[NQ];
+    const int steps = (n_k + BK - 1) / BK;
+    auto feed_p = [&](int s, int i) { fp.issue(p, lp + (s & 1) * PB, s * BK, n_k, i); };
+    auto feed_q = [&](int s, int i) { fq.issue(q, lq + (s & 1) * QB, s * BK, n_k, i); };
+    auto read_p = [&](int s, int kk, int half, int i) { return rp.get(lp + (s & 1) * PB, kk, half * NP + i); };
+    auto read_q = [&](int s, int kk, int j) { return rq.get(lq + (s & 1) * QB, kk, j); };
+    constexpr int LP = decltype(fp)::L, LQ = decltype(fq)::L;
+    // a unit's products, row by row, with a part of what else has to be issued before each
+    auto unit = [&](int half, const u32x4(&a)[NP], const u32x4(&b)[NQ], auto &&before) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            before(i);
+#pragma unroll
+            for (int j = 0; j < NQ; ++j) acc[half][i][j] = mfma_16x16x32(b[j], a[i], acc[half][i][j], T{});
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // f(x) for the i-th of NP parts of 0 .. n
+    auto part = [&](int n, int i, auto &&f) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+            if (x < n && x * NP / n == i) f(x);
+    };
+    // more: tiles s + 1 and s + 2 are fed here, next: step s + 1 follows
+    auto step = [&](int s, auto fed, auto more, auto next) {
+        unit(0, a0, b0, [&](int i) {
+            a1[i] = read_p(s, 0, 1, i);
+            if constexpr (decltype(fed)::value) part(LQ, i, [&](int x) { feed_q(s + 1, x); });
+        });
+        if constexpr (decltype(fed)::value) fq.fetch_ids(q, (s + 2) * BK, n_k);
+        unit(1, a1, b0, [&](int i) {
+            a0[i] = read_p(s, 1, 0, i);
+            part(NQ, i, [&](int x) { b1[x] = read_q(s, 1, x); });
+        });
+        unit(0, a0, b1, [&](int i) { a1[i] = read_p(s, 1, 1, i); });
+        if constexpr (decltype(next)::value) {
+            wait_and_barrier();
+            unit(1, a1, b1, [&](int i) {
+                a0[i] = read_p(s + 1, 0, 0, i);
+                part(NQ, i, [&](int x) { b0[x] = read_q(s + 1, 0, x); });
+                if constexpr (decltype(more)::value) part(LP, i, [&](int x) { feed_p(s + 2, x); });
+            });
+            if constexpr (decltype(more)::value) fp.fetch_ids(p, (s + 3) * BK, n_k);
+        } else {
+            unit(1, a1, b1, [](int) {});
+        }
+    };
+    wait_and_barrier();  // (the last tile's reads of LDS)
+    if (steps > 0) {
+        fp.fetch_ids(p, 0, n_k);
+        fq.fetch_ids(q, 0, n_k);
+#pragma unroll
+        for (int x = 0; x < LP; ++x) feed_p(0, x);
+#pragma unroll
+        for (int x = 0; x < LQ; ++x) feed_q(0, x);
+        fp.fetch_ids(p, BK, n_k);
+        fq.fetch_ids(q, BK, n_k);
+        wait_and_barrier();
+        if (steps > 1) {
+#pragma unroll
+            for (int x = 0; x < LP; ++x) feed_p(1, x);
+            fp.fetch_ids(p, 2 * BK, n_k);
+        }
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) b0[j] = read_q(0, 0, j);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) a0[i] = read_p(0, 0, 0, i);
+        const std::true_type yes;
+        const std::false_type no;
+        for (int s = 0; s < steps - 2; ++s) step(s, yes, yes, yes);
+        if (steps > 1) step(steps - 2, yes, no, yes);
+        step(steps - 1, no, no, no);
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * NP; ++i) {
+        const int r = p0 + 16 * i + lane % 16;
+        if (r < p.valid) {
+#pragma unroll
+            for (int j = 0; j < NQ; ++j) {
+                const int c = q0 + 16 * j + lane / 16 * 4;
+                store4(out + r * out_stride + c, acc[i / NP][i % NP][j], q.valid - c, wide);
+            }
+        }
+    }
+}
+
 struct ProductArgs {
     const int64_t *gp;
     const int32_t *index;
@@ -188,6 +431,36 @@ __global__ __launch_bounds__(GEN_T) void k_group_product_any(ProductArgs a) {
     }
 }
 
+template <typename T, typename OUT, bool TRANS, int BP, int BQ, int WP, int WQ>
+__global__ __launch_bounds__(64 * WP * WQ) void k_group_product_fast(ProductArgs a) {
+    extern __shared__ char lds_fast[];
+    const int64_t n_row = min(count_row_tiles<BP>(a.gp, a.n_groups, a.n_rows), a.max_row_tiles);
+    const int64_t n_col = (a.n + BQ - 1) / BQ, total = n_row * n_col;
+    for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
+        int64_t tr, tc;
+        band_tile(xcd_tile(b, total), n_row, n_col, tr, tc);
+        const RowTile t = find_row_tile<BP>(a.gp, a.n_groups, a.n_rows, tr);
+        const int64_t q0 = tc * BQ;
+        const int cols = (int)(a.n - q0 < BQ ? a.n - q0 : BQ);
+        OUT *out = static_cast<OUT *>(a.y) + t.begin * a.ys + q0;
+        if (t.group >= a.n_groups) {
+            zero_tile(out, a.ys, t.rows, cols);
+            continue;
+        }
+        Dma p{static_cast<const char *>(a.x), (uint32_t)(((a.n_x - 1) * a.xs + a.k) * 2), a.xs * 2, nullptr, a.n_x, t.rows};
+        if (a.index) {
+            p.index = a.index + t.begin;
+        } else {
+            p.base += t.begin * p.stride;
+            p.records = (uint32_t)((t.rows - 1) * p.stride + a.k * 2);
+        }
+        const char *w = static_cast<const char *>(a.w) + (t.group * a.wg + (TRANS ? q0 : q0 * a.ws)) * 2;
+        const uint32_t wb = (uint32_t)(TRANS ? cols * 2 : ((cols - 1) * a.ws + a.k) * 2);
+        const Dma q{w, wb, a.ws * 2, nullptr, 0, cols};
+        tile_fast<T, OUT, false, TRANS, true, false, BP, BQ, WP, WQ>(p, q, (int)a.k, out, a.ys, a.wide, lds_fast);
+    }
+}
+
 struct OuterArgs {
     const int64_t *gp;
     const int32_t *index;
@@ -198,15 +471,35 @@ struct OuterArgs {
     bool wide;
 };
 
+// Tile t of the stack of gradients: its group, tile row and tile column. A tile
+// costs as much as its group has rows, so of each 64 groups the longest come
+// first and the last work groups to start have little to do; a group's tiles
+// are spread over the XCDs, neighbours together (measured on 16 groups of 16384
+// rows cut at random, 2048 x 2048, against groups in order with a run of them
+// for each XCD: see the kernels below).
+GM_DEV void outer_tile(const OuterArgs &a, int64_t t, int64_t n_row, int64_t n_col, int64_t &e, int64_t &tr, int64_t &tc) {
+    const int64_t per = n_row * n_col, place = t / per, e0 = place / GM_WAVE * GM_WAVE;
+    const int lane = threadIdx.x & 63, want = (int)(place - e0);
+    int64_t b = 0, f = -1;
+    if (e0 + lane < a.n_groups) group_rows(a.gp, a.n_groups, a.n_rows, e0 + lane, b, f);
+    const int size = (int)(f - b);  // (lanes past the last group: -1, after all others)
+    int rank = 0;
+    for (int o = 0; o < GM_WAVE; ++o) {
+        const int other = __builtin_amdgcn_readlane(size, o);
+        rank += other > size || (other == size && o < lane);
+    }
+    e = e0 + __ffsll((unsigned long long)ballot(rank == want)) - 1;
+    band_tile(xcd_tile(t - place * per, per), n_row, n_col, tr, tc);
+}
+
 template <typename T, typename OUT>
 __global__ __launch_bounds__(GEN_T) void k_group_outer_any(OuterArgs a) {
     __shared__ u32x4 lds[2 * GEN_B * BK / 8];
     const int64_t n_row = (a.n + GEN_B - 1) / GEN_B, n_col = (a.k + GEN_B - 1) / GEN_B;
     const int64_t per = n_row * n_col, total = per * a.n_groups;
     for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
-        const int64_t t = xcd_tile(b, total), e = t / per;
-        int64_t tr, tc, begin, end;
-        band_tile(t - e * per, n_row, n_col, tr, tc);
+        int64_t e, tr, tc, begin, end;
+        outer_tile(a, b, n_row, n_col, e, tr, tc);
         group_rows(a.gp, a.n_groups, a.n_rows, e, begin, end);
         const int64_t p0 = tr * GEN_B, q0 = tc * GEN_B;
         const Side p{static_cast<const T *>(a.dy) + begin * a.dys + p0, a.dys, nullptr, 0,
@@ -231,6 +524,50 @@ void with_elem(int32_t type, int32_t out, F &&f) {
     } else {
         if (out == GMAGNUS_DATA_FP32) f(_Float16{}, float{}); else f(_Float16{}, _Float16{});
     }
+}
+
+template <typename T, typename OUT, bool IDX, int BP, int BQ, int WP, int WQ>
+__global__ __launch_bounds__(64 * WP * WQ) void k_group_outer_fast(OuterArgs a) {
+    extern __shared__ char lds_fast[];
+    const int64_t n_row = (a.n + BP - 1) / BP, n_col = (a.k + BQ - 1) / BQ;
+    const int64_t per = n_row * n_col, total = per * a.n_groups;
+    for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
+        int64_t e, tr, tc, begin, end;
+        outer_tile(a, b, n_row, n_col, e, tr, tc);
+        group_rows(a.gp, a.n_groups, a.n_rows, e, begin, end);
+        const int64_t p0 = tr * BP, q0 = tc * BQ;
+        const int pv = (int)(a.n - p0 < BP ? a.n - p0 : BP), qv = (int)(a.k - q0 < BQ ? a.k - q0 : BQ);
+        const Dma p{static_cast<const char *>(a.dy) + (begin * a.dys + p0) * 2, (uint32_t)(pv * 2), a.dys * 2, nullptr, 0, pv};
+        Dma q{static_cast<const char *>(a.x) + q0 * 2, (uint32_t)(qv * 2), a.xs * 2, nullptr, a.n_x, qv};
+        if constexpr (IDX) {
+            q.index = a.index + begin;
+            q.records = (uint32_t)((a.n_x - 1) * q.stride + qv * 2);
+        } else {
+            q.base += begin * q.stride;
+        }
+        OUT *out = static_cast<OUT *>(a.d) + e * a.dg + p0 * a.ds + q0;
+        tile_fast<T, OUT, true, true, false, IDX, BP, BQ, WP, WQ>(p, q, (int)(end - begin), out, a.ds, a.wide, lds_fast);
+    }
+}
+
+// Whether an operand's rows can be brought in by 16-byte pieces, with 32-bit
+// offsets over `rows` rows.
+bool fast_side(const void *p, int64_t stride, int64_t stack, int64_t axis, int64_t rows) {
+    return aligned16(p, stride, stack, 2) && axis % 8 == 0 && (rows * stride + axis) * 2 < (int64_t)NOWHERE;
+}
+
+// 256 x 256 tiles (one work group a CU, the fewest bytes a product) where about as
+// many as CUs come out of `n_groups` outputs of m x n and rows are not mostly
+// padding, else 128 x 128 (two a CU).
+bool big_tiles(int64_t m, int64_t n, int64_t n_groups) {
+    const int64_t tiles = (m + 255) / 256 * ((n + 255) / 256);
+    return m >= 384 && (tiles >= 192 || tiles * n_groups >= 192);
+}
+
+template <typename K, typename A>
+void launch_fast(K kernel, int64_t tiles, int threads, int lds, const A &a, hipStream_t s) {
+    allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles < MAX_GRID ? tiles : MAX_GRID)), dim3(threads), lds, s, a);
 }
 
 }  // namespace
@@ -262,6 +599,31 @@ extern "C" gmagnus_status_t gmagnus_group_product(const gmagnus_groups_t *groups
                             X->data, W->data, Y->data, X->row_stride, W->row_stride, W->stack_stride, Y->row_stride,
                             aligned16(Y->data, Y->row_stride, 0, data_size(Y->data_type)), row_tiles};
         hipStream_t s = (hipStream_t)hip_stream;
+        if (fast_side(a.x, a.xs, 0, k, a.index ? a.n_x : 256) &&
+            fast_side(a.w, a.ws, groups->n_groups > 1 ? a.wg : 0, transposed ? n : k, 256)) {
+            const bool big = big_tiles(a.n_rows / a.n_groups, n, a.n_groups);
+            with_elem(X->data_type, Y->data_type, [&](auto t, auto o) {
+                using T = decltype(t);
+                using O = decltype(o);
+                auto go = [&](auto trans) {
+                    constexpr bool TR = decltype(trans)::value;
+                    ProductArgs f = a;
+                    if (big) {
+                        f.max_row_tiles = row_tiles_bound(a.n_groups, a.n_rows, 256);
+                        launch_fast(k_group_product_fast<T, O, TR, 256, 256, 2, 4>, f.max_row_tiles * ((n + 255) / 256), 512, 131072, f, s);
+                    } else {
+                        f.max_row_tiles = row_tiles_bound(a.n_groups, a.n_rows, 128);
+                        launch_fast(k_group_product_fast<T, O, TR, 128, 128, 2, 2>, f.max_row_tiles * ((n + 127) / 128), 256, 65536, f, s);
+                    }
+                };
+                if (transposed)
+                    go(std::true_type{});
+                else
+                    go(std::false_type{});
+            });
+            GM_CHECK_LAUNCH();
+            return;
+        }
         const int64_t tiles = row_tiles * ((n + GEN_B - 1) / GEN_B);
         const dim3 grid((unsigned)(tiles < MAX_GRID ? tiles : MAX_GRID));
         with_elem(X->data_type, Y->data_type, [&](auto t, auto o) {
@@ -298,6 +660,26 @@ extern "C" gmagnus_status_t gmagnus_group_outer(const gmagnus_groups_t *groups, 
                           DY->data, X->data, D->data, DY->row_stride, X->row_stride, D->row_stride, D->stack_stride,
                           aligned16(D->data, D->row_stride, D->stack_stride, data_size(D->data_type))};
         hipStream_t s = (hipStream_t)hip_stream;
+        if (fast_side(a.dy, a.dys, 0, n, BK) && fast_side(a.x, a.xs, 0, k, a.index ? a.n_x : BK)) {
+            const bool big = big_tiles(n, k, a.n_groups);
+            with_elem(X->data_type, D->data_type, [&](auto t, auto o) {
+                using T = decltype(t);
+                using O = decltype(o);
+                auto go = [&](auto idx) {
+                    constexpr bool IX = decltype(idx)::value;
+                    if (big)
+                        launch_fast(k_group_outer_fast<T, O, IX, 256, 256, 2, 4>, (n + 255) / 256 * ((k + 255) / 256) * a.n_groups, 512, 131072, a, s);
+                    else
+                        launch_fast(k_group_outer_fast<T, O, IX, 128, 128, 2, 2>, (n + 127) / 128 * ((k + 127) / 128) * a.n_groups, 256, 65536, a, s);
+                };
+                if (a.index)
+                    go(std::true_type{});
+                else
+                    go(std::false_type{});
+            });
+            GM_CHECK_LAUNCH();
+            return;
+        }
         const int64_t tiles = ((n + GEN_B - 1) / GEN_B) * ((k + GEN_B - 1) / GEN_B);
         const int64_t total = tiles > MAX_GRID / a.n_groups ? MAX_GRID : tiles * a.n_groups;
         with_elem(X->data_type, D->data_type, [&](auto t, auto o) {
