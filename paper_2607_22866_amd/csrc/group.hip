@@ -10,21 +10,10 @@
 // operand, so that a lane's four results are neighbours on the q axis.
 #include <type_traits>
 
-#include "dense.hpp"
+#include "tile.hpp"
 
 namespace gm {
 namespace {
-
-constexpr int BK = 64;  // reduction elements a step
-
-// LDS layout of an operand tile, in 16-byte chunks (8 elements).
-// k contiguous: 128-byte rows; chunk c of row r sits at c ^ swz(r).
-// k as rows: rows of B elements; 32-byte unit u of row k sits at u ^ swz(k).
-// Either swizzle spreads the chunks that a wave reads at once over the banks.
-template <bool KROWS>
-GM_DEV int swz(int r) {
-    return KROWS ? (r & 3) | ((r >> 3) & 1) << 2 : (r >> 1) & 7;
-}
 
 // ---------------------------------------------------------------- any layout
 // Tiles staged through registers: any alignment and stride. 128 x 128 tiles, four waves
@@ -152,140 +141,6 @@ GM_DEV void tile_any(const Side &p, const Side &q, int64_t n_k, OUT *out, int64_
     }
 }
 
-// ---------------------------------------------------------------- fast layout
-// Tiles brought straight from memory into LDS, 16 bytes a lane, for operands
-// whose rows are 16-byte aligned and whose contiguous axis is a multiple of 8.
-// LDS positions follow the lane order, so the swizzle is applied to what a lane
-// fetches. Two buffers: while the matrix units work on one step's tile the next
-// one is on its way.
-struct Dma {
-    const char *base;   // of the tile
-    uint32_t records;   // bytes that may be read from base (k as rows without an index: of one row)
-    int64_t stride;     // bytes between rows
-    const int32_t *index;
-    int64_t n_mem;
-    int valid;
-};
-
-constexpr uint32_t NOWHERE = 0x80000000u;  // beyond any operand's bytes: reads as zeros
-
-// Lane l's 16 bytes at base + soff + v go to LDS at `to` + 16 l; zeros where v is not
-// below `records`. An instruction without results: the compiler, which would
-// wait for it before every transposing read of LDS, counts no load, and
-// wait_and_barrier() is what waits.
-GM_DEV void load_to_lds(const char *base, uint32_t records, uint32_t v, uint32_t soff, char *to) {
-    typedef __attribute__((address_space(3))) char lds_char;
-    const uint64_t b = (uint64_t)base;
-    const u32x4 rsrc = {(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, records, 0x00027000u};
-    const uint32_t m0 = (uint32_t)(uintptr_t)(lds_char *)to;
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 :
-                 : "s"(m0), "v"(v), "s"(rsrc), "s"(soff)
-                 : "memory");
-}
-
-// IDX: k as rows, their numbers by an index (k contiguous: the index is read once, at init).
-template <bool KROWS, bool IDX, int B, int THREADS>
-struct Feed {
-    static constexpr int W = THREADS / 64, L = B * BK * 2 / 1024 / W;  // loads of a wave a step
-    static constexpr int PITCH = KROWS ? B * 2 : BK * 2;               // bytes of an LDS row
-    static constexpr int SLOTS = PITCH / 16, ROWS = 1024 / PITCH;      // of one load
-    uint32_t at[L];
-    int32_t ids[KROWS && IDX ? L : 1];
-
-    GM_DEV static int wave() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)); }
-    GM_DEV static int row_of(int i) { return (wave() * L + i) * ROWS + (threadIdx.x & 63) / SLOTS; }
-    // first element on the contiguous axis that this lane fetches in load i
-    GM_DEV static int elem_of(int i) {
-        const int r = row_of(i), s = (threadIdx.x & 63) % SLOTS;
-        if constexpr (KROWS) return (((s >> 1) ^ swz<true>(r)) << 1 | (s & 1)) * 8;
-        return (s ^ swz<false>(r)) * 8;
-    }
-    GM_DEV void init(const Dma &d) {
-#pragma unroll
-        for (int i = 0; i < L; ++i) {
-            const int r = row_of(i), x = elem_of(i);
-            if constexpr (KROWS) {
-                at[i] = x < d.valid ? (IDX ? 0u : (uint32_t)(r * d.stride)) + x * 2 : NOWHERE;
-            } else {
-                int64_t m = r;
-                bool ok = r < d.valid;
-                if (IDX && d.index && ok) {
-                    m = d.index[r];
-                    ok = m >= 0 && m < d.n_mem;
-                }
-                at[i] = ok ? (uint32_t)(m * d.stride) + x * 2 : NOWHERE;
-            }
-        }
-    }
-    // the rows' numbers of step k0
-    GM_DEV void fetch_ids(const Dma &d, int k0, int n_k) {
-        if constexpr (KROWS && IDX) {
-#pragma unroll
-            for (int i = 0; i < L; ++i) {
-                const int k = k0 + row_of(i);
-                ids[i] = k < n_k ? d.index[k] : -1;
-            }
-        }
-    }
-    // load i of step k0
-    GM_DEV void issue(const Dma &d, char *lds, int k0, int n_k, int i) {
-        const char *base = d.base;
-        uint32_t records = d.records, soff = 0, v = at[i];
-        if constexpr (KROWS && IDX) {
-            const bool ok = ids[i] >= 0 && ids[i] < (int)d.n_mem && v != NOWHERE;
-            v = ok ? v + (uint32_t)ids[i] * (uint32_t)d.stride : NOWHERE;
-        } else if constexpr (KROWS) {
-            // the rows below n_k: what lies past them reads as zeros
-            const int rows = n_k - k0 < BK ? n_k - k0 : BK;
-            base += k0 * d.stride;
-            records = (uint32_t)((rows - 1) * d.stride) + d.records;
-        } else {
-            soff = (uint32_t)k0 * 2;
-            v = elem_of(i) < n_k - k0 ? v : NOWHERE;
-        }
-        load_to_lds(base, records, v, soff, lds + (wave() * L + i) * 1024);
-    }
-};
-
-// Every wave's loads into LDS have landed and its reads are done, for all waves.
-// (Loads into LDS count as memory operations that a barrier alone does not wait
-// for.)
-GM_DEV void wait_and_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-
-// What a wave reads of an operand's tile: its fragments from row (column) x0 on.
-template <bool KROWS, int B>
-struct Reader {
-    typedef __attribute__((address_space(3))) const char lds_char;
-    uint32_t at[KROWS ? 1 : 2];  // byte offset in a tile, for each half of the step (k contiguous)
-    GM_DEV Reader(int x0) {
-        const int lane = threadIdx.x & 63, i = lane % 16, g = lane / 16;
-        if constexpr (KROWS) {
-            // row 8g + i/4 of the step's half; unit x0/16 + t (t below 8) sits at (x0/16 + t) ^ swz
-            const int k = g * 8 + i / 4;
-            at[0] = k * (B * 2) + ((x0 / 16) ^ swz<true>(k)) * 32 + (i % 4) * 8;
-        } else {
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) at[kk] = (x0 + i) * 128 + ((kk * 4 + g) ^ swz<false>(i)) * 16;
-        }
-    }
-    // fragment t (16 rows) of half kk of the tile at `tile`
-    GM_DEV u32x4 get(const char *tile, int kk, int t) const {
-        lds_char *p = (lds_char *)tile;
-        if constexpr (KROWS) {
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            p += (at[0] ^ (uint32_t)(t * 32)) + kk * 32 * (B * 2);
-            const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p));
-            const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 4 * (B * 2))));
-            return u32x4{lo[0], lo[1], hi[0], hi[1]};
-        } else {
-            typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
-            return *(lds_u32x4 *)(p + at[kk] + t * 16 * 128);
-        }
-    }
-};
-
 // A tile by WP x WQ waves. A wave's share of a step is four units of (32
 // reduction elements, half of its p rows); a unit's fragments are read from LDS
 // while the one before is multiplied. The barrier stands before a step's last
@@ -298,7 +153,7 @@ GM_DEV void tile_fast(const Dma &p, const Dma &q, int n_k, OUT *out, int64_t out
     constexpr int THREADS = 64 * WP * WQ, MP = BP / WP, MQ = BQ / WQ, NP = MP / 32, NQ = MQ / 16;
     constexpr int PB = BP * BK * 2, QB = BQ * BK * 2;
     char *lp = lds, *lq = lds + 2 * PB;
-    const int lane = threadIdx.x & 63, w = threadIdx.x / 64;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
     const int p0 = w / WQ * MP, q0 = w % WQ * MQ;
     Feed<PK, PI, BP, THREADS> fp;
     Feed<QK, QI, BQ, THREADS> fq;
@@ -330,56 +185,44 @@ GM_DEV void tile_fast(const Dma &p, const Dma &q, int n_k, OUT *out, int64_t out
         for (int x = 0; x < 16; ++x)
             if (x < n && x * NP / n == i) f(x);
     };
-    // more: tiles s + 1 and s + 2 are fed here, next: step s + 1 follows
-    auto step = [&](int s, auto fed, auto more, auto next) {
+    wait_and_barrier();  // (the last tile's reads of LDS)
+    fp.fetch_ids(p, 0, n_k);
+    fq.fetch_ids(q, 0, n_k);
+#pragma unroll
+    for (int x = 0; x < LP; ++x) feed_p(0, x);
+#pragma unroll
+    for (int x = 0; x < LQ; ++x) feed_q(0, x);
+    fp.fetch_ids(p, BK, n_k);
+    fq.fetch_ids(q, BK, n_k);
+    wait_and_barrier();
+#pragma unroll
+    for (int x = 0; x < LP; ++x) feed_p(1, x);
+    fp.fetch_ids(p, 2 * BK, n_k);
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) b0[j] = read_q(0, 0, j);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) a0[i] = read_p(0, 0, 0, i);
+    // Steps past the last are fed as zeros and their fragments never used: one body for all steps.
+    for (int s = 0; s < steps; ++s) {
         unit(0, a0, b0, [&](int i) {
             a1[i] = read_p(s, 0, 1, i);
-            if constexpr (decltype(fed)::value) part(LQ, i, [&](int x) { feed_q(s + 1, x); });
+            part(LQ, i, [&](int x) { feed_q(s + 1, x); });
         });
-        if constexpr (decltype(fed)::value) fq.fetch_ids(q, (s + 2) * BK, n_k);
+        fq.fetch_ids(q, (s + 2) * BK, n_k);
         unit(1, a1, b0, [&](int i) {
             a0[i] = read_p(s, 1, 0, i);
             part(NQ, i, [&](int x) { b1[x] = read_q(s, 1, x); });
         });
         unit(0, a0, b1, [&](int i) { a1[i] = read_p(s, 1, 1, i); });
-        if constexpr (decltype(next)::value) {
-            wait_and_barrier();
-            unit(1, a1, b1, [&](int i) {
-                a0[i] = read_p(s + 1, 0, 0, i);
-                part(NQ, i, [&](int x) { b0[x] = read_q(s + 1, 0, x); });
-                if constexpr (decltype(more)::value) part(LP, i, [&](int x) { feed_p(s + 2, x); });
-            });
-            if constexpr (decltype(more)::value) fp.fetch_ids(p, (s + 3) * BK, n_k);
-        } else {
-            unit(1, a1, b1, [](int) {});
-        }
-    };
-    wait_and_barrier();  // (the last tile's reads of LDS)
-    if (steps > 0) {
-        fp.fetch_ids(p, 0, n_k);
-        fq.fetch_ids(q, 0, n_k);
-#pragma unroll
-        for (int x = 0; x < LP; ++x) feed_p(0, x);
-#pragma unroll
-        for (int x = 0; x < LQ; ++x) feed_q(0, x);
-        fp.fetch_ids(p, BK, n_k);
-        fq.fetch_ids(q, BK, n_k);
         wait_and_barrier();
-        if (steps > 1) {
-#pragma unroll
-            for (int x = 0; x < LP; ++x) feed_p(1, x);
-            fp.fetch_ids(p, 2 * BK, n_k);
-        }
-#pragma unroll
-        for (int j = 0; j < NQ; ++j) b0[j] = read_q(0, 0, j);
-#pragma unroll
-        for (int i = 0; i < NP; ++i) a0[i] = read_p(0, 0, 0, i);
-        const std::true_type yes;
-        const std::false_type no;
-        for (int s = 0; s < steps - 2; ++s) step(s, yes, yes, yes);
-        if (steps > 1) step(steps - 2, yes, no, yes);
-        step(steps - 1, no, no, no);
+        unit(1, a1, b1, [&](int i) {
+            a0[i] = read_p(s + 1, 0, 0, i);
+            part(NQ, i, [&](int x) { b0[x] = read_q(s + 1, 0, x); });
+            part(LP, i, [&](int x) { feed_p(s + 2, x); });
+        });
+        fp.fetch_ids(p, (s + 3) * BK, n_k);
     }
+    wait_and_barrier();  // (no load may be on its way to LDS when the work group ends)
 #pragma unroll
     for (int i = 0; i < 2 * NP; ++i) {
         const int r = p0 + 16 * i + lane % 16;
@@ -432,7 +275,7 @@ __global__ __launch_bounds__(GEN_T) void k_group_product_any(ProductArgs a) {
 }
 
 template <typename T, typename OUT, bool TRANS, int BP, int BQ, int WP, int WQ>
-__global__ __launch_bounds__(64 * WP * WQ) void k_group_product_fast(ProductArgs a) {
+__global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_product_fast(ProductArgs a) {
     extern __shared__ char lds_fast[];
     const int64_t n_row = min(count_row_tiles<BP>(a.gp, a.n_groups, a.n_rows), a.max_row_tiles);
     const int64_t n_col = (a.n + BQ - 1) / BQ, total = n_row * n_col;
@@ -527,7 +370,7 @@ void with_elem(int32_t type, int32_t out, F &&f) {
 }
 
 template <typename T, typename OUT, bool IDX, int BP, int BQ, int WP, int WQ>
-__global__ __launch_bounds__(64 * WP * WQ) void k_group_outer_fast(OuterArgs a) {
+__global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_outer_fast(OuterArgs a) {
     extern __shared__ char lds_fast[];
     const int64_t n_row = (a.n + BP - 1) / BP, n_col = (a.k + BQ - 1) / BQ;
     const int64_t per = n_row * n_col, total = per * a.n_groups;
@@ -548,26 +391,6 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_group_outer_fast(OuterArgs a) 
         OUT *out = static_cast<OUT *>(a.d) + e * a.dg + p0 * a.ds + q0;
         tile_fast<T, OUT, true, true, false, IDX, BP, BQ, WP, WQ>(p, q, (int)(end - begin), out, a.ds, a.wide, lds_fast);
     }
-}
-
-// Whether an operand's rows can be brought in by 16-byte pieces, with 32-bit
-// offsets over `rows` rows.
-bool fast_side(const void *p, int64_t stride, int64_t stack, int64_t axis, int64_t rows) {
-    return aligned16(p, stride, stack, 2) && axis % 8 == 0 && (rows * stride + axis) * 2 < (int64_t)NOWHERE;
-}
-
-// 256 x 256 tiles (one work group a CU, the fewest bytes a product) where about as
-// many as CUs come out of `n_groups` outputs of m x n and rows are not mostly
-// padding, else 128 x 128 (two a CU).
-bool big_tiles(int64_t m, int64_t n, int64_t n_groups) {
-    const int64_t tiles = (m + 255) / 256 * ((n + 255) / 256);
-    return m >= 384 && (tiles >= 192 || tiles * n_groups >= 192);
-}
-
-template <typename K, typename A>
-void launch_fast(K kernel, int64_t tiles, int threads, int lds, const A &a, hipStream_t s) {
-    allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles < MAX_GRID ? tiles : MAX_GRID)), dim3(threads), lds, s, a);
 }
 
 }  // namespace

@@ -3,7 +3,7 @@
 //   Y[r,n] = sum over blocks b of sx[r,b] * sw[n/128,b] * (sum over k in b of x[r,k] * w[n,k])
 // A step of the reduction is one block, so its sum leaves the matrix unit
 // unscaled and is scaled as it joins the fp32 result.
-#include "dense.hpp"
+#include "tile.hpp"
 
 namespace gm {
 namespace {
@@ -116,11 +116,11 @@ __global__ __launch_bounds__(256) void k_quantise_tiles(QuantArgs a) {
 // ------------------------------------------------------------------ product
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// 16x16x128 on E4M3 operands, block scales of one (exponent byte 127).
+// 16x16x128 on E4M3 operands (without the unit's own scales).
 GM_DEV f32x4 mfma_fp8(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b1, f32x4 c) {
     const i32x8 a = {(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3], (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
     const i32x8 b = {(int)b0[0], (int)b0[1], (int)b0[2], (int)b0[3], (int)b1[0], (int)b1[1], (int)b1[2], (int)b1[3]};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
 }
 
 struct Fp8Args {
@@ -246,6 +246,161 @@ __global__ __launch_bounds__(GEN_T) void k_group_product_fp8_any(Fp8Args a) {
     }
 }
 
+// Tiles brought straight from memory into LDS, as the 16-bit products have
+// them (tile.hpp): a step is one block of 128 bytes a row. A wave takes its p
+// rows 16 at a time against its 64 q columns. What the matrix units return for
+// a block goes into the fp32 sums with the row's scale times the column
+// block's, on the vector units while the other wave of the SIMD multiplies. The
+// scales of X's rows come with their tile, 64 rows by each of the first waves.
+template <int BP, int BQ>
+constexpr int fast_lds() { return 2 * ((BP + BQ) * SB + (BP + 64) * 4); }
+
+template <typename OUT, int BP, int BQ, int WP, int WQ>
+GM_DEV void tile_fp8_fast(const Fp8Args &a, const RowTile &t, int64_t n0, int cols, char *lds) {
+    constexpr int THREADS = 64 * WP * WQ, MP = BP / WP, MQ = BQ / WQ, NP = MP / 16, NQ = MQ / 16;
+    static_assert(NP % 2 == 0, "units alternate between two sets of fragments");
+    constexpr int PB = BP * SB, QB = BQ * SB;
+    char *lp = lds, *lq = lds + 2 * PB;
+    float *ls = reinterpret_cast<float *>(lds + 2 * PB + 2 * QB);
+    const int lane = threadIdx.x & 63, i16 = lane % 16, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
+    const int p0 = w / WQ * MP, q0 = w % WQ * MQ;
+    Dma p{reinterpret_cast<const char *>(a.x), (uint32_t)((a.n_x - 1) * a.xs + a.k), a.xs, nullptr, a.n_x, t.rows};
+    if (a.index) {
+        p.index = a.index + t.begin;
+    } else {
+        p.base += t.begin * a.xs;
+        p.records = (uint32_t)((t.rows - 1) * a.xs + a.k);
+    }
+    const Dma q{reinterpret_cast<const char *>(a.w) + t.group * a.wg + n0 * a.ws, (uint32_t)((cols - 1) * a.ws + a.k), a.ws,
+                nullptr, 0, cols};
+    // The step's scales come as single values: a row's to each thread of the first
+    // BP / 64 waves, the column blocks' to the next waves (which repeat each other:
+    // a branch around them would split the loop's body, and the compiler would move
+    // the sums past it, out of the units).
+    constexpr int SR = BP + 64;  // BP rows' scales, then the column blocks'
+    const int kb = (int)((a.k + SB - 1) / SB);
+    const bool row_wave = w < BP / 64;
+    const float *s_base = row_wave ? a.sx : a.sw + t.group * a.swg + n0 / SB * a.sws;
+    const int s_blocks = (cols + SB - 1) / SB;
+    const uint32_t s_records = (uint32_t)(((row_wave ? a.n_x - 1 : s_blocks - 1) * (row_wave ? a.sxs : a.sws) + kb) * 4);
+    uint32_t sat = NOWHERE;
+    if (row_wave && (int)threadIdx.x < t.rows) {
+        const int64_t r = a.index ? a.index[t.begin + threadIdx.x] : t.begin + threadIdx.x;
+        if (r >= 0 && r < a.n_x) sat = (uint32_t)(r * a.sxs * 4);
+    } else if (!row_wave && lane < s_blocks) {
+        sat = (uint32_t)(lane * a.sws * 4);
+    }
+    const int n_k = (int)(a.k / 2), steps = (n_k + BK - 1) / BK;  // (in pairs of bytes, as Feed counts)
+    Feed<false, true, BP, THREADS> fp;
+    Feed<false, false, BQ, THREADS> fq;
+    fp.init(p);
+    fq.init(q);
+    const Reader<false, BP> rp(p0);
+    const Reader<false, BQ> rq(q0);
+    constexpr int LP = decltype(fp)::L, LQ = decltype(fq)::L;
+    f32x4 acc[NP][NQ] = {};
+    u32x4 a0[2], a1[2], b[NQ][2];
+    float c0, c1;
+    auto feed_p = [&](int s, int i) { fp.issue(p, lp + (s & 1) * PB, s * BK, n_k, i); };
+    auto feed_q = [&](int s, int i) { fq.issue(q, lq + (s & 1) * QB, s * BK, n_k, i); };
+    auto read_p = [&](int s, int u, u32x4(&f)[2], float &c) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) f[h] = rp.get(lp + (s & 1) * PB, h, u);
+        c = ls[(s & 1) * SR + p0 + 16 * u + i16];
+    };
+    auto read_q = [&](int s, int j) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) b[j][h] = rq.get(lq + (s & 1) * QB, h, j);
+    };
+    auto feed_scales = [&](int s) {
+        load_to_lds<4>(s_base, s_records, sat, (uint32_t)s * 4, ls + (s & 1) * SR + (row_wave ? w : BP / 64) * 64);
+    };
+    auto read_sq = [&](int s) { return ls[(s & 1) * SR + BP + q0 / SB]; };
+    // a unit's products column by column, with a part of what else has to be issued after each
+    auto unit = [&](int u, const u32x4(&f)[2], float sc, auto &&after) {
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) {
+            const f32x4 d = mfma_fp8(b[j][0], b[j][1], f[0], f[1], f32x4{0, 0, 0, 0});
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[u][j][e] += sc * d[e];
+            after(j);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    wait_and_barrier();  // (the last tile's reads of LDS)
+#pragma unroll
+    for (int x = 0; x < LP; ++x) feed_p(0, x);
+#pragma unroll
+    for (int x = 0; x < LQ; ++x) feed_q(0, x);
+    feed_scales(0);
+    wait_and_barrier();
+#pragma unroll
+    for (int x = 0; x < LP; ++x) feed_p(1, x);
+    feed_scales(1);
+    read_p(0, 0, a0, c0);
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) read_q(0, j);
+    float sq = read_sq(0);
+    // Steps past the last are fed as zeros and their fragments never used: one body for all steps.
+    for (int s = 0; s < steps; ++s) {
+#pragma unroll
+        for (int u = 0; u + 2 < NP; u += 2) {
+            read_p(s, u + 1, a1, c1);
+            unit(u, a0, c0 * sq, [&](int j) {
+#pragma unroll
+                for (int x = 0; x < LQ; ++x)
+                    if (u == 0 && x * NQ / LQ == j) feed_q(s + 1, x);
+            });
+            read_p(s, u + 2, a0, c0);
+            unit(u + 1, a1, c1 * sq, [](int) {});
+        }
+        read_p(s, NP - 1, a1, c1);
+        unit(NP - 2, a0, c0 * sq, [](int) {});
+        wait_and_barrier();
+        feed_scales(s + 2);
+        read_p(s + 1, 0, a0, c0);
+        const float sn = read_sq(s + 1);
+        unit(NP - 1, a1, c1 * sq, [&](int j) {
+            read_q(s + 1, j);
+#pragma unroll
+            for (int x = 0; x < LP; ++x)
+                if (x * NQ / LP == j) feed_p(s + 2, x);
+        });
+        sq = sn;
+    }
+    wait_and_barrier();  // (no load may be on its way to LDS when the work group ends)
+    OUT *out = static_cast<OUT *>(a.y) + t.begin * a.ys + n0;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int r = p0 + 16 * i + i16;
+        if (r < t.rows) {
+#pragma unroll
+            for (int j = 0; j < NQ; ++j) {
+                const int c = q0 + 16 * j + lane / 16 * 4;
+                store4(out + r * a.ys + c, acc[i][j], cols - c, a.wide);
+            }
+        }
+    }
+}
+
+template <typename OUT, int BP, int BQ, int WP, int WQ>
+__global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_product_fp8_fast(Fp8Args a) {
+    extern __shared__ char lds_fast[];
+    const int64_t n_row = min(count_row_tiles<BP>(a.gp, a.n_groups, a.n_rows), a.max_row_tiles);
+    const int64_t n_col = (a.n + BQ - 1) / BQ, total = n_row * n_col;
+    for (int64_t blk = blockIdx.x; blk < total; blk += gridDim.x) {
+        int64_t tr, tc;
+        band_tile(xcd_tile(blk, total), n_row, n_col, tr, tc);
+        const RowTile t = find_row_tile<BP>(a.gp, a.n_groups, a.n_rows, tr);
+        const int64_t n0 = tc * BQ;
+        const int cols = (int)(a.n - n0 < BQ ? a.n - n0 : BQ);
+        if (t.group >= a.n_groups)
+            zero_tile(static_cast<OUT *>(a.y) + t.begin * a.ys + n0, a.ys, t.rows, cols);
+        else
+            tile_fp8_fast<OUT, BP, BQ, WP, WQ>(a, t, n0, cols, lds_fast);
+    }
+}
+
 }  // namespace
 }  // namespace gm
 
@@ -320,14 +475,32 @@ extern "C" gmagnus_status_t gmagnus_group_product_fp8(const gmagnus_groups_t *gr
                         W->stack_stride, W_scale->row_stride, W_scale->stack_stride, Y->row_stride,
                         aligned16(Y->data, Y->row_stride, 0, data_size(Y->data_type)), row_tiles};
         hipStream_t s = (hipStream_t)hip_stream;
-        const int64_t tiles = row_tiles * ((n + GEN_B - 1) / GEN_B);
-        const dim3 grid((unsigned)(tiles < MAX_GRID ? tiles : MAX_GRID));
+        auto launch = [&](auto o) {
+            using O = decltype(o);
+            if (fast_side(a.x, a.xs, 0, k, a.index ? n_x : 256, 1) &&
+                fast_side(a.w, a.ws, groups->n_groups > 1 ? a.wg : 0, k, 256, 1) && (n_x * a.sxs + kb) * 4 < (int64_t)NOWHERE && 2 * a.sws * 4 + kb * 4 < (int64_t)NOWHERE) {
+                Fp8Args f = a;
+                if (big_tiles(a.n_rows / a.n_groups, n, a.n_groups)) {
+                    f.max_row_tiles = row_tiles_bound(a.n_groups, a.n_rows, 256);
+                    launch_fast(k_group_product_fp8_fast<O, 256, 256, 2, 4>, f.max_row_tiles * ((n + 255) / 256), 512,
+                                fast_lds<256, 256>(), f, s);
+                } else {
+                    f.max_row_tiles = row_tiles_bound(a.n_groups, a.n_rows, 128);
+                    launch_fast(k_group_product_fp8_fast<O, 128, 128, 2, 2>, f.max_row_tiles * ((n + 127) / 128), 256,
+                                fast_lds<128, 128>(), f, s);
+                }
+                return;
+            }
+            const int64_t tiles = row_tiles * ((n + GEN_B - 1) / GEN_B);
+            hipLaunchKernelGGL(k_group_product_fp8_any<O>, dim3((unsigned)(tiles < MAX_GRID ? tiles : MAX_GRID)), dim3(GEN_T),
+                               0, s, a);
+        };
         if (Y->data_type == GMAGNUS_DATA_BF16)
-            hipLaunchKernelGGL(k_group_product_fp8_any<__bf16>, grid, dim3(GEN_T), 0, s, a);
+            launch(__bf16{});
         else if (Y->data_type == GMAGNUS_DATA_FP16)
-            hipLaunchKernelGGL(k_group_product_fp8_any<_Float16>, grid, dim3(GEN_T), 0, s, a);
+            launch(_Float16{});
         else
-            hipLaunchKernelGGL(k_group_product_fp8_any<float>, grid, dim3(GEN_T), 0, s, a);
+            launch(float{});
         GM_CHECK_LAUNCH();
     });
 }
