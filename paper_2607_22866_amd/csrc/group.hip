@@ -304,6 +304,98 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_product_fast(ProductA
     }
 }
 
+// ------------------------------------------------------------------ few rows
+// Groups of a few rows each: the weights are read once and bound the time, so they
+// go straight from memory into the matrix unit's registers, any alignment. A
+// work group takes 16 rows of a group and 16 NT columns; its waves take turns at blocks
+// of 64 reduction elements, FEW_U blocks' loads in flight each, and their sums
+// are joined in LDS in the waves' order. A lane's 16 bytes of a row (chunks g
+// and g + 4 of the block, the same for both operands) lie next to its
+// neighbours'.
+constexpr int FEW_U = 4;
+
+// Row of X that the tile's row r stands for, -1 if there is none.
+GM_DEV int64_t x_row(const ProductArgs &a, const RowTile &t, int r) {
+    if (r >= t.rows) return -1;
+    const int64_t i = a.index ? a.index[t.begin + r] : t.begin + r;
+    return i >= a.n_x ? -1 : i;
+}
+
+template <typename T, typename OUT, int NT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_group_product_few(ProductArgs a) {
+    constexpr int BP = 16, BQ = 16 * NT, THREADS = 64 * WAVES;
+    __shared__ float part[WAVES][BP][BQ + 4];
+    const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16;
+    const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
+    const int64_t n_row = min(count_row_tiles<BP>(a.gp, a.n_groups, a.n_rows), a.max_row_tiles);
+    const int64_t n_col = (a.n + BQ - 1) / BQ, total = n_row * n_col;
+    const int n_k = (int)a.k, full = n_k / 64;
+    for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
+        // the row tiles of a group meet its weights one after the other
+        const int64_t tr = b % n_row, q0 = b / n_row * BQ;
+        const RowTile t = find_row_tile<BP>(a.gp, a.n_groups, a.n_rows, tr);
+        const int cols = (int)(a.n - q0 < BQ ? a.n - q0 : BQ);
+        OUT *out = static_cast<OUT *>(a.y) + t.begin * a.ys + q0;
+        if (t.group >= a.n_groups) {
+            zero_tile(out, a.ys, t.rows, cols);
+            continue;
+        }
+        const T *xr, *wr[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int c = 16 * j + i16;
+            wr[j] = static_cast<const T *>(a.w) + t.group * a.wg + (q0 + (c < cols ? c : cols - 1)) * a.ws;
+        }
+        // (a row that is not there reads another: its results are not stored)
+        const int64_t xi = x_row(a, t, i16);
+        xr = xi < 0 ? wr[0] : static_cast<const T *>(a.x) + xi * a.xs;
+        f32x4 acc[NT] = {};
+        for (int k0 = w; k0 < full; k0 += WAVES * FEW_U) {
+            u32x4 fx[FEW_U][2], fw[FEW_U][NT][2];
+#pragma unroll
+            for (int u = 0; u < FEW_U; ++u) {
+                const int at = min(k0 + u * WAVES, full - 1) * 64 + g * 8;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) fw[u][j][h] = load8(wr[j] + at + h * 32, 8);
+                    fx[u][h] = load8(xr + at + h * 32, 8);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < FEW_U; ++u)
+                if (k0 + u * WAVES < full)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) acc[j] = mfma_16x16x32(fw[u][j][h], fx[u][h], acc[j], T{});
+        }
+        if (full * 64 < n_k && w == full % WAVES) {  // what is left of the last block
+            for (int h = 0; h < 2; ++h) {
+                const int k = full * 64 + h * 32 + g * 8;
+                u32x4 fw[NT];
+#pragma unroll
+                for (int j = 0; j < NT; ++j) fw[j] = load8(wr[j] + k, n_k - k);
+                const u32x4 fx = load8(xr + k, n_k - k);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[j] = mfma_16x16x32(fw[j], fx, acc[j], T{});
+            }
+        }
+        __syncthreads();  // (the last tile's sums)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) *reinterpret_cast<f32x4 *>(&part[w][i16][16 * j + 4 * g]) = acc[j];
+        __syncthreads();
+        for (int i = threadIdx.x; i < t.rows * (BQ / 4); i += THREADS) {
+            const int r = i / (BQ / 4), c = i % (BQ / 4) * 4;
+            f32x4 s = *reinterpret_cast<const f32x4 *>(&part[0][r][c]);
+#pragma unroll
+            for (int v = 1; v < WAVES; ++v) s += *reinterpret_cast<const f32x4 *>(&part[v][r][c]);
+            if (x_row(a, t, r) < 0) s = f32x4{0, 0, 0, 0};
+            store4(out + r * a.ys + c, s, cols - c, a.wide);
+        }
+    }
+}
+
 struct OuterArgs {
     const int64_t *gp;
     const int32_t *index;
@@ -393,6 +485,31 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_outer_fast(OuterArgs 
     }
 }
 
+// The kernel of a product. The host knows the groups' mean size only; every
+// kernel is right for any sizes.
+enum class Shape { FEW16, FEW64, ANY, T32, T64, T128, T256 };
+
+Shape product_shape(const ProductArgs &a, bool transposed) {
+    const int64_t mean = (a.n_rows + a.n_groups - 1) / a.n_groups, groups = a.n_groups < a.n_rows ? a.n_groups : a.n_rows;
+    const bool fast = fast_side(a.x, a.xs, 0, a.k, a.index ? a.n_x : 256) &&
+                      fast_side(a.w, a.ws, a.n_groups > 1 ? a.wg : 0, transposed ? a.n : a.k, 256);
+    // Up to 16 rows a group the weights' bytes are all there is. 64 columns a work
+    // group (64 groups of 1 to 2 rows, 2048 x 2048: 79 us, 32 x 128 tiles 98) unless
+    // that leaves CUs without one, then 16 (one row, 4096 x 4096: 12.5 us against 23).
+    // Rows that are not aligned are slower that way (2047 wide: 121 us, staged tiles 61).
+    if (!transposed && mean <= 16) {
+        if (groups * ((a.n + 63) / 64) < 256) return Shape::FEW16;
+        if (fast) return Shape::FEW64;
+    }
+    if (!fast) return Shape::ANY;
+    // Tiles as high as the groups: 64 groups, 2048 x 2048, of 32 rows 146 us (64-row
+    // tiles 171, 128-row 161), of 125 rows 203 (179, 160); 40 groups of 50 rows, 776 x
+    // 1296, 26.9 (24.1, 25.7).
+    if (mean <= 40) return Shape::T32;
+    if (mean <= 96) return Shape::T64;
+    return big_tiles(mean, a.n, a.n_groups) ? Shape::T256 : Shape::T128;
+}
+
 }  // namespace
 }  // namespace gm
 
@@ -417,45 +534,42 @@ extern "C" gmagnus_status_t gmagnus_group_product(const gmagnus_groups_t *groups
         GM_REQUIRE(Y->data_type == X->data_type || Y->data_type == GMAGNUS_DATA_FP32, GMAGNUS_ERROR_INVALID_VALUE,
                    "Y must have the type of X, or fp32");
         if (groups->n_rows == 0) return;
-        const int64_t row_tiles = row_tiles_bound(groups->n_groups, groups->n_rows, GEN_B);
         const ProductArgs a{groups->group_ptr, groups->index, groups->n_groups, groups->n_rows, X->n_rows, n, k,
                             X->data, W->data, Y->data, X->row_stride, W->row_stride, W->stack_stride, Y->row_stride,
-                            aligned16(Y->data, Y->row_stride, 0, data_size(Y->data_type)), row_tiles};
+                            aligned16(Y->data, Y->row_stride, 0, data_size(Y->data_type)), 0};
         hipStream_t s = (hipStream_t)hip_stream;
-        if (fast_side(a.x, a.xs, 0, k, a.index ? a.n_x : 256) &&
-            fast_side(a.w, a.ws, groups->n_groups > 1 ? a.wg : 0, transposed ? n : k, 256)) {
-            const bool big = big_tiles(a.n_rows / a.n_groups, n, a.n_groups);
-            with_elem(X->data_type, Y->data_type, [&](auto t, auto o) {
-                using T = decltype(t);
-                using O = decltype(o);
-                auto go = [&](auto trans) {
-                    constexpr bool TR = decltype(trans)::value;
-                    ProductArgs f = a;
-                    if (big) {
-                        f.max_row_tiles = row_tiles_bound(a.n_groups, a.n_rows, 256);
-                        launch_fast(k_group_product_fast<T, O, TR, 256, 256, 2, 4>, f.max_row_tiles * ((n + 255) / 256), 512, 131072, f, s);
-                    } else {
-                        f.max_row_tiles = row_tiles_bound(a.n_groups, a.n_rows, 128);
-                        launch_fast(k_group_product_fast<T, O, TR, 128, 128, 2, 2>, f.max_row_tiles * ((n + 127) / 128), 256, 65536, f, s);
-                    }
-                };
-                if (transposed)
-                    go(std::true_type{});
-                else
-                    go(std::false_type{});
-            });
-            GM_CHECK_LAUNCH();
-            return;
-        }
-        const int64_t tiles = row_tiles * ((n + GEN_B - 1) / GEN_B);
-        const dim3 grid((unsigned)(tiles < MAX_GRID ? tiles : MAX_GRID));
+        const Shape shape = product_shape(a, transposed);
         with_elem(X->data_type, Y->data_type, [&](auto t, auto o) {
             using T = decltype(t);
             using O = decltype(o);
-            if (transposed)
-                hipLaunchKernelGGL((k_group_product_any<T, O, true>), grid, dim3(GEN_T), 0, s, a);
+            auto launch = [&](auto kernel, int bp, int bq, int threads, int lds) {
+                ProductArgs f = a;
+                f.max_row_tiles = row_tiles_bound(a.n_groups, a.n_rows, bp);
+                launch_fast(kernel, f.max_row_tiles * ((n + bq - 1) / bq), threads, lds, f, s);
+            };
+            auto fast = [&](auto trans) {
+                constexpr bool TR = decltype(trans)::value;
+                if (shape == Shape::T32)
+                    launch(k_group_product_fast<T, O, TR, 32, 128, 1, 4>, 32, 128, 256, fast_bytes(32, 128));
+                else if (shape == Shape::T64)
+                    launch(k_group_product_fast<T, O, TR, 64, 128, 2, 2>, 64, 128, 256, fast_bytes(64, 128));
+                else if (shape == Shape::T128)
+                    launch(k_group_product_fast<T, O, TR, 128, 128, 2, 2>, 128, 128, 256, fast_bytes(128, 128));
+                else
+                    launch(k_group_product_fast<T, O, TR, 256, 256, 2, 4>, 256, 256, 512, fast_bytes(256, 256));
+            };
+            if (shape == Shape::FEW16)
+                launch(k_group_product_few<T, O, 1, 4>, 16, 16, 256, 0);
+            else if (shape == Shape::FEW64)
+                launch(k_group_product_few<T, O, 4, 4>, 16, 64, 256, 0);
+            else if (shape == Shape::ANY && transposed)
+                launch(k_group_product_any<T, O, true>, GEN_B, GEN_B, GEN_T, 0);
+            else if (shape == Shape::ANY)
+                launch(k_group_product_any<T, O, false>, GEN_B, GEN_B, GEN_T, 0);
+            else if (transposed)
+                fast(std::true_type{});
             else
-                hipLaunchKernelGGL((k_group_product_any<T, O, false>), grid, dim3(GEN_T), 0, s, a);
+                fast(std::false_type{});
         });
         GM_CHECK_LAUNCH();
     });
@@ -491,9 +605,11 @@ extern "C" gmagnus_status_t gmagnus_group_outer(const gmagnus_groups_t *groups, 
                 auto go = [&](auto idx) {
                     constexpr bool IX = decltype(idx)::value;
                     if (big)
-                        launch_fast(k_group_outer_fast<T, O, IX, 256, 256, 2, 4>, (n + 255) / 256 * ((k + 255) / 256) * a.n_groups, 512, 131072, a, s);
+                        launch_fast(k_group_outer_fast<T, O, IX, 256, 256, 2, 4>, (n + 255) / 256 * ((k + 255) / 256) * a.n_groups,
+                                    512, fast_bytes(256, 256), a, s);
                     else
-                        launch_fast(k_group_outer_fast<T, O, IX, 128, 128, 2, 2>, (n + 127) / 128 * ((k + 127) / 128) * a.n_groups, 256, 65536, a, s);
+                        launch_fast(k_group_outer_fast<T, O, IX, 128, 128, 2, 2>, (n + 127) / 128 * ((k + 127) / 128) * a.n_groups,
+                                    256, fast_bytes(128, 128), a, s);
                 };
                 if (a.index)
                     go(std::true_type{});

@@ -135,6 +135,13 @@ struct Fp8Args {
     int64_t max_row_tiles;
 };
 
+// Row of X that the tile's row r stands for, -1 if there is none.
+GM_DEV int64_t x_row(const Fp8Args &a, const RowTile &t, int r) {
+    if (r >= t.rows) return -1;
+    const int64_t i = a.index ? a.index[t.begin + r] : t.begin + r;
+    return i >= a.n_x ? -1 : i;
+}
+
 // 16 bytes, those from `valid` on zero and not read.
 GM_DEV u32x4 load16(const uint8_t *p, int64_t valid) {
     u32x4 r = {0, 0, 0, 0};
@@ -174,18 +181,13 @@ __global__ __launch_bounds__(GEN_T) void k_group_product_fp8_any(Fp8Args a) {
             zero_tile(out, a.ys, t.rows, cols);
             continue;
         }
-        auto x_row = [&](int r) -> int64_t {  // row of X, or -1
-            if (r >= t.rows) return -1;
-            const int64_t i = a.index ? a.index[t.begin + r] : t.begin + r;
-            return i < 0 || i >= a.n_x ? -1 : i;
-        };
         const uint8_t *pr[4], *qr[4];
         const float *sp[4];
         const float *sq = a.sw + t.group * a.swg + n0 / SB * a.sws;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = (threadIdx.x + i * GEN_T) / 8;
-            const int64_t xr = x_row(r), sr = x_row(p0 + 16 * i + i16);
+            const int64_t xr = x_row(a, t, r), sr = x_row(a, t, p0 + 16 * i + i16);
             pr[i] = xr < 0 ? nullptr : a.x + xr * a.xs;
             qr[i] = r < cols ? a.w + t.group * a.wg + (n0 + r) * a.ws : nullptr;
             sp[i] = sr < 0 ? nullptr : a.sx + sr * a.sxs;
@@ -253,7 +255,7 @@ __global__ __launch_bounds__(GEN_T) void k_group_product_fp8_any(Fp8Args a) {
 // block's, on the vector units while the other wave of the SIMD multiplies. The
 // scales of X's rows come with their tile, 64 rows by each of the first waves.
 template <int BP, int BQ>
-constexpr int fast_lds() { return 2 * ((BP + BQ) * SB + (BP + 64) * 4); }
+constexpr int fast_lds() { return 2 * ((BP + BQ) * SB + ((BP + 63) / 64 * 64 + 64) * 4); }
 
 template <typename OUT, int BP, int BQ, int WP, int WQ>
 GM_DEV void tile_fp8_fast(const Fp8Args &a, const RowTile &t, int64_t n0, int cols, char *lds) {
@@ -274,12 +276,12 @@ GM_DEV void tile_fp8_fast(const Fp8Args &a, const RowTile &t, int64_t n0, int co
     const Dma q{reinterpret_cast<const char *>(a.w) + t.group * a.wg + n0 * a.ws, (uint32_t)((cols - 1) * a.ws + a.k), a.ws,
                 nullptr, 0, cols};
     // The step's scales come as single values: a row's to each thread of the first
-    // BP / 64 waves, the column blocks' to the next waves (which repeat each other:
+    // RW waves, the column blocks' to the next waves (which repeat each other:
     // a branch around them would split the loop's body, and the compiler would move
     // the sums past it, out of the units).
-    constexpr int SR = BP + 64;  // BP rows' scales, then the column blocks'
+    constexpr int RW = (BP + 63) / 64, SR = RW * 64 + 64;  // the rows' scales, then the column blocks'
     const int kb = (int)((a.k + SB - 1) / SB);
-    const bool row_wave = w < BP / 64;
+    const bool row_wave = w < RW;
     const float *s_base = row_wave ? a.sx : a.sw + t.group * a.swg + n0 / SB * a.sws;
     const int s_blocks = (cols + SB - 1) / SB;
     const uint32_t s_records = (uint32_t)(((row_wave ? a.n_x - 1 : s_blocks - 1) * (row_wave ? a.sxs : a.sws) + kb) * 4);
@@ -313,9 +315,9 @@ GM_DEV void tile_fp8_fast(const Fp8Args &a, const RowTile &t, int64_t n0, int co
         for (int h = 0; h < 2; ++h) b[j][h] = rq.get(lq + (s & 1) * QB, h, j);
     };
     auto feed_scales = [&](int s) {
-        load_to_lds<4>(s_base, s_records, sat, (uint32_t)s * 4, ls + (s & 1) * SR + (row_wave ? w : BP / 64) * 64);
+        load_to_lds<4>(s_base, s_records, sat, (uint32_t)s * 4, ls + (s & 1) * SR + (row_wave ? w : RW) * 64);
     };
-    auto read_sq = [&](int s) { return ls[(s & 1) * SR + BP + q0 / SB]; };
+    auto read_sq = [&](int s) { return ls[(s & 1) * SR + RW * 64 + q0 / SB]; };
     // a unit's products column by column, with a part of what else has to be issued after each
     auto unit = [&](int u, const u32x4(&f)[2], float sc, auto &&after) {
 #pragma unroll
@@ -343,19 +345,20 @@ GM_DEV void tile_fp8_fast(const Fp8Args &a, const RowTile &t, int64_t n0, int co
     float sq = read_sq(0);
     // Steps past the last are fed as zeros and their fragments never used: one body for all steps.
     for (int s = 0; s < steps; ++s) {
+        auto feed_at = [&](int u, int j) {  // the next tile's second operand, in the first unit
+#pragma unroll
+            for (int x = 0; x < LQ; ++x)
+                if (u == 0 && x * NQ / LQ == j) feed_q(s + 1, x);
+        };
 #pragma unroll
         for (int u = 0; u + 2 < NP; u += 2) {
             read_p(s, u + 1, a1, c1);
-            unit(u, a0, c0 * sq, [&](int j) {
-#pragma unroll
-                for (int x = 0; x < LQ; ++x)
-                    if (u == 0 && x * NQ / LQ == j) feed_q(s + 1, x);
-            });
+            unit(u, a0, c0 * sq, [&](int j) { feed_at(u, j); });
             read_p(s, u + 2, a0, c0);
             unit(u + 1, a1, c1 * sq, [](int) {});
         }
         read_p(s, NP - 1, a1, c1);
-        unit(NP - 2, a0, c0 * sq, [](int) {});
+        unit(NP - 2, a0, c0 * sq, [&](int j) { feed_at(NP - 2, j); });
         wait_and_barrier();
         feed_scales(s + 2);
         read_p(s + 1, 0, a0, c0);
@@ -399,6 +402,116 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_product_fp8_fast(Fp8A
         else
             tile_fp8_fast<OUT, BP, BQ, WP, WQ>(a, t, n0, cols, lds_fast);
     }
+}
+
+// Groups of a few rows: the weights go straight into the matrix unit's
+// registers, any alignment. A work group takes 16 rows of a group and 16 NT
+// columns, its waves take turns at blocks of 128, FEW_U blocks' loads in flight
+// each, and their sums are joined in LDS in the waves' order.
+constexpr int FEW_U = 4;
+
+template <typename OUT, int NT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_group_product_fp8_few(Fp8Args a) {
+    constexpr int BP = 16, BQ = 16 * NT, THREADS = 64 * WAVES;
+    __shared__ float part[WAVES][BP][BQ + 4];
+    const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16;
+    const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
+    const int64_t n_row = min(count_row_tiles<BP>(a.gp, a.n_groups, a.n_rows), a.max_row_tiles);
+    const int64_t n_col = (a.n + BQ - 1) / BQ, total = n_row * n_col;
+    const int n_k = (int)a.k, full = n_k / SB;
+    for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
+        const int64_t tr = b % n_row, q0 = b / n_row * BQ;
+        const RowTile t = find_row_tile<BP>(a.gp, a.n_groups, a.n_rows, tr);
+        const int cols = (int)(a.n - q0 < BQ ? a.n - q0 : BQ);
+        OUT *out = static_cast<OUT *>(a.y) + t.begin * a.ys + q0;
+        if (t.group >= a.n_groups) {
+            zero_tile(out, a.ys, t.rows, cols);
+            continue;
+        }
+        const uint8_t *wr[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int c = 16 * j + i16;
+            wr[j] = a.w + t.group * a.wg + (q0 + (c < cols ? c : cols - 1)) * a.ws;
+        }
+        // (a row that is not there reads another: its results are not stored)
+        const int64_t xi = x_row(a, t, i16);
+        const uint8_t *xr = xi < 0 ? wr[0] : a.x + xi * a.xs;
+        const float *sq = a.sw + t.group * a.swg + q0 / SB * a.sws, *sp = xi < 0 ? sq : a.sx + xi * a.sxs;
+        f32x4 acc[NT] = {};
+        auto block = [&](const u32x4(&fx)[2], const u32x4(&fw)[NT][2], float s) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const f32x4 d = mfma_fp8(fw[j][0], fw[j][1], fx[0], fx[1], f32x4{0, 0, 0, 0});
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[j][e] += s * d[e];
+            }
+        };
+        for (int k0 = w; k0 < full; k0 += WAVES * FEW_U) {
+            u32x4 fx[FEW_U][2], fw[FEW_U][NT][2];
+            float s[FEW_U];
+#pragma unroll
+            for (int u = 0; u < FEW_U; ++u) {
+                const int kb = min(k0 + u * WAVES, full - 1);
+                s[u] = sp[kb] * sq[kb];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) fw[u][j][h] = load16(wr[j] + kb * SB + h * 64 + g * 16, 16);
+                    fx[u][h] = load16(xr + kb * SB + h * 64 + g * 16, 16);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < FEW_U; ++u)
+                if (k0 + u * WAVES < full) block(fx[u], fw[u], s[u]);
+        }
+        if (full * SB < n_k && w == full % WAVES) {  // what is left of the last block
+            u32x4 fx[2], fw[NT][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = full * SB + h * 64 + g * 16;
+#pragma unroll
+                for (int j = 0; j < NT; ++j) fw[j][h] = load16(wr[j] + k, n_k - k);
+                fx[h] = load16(xr + k, n_k - k);
+            }
+            block(fx, fw, sp[full] * sq[full]);
+        }
+        __syncthreads();  // (the last tile's sums)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) *reinterpret_cast<f32x4 *>(&part[w][i16][16 * j + 4 * g]) = acc[j];
+        __syncthreads();
+        for (int i = threadIdx.x; i < t.rows * (BQ / 4); i += THREADS) {
+            const int r = i / (BQ / 4), c = i % (BQ / 4) * 4;
+            f32x4 s = *reinterpret_cast<const f32x4 *>(&part[0][r][c]);
+#pragma unroll
+            for (int v = 1; v < WAVES; ++v) s += *reinterpret_cast<const f32x4 *>(&part[v][r][c]);
+            if (x_row(a, t, r) < 0) s = f32x4{0, 0, 0, 0};
+            store4(out + r * a.ys + c, s, cols - c, a.wide);
+        }
+    }
+}
+
+// The kernel of a product, as for 16 bits (group.hip). Without a fast layout
+// only one tile is there.
+enum class Shape { FEW16, FEW64, ANY, T32, T64, T128, T256 };
+
+Shape fp8_shape(const Fp8Args &a) {
+    const int64_t mean = (a.n_rows + a.n_groups - 1) / a.n_groups, groups = a.n_groups < a.n_rows ? a.n_groups : a.n_rows;
+    const int64_t kb = (a.k + SB - 1) / SB;
+    const bool fast = fast_side(a.x, a.xs, 0, a.k, a.index ? a.n_x : 256, 1) &&
+                      fast_side(a.w, a.ws, a.n_groups > 1 ? a.wg : 0, a.k, 256, 1) &&
+                      (a.n_x * a.sxs + kb) * 4 < (int64_t)NOWHERE && (2 * a.sws + kb) * 4 < (int64_t)NOWHERE;
+    // (64 groups, 2048 x 4096, of 1 row: 79 us with 64 columns a work group, 106 with
+    // 32 x 128 tiles; of 31 rows: 32-row tiles 141, 64-row 173, 128-row 162; one row, 4096
+    // x 4096: 13.4 with 16 columns, 15.0 with 64)
+    if (mean <= 16) {
+        if (groups * ((a.n + 63) / 64) < 256) return Shape::FEW16;
+        if (fast) return Shape::FEW64;
+    }
+    if (!fast) return Shape::ANY;
+    if (mean <= 40) return Shape::T32;
+    if (mean <= 96) return Shape::T64;
+    return big_tiles(mean, a.n, a.n_groups) ? Shape::T256 : Shape::T128;
 }
 
 }  // namespace
@@ -468,32 +581,28 @@ extern "C" gmagnus_status_t gmagnus_group_product_fp8(const gmagnus_groups_t *gr
                        Y->data_type != GMAGNUS_DATA_FP8_E4M3,
                    GMAGNUS_ERROR_INVALID_VALUE, "X and W must be E4M3, their scales fp32, Y fp32, bf16 or fp16");
         if (groups->n_rows == 0) return;
-        const int64_t row_tiles = row_tiles_bound(groups->n_groups, groups->n_rows, GEN_B);
         const Fp8Args a{groups->group_ptr, groups->index, groups->n_groups, groups->n_rows, n_x, n, k,
                         (const uint8_t *)X->data, (const uint8_t *)W->data, (const float *)X_scale->data,
                         (const float *)W_scale->data, Y->data, X->row_stride, X_scale->row_stride, W->row_stride,
                         W->stack_stride, W_scale->row_stride, W_scale->stack_stride, Y->row_stride,
-                        aligned16(Y->data, Y->row_stride, 0, data_size(Y->data_type)), row_tiles};
+                        aligned16(Y->data, Y->row_stride, 0, data_size(Y->data_type)), 0};
         hipStream_t s = (hipStream_t)hip_stream;
         auto launch = [&](auto o) {
             using O = decltype(o);
-            if (fast_side(a.x, a.xs, 0, k, a.index ? n_x : 256, 1) &&
-                fast_side(a.w, a.ws, groups->n_groups > 1 ? a.wg : 0, k, 256, 1) && (n_x * a.sxs + kb) * 4 < (int64_t)NOWHERE && 2 * a.sws * 4 + kb * 4 < (int64_t)NOWHERE) {
+            auto go = [&](auto kernel, int bp, int bq, int threads, int lds) {
                 Fp8Args f = a;
-                if (big_tiles(a.n_rows / a.n_groups, n, a.n_groups)) {
-                    f.max_row_tiles = row_tiles_bound(a.n_groups, a.n_rows, 256);
-                    launch_fast(k_group_product_fp8_fast<O, 256, 256, 2, 4>, f.max_row_tiles * ((n + 255) / 256), 512,
-                                fast_lds<256, 256>(), f, s);
-                } else {
-                    f.max_row_tiles = row_tiles_bound(a.n_groups, a.n_rows, 128);
-                    launch_fast(k_group_product_fp8_fast<O, 128, 128, 2, 2>, f.max_row_tiles * ((n + 127) / 128), 256,
-                                fast_lds<128, 128>(), f, s);
-                }
-                return;
+                f.max_row_tiles = row_tiles_bound(a.n_groups, a.n_rows, bp);
+                launch_fast(kernel, f.max_row_tiles * ((n + bq - 1) / bq), threads, lds, f, s);
+            };
+            switch (fp8_shape(a)) {
+            case Shape::FEW16: return go(k_group_product_fp8_few<O, 1, 4>, 16, 16, 256, 0);
+            case Shape::FEW64: return go(k_group_product_fp8_few<O, 4, 4>, 16, 64, 256, 0);
+            case Shape::ANY: return go(k_group_product_fp8_any<O>, GEN_B, GEN_B, GEN_T, 0);
+            case Shape::T32: return go(k_group_product_fp8_fast<O, 32, 128, 1, 4>, 32, 128, 256, fast_lds<32, 128>());
+            case Shape::T64: return go(k_group_product_fp8_fast<O, 64, 128, 2, 2>, 64, 128, 256, fast_lds<64, 128>());
+            case Shape::T128: return go(k_group_product_fp8_fast<O, 128, 128, 2, 2>, 128, 128, 256, fast_lds<128, 128>());
+            case Shape::T256: return go(k_group_product_fp8_fast<O, 256, 256, 2, 4>, 256, 256, 512, fast_lds<256, 256>());
             }
-            const int64_t tiles = row_tiles * ((n + GEN_B - 1) / GEN_B);
-            hipLaunchKernelGGL(k_group_product_fp8_any<O>, dim3((unsigned)(tiles < MAX_GRID ? tiles : MAX_GRID)), dim3(GEN_T),
-                               0, s, a);
         };
         if (Y->data_type == GMAGNUS_DATA_BF16)
             launch(__bf16{});

@@ -61,6 +61,7 @@ GM_DEV void load_to_lds(const void *base, uint32_t records, uint32_t v, uint32_t
 // IDX: k as rows, their numbers by an index (k contiguous: the index is read once, at init).
 template <bool KROWS, bool IDX, int B, int THREADS>
 struct Feed {
+    static_assert(!KROWS || B >= 128, "a row holds the 8 units that the swizzle permutes");
     static constexpr int W = THREADS / 64, L = B * BK * 2 / 1024 / W;  // loads of a wave a step
     static constexpr int PITCH = KROWS ? B * 2 : BK * 2;               // bytes of an LDS row
     static constexpr int SLOTS = PITCH / 16, ROWS = 1024 / PITCH;      // of one load
@@ -174,9 +175,12 @@ inline bool big_tiles(int64_t m, int64_t n, int64_t n_groups) {
     return m >= 384 && (tiles >= 192 || tiles * n_groups >= 192);
 }
 
+// LDS of two buffers of tiles of bp and bq rows.
+constexpr int fast_bytes(int bp, int bq) { return 2 * (bp + bq) * BK * 2; }
+
 template <typename K, typename A>
 void launch_fast(K kernel, int64_t tiles, int threads, int lds, const A &a, hipStream_t s) {
-    allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds);
+    if (lds > 0) allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles < MAX_GRID ? tiles : MAX_GRID)), dim3(threads), lds, s, a);
 }
 

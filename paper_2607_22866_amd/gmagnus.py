@@ -7,6 +7,7 @@ no fallback: if the library is missing or no GPU is present, calls raise.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -453,60 +454,72 @@ def release_cache():
 
 
 # ------------------------------------------------------------ routed expert products
-def _dense(t: torch.Tensor, device: torch.device, name: str, dims: int = 2) -> DenseDesc:
+_raw_stream = torch._C._cuda_getCurrentRawStream  # the current stream's handle (a tenth of current_stream()'s time)
+
+
+def _on_stream(f):
+    """Adds the argument stream: the call's work and the arrays it makes belong to that
+    stream, and its inputs are not given to others before the stream has read them."""
+
+    @functools.wraps(f)
+    def call(*args, stream=None, **kw):
+        if stream is None:
+            return f(*args, **kw)
+        for x in args + tuple(kw.values()):
+            for t in x.arrays() if isinstance(x, Routing) else (x,):
+                if isinstance(t, torch.Tensor) and t.is_cuda:
+                    t.record_stream(stream)
+        with torch.cuda.stream(stream):
+            return f(*args, **kw)
+
+    return call
+
+
+def _device_of(t, name: str) -> int:
+    """The device index of a call's first operand, which has to be the current device."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor" % name)
+    dev = t.get_device()
+    if dev != torch.cuda.current_device():
+        raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (name, dev, torch.cuda.current_device()))
+    return dev
+
+
+def _check_device(t, dev: int, name: str):
+    if not isinstance(t, torch.Tensor) or t.get_device() != dev:
+        raise ValueError("%s must be a CUDA tensor on cuda:%d" % (name, dev))
+
+
+def _dense(t: torch.Tensor, dev: int, name: str, dims: int = 2) -> DenseDesc:
     """Descriptor of a matrix (dims 2) or a stack of them (dims 3) whose columns are contiguous."""
-    _require_device(t, device, name)
-    if t.dim() != dims:
+    _check_device(t, dev, name)
+    st, shape = t.stride(), t.shape
+    if len(st) != dims:
         raise ValueError("%s must have %d dimensions" % (name, dims))
-    if t.dtype not in DATA_TYPES:
+    kind = DATA_TYPES.get(t.dtype)
+    if kind is None:
         raise ValueError("%s has an unsupported type %s" % (name, t.dtype))
-    n_rows, n_cols = t.shape[-2:]
-    st = t.stride()
-    if n_cols > 1 and st[-1] != 1:
+    n_rows, n_cols = shape[-2], shape[-1]
+    if st[-1] != 1 and n_cols > 1:
         raise ValueError("%s must have contiguous columns" % name)
-    return DenseDesc(t.data_ptr(), n_rows, n_cols, max(st[-2], n_cols) if n_rows <= 1 else st[-2],
-                     st[0] if dims == 3 else 0, DATA_TYPES[t.dtype])
+    row = st[-2]
+    if n_rows <= 1 and row < n_cols:
+        row = n_cols
+    return DenseDesc(t.data_ptr(), n_rows, n_cols, row, st[0] if dims == 3 else 0, kind)
 
 
-def _array(t: torch.Tensor, device: torch.device, name: str, dtype, numel: int) -> int:
-    _require_device(t, device, name)
-    if t.dtype != dtype or not t.is_contiguous() or t.numel() != numel:
+def _array(t: torch.Tensor, dev: int, name: str, dtype, numel: int) -> int:
+    _check_device(t, dev, name)
+    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s array of %d entries" % (name, dtype, numel))
     return t.data_ptr()
 
 
-class _Launch:
-    """The stream of a call on device tensors; arrays made inside belong to that stream, and inputs of others
-    are not reused before it has read them."""
-
-    def __init__(self, stream, t: torch.Tensor, *inputs):
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise ValueError("operands must be CUDA tensors")
-        if t.device.index != torch.cuda.current_device():
-            raise ValueError("operands are on %s, the current device is cuda:%d" % (t.device, torch.cuda.current_device()))
-        self._ctx = None
-        if stream is not None:
-            for x in (t,) + inputs:
-                if isinstance(x, torch.Tensor) and x.is_cuda:
-                    x.record_stream(stream)
-            self._ctx = torch.cuda.stream(stream)
-        self.stream = _stream(stream)
-
-    def __enter__(self):
-        if self._ctx is not None:
-            self._ctx.__enter__()
-        return self.stream
-
-    def __exit__(self, *a):
-        if self._ctx is not None:
-            self._ctx.__exit__(*a)
-
-
-def _out(out, shape, dtype, device, name):
+def _out(out, shape, dtype, like, name):
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(out.shape) != tuple(shape):
-        raise ValueError("%s must have shape %s" % (name, tuple(shape)))
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    if tuple(out.shape) != shape:
+        raise ValueError("%s must have shape %s" % (name, shape))
     return out
 
 
@@ -543,166 +556,171 @@ class Routing:
         n = self.nnz
         return DeviceCSR(self.n_experts, self.n_tokens, self.group_ptr, self.token[:n], self.group_weight[:n])
 
+    def arrays(self):
+        return (self.row_ptr, self.expert, self.weight, self.group_ptr, self.token, self.slot, self.group_weight)
+
     def _desc(self) -> RoutingDesc:
         return RoutingDesc(self.row_ptr.data_ptr(), self.expert.data_ptr(), self.weight.data_ptr(),
                            self.group_ptr.data_ptr(), self.token.data_ptr(), self.slot.data_ptr(),
                            self.group_weight.data_ptr())
 
 
-def route(logits: torch.Tensor, top_k: int, normalise: bool = True, stream=None) -> Routing:
+@_on_stream
+def route(logits: torch.Tensor, top_k: int, normalise: bool = True) -> Routing:
     """The top_k largest logits of each token (-inf and NaN are masked; ties: the
     lowest expert) with softmax weights over them (normalise) or over all experts."""
-    with _Launch(stream, logits) as s:
-        dev = logits.device
-        d = _dense(logits, dev, "logits")
-        t, e = logits.shape
-        lib = load()
-        n = t * top_k if top_k > 0 else 0
-        i32 = torch.empty(3, n, dtype=torch.int32, device=dev)
-        f32 = torch.empty(2, n, dtype=torch.float32, device=dev)
-        ptr = torch.empty(t + e + 2, dtype=torch.int64, device=dev)
-        nbytes = lib.gmagnus_route_workspace_bytes(t, e, top_k)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        r = Routing(t, e, top_k, bool(normalise), ptr[:t + 1], i32[0], f32[0], ptr[t + 1:], i32[1], i32[2], f32[1])
-        _check(lib.gmagnus_route(ctypes.byref(d), top_k, int(r.normalise), ctypes.byref(r._desc()), ws.data_ptr(), nbytes, s))
-        return r
+    dev = _device_of(logits, "logits")
+    d = _dense(logits, dev, "logits")
+    t, e = logits.shape
+    lib = load()
+    n = t * top_k if top_k > 0 else 0
+    nbytes = lib.gmagnus_route_workspace_bytes(t, e, top_k)
+    device = logits.device
+    row_ptr, group_ptr = torch.empty(t + e + 2, dtype=torch.int64, device=device).split((t + 1, e + 1))
+    expert, token, slot = torch.empty((3, n), dtype=torch.int32, device=device).unbind(0)
+    weight, group_weight = torch.empty((2, n), dtype=torch.float32, device=device).unbind(0)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    r = Routing(t, e, top_k, bool(normalise), row_ptr, expert, weight, group_ptr, token, slot, group_weight)
+    _check(lib.gmagnus_route(ctypes.byref(d), top_k, int(r.normalise), ctypes.byref(r._desc()), ws.data_ptr(), nbytes,
+                             _raw_stream(dev)))
+    return r
 
 
+@_on_stream
 def route_backward(logits: torch.Tensor, routing: Routing, d_weight: torch.Tensor,
-                   out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient of the logits from the gradient of routing.weight (float32, n_tokens * top_k)."""
-    with _Launch(stream, logits, d_weight, routing.row_ptr, routing.expert, routing.weight, out) as s:
-        dev = logits.device
-        d = _dense(logits, dev, "logits")
-        if tuple(logits.shape) != (routing.n_tokens, routing.n_experts):
-            raise ValueError("logits must have the routing's shape")
-        _require_device(routing.row_ptr, dev, "routing")
-        g = _array(d_weight, dev, "d_weight", torch.float32, routing.n_tokens * routing.top_k)
-        out = _out(out, logits.shape, logits.dtype, dev, "out")
-        o = _dense(out, dev, "out")
-        _check(load().gmagnus_route_backward(ctypes.byref(d), routing.top_k, int(routing.normalise),
-                                             ctypes.byref(routing._desc()), g, ctypes.byref(o), s))
-        return out
+    dev = _device_of(logits, "logits")
+    d = _dense(logits, dev, "logits")
+    if tuple(logits.shape) != (routing.n_tokens, routing.n_experts):
+        raise ValueError("logits must have the routing's shape")
+    _check_device(routing.row_ptr, dev, "routing")
+    g = _array(d_weight, dev, "d_weight", torch.float32, routing.n_tokens * routing.top_k)
+    out = _out(out, tuple(logits.shape), logits.dtype, logits, "out")
+    o = _dense(out, dev, "out")
+    _check(load().gmagnus_route_backward(ctypes.byref(d), routing.top_k, int(routing.normalise),
+                                         ctypes.byref(routing._desc()), g, ctypes.byref(o), _raw_stream(dev)))
+    return out
 
 
-def _groups(group_ptr, index, n_rows: int, device) -> GroupsDesc:
-    gp = _array(group_ptr, device, "group_ptr", torch.int64, group_ptr.numel())
-    if group_ptr.numel() < 2:
-        raise ValueError("group_ptr must have at least two entries")
-    ix = None if index is None else _array(index, device, "index", torch.int32, n_rows)
-    return GroupsDesc(group_ptr.numel() - 1, n_rows, gp, ix)
+def _groups(group_ptr, index, n_rows: int, dev: int) -> GroupsDesc:
+    if not isinstance(group_ptr, torch.Tensor) or group_ptr.numel() < 2:
+        raise ValueError("group_ptr must be a tensor of at least two entries")
+    n = group_ptr.numel()
+    gp = _array(group_ptr, dev, "group_ptr", torch.int64, n)
+    ix = None if index is None else _array(index, dev, "index", torch.int32, n_rows)
+    return GroupsDesc(n - 1, n_rows, gp, ix)
 
 
+@_on_stream
 def group_product(x: torch.Tensor, w: torch.Tensor, group_ptr: torch.Tensor, index: Optional[torch.Tensor] = None,
-                  transposed: bool = False, out_dtype=None, out: Optional[torch.Tensor] = None,
-                  stream=None) -> torch.Tensor:
+                  transposed: bool = False, out_dtype=None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y[r] = x[index[r]] @ w[e].T (transposed: @ w[e]) for every row r of every
     group e, group_ptr[e] <= r < group_ptr[e + 1]. index None: x's own rows.
     bfloat16 or float16, sums in fp32; out_dtype: the inputs' type or float32."""
-    with _Launch(stream, x, w, group_ptr, index, out) as s:
-        dev = x.device
-        dx, dw = _dense(x, dev, "x"), _dense(w, dev, "w", 3)
-        n_rows = x.shape[0] if index is None else index.numel()
-        gd = _groups(group_ptr, index, n_rows, dev)
-        if w.shape[0] != gd.n_groups:
-            raise ValueError("w must have one matrix a group")
-        out = _out(out, (n_rows, dw.n_cols if transposed else dw.n_rows),
-                   out_dtype or x.dtype, dev, "out")
-        dy = _dense(out, dev, "out")
-        _check(load().gmagnus_group_product(ctypes.byref(gd), ctypes.byref(dx), ctypes.byref(dw), int(transposed),
-                                            ctypes.byref(dy), s))
-        return out
+    dev = _device_of(x, "x")
+    dx, dw = _dense(x, dev, "x"), _dense(w, dev, "w", 3)
+    n_rows = dx.n_rows if index is None else index.numel()
+    gd = _groups(group_ptr, index, n_rows, dev)
+    if w.shape[0] != gd.n_groups:
+        raise ValueError("w must have one matrix a group")
+    out = _out(out, (n_rows, dw.n_cols if transposed else dw.n_rows), out_dtype or x.dtype, x, "out")
+    dy = _dense(out, dev, "out")
+    _check(load().gmagnus_group_product(ctypes.byref(gd), ctypes.byref(dx), ctypes.byref(dw), int(transposed),
+                                        ctypes.byref(dy), _raw_stream(dev)))
+    return out
 
 
+@_on_stream
 def group_outer(d_y: torch.Tensor, x: torch.Tensor, group_ptr: torch.Tensor, index: Optional[torch.Tensor] = None,
-                out_dtype=None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+                out_dtype=None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient of group_product's w: for every group e the sum of d_y[r].T @ x[index[r]] over its rows."""
-    with _Launch(stream, d_y, x, group_ptr, index, out) as s:
-        dev = d_y.device
-        ddy, dx = _dense(d_y, dev, "d_y"), _dense(x, dev, "x")
-        gd = _groups(group_ptr, index, d_y.shape[0], dev)
-        out = _out(out, (gd.n_groups, ddy.n_cols, dx.n_cols), out_dtype or x.dtype, dev, "out")
-        dd = _dense(out, dev, "out", 3)
-        _check(load().gmagnus_group_outer(ctypes.byref(gd), ctypes.byref(ddy), ctypes.byref(dx), ctypes.byref(dd), s))
-        return out
+    dev = _device_of(d_y, "d_y")
+    ddy, dx = _dense(d_y, dev, "d_y"), _dense(x, dev, "x")
+    gd = _groups(group_ptr, index, ddy.n_rows, dev)
+    out = _out(out, (gd.n_groups, ddy.n_cols, dx.n_cols), out_dtype or x.dtype, x, "out")
+    dd = _dense(out, dev, "out", 3)
+    _check(load().gmagnus_group_outer(ctypes.byref(gd), ctypes.byref(ddy), ctypes.byref(dx), ctypes.byref(dd),
+                                      _raw_stream(dev)))
+    return out
 
 
-def quantise_blocks(x: torch.Tensor, block_rows: int = 1, stream=None):
+@_on_stream
+def quantise_blocks(x: torch.Tensor, block_rows: int = 1):
     """(q, scale): x / scale as float8_e4m3fn, with one float32 scale for each block
     of block_rows (1: activations, 128: weights) x 128 values. x: a matrix or a stack."""
-    with _Launch(stream, x) as s:
-        dev = x.device
-        dims = 3 if x.dim() == 3 else 2
-        dx = _dense(x, dev, "x", dims)
-        if block_rows not in (1, SCALE_BLOCK):
-            raise ValueError("block_rows must be 1 or %d" % SCALE_BLOCK)
-        q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=dev)
-        scale = torch.empty(tuple(x.shape[:-2]) + (-(-dx.n_rows // block_rows), -(-dx.n_cols // SCALE_BLOCK)),
-                            dtype=torch.float32, device=dev)
-        dq, ds = _dense(q, dev, "q", dims), _dense(scale, dev, "scale", dims)
-        _check(load().gmagnus_quantise_blocks(ctypes.byref(dx), x.shape[0] if dims == 3 else 1, block_rows,
-                                              ctypes.byref(dq), ctypes.byref(ds), s))
-        return q, scale
+    dev = _device_of(x, "x")
+    dims = 3 if x.dim() == 3 else 2
+    dx = _dense(x, dev, "x", dims)
+    if block_rows not in (1, SCALE_BLOCK):
+        raise ValueError("block_rows must be 1 or %d" % SCALE_BLOCK)
+    q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
+    scale = torch.empty(tuple(x.shape[:-2]) + (-(-dx.n_rows // block_rows), -(-dx.n_cols // SCALE_BLOCK)),
+                        dtype=torch.float32, device=x.device)
+    dq, ds = _dense(q, dev, "q", dims), _dense(scale, dev, "scale", dims)
+    _check(load().gmagnus_quantise_blocks(ctypes.byref(dx), x.shape[0] if dims == 3 else 1, block_rows,
+                                          ctypes.byref(dq), ctypes.byref(ds), _raw_stream(dev)))
+    return q, scale
 
 
+@_on_stream
 def group_product_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
                       group_ptr: torch.Tensor, index: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
-                      out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """group_product of float8_e4m3fn operands with the scales quantise_blocks gives
     (x: block_rows 1, w: block_rows 128). One group is the plain product."""
-    with _Launch(stream, x, x_scale, w, w_scale, group_ptr, index, out) as s:
-        dev = x.device
-        dx, dxs = _dense(x, dev, "x"), _dense(x_scale, dev, "x_scale")
-        dw, dws = _dense(w, dev, "w", 3), _dense(w_scale, dev, "w_scale", 3)
-        n_rows = x.shape[0] if index is None else index.numel()
-        gd = _groups(group_ptr, index, n_rows, dev)
-        if w.shape[0] != gd.n_groups or w_scale.shape[0] != gd.n_groups:
-            raise ValueError("w and w_scale must have one matrix a group")
-        out = _out(out, (n_rows, dw.n_rows), out_dtype, dev, "out")
-        dy = _dense(out, dev, "out")
-        _check(load().gmagnus_group_product_fp8(ctypes.byref(gd), ctypes.byref(dx), ctypes.byref(dxs), ctypes.byref(dw),
-                                                ctypes.byref(dws), ctypes.byref(dy), s))
-        return out
+    dev = _device_of(x, "x")
+    dx, dxs = _dense(x, dev, "x"), _dense(x_scale, dev, "x_scale")
+    dw, dws = _dense(w, dev, "w", 3), _dense(w_scale, dev, "w_scale", 3)
+    n_rows = dx.n_rows if index is None else index.numel()
+    gd = _groups(group_ptr, index, n_rows, dev)
+    if w.shape[0] != gd.n_groups or w_scale.shape[0] != gd.n_groups:
+        raise ValueError("w and w_scale must have one matrix a group")
+    out = _out(out, (n_rows, dw.n_rows), out_dtype, x, "out")
+    dy = _dense(out, dev, "out")
+    _check(load().gmagnus_group_product_fp8(ctypes.byref(gd), ctypes.byref(dx), ctypes.byref(dxs), ctypes.byref(dw),
+                                            ctypes.byref(dws), ctypes.byref(dy), _raw_stream(dev)))
+    return out
 
 
-def _combine_args(row_ptr, slot, weight, dev):
-    rp = _array(row_ptr, dev, "row_ptr", torch.int64, row_ptr.numel())
-    if row_ptr.numel() < 1:
-        raise ValueError("row_ptr is empty")
+def _combine_args(row_ptr, slot, weight, dev: int):
+    if not isinstance(row_ptr, torch.Tensor) or row_ptr.numel() < 1:
+        raise ValueError("row_ptr must be a tensor of at least one entry")
+    _check_device(slot, dev, "slot")
     n = slot.numel()
-    return rp, _array(slot, dev, "slot", torch.int32, n), \
-        None if weight is None else _array(weight, dev, "weight", torch.float32, n), n
+    return (_array(row_ptr, dev, "row_ptr", torch.int64, row_ptr.numel()), _array(slot, dev, "slot", torch.int32, n),
+            None if weight is None else _array(weight, dev, "weight", torch.float32, n), n)
 
 
+@_on_stream
 def combine(y: torch.Tensor, row_ptr: torch.Tensor, slot: torch.Tensor, weight: Optional[torch.Tensor] = None,
-            out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+            out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """out[t] = sum over the entries j of token t of weight[j] * y[slot[j]] (weight None: 1)."""
-    with _Launch(stream, y, row_ptr, slot, weight, out) as s:
-        dev = y.device
-        d = _dense(y, dev, "y")
-        rp, sl, w, n = _combine_args(row_ptr, slot, weight, dev)
-        out = _out(out, (row_ptr.numel() - 1, d.n_cols), y.dtype, dev, "out")
-        o = _dense(out, dev, "out")
-        _check(load().gmagnus_combine(rp, sl, w, n, ctypes.byref(d), ctypes.byref(o), s))
-        return out
+    dev = _device_of(y, "y")
+    d = _dense(y, dev, "y")
+    rp, sl, w, n = _combine_args(row_ptr, slot, weight, dev)
+    out = _out(out, (row_ptr.numel() - 1, d.n_cols), y.dtype, y, "out")
+    o = _dense(out, dev, "out")
+    _check(load().gmagnus_combine(rp, sl, w, n, ctypes.byref(d), ctypes.byref(o), _raw_stream(dev)))
+    return out
 
 
+@_on_stream
 def combine_backward(y: Optional[torch.Tensor], row_ptr: torch.Tensor, slot: torch.Tensor,
-                     weight: Optional[torch.Tensor], d_out: torch.Tensor, n_rows: Optional[int] = None, stream=None):
+                     weight: Optional[torch.Tensor], d_out: torch.Tensor, n_rows: Optional[int] = None):
     """(gradient of y, gradient of weight) of combine. y None (with n_rows, the rows
     of y): the weights' gradient is not wanted and None."""
-    with _Launch(stream, d_out, y, row_ptr, slot, weight) as s:
-        dev = d_out.device
-        do = _dense(d_out, dev, "d_out")
-        rp, sl, w, n = _combine_args(row_ptr, slot, weight, dev)
-        if row_ptr.numel() - 1 != do.n_rows:
-            raise ValueError("d_out must have a row a token")
-        if y is None and n_rows is None:
-            raise ValueError("n_rows is required without y")
-        dy = None if y is None else _dense(y, dev, "y")
-        d_y = torch.empty((n_rows if y is None else y.shape[0], do.n_cols), dtype=d_out.dtype, device=dev)
-        d_w = None if y is None else torch.empty(n, dtype=torch.float32, device=dev)
-        _check(load().gmagnus_combine_backward(rp, sl, w, n, None if dy is None else ctypes.byref(dy), ctypes.byref(do),
-                                               ctypes.byref(_dense(d_y, dev, "d_y")),
-                                               None if d_w is None else d_w.data_ptr(), s))
-        return d_y, d_w
+    dev = _device_of(d_out, "d_out")
+    do = _dense(d_out, dev, "d_out")
+    rp, sl, w, n = _combine_args(row_ptr, slot, weight, dev)
+    if row_ptr.numel() - 1 != do.n_rows:
+        raise ValueError("d_out must have a row a token")
+    if y is None and n_rows is None:
+        raise ValueError("n_rows is required without y")
+    dy = None if y is None else _dense(y, dev, "y")
+    d_y = torch.empty((n_rows if y is None else dy.n_rows, do.n_cols), dtype=d_out.dtype, device=d_out.device)
+    d_w = None if y is None else torch.empty(n, dtype=torch.float32, device=d_out.device)
+    _check(load().gmagnus_combine_backward(rp, sl, w, n, None if dy is None else ctypes.byref(dy), ctypes.byref(do),
+                                           ctypes.byref(_dense(d_y, dev, "d_y")),
+                                           None if d_w is None else d_w.data_ptr(), _raw_stream(dev)))
+    return d_y, d_w
