@@ -49,9 +49,11 @@ GM_DEV u32x4 load8(const T *p, int valid) {
         r = u32x4{b.v[0], b.v[1], b.v[2], b.v[3]};
     } else if (valid > 0) {
         const uint16_t *s = reinterpret_cast<const uint16_t *>(p);
+        uint32_t e[8];
 #pragma unroll
-        for (int i = 0; i < 7; ++i)
-            if (i < valid) r[i >> 1] |= (uint32_t)s[i] << (16 * (i & 1));
+        for (int i = 0; i < 8; ++i) e[i] = s[i < valid ? i : 0];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i >> 1] |= (i < valid ? e[i] : 0u) << (16 * (i & 1));
     }
     return r;
 }
@@ -194,14 +196,19 @@ GM_DEV const T *row_at(const Side &s, int64_t r) {
     return static_cast<const T *>(s.base) + r * s.stride;
 }
 
-// Four neighbours of an output row, as many as there are.
+// Four neighbours of an output row, as many as there are, at any alignment.
 template <typename OUT>
-GM_DEV void store4(OUT *p, f32x4 v, int64_t left, bool wide) {
-    if (wide && left >= 4) {
-        if constexpr (sizeof(OUT) == 4)
-            *reinterpret_cast<f32x4 *>(p) = v;
-        else
-            *reinterpret_cast<u32x2 *>(p) = u32x2{pack2<OUT>(v[0], v[1]), pack2<OUT>(v[2], v[3])};
+GM_DEV void store4(OUT *p, f32x4 v, int64_t left) {
+    if (left >= 4) {
+        if constexpr (sizeof(OUT) == 4) {
+            *reinterpret_cast<Bytes16<4> *>(p) = Bytes16<4>{{__float_as_uint(v[0]), __float_as_uint(v[1]),
+                                                             __float_as_uint(v[2]), __float_as_uint(v[3])}};
+        } else {
+            struct Bytes8 {
+                uint32_t v[2] __attribute__((packed, aligned(2)));
+            };
+            *reinterpret_cast<Bytes8 *>(p) = Bytes8{{pack2<OUT>(v[0], v[1]), pack2<OUT>(v[2], v[3])}};
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)

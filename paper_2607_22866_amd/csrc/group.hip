@@ -16,116 +16,135 @@ namespace gm {
 namespace {
 
 // ---------------------------------------------------------------- any layout
-// Tiles staged through registers: any alignment and stride. 128 x 128 tiles, four waves
-// of 64 x 64.
+// Tiles staged through registers, for operands at any alignment: 128 x 128, four
+// waves of 64 x 64. Two steps' loads are in flight in registers while a third
+// step's tile is multiplied from one of two LDS buffers.
 constexpr int GEN_B = 128, GEN_T = 256;
 
-template <typename T, bool KROWS>
+// IDX: k as rows, their numbers by an index.
+template <typename T, bool KROWS, bool IDX>
 struct Staged {
     static constexpr int N = GEN_B * BK / 8 / GEN_T;  // chunks a thread moves
-    const T *row[N];
-    u32x4 v[N];
+    const T *at[N];   // chunk i: its row, null if it is not there; k as rows: its place in the next step
+    uint32_t to[N];   // its place in the tile, in chunks
+    int32_t ids[KROWS && IDX ? N : 1];
+
+    GM_DEV static int row_of(int i) { return (threadIdx.x + i * GEN_T) / (KROWS ? GEN_B / 8 : 8); }
+    GM_DEV static int elem_of() { return threadIdx.x % (KROWS ? GEN_B / 8 : 8) * 8; }
 
     GM_DEV void init(const Side &s) {
-        if constexpr (!KROWS) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int r = row_of(i), x = elem_of() / 8;
+            if constexpr (KROWS) {
+                to[i] = r * (GEN_B / 8) + (((x >> 1) ^ swz<true>(r)) << 1 | (x & 1));
+                // (columns that are not there read the first ones: their results are not stored)
+                at[i] = static_cast<const T *>(s.base) + (elem_of() < s.valid ? elem_of() : 0) + (IDX ? 0 : r * s.stride);
+            } else {
+                to[i] = r * 8 + (x ^ swz<false>(r));
+                at[i] = r < s.valid ? row_at<T>(s, r) : nullptr;
+            }
+        }
+    }
+    // the rows' numbers of step k0, -1 where there is none
+    GM_DEV void fetch_ids(const Side &s, int k0, int n_k) {
+        if constexpr (KROWS && IDX) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const int r = (threadIdx.x + i * GEN_T) / 8;
-                row[i] = r < s.valid ? row_at<T>(s, r) : nullptr;
+                const int k = k0 + row_of(i);
+                ids[i] = k < n_k ? s.index[k] : -1;
             }
         }
     }
-    // chunk i of this thread, reduction elements k0 .. k0 + BK of n_k
-    GM_DEV void load(const Side &s, int64_t k0, int64_t n_k) {
+    // the chunks of reduction elements k0 .. k0 + BK of n_k, step after step (by index: of the numbers fetched
+    // last; the next step's are on their way before the chunks are, so that waiting for them does not wait
+    // for these)
+    GM_DEV void load(const Side &s, int k0, int n_k, u32x4(&v)[N]) {
+        if constexpr (KROWS) {
+            const int left = s.valid - (elem_of() < s.valid ? elem_of() : 0);
+            const bool whole = (s.valid & 7) == 0;
+            if constexpr (IDX) {
+                int32_t now[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = threadIdx.x + i * GEN_T;
-            if constexpr (KROWS) {
-                const int64_t k = k0 + c / (GEN_B / 8);
-                const int col = c % (GEN_B / 8) * 8;
-                const T *p = k < n_k && col < s.valid ? row_at<T>(s, k) : nullptr;
-                v[i] = p ? load8(p + col, s.valid - col) : u32x4{0, 0, 0, 0};
+                for (int i = 0; i < N; ++i) now[i] = ids[i] >= (int)s.n_mem ? -1 : ids[i];
+                fetch_ids(s, k0 + BK, n_k);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const T *p = at[i] + (int64_t)(now[i] < 0 ? 0 : now[i]) * s.stride;
+                    v[i] = whole ? load8(p, 8) : load8(p, left);
+                    if (now[i] < 0) v[i] = u32x4{0, 0, 0, 0};
+                }
+            } else if (whole && n_k - k0 >= BK) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[i] = load8(at[i], 8);
             } else {
-                const int64_t k = k0 + c % 8 * 8;
-                const int64_t left = n_k - k;
-                v[i] = row[i] ? load8(row[i] + k, left > 8 ? 8 : (int)left) : u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[i] = load8(at[i], k0 + row_of(i) < n_k ? left : 0);
+            }
+            if constexpr (!IDX)
+#pragma unroll
+                for (int i = 0; i < N; ++i) at[i] += BK * s.stride;
+        } else {
+            const int x = k0 + elem_of();
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                v[i] = u32x4{0, 0, 0, 0};
+                if (at[i]) v[i] = n_k - k0 >= BK ? load8(at[i] + x, 8) : load8(at[i] + x, n_k - x);
             }
         }
     }
-    GM_DEV void store(u32x4 *lds) const {
+    GM_DEV void store(u32x4 *lds, const u32x4(&v)[N]) const {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = threadIdx.x + i * GEN_T;
-            if constexpr (KROWS) {
-                const int k = c / (GEN_B / 8), s = c % (GEN_B / 8);
-                lds[k * (GEN_B / 8) + (((s >> 1) ^ swz<true>(k)) << 1 | (s & 1))] = v[i];
-            } else {
-                const int r = c / 8;
-                lds[r * 8 + ((c % 8) ^ swz<false>(r))] = v[i];
-            }
-        }
+        for (int i = 0; i < N; ++i) lds[to[i]] = v[i];
     }
 };
 
-// A wave's fragment of 16 rows from x0 and 32 reduction elements from 32 * kk:
-// lane l holds row l % 16, elements 8 * (l / 16) .. + 8.
-template <bool KROWS, int B>
-GM_DEV u32x4 fragment(const u32x4 *lds, int x0, int kk) {
-    const int lane = threadIdx.x & 63, i = lane % 16, g = lane / 16;
-    if constexpr (KROWS) {
-        // the transposing read: of 16 lanes, lane 4j + p brings four elements from
-        // column 4p of row j; lane i gets column i of the four rows
-        u32x2 h[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int k = kk * 32 + g * 8 + j * 4 + i / 4;
-            const int u = (x0 / 16) ^ swz<true>(k);
-            const char *p = reinterpret_cast<const char *>(lds) + k * (B * 2) + u * 32 + (i % 4) * 8;
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            h[j] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p));
-        }
-        return u32x4{h[0][0], h[0][1], h[1][0], h[1][1]};
-    } else {
-        const int r = x0 + i;
-        return lds[r * 8 + ((kk * 4 + g) ^ swz<false>(r))];
-    }
-}
-
-template <typename T, typename OUT, bool PK, bool QK>
-GM_DEV void tile_any(const Side &p, const Side &q, int64_t n_k, OUT *out, int64_t out_stride, bool wide, u32x4 *lds) {
-    u32x4 *lp = lds, *lq = lds + GEN_B * BK / 8;
-    Staged<T, PK> sp;
-    Staged<T, QK> sq;
+template <typename T, typename OUT, bool PK, bool QK, bool QI>
+GM_DEV void tile_any(const Side &p, const Side &q, int n_k, OUT *out, int64_t out_stride, u32x4 *lds) {
+    constexpr int BUF = GEN_B * BK / 8;  // chunks of a tile
+    Staged<T, PK, false> sp;
+    Staged<T, QK, QI> sq;
     sp.init(p);
     sq.init(q);
     const int lane = threadIdx.x & 63, w = threadIdx.x / 64;
     const int p0 = w / 2 * 64, q0 = w % 2 * 64;
+    const Reader<PK, GEN_B> rp(p0);
+    const Reader<QK, GEN_B> rq(q0);
     f32x4 acc[4][4] = {};
-    sp.load(p, 0, n_k);
-    sq.load(q, 0, n_k);
-    for (int64_t k0 = 0; k0 < n_k; k0 += BK) {
-        __syncthreads();
-        sp.store(lp);
-        sq.store(lq);
-        __syncthreads();
-        if (k0 + BK < n_k) {
-            sp.load(p, k0 + BK, n_k);
-            sq.load(q, k0 + BK, n_k);
+    u32x4 vp[2][decltype(sp)::N], vq[2][decltype(sq)::N];
+    auto load = [&](int k0, int set) {
+        if (k0 < n_k) {
+            sp.load(p, k0, n_k, vp[set]);
+            sq.load(q, k0, n_k, vq[set]);
         }
+    };
+    auto step = [&](int k0, int set) {
+        u32x4 *lp = lds + set * 2 * BUF, *lq = lp + BUF;
+        sp.store(lp, vp[set]);
+        sq.store(lq, vq[set]);
+        __syncthreads();
+        load(k0 + 2 * BK, set);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
             u32x4 fp[4], fq[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                fp[i] = fragment<PK, GEN_B>(lp, p0 + 16 * i, kk);
-                fq[i] = fragment<QK, GEN_B>(lq, q0 + 16 * i, kk);
+                fp[i] = rp.get(reinterpret_cast<const char *>(lp), kk, i);
+                fq[i] = rq.get(reinterpret_cast<const char *>(lq), kk, i);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[i][j] = mfma_16x16x32(fq[j], fp[i], acc[i][j], T{});
         }
+    };
+    sq.fetch_ids(q, 0, n_k);
+    load(0, 0);
+    load(BK, 1);
+    __syncthreads();  // (the last tile's reads of LDS)
+    for (int k0 = 0; k0 < n_k; k0 += 2 * BK) {
+        step(k0, 0);
+        if (k0 + BK < n_k) step(k0 + BK, 1);
     }
     __syncthreads();
 #pragma unroll
@@ -135,7 +154,7 @@ GM_DEV void tile_any(const Side &p, const Side &q, int64_t n_k, OUT *out, int64_
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int c = q0 + 16 * j + lane / 16 * 4;
-                store4(out + r * out_stride + c, acc[i][j], q.valid - c, wide);
+                store4(out + r * out_stride + c, acc[i][j], q.valid - c);
             }
         }
     }
@@ -149,7 +168,7 @@ GM_DEV void tile_any(const Side &p, const Side &q, int64_t n_k, OUT *out, int64_
 // into LDS are spread over two units: issued together they hold every wave up
 // at the memory pipeline while the matrix units idle.
 template <typename T, typename OUT, bool PK, bool QK, bool PI, bool QI, int BP, int BQ, int WP, int WQ>
-GM_DEV void tile_fast(const Dma &p, const Dma &q, int n_k, OUT *out, int64_t out_stride, bool wide, char *lds) {
+GM_DEV void tile_fast(const Dma &p, const Dma &q, int n_k, OUT *out, int64_t out_stride, char *lds) {
     constexpr int THREADS = 64 * WP * WQ, MP = BP / WP, MQ = BQ / WQ, NP = MP / 32, NQ = MQ / 16;
     constexpr int PB = BP * BK * 2, QB = BQ * BK * 2;
     char *lp = lds, *lq = lds + 2 * PB;
@@ -230,7 +249,7 @@ GM_DEV void tile_fast(const Dma &p, const Dma &q, int n_k, OUT *out, int64_t out
 #pragma unroll
             for (int j = 0; j < NQ; ++j) {
                 const int c = q0 + 16 * j + lane / 16 * 4;
-                store4(out + r * out_stride + c, acc[i / NP][i % NP][j], q.valid - c, wide);
+                store4(out + r * out_stride + c, acc[i / NP][i % NP][j], q.valid - c);
             }
         }
     }
@@ -243,13 +262,12 @@ struct ProductArgs {
     const void *x, *w;
     void *y;
     int64_t xs, ws, wg, ys;  // strides: rows of X, rows of W, matrices of W, rows of Y
-    bool wide;               // 16-byte aligned rows of Y
     int64_t max_row_tiles;   // what the rows allow, whatever group_ptr holds
 };
 
 template <typename T, typename OUT, bool TRANS>
-__global__ __launch_bounds__(GEN_T) void k_group_product_any(ProductArgs a) {
-    __shared__ u32x4 lds[2 * GEN_B * BK / 8];
+__global__ __launch_bounds__(GEN_T, 2) void k_group_product_any(ProductArgs a) {
+    __shared__ u32x4 lds[4 * GEN_B * BK / 8];
     const int64_t n_row = min(count_row_tiles<GEN_B>(a.gp, a.n_groups, a.n_rows), a.max_row_tiles);
     const int64_t n_col = (a.n + GEN_B - 1) / GEN_B, total = n_row * n_col;
     for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
@@ -270,7 +288,7 @@ __global__ __launch_bounds__(GEN_T) void k_group_product_any(ProductArgs a) {
             p.base = static_cast<const T *>(a.x) + t.begin * a.xs;
         const T *w = static_cast<const T *>(a.w) + t.group * a.wg + (TRANS ? q0 : q0 * a.ws);
         const Side q{w, a.ws, nullptr, 0, cols};
-        tile_any<T, OUT, false, TRANS>(p, q, a.k, out, a.ys, a.wide, lds);
+        tile_any<T, OUT, false, TRANS, false>(p, q, (int)a.k, out, a.ys, lds);
     }
 }
 
@@ -300,7 +318,7 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_product_fast(ProductA
         const char *w = static_cast<const char *>(a.w) + (t.group * a.wg + (TRANS ? q0 : q0 * a.ws)) * 2;
         const uint32_t wb = (uint32_t)(TRANS ? cols * 2 : ((cols - 1) * a.ws + a.k) * 2);
         const Dma q{w, wb, a.ws * 2, nullptr, 0, cols};
-        tile_fast<T, OUT, false, TRANS, true, false, BP, BQ, WP, WQ>(p, q, (int)a.k, out, a.ys, a.wide, lds_fast);
+        tile_fast<T, OUT, false, TRANS, true, false, BP, BQ, WP, WQ>(p, q, (int)a.k, out, a.ys, lds_fast);
     }
 }
 
@@ -391,7 +409,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_group_product_few(ProductArgs a)
 #pragma unroll
             for (int v = 1; v < WAVES; ++v) s += *reinterpret_cast<const f32x4 *>(&part[v][r][c]);
             if (x_row(a, t, r) < 0) s = f32x4{0, 0, 0, 0};
-            store4(out + r * a.ys + c, s, cols - c, a.wide);
+            store4(out + r * a.ys + c, s, cols - c);
         }
     }
 }
@@ -403,7 +421,6 @@ struct OuterArgs {
     const void *dy, *x;
     void *d;
     int64_t dys, xs, ds, dg;
-    bool wide;
 };
 
 // Tile t of the stack of gradients: its group, tile row and tile column. A tile
@@ -427,9 +444,9 @@ GM_DEV void outer_tile(const OuterArgs &a, int64_t t, int64_t n_row, int64_t n_c
     band_tile(xcd_tile(t - place * per, per), n_row, n_col, tr, tc);
 }
 
-template <typename T, typename OUT>
-__global__ __launch_bounds__(GEN_T) void k_group_outer_any(OuterArgs a) {
-    __shared__ u32x4 lds[2 * GEN_B * BK / 8];
+template <typename T, typename OUT, bool IDX>
+__global__ __launch_bounds__(GEN_T, 2) void k_group_outer_any(OuterArgs a) {
+    __shared__ u32x4 lds[4 * GEN_B * BK / 8];
     const int64_t n_row = (a.n + GEN_B - 1) / GEN_B, n_col = (a.k + GEN_B - 1) / GEN_B;
     const int64_t per = n_row * n_col, total = per * a.n_groups;
     for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
@@ -440,12 +457,14 @@ __global__ __launch_bounds__(GEN_T) void k_group_outer_any(OuterArgs a) {
         const Side p{static_cast<const T *>(a.dy) + begin * a.dys + p0, a.dys, nullptr, 0,
                      (int)(a.n - p0 < GEN_B ? a.n - p0 : GEN_B)};
         Side q{static_cast<const T *>(a.x) + q0, a.xs, nullptr, a.n_x, (int)(a.k - q0 < GEN_B ? a.k - q0 : GEN_B)};
-        if (a.index)
+        if constexpr (IDX) {
             q.index = a.index + begin;
-        else
+            if (a.n_x == 0) end = begin;  // (no row to read: all zeros)
+        } else {
             q.base = static_cast<const T *>(a.x) + begin * a.xs + q0;
+        }
         OUT *out = static_cast<OUT *>(a.d) + e * a.dg + p0 * a.ds + q0;
-        tile_any<T, OUT, true, true>(p, q, end - begin, out, a.ds, a.wide, lds);
+        tile_any<T, OUT, true, true, IDX>(p, q, (int)(end - begin), out, a.ds, lds);
     }
 }
 
@@ -481,7 +500,7 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_outer_fast(OuterArgs 
             q.base += begin * q.stride;
         }
         OUT *out = static_cast<OUT *>(a.d) + e * a.dg + p0 * a.ds + q0;
-        tile_fast<T, OUT, true, true, false, IDX, BP, BQ, WP, WQ>(p, q, (int)(end - begin), out, a.ds, a.wide, lds_fast);
+        tile_fast<T, OUT, true, true, false, IDX, BP, BQ, WP, WQ>(p, q, (int)(end - begin), out, a.ds, lds_fast);
     }
 }
 
@@ -535,8 +554,7 @@ extern "C" gmagnus_status_t gmagnus_group_product(const gmagnus_groups_t *groups
                    "Y must have the type of X, or fp32");
         if (groups->n_rows == 0) return;
         const ProductArgs a{groups->group_ptr, groups->index, groups->n_groups, groups->n_rows, X->n_rows, n, k,
-                            X->data, W->data, Y->data, X->row_stride, W->row_stride, W->stack_stride, Y->row_stride,
-                            aligned16(Y->data, Y->row_stride, 0, data_size(Y->data_type)), 0};
+                            X->data, W->data, Y->data, X->row_stride, W->row_stride, W->stack_stride, Y->row_stride, 0};
         hipStream_t s = (hipStream_t)hip_stream;
         const Shape shape = product_shape(a, transposed);
         with_elem(X->data_type, Y->data_type, [&](auto t, auto o) {
@@ -594,35 +612,30 @@ extern "C" gmagnus_status_t gmagnus_group_outer(const gmagnus_groups_t *groups, 
         GM_REQUIRE(groups->n_groups <= 1 || D->stack_stride >= (n - 1) * D->row_stride + k, GMAGNUS_ERROR_INVALID_VALUE,
                    "matrices of D overlap");
         const OuterArgs a{groups->group_ptr, groups->index, groups->n_groups, groups->n_rows, X->n_rows, n, k,
-                          DY->data, X->data, D->data, DY->row_stride, X->row_stride, D->row_stride, D->stack_stride,
-                          aligned16(D->data, D->row_stride, D->stack_stride, data_size(D->data_type))};
+                          DY->data, X->data, D->data, DY->row_stride, X->row_stride, D->row_stride, D->stack_stride};
         hipStream_t s = (hipStream_t)hip_stream;
-        if (fast_side(a.dy, a.dys, 0, n, BK) && fast_side(a.x, a.xs, 0, k, a.index ? a.n_x : BK)) {
-            const bool big = big_tiles(n, k, a.n_groups);
-            with_elem(X->data_type, D->data_type, [&](auto t, auto o) {
-                using T = decltype(t);
-                using O = decltype(o);
-                auto go = [&](auto idx) {
-                    constexpr bool IX = decltype(idx)::value;
-                    if (big)
-                        launch_fast(k_group_outer_fast<T, O, IX, 256, 256, 2, 4>, (n + 255) / 256 * ((k + 255) / 256) * a.n_groups,
-                                    512, fast_bytes(256, 256), a, s);
-                    else
-                        launch_fast(k_group_outer_fast<T, O, IX, 128, 128, 2, 2>, (n + 127) / 128 * ((k + 127) / 128) * a.n_groups,
-                                    256, fast_bytes(128, 128), a, s);
-                };
-                if (a.index)
-                    go(std::true_type{});
-                else
-                    go(std::false_type{});
-            });
-            GM_CHECK_LAUNCH();
-            return;
-        }
-        const int64_t tiles = ((n + GEN_B - 1) / GEN_B) * ((k + GEN_B - 1) / GEN_B);
-        const int64_t total = tiles > MAX_GRID / a.n_groups ? MAX_GRID : tiles * a.n_groups;
+        const bool fast = fast_side(a.dy, a.dys, 0, n, BK) && fast_side(a.x, a.xs, 0, k, a.index ? a.n_x : BK);
+        const bool big = big_tiles(n, k, a.n_groups);
         with_elem(X->data_type, D->data_type, [&](auto t, auto o) {
-            hipLaunchKernelGGL((k_group_outer_any<decltype(t), decltype(o)>), dim3((unsigned)total), dim3(GEN_T), 0, s, a);
+            using T = decltype(t);
+            using O = decltype(o);
+            auto launch = [&](auto kernel, int b, int threads, int lds) {
+                const int64_t tiles = (n + b - 1) / b * ((k + b - 1) / b);
+                launch_fast(kernel, tiles > MAX_GRID / a.n_groups ? MAX_GRID : tiles * a.n_groups, threads, lds, a, s);
+            };
+            auto go = [&](auto idx) {
+                constexpr bool IX = decltype(idx)::value;
+                if (!fast)
+                    launch(k_group_outer_any<T, O, IX>, GEN_B, GEN_T, 0);
+                else if (big)
+                    launch(k_group_outer_fast<T, O, IX, 256, 256, 2, 4>, 256, 512, fast_bytes(256, 256));
+                else
+                    launch(k_group_outer_fast<T, O, IX, 128, 128, 2, 2>, 128, 256, fast_bytes(128, 128));
+            };
+            if (a.index)
+                go(std::true_type{});
+            else
+                go(std::false_type{});
         });
         GM_CHECK_LAUNCH();
     });

@@ -131,7 +131,6 @@ struct Fp8Args {
     const float *sx, *sw;
     void *y;
     int64_t xs, sxs, ws, wg, sws, swg, ys;
-    bool wide;
     int64_t max_row_tiles;
 };
 
@@ -149,9 +148,11 @@ GM_DEV u32x4 load16(const uint8_t *p, int64_t valid) {
         const Bytes16<1> b = *reinterpret_cast<const Bytes16<1> *>(p);
         r = u32x4{b.v[0], b.v[1], b.v[2], b.v[3]};
     } else if (valid > 0) {
+        uint32_t e[16];
 #pragma unroll
-        for (int i = 0; i < 15; ++i)
-            if (i < valid) r[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+        for (int i = 0; i < 16; ++i) e[i] = p[i < valid ? i : 0];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) r[i >> 2] |= (i < valid ? e[i] : 0u) << (8 * (i & 3));
     }
     return r;
 }
@@ -163,7 +164,7 @@ GM_DEV u32x4 load16(const uint8_t *p, int64_t valid) {
 constexpr int GEN_B = 128, GEN_T = 256;
 
 template <typename OUT>
-__global__ __launch_bounds__(GEN_T) void k_group_product_fp8_any(Fp8Args a) {
+__global__ __launch_bounds__(GEN_T, 2) void k_group_product_fp8_any(Fp8Args a) {
     __shared__ u32x4 lds[2 * GEN_B * 8];
     u32x4 *lp = lds, *lq = lds + GEN_B * 8;
     const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16, wv = threadIdx.x / 64;
@@ -242,7 +243,7 @@ __global__ __launch_bounds__(GEN_T) void k_group_product_fp8_any(Fp8Args a) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int c = q0 + 16 * j + g * 4;
-                    store4(out + r * a.ys + c, acc[i][j], cols - c, a.wide);
+                    store4(out + r * a.ys + c, acc[i][j], cols - c);
                 }
         }
     }
@@ -380,7 +381,7 @@ GM_DEV void tile_fp8_fast(const Fp8Args &a, const RowTile &t, int64_t n0, int co
 #pragma unroll
             for (int j = 0; j < NQ; ++j) {
                 const int c = q0 + 16 * j + lane / 16 * 4;
-                store4(out + r * a.ys + c, acc[i][j], cols - c, a.wide);
+                store4(out + r * a.ys + c, acc[i][j], cols - c);
             }
         }
     }
@@ -486,7 +487,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_group_product_fp8_few(Fp8Args a)
 #pragma unroll
             for (int v = 1; v < WAVES; ++v) s += *reinterpret_cast<const f32x4 *>(&part[v][r][c]);
             if (x_row(a, t, r) < 0) s = f32x4{0, 0, 0, 0};
-            store4(out + r * a.ys + c, s, cols - c, a.wide);
+            store4(out + r * a.ys + c, s, cols - c);
         }
     }
 }
@@ -584,8 +585,7 @@ extern "C" gmagnus_status_t gmagnus_group_product_fp8(const gmagnus_groups_t *gr
         const Fp8Args a{groups->group_ptr, groups->index, groups->n_groups, groups->n_rows, n_x, n, k,
                         (const uint8_t *)X->data, (const uint8_t *)W->data, (const float *)X_scale->data,
                         (const float *)W_scale->data, Y->data, X->row_stride, X_scale->row_stride, W->row_stride,
-                        W->stack_stride, W_scale->row_stride, W_scale->stack_stride, Y->row_stride,
-                        aligned16(Y->data, Y->row_stride, 0, data_size(Y->data_type)), 0};
+                        W->stack_stride, W_scale->row_stride, W_scale->stack_stride, Y->row_stride, 0};
         hipStream_t s = (hipStream_t)hip_stream;
         auto launch = [&](auto o) {
             using O = decltype(o);
