@@ -196,10 +196,10 @@ GM_DEV const T *row_at(const Side &s, int64_t r) {
     return static_cast<const T *>(s.base) + r * s.stride;
 }
 
-// Four neighbours of an output row, as many as there are, at any alignment.
+// Four neighbours of an output row, from `first` on as many as there are, at any alignment.
 template <typename OUT>
-GM_DEV void store4(OUT *p, f32x4 v, int64_t left) {
-    if (left >= 4) {
+GM_DEV void store4(OUT *p, f32x4 v, int64_t left, int first = 0) {
+    if (left >= 4 && first <= 0) {
         if constexpr (sizeof(OUT) == 4) {
             *reinterpret_cast<Bytes16<4> *>(p) = Bytes16<4>{{__float_as_uint(v[0]), __float_as_uint(v[1]),
                                                              __float_as_uint(v[2]), __float_as_uint(v[3])}};
@@ -212,7 +212,7 @@ GM_DEV void store4(OUT *p, f32x4 v, int64_t left) {
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (i < left) p[i] = (OUT)v[i];
+            if (i >= first && i < left) p[i] = (OUT)v[i];
     }
 }
 

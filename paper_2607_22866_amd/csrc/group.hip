@@ -99,8 +99,14 @@ struct Staged {
     }
 };
 
+// First element of tile `t` of B on an axis of n elements that is contiguous in
+// memory: the last tile is moved back to end with the axis, so that no piece of
+// 8 elements is cut (16384 rows, 2047 x 2047, transposed product and gradient:
+// 364 -> 239 us, 472 -> 323). What an earlier tile stores as well is skipped.
+GM_DEV int64_t tile_start(int64_t t, int64_t n, int b) { return t * b + b > n && n > b ? n - b : t * b; }
+
 template <typename T, typename OUT, bool PK, bool QK, bool QI>
-GM_DEV void tile_any(const Side &p, const Side &q, int n_k, OUT *out, int64_t out_stride, u32x4 *lds) {
+GM_DEV void tile_any(const Side &p, const Side &q, int n_k, OUT *out, int64_t out_stride, int skip_p, int skip_q, u32x4 *lds) {
     constexpr int BUF = GEN_B * BK / 8;  // chunks of a tile
     Staged<T, PK, false> sp;
     Staged<T, QK, QI> sq;
@@ -150,11 +156,11 @@ GM_DEV void tile_any(const Side &p, const Side &q, int n_k, OUT *out, int64_t ou
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = p0 + 16 * i + lane % 16;
-        if (r < p.valid) {
+        if (r >= skip_p && r < p.valid) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int c = q0 + 16 * j + lane / 16 * 4;
-                store4(out + r * out_stride + c, acc[i][j], q.valid - c);
+                store4(out + r * out_stride + c, acc[i][j], q.valid - c, skip_q - c);
             }
         }
     }
@@ -274,7 +280,7 @@ __global__ __launch_bounds__(GEN_T, 2) void k_group_product_any(ProductArgs a) {
         int64_t tr, tc;
         band_tile(xcd_tile(b, total), n_row, n_col, tr, tc);
         const RowTile t = find_row_tile<GEN_B>(a.gp, a.n_groups, a.n_rows, tr);
-        const int64_t q0 = tc * GEN_B;
+        const int64_t q0 = TRANS ? tile_start(tc, a.n, GEN_B) : tc * GEN_B;
         const int cols = (int)(a.n - q0 < GEN_B ? a.n - q0 : GEN_B);
         OUT *out = static_cast<OUT *>(a.y) + t.begin * a.ys + q0;
         if (t.group >= a.n_groups) {
@@ -288,7 +294,7 @@ __global__ __launch_bounds__(GEN_T, 2) void k_group_product_any(ProductArgs a) {
             p.base = static_cast<const T *>(a.x) + t.begin * a.xs;
         const T *w = static_cast<const T *>(a.w) + t.group * a.wg + (TRANS ? q0 : q0 * a.ws);
         const Side q{w, a.ws, nullptr, 0, cols};
-        tile_any<T, OUT, false, TRANS, false>(p, q, (int)a.k, out, a.ys, lds);
+        tile_any<T, OUT, false, TRANS, false>(p, q, (int)a.k, out, a.ys, 0, (int)(tc * GEN_B - q0), lds);
     }
 }
 
@@ -453,7 +459,7 @@ __global__ __launch_bounds__(GEN_T, 2) void k_group_outer_any(OuterArgs a) {
         int64_t e, tr, tc, begin, end;
         outer_tile(a, b, n_row, n_col, e, tr, tc);
         group_rows(a.gp, a.n_groups, a.n_rows, e, begin, end);
-        const int64_t p0 = tr * GEN_B, q0 = tc * GEN_B;
+        const int64_t p0 = tile_start(tr, a.n, GEN_B), q0 = tile_start(tc, a.k, GEN_B);
         const Side p{static_cast<const T *>(a.dy) + begin * a.dys + p0, a.dys, nullptr, 0,
                      (int)(a.n - p0 < GEN_B ? a.n - p0 : GEN_B)};
         Side q{static_cast<const T *>(a.x) + q0, a.xs, nullptr, a.n_x, (int)(a.k - q0 < GEN_B ? a.k - q0 : GEN_B)};
@@ -464,7 +470,7 @@ __global__ __launch_bounds__(GEN_T, 2) void k_group_outer_any(OuterArgs a) {
             q.base = static_cast<const T *>(a.x) + begin * a.xs + q0;
         }
         OUT *out = static_cast<OUT *>(a.d) + e * a.dg + p0 * a.ds + q0;
-        tile_any<T, OUT, true, true, IDX>(p, q, (int)(end - begin), out, a.ds, lds);
+        tile_any<T, OUT, true, true, IDX>(p, q, (int)(end - begin), out, a.ds, (int)(tr * GEN_B - p0), (int)(tc * GEN_B - q0), lds);
     }
 }
 
