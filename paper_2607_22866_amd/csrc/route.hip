@@ -2,25 +2,46 @@
 // with their softmax weights, as CSR by token and by expert; its gradient; and
 // the products of that matrix with a tall dense one (a token's weighted sum of
 // its results) with theirs.
+#include <type_traits>
+
 #include "dense.hpp"
 
 namespace gm {
 namespace {
 
 constexpr int MAX_EXPERTS = 1024;
-constexpr int TOK = 64;            // tokens a work group of the routing takes: one bit each in an expert's mask
+constexpr int TOK = 32;            // tokens a work group of the routing takes: one bit each in an expert's mask
 constexpr int ROUTE_T = 1024;      // its threads
 constexpr int ROUTE_W = ROUTE_T / GM_WAVE;
 
 // ---------------------------------------------------------------- selection
-// A logit as an unsigned number of the same order; 0 for what is masked (-inf,
-// NaN). -0 counts as +0.
-GM_DEV uint32_t order_key(float x) {
-    const uint32_t u = __float_as_uint(x + 0.0f);
-    const uint32_t k = u >> 31 ? ~u : u | 0x80000000u;
-    return x > -INFINITY ? k : 0u;
+// A logit as an unsigned number of the same order, in as many bits as its type
+// has (KEY_BITS); 0 for what is masked (-inf, NaN). -0 counts as +0.
+template <typename T>
+constexpr int KEY_BITS = 8 * (int)sizeof(T);
+
+template <typename T>
+GM_DEV uint32_t order_key(T v) {
+    const float x = to_f32(v);
+    if constexpr (sizeof(T) == 4) {
+        const uint32_t u = __float_as_uint(x + 0.0f);
+        return x > -INFINITY ? (u >> 31 ? ~u : u | 0x80000000u) : 0u;
+    } else {
+        const uint32_t u = x == 0.f ? 0u : __builtin_bit_cast(uint16_t, v);
+        return x > -INFINITY ? (u >> 15 ? ~u & 0xffffu : u | 0x8000u) : 0u;
+    }
 }
-GM_DEV float key_value(uint32_t k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
+template <typename T>
+GM_DEV float key_value(uint32_t k) {
+    if constexpr (sizeof(T) == 4)
+        return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k);
+    else
+        return to_f32(__builtin_bit_cast(T, (uint16_t)(k >> 15 ? k & 0x7fffu : ~k)));
+}
+
+// e^x for x <= 0, by the hardware's power of two: a few units more off than expf
+// and, like the rounding of x itself, by |x| units of 2^-24.
+GM_DEV float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 GM_DEV uint32_t wave_max(uint32_t x) {
 #define GM_STEP(ctrl, rows) \
@@ -43,7 +64,7 @@ struct RouteArgs {
     int64_t n_blocks;
     gmagnus_routing_t out;
     // workspace
-    uint64_t *mask;     // [n_blocks][n_experts]: the tokens of the block that chose the expert
+    uint32_t *mask;     // [n_blocks][n_experts]: the tokens of the block that chose the expert
     int32_t *base;      // [n_blocks][n_experts]: entries of the expert in earlier blocks
     int32_t *total;     // [n_experts]
     int32_t *block_n;   // [n_blocks]: entries
@@ -54,50 +75,65 @@ struct RouteArgs {
 };
 
 // One token by one wave: marks its bit in the chosen experts' masks (LDS) and
-// writes its list. Lane l holds experts l, l + 64, ... (V of them). The largest
-// left is taken top_k times: a maximum over the wave, then the lowest expert
-// that holds it.
+// writes its list. Lane l holds experts l, l + 64, ... (V of them). The top_k-th
+// largest key is found bit by bit from the top: a bit stays if at least top_k
+// keys reach it, and once just top_k do, those are the choice (16384 tokens, 256
+// experts, top_k 8: 20 us; taking the maximum over the wave top_k times: 37).
+// Keys equal to the last one are taken from the lowest expert on.
 template <typename T, int V>
-GM_DEV int select_token(const RouteArgs &a, int64_t t, int bit, uint64_t *mask) {
+GM_DEV int select_token(const RouteArgs &a, int64_t t, int bit, const T (&l)[V], uint32_t *mask) {
     const int lane = threadIdx.x & 63;
-    const T *row = static_cast<const T *>(a.logits) + t * a.stride;
-    uint32_t key[V], left[V];
+    uint32_t key[V], best = 0;
     uint64_t chosen[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const int e = j * 64 + lane;
-        left[j] = key[j] = e < a.n_experts ? order_key(to_f32(row[e])) : 0u;
-        chosen[j] = 0;
+        key[j] = j * 64 + lane < a.n_experts ? order_key(l[j]) : 0u;
+        best = best > key[j] ? best : key[j];
     }
-    uint32_t best = 0;
-    int n = 0;
-    for (; n < a.top_k; ++n) {
-        uint32_t m = left[0];
+    best = wave_max(best);
+    const float top = key_value<T>(best);
+    auto reach = [&](uint32_t least) {  // keys of at least `least` (above 0)
+        int n = 0;
 #pragma unroll
-        for (int j = 1; j < V; ++j) m = m > left[j] ? m : left[j];
-        m = wave_max(m);
-        if (m == 0) break;
-        if (n == 0) best = m;
-        bool found = false;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const uint64_t hit = found ? 0 : ballot(left[j] == m);
-            if (hit) {
-                found = true;
-                const int l = __ffsll((unsigned long long)hit) - 1;
-                chosen[j] |= uint64_t(1) << l;
-                if (lane == l) left[j] = 0;
+        for (int j = 0; j < V; ++j) n += __popcll(ballot(key[j] >= least));
+        return n;
+    };
+    int n = reach(1);
+    uint32_t least = 1;
+    if (n > a.top_k) {
+        least = 0;
+        for (uint32_t b = 1u << (KEY_BITS<T> - 1); b; b >>= 1) {
+            const int m = reach(least | b);
+            if (m >= a.top_k) {
+                least |= b;
+                n = m;
+                if (m == a.top_k) break;
             }
         }
     }
-    const float top = key_value(best);
+    // n keys reach `least`; more than top_k only where several equal it
+    int spare = n > a.top_k ? n - a.top_k : 0;
+#pragma unroll
+    for (int j = V - 1; j >= 0; --j) {
+        chosen[j] = ballot(key[j] >= least);
+        if (spare > 0) {
+            uint64_t last = ballot(key[j] == least);
+            while (spare > 0 && last) {
+                const uint64_t high = uint64_t(1) << (63 - __clzll((long long)last));
+                last ^= high;
+                chosen[j] ^= high;
+                --spare;
+            }
+        }
+    }
+    n = n < a.top_k ? n : a.top_k;
     float p[V], sum = 0.f;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        p[j] = key[j] ? expf(key_value(key[j]) - top) : 0.f;
+        p[j] = key[j] ? exp_neg(key_value<T>(key[j]) - top) : 0.f;
         if (!a.normalise || (chosen[j] >> lane & 1)) sum += p[j];
     }
-    sum = wave_sum(sum);
+    const float scale = 1.f / wave_sum(sum);
     int before = 0;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
@@ -105,8 +141,8 @@ GM_DEV int select_token(const RouteArgs &a, int64_t t, int bit, uint64_t *mask) 
             const int e = j * 64 + lane;
             const int64_t at = t * a.top_k + before + __popcll(chosen[j] & lanemask_lt());
             a.list_e[at] = (uint16_t)e;
-            a.list_w[at] = p[j] / sum;
-            atomicOr((unsigned long long *)&mask[e], 1ull << bit);
+            a.list_w[at] = p[j] * scale;
+            atomicOr(&mask[e], 1u << bit);
         }
         before += __popcll(chosen[j]);
     }
@@ -114,40 +150,49 @@ GM_DEV int select_token(const RouteArgs &a, int64_t t, int bit, uint64_t *mask) 
     return n;
 }
 
-template <typename T>
-GM_DEV void select_block(const RouteArgs &a, int64_t blk, uint64_t *mask, int *block_n) {
+// The tokens of a wave, the next one's logits on their way while one is chosen from.
+template <typename T, int V>
+GM_DEV int select_tokens(const RouteArgs &a, int64_t t0, int tokens, uint32_t *mask) {
+    const int lane = threadIdx.x & 63;
+    T l[V], next[V];
+    auto fetch = [&](int i, T(&v)[V]) {
+        const T *row = static_cast<const T *>(a.logits) + (t0 + i) * a.stride;
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = row[j * 64 + lane < a.n_experts ? j * 64 + lane : 0];
+    };
+    int n = 0, i = threadIdx.x / 64;
+    if (i < tokens) fetch(i, l);
+    for (; i < tokens; i += ROUTE_W) {
+        if (i + ROUTE_W < tokens) fetch(i + ROUTE_W, next);
+        n += select_token<T, V>(a, t0 + i, i, l, mask);
+#pragma unroll
+        for (int j = 0; j < V; ++j) l[j] = next[j];
+    }
+    return n;
+}
+
+template <typename T, int V>
+GM_DEV void select_block(const RouteArgs &a, int64_t blk, uint32_t *mask, int *block_n) {
     const int64_t t0 = blk * TOK;
     const int tokens = (int)(a.n_tokens - t0 < TOK ? a.n_tokens - t0 : TOK);
     for (int e = threadIdx.x; e < a.n_experts; e += ROUTE_T) mask[e] = 0;
     if (threadIdx.x == 0) *block_n = 0;
     __syncthreads();
-    int n = 0;
-    for (int i = threadIdx.x / 64; i < tokens; i += ROUTE_W) {
-        if (a.n_experts <= 64)
-            n += select_token<T, 1>(a, t0 + i, i, mask);
-        else if (a.n_experts <= 128)
-            n += select_token<T, 2>(a, t0 + i, i, mask);
-        else if (a.n_experts <= 256)
-            n += select_token<T, 4>(a, t0 + i, i, mask);
-        else if (a.n_experts <= 512)
-            n += select_token<T, 8>(a, t0 + i, i, mask);
-        else
-            n += select_token<T, 16>(a, t0 + i, i, mask);
-    }
+    const int n = select_tokens<T, V>(a, t0, tokens, mask);
     if ((threadIdx.x & 63) == 0 && n) atomicAdd(block_n, n);
     __syncthreads();
 }
 
 // Writes a block's entries in both orders. start[e]: the expert's first grouped
 // row that is this block's; first: the block's first entry.
-GM_DEV void place_block(const RouteArgs &a, int64_t blk, const uint64_t *mask, const int32_t *start, int64_t first,
+GM_DEV void place_block(const RouteArgs &a, int64_t blk, const uint32_t *mask, const int32_t *start, int64_t first,
                         int64_t n_entries, int *upto) {
     const int64_t t0 = blk * TOK;
     const int tokens = (int)(a.n_tokens - t0 < TOK ? a.n_tokens - t0 : TOK);
-    if (threadIdx.x < TOK) {
+    if (threadIdx.x < GM_WAVE) {
         const int c = (int)threadIdx.x < tokens ? a.count[t0 + threadIdx.x] : 0;
         const int inc = wave_incl_scan<int32_t>(c);
-        upto[threadIdx.x] = inc - c;
+        if (threadIdx.x < TOK) upto[threadIdx.x] = inc - c;
         if ((int)threadIdx.x < tokens) a.out.row_ptr[t0 + threadIdx.x] = first + inc - c;
     }
     __syncthreads();
@@ -159,7 +204,7 @@ GM_DEV void place_block(const RouteArgs &a, int64_t blk, const uint64_t *mask, c
             const int e = a.list_e[src];
             const float w = a.list_w[src];
             const int64_t at = first + upto[t] + j;
-            const int32_t row = start[e] + __popcll(mask[e] & ((uint64_t(1) << t) - 1));
+            const int32_t row = start[e] + __popc(mask[e] & ((1u << t) - 1));
             a.out.expert[at] = e;
             a.out.weight[at] = w;
             a.out.slot[at] = row;
@@ -173,15 +218,15 @@ GM_DEV void place_block(const RouteArgs &a, int64_t blk, const uint64_t *mask, c
     }
 }
 
-// At most 64 tokens: one work group does it all.
-template <typename T>
+// At most 32 tokens: one work group does it all.
+template <typename T, int V>
 __global__ __launch_bounds__(ROUTE_T) void k_route_small(RouteArgs a) {
-    __shared__ uint64_t mask[MAX_EXPERTS];
+    __shared__ uint32_t mask[MAX_EXPERTS];
     __shared__ int32_t start[MAX_EXPERTS], scan[ROUTE_W], upto[TOK];
     __shared__ int block_n;
-    select_block<T>(a, 0, mask, &block_n);
+    select_block<T, V>(a, 0, mask, &block_n);
     const int e = threadIdx.x;
-    const int n = e < a.n_experts ? __popcll(mask[e]) : 0;
+    const int n = e < a.n_experts ? __popc(mask[e]) : 0;
     const int at = block_excl_scan<ROUTE_T, int32_t>(n, scan);
     if (e < a.n_experts) {
         start[e] = at;
@@ -192,12 +237,12 @@ __global__ __launch_bounds__(ROUTE_T) void k_route_small(RouteArgs a) {
     place_block(a, 0, mask, start, 0, block_n, upto);
 }
 
-template <typename T>
+template <typename T, int V>
 __global__ __launch_bounds__(ROUTE_T) void k_route_select(RouteArgs a) {
-    __shared__ uint64_t mask[MAX_EXPERTS];
+    __shared__ uint32_t mask[MAX_EXPERTS];
     __shared__ int block_n;
     for (int64_t blk = blockIdx.x; blk < a.n_blocks; blk += gridDim.x) {
-        select_block<T>(a, blk, mask, &block_n);
+        select_block<T, V>(a, blk, mask, &block_n);
         for (int e = threadIdx.x; e < a.n_experts; e += ROUTE_T) a.mask[blk * a.n_experts + e] = mask[e];
         if (threadIdx.x == 0) a.block_n[blk] = block_n;
         __syncthreads();
@@ -228,7 +273,7 @@ __global__ __launch_bounds__(ROUTE_T) void k_route_scan(RouteArgs a) {
     const int64_t b0 = run * per, b1 = b0 + per < a.n_blocks ? b0 + per : a.n_blocks;
     int32_t n = 0;
     if (e < a.n_experts)
-        for (int64_t b = b0; b < b1; ++b) n += __popcll(a.mask[b * a.n_experts + e]);
+        for (int64_t b = b0; b < b1; ++b) n += __popc(a.mask[b * a.n_experts + e]);
     part[run][x] = n;
     __syncthreads();
     int32_t at = 0;
@@ -237,13 +282,13 @@ __global__ __launch_bounds__(ROUTE_T) void k_route_scan(RouteArgs a) {
         if (run == SCAN_RUNS - 1) a.total[e] = at + n;
         for (int64_t b = b0; b < b1; ++b) {
             a.base[b * a.n_experts + e] = at;
-            at += __popcll(a.mask[b * a.n_experts + e]);
+            at += __popc(a.mask[b * a.n_experts + e]);
         }
     }
 }
 
 __global__ __launch_bounds__(ROUTE_T) void k_route_place(RouteArgs a) {
-    __shared__ uint64_t mask[MAX_EXPERTS];
+    __shared__ uint32_t mask[MAX_EXPERTS];
     __shared__ int32_t start[MAX_EXPERTS], scan[ROUTE_W], upto[TOK];
     const int e = threadIdx.x;
     const int32_t at = block_excl_scan<ROUTE_T, int32_t>(e < a.n_experts ? a.total[e] : 0, scan);
@@ -274,64 +319,69 @@ struct RouteBackArgs {
     const float *weight, *d_weight;
 };
 
-// A wave a token. Lane l holds experts l, l + 64, ...
+// A wave a token. Lane l holds experts l, l + 64, ...; the entries' gradients (and
+// weights) reach their lanes through LDS.
 template <typename T, int V>
 __global__ __launch_bounds__(256) void k_route_backward(RouteBackArgs a) {
-    const int lane = threadIdx.x & 63;
-    for (int64_t t = blockIdx.x * 4ll + threadIdx.x / 64; t < a.n_tokens; t += gridDim.x * 4ll) {
+    __shared__ float grad[4][V * 64], prob[4][V * 64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x / 64;
+    for (int64_t t = blockIdx.x * 4ll + w; t < a.n_tokens; t += gridDim.x * 4ll) {
+        T l[V];  // (on their way while the row's entries are looked up)
+        if (!a.normalise) {
+            const T *row = static_cast<const T *>(a.logits) + t * a.stride;
+#pragma unroll
+            for (int j = 0; j < V; ++j) l[j] = row[j * 64 + lane < a.n_experts ? j * 64 + lane : 0];
+        }
         int64_t b = a.row_ptr[t], f = a.row_ptr[t + 1];
         b = b < 0 ? 0 : b > a.cap ? a.cap : b;
         f = f < b ? b : f > a.cap ? a.cap : f;
-        float p[V], g[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) p[j] = g[j] = 0.f;
-        if (!a.normalise) {
-            const T *row = static_cast<const T *>(a.logits) + t * a.stride;
+        for (int j = 0; j < V; ++j) {
+            grad[w][j * 64 + lane] = 0.f;
+            if (a.normalise) prob[w][j * 64 + lane] = 0.f;
+        }
+        wave_lds_fence();
+        float dot = 0.f;
+        for (int64_t i = b + lane; i < f; i += 64) {
+            const uint32_t e = (uint32_t)a.expert[i];
+            const float p = a.weight[i], g = a.d_weight[i];
+            if (e < (uint32_t)a.n_experts) {
+                grad[w][e] = g;
+                if (a.normalise) prob[w][e] = p;
+                dot += p * g;
+            }
+        }
+        wave_lds_fence();
+        dot = wave_sum(dot);
+        float p[V];
+        if (a.normalise) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) p[j] = prob[w][j * 64 + lane];
+        } else {
             uint32_t key[V], m = 0;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const int e = j * 64 + lane;
-                key[j] = e < a.n_experts ? order_key(to_f32(row[e])) : 0u;
+                key[j] = j * 64 + lane < a.n_experts ? order_key(l[j]) : 0u;
                 m = m > key[j] ? m : key[j];
             }
-            const float top = key_value(wave_max(m));
+            const float top = key_value<T>(wave_max(m));
             float sum = 0.f;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                p[j] = key[j] ? expf(key_value(key[j]) - top) : 0.f;
+                p[j] = key[j] ? exp_neg(key_value<T>(key[j]) - top) : 0.f;
                 sum += p[j];
             }
-            sum = wave_sum(sum);
+            const float scale = 1.f / wave_sum(sum);
 #pragma unroll
-            for (int j = 0; j < V; ++j) p[j] = key[j] ? p[j] / sum : 0.f;
+            for (int j = 0; j < V; ++j) p[j] = key[j] ? p[j] * scale : 0.f;
         }
-        for (int64_t i0 = b; i0 < f; i0 += 64) {
-            const int n = (int)(f - i0 < 64 ? f - i0 : 64);
-            const int64_t i = i0 + (lane < n ? lane : 0);
-            const int le = a.expert[i];
-            const float lw = a.weight[i], lg = a.d_weight[i];
-            for (int s = 0; s < n; ++s) {
-                const int e = __builtin_amdgcn_readlane(le, s);
-                const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lw), s));
-                const float d = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lg), s));
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if (e == j * 64 + lane) {
-                        g[j] = d;
-                        if (a.normalise) p[j] = w;
-                    }
-            }
-        }
-        float dot = 0.f;
-#pragma unroll
-        for (int j = 0; j < V; ++j) dot += p[j] * g[j];
-        dot = wave_sum(dot);
         T *out = static_cast<T *>(a.d_logits) + t * a.d_stride;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const int e = j * 64 + lane;
-            if (e < a.n_experts) out[e] = (T)(p[j] * (g[j] - dot));
+            if (e < a.n_experts) out[e] = (T)(p[j] * (grad[w][e] - dot));
         }
+        wave_lds_fence();
     }
 }
 
@@ -470,6 +520,23 @@ void with_float(int32_t type, F &&f) {
         f(float{});
 }
 
+// f(T{}, V{}): the logits' type, and how many of a row's e experts a lane holds.
+template <class F>
+void with_logits(int32_t type, int64_t e, F &&f) {
+    with_float(type, [&](auto v) {
+        if (e <= 64)
+            f(v, std::integral_constant<int, 1>{});
+        else if (e <= 128)
+            f(v, std::integral_constant<int, 2>{});
+        else if (e <= 256)
+            f(v, std::integral_constant<int, 4>{});
+        else if (e <= 512)
+            f(v, std::integral_constant<int, 8>{});
+        else
+            f(v, std::integral_constant<int, 16>{});
+    });
+}
+
 struct RouteLayout {
     int64_t n_blocks, mask, base, total, block_n, block_at, count, list_e, list_w, bytes;
     RouteLayout(int64_t t, int64_t e, int64_t k) {
@@ -481,7 +548,7 @@ struct RouteLayout {
         };
         n_blocks = (t + TOK - 1) / TOK;
         const bool small = t <= TOK;  // one work group: lists only
-        mask = take(small ? 0 : n_blocks * e * 8);
+        mask = take(small ? 0 : n_blocks * e * 4);
         base = take(small ? 0 : n_blocks * e * 4);
         total = take(small ? 0 : e * 4);
         block_n = take(small ? 0 : n_blocks * 4);
@@ -539,17 +606,18 @@ extern "C" gmagnus_status_t gmagnus_route(const gmagnus_dense_t *logits, int64_t
         GM_REQUIRE((uintptr_t)workspace % 16 == 0, GMAGNUS_ERROR_INVALID_VALUE, "workspace is not 16-byte aligned");
         char *w = static_cast<char *>(workspace);
         const RouteArgs a{logits->data, t, logits->row_stride, (int)e, (int)top_k, normalise, l.n_blocks, *out,
-                          (uint64_t *)(w + l.mask), (int32_t *)(w + l.base), (int32_t *)(w + l.total),
+                          (uint32_t *)(w + l.mask), (int32_t *)(w + l.base), (int32_t *)(w + l.total),
                           (int32_t *)(w + l.block_n), (int64_t *)(w + l.block_at), (int32_t *)(w + l.count),
                           (uint16_t *)(w + l.list_e), (float *)(w + l.list_w)};
-        with_float(logits->data_type, [&](auto v) {
+        with_logits(logits->data_type, e, [&](auto v, auto per_lane) {
             using T = decltype(v);
+            constexpr int V = decltype(per_lane)::value;
             if (l.n_blocks == 1) {
-                hipLaunchKernelGGL(k_route_small<T>, dim3(1), dim3(ROUTE_T), 0, s, a);
+                hipLaunchKernelGGL((k_route_small<T, V>), dim3(1), dim3(ROUTE_T), 0, s, a);
                 return;
             }
             const dim3 grid(grid_for(l.n_blocks, 1, 1 << 20));
-            hipLaunchKernelGGL(k_route_select<T>, grid, dim3(ROUTE_T), 0, s, a);
+            hipLaunchKernelGGL((k_route_select<T, V>), grid, dim3(ROUTE_T), 0, s, a);
             hipLaunchKernelGGL(k_route_scan, dim3((unsigned)((e + SCAN_E - 1) / SCAN_E + 1)), dim3(ROUTE_T), 0, s, a);
             hipLaunchKernelGGL(k_route_place, grid, dim3(ROUTE_T), 0, s, a);
         });
@@ -573,18 +641,8 @@ extern "C" gmagnus_status_t gmagnus_route_backward(const gmagnus_dense_t *logits
                               (int)e, normalise, routing->row_ptr, routing->expert, routing->weight, d_weight};
         hipStream_t s = (hipStream_t)hip_stream;
         const dim3 grid(grid_for(t, 4, 1 << 16));
-        with_float(logits->data_type, [&](auto v) {
-            using T = decltype(v);
-            if (e <= 64)
-                hipLaunchKernelGGL((k_route_backward<T, 1>), grid, dim3(256), 0, s, a);
-            else if (e <= 128)
-                hipLaunchKernelGGL((k_route_backward<T, 2>), grid, dim3(256), 0, s, a);
-            else if (e <= 256)
-                hipLaunchKernelGGL((k_route_backward<T, 4>), grid, dim3(256), 0, s, a);
-            else if (e <= 512)
-                hipLaunchKernelGGL((k_route_backward<T, 8>), grid, dim3(256), 0, s, a);
-            else
-                hipLaunchKernelGGL((k_route_backward<T, 16>), grid, dim3(256), 0, s, a);
+        with_logits(logits->data_type, e, [&](auto v, auto per_lane) {
+            hipLaunchKernelGGL((k_route_backward<decltype(v), decltype(per_lane)::value>), grid, dim3(256), 0, s, a);
         });
         GM_CHECK_LAUNCH();
     });
