@@ -96,44 +96,63 @@ GM_DEV void group_rows(const int64_t *gp, int64_t n_groups, int64_t n_rows, int6
     end = f < begin ? begin : f > n_rows ? n_rows : f;
 }
 
-// Row tiles of at most BM rows, group after group, the rows past the last
-// group as one more. A wave counts them 64 groups at a time; all lanes get the
-// same answer.
-template <int BM>
-GM_DEV int64_t count_row_tiles(const int64_t *gp, int64_t n_groups, int64_t n_rows) {
+// Row tiles of at most BM rows, group after group, the rows past the last group
+// as one more. With HALF a group's last tile of at most BM / 2 rows is a tile of
+// that height, and those come after all others: less padding is computed, and
+// the work groups that start last have little to do. A wave counts 64 groups at
+// a time; all lanes get the same answer.
+struct RowTiles {
+    int64_t full, half;
+};
+
+template <int BM, bool HALF>
+GM_DEV void tiles_of(const int64_t *gp, int64_t n_groups, int64_t n_rows, int64_t e, int64_t &b, int64_t &f, int &full, int &half) {
+    b = f = 0;
+    if (e <= n_groups) group_rows(gp, n_groups, n_rows, e, b, f);
+    const int rows = (int)(f - b), rem = rows % BM;
+    half = HALF && e < n_groups && rem > 0 && rem <= BM / 2;
+    full = (rows + BM - 1) / BM - half;
+}
+
+template <int BM, bool HALF = false>
+GM_DEV RowTiles count_row_tiles(const int64_t *gp, int64_t n_groups, int64_t n_rows, int64_t most) {
     const int lane = threadIdx.x & (GM_WAVE - 1);
-    int n = 0;
+    int n = 0, h = 0;
     for (int64_t e = lane; e <= n_groups; e += GM_WAVE) {
         int64_t b, f;
-        group_rows(gp, n_groups, n_rows, e, b, f);
-        n += (int)((f - b + BM - 1) / BM);
+        int full, half;
+        tiles_of<BM, HALF>(gp, n_groups, n_rows, e, b, f, full, half);
+        n += full;
+        h += half;
     }
-    return wave_reduce_sum<int32_t>(n);
+    const int64_t full = wave_reduce_sum<int32_t>(n), half = HALF ? wave_reduce_sum<int32_t>(h) : 0;
+    // (`most`: what the rows allow, whatever group_ptr holds)
+    return RowTiles{full < most ? full : most, half < most ? half : most};
 }
 
 struct RowTile {
     int64_t group;  // n_groups: rows past the last group
     int64_t begin;  // first row
-    int rows;       // at most BM
+    int rows;       // at most BM, a half tile's at most BM / 2
 };
 
-// Tile t of the order above (t is below the count).
-template <int BM>
-GM_DEV RowTile find_row_tile(const int64_t *gp, int64_t n_groups, int64_t n_rows, int64_t t) {
+// Tile t of the full (`half`: of the half) ones in the order above, t below their count.
+template <int BM, bool HALF = false>
+GM_DEV RowTile find_row_tile(const int64_t *gp, int64_t n_groups, int64_t n_rows, int64_t t, bool half = false) {
     const int lane = threadIdx.x & (GM_WAVE - 1);
     int left = (int)t;
     for (int64_t e0 = 0; e0 <= n_groups; e0 += GM_WAVE) {
-        const int64_t e = e0 + lane;
-        int64_t b = 0, f = 0;
-        if (e <= n_groups) group_rows(gp, n_groups, n_rows, e, b, f);
-        const int n = (int)((f - b + BM - 1) / BM);
+        int64_t b, f;
+        int n, h;
+        tiles_of<BM, HALF>(gp, n_groups, n_rows, e0 + lane, b, f, n, h);
+        if (HALF && half) n = h;
         const int upto = wave_incl_scan<int32_t>(n);
         const uint64_t hit = ballot(upto > left);
         if (hit) {
             const int src = __ffsll((unsigned long long)hit) - 1;
             const int in = left - (__builtin_amdgcn_readlane(upto, src) - __builtin_amdgcn_readlane(n, src));
             const int64_t gb = __builtin_amdgcn_readlane((int)b, src), gf = __builtin_amdgcn_readlane((int)f, src);
-            const int64_t begin = gb + (int64_t)in * BM;
+            const int64_t begin = HALF && half ? gf - (gf - gb) % BM : gb + (int64_t)in * BM;
             return RowTile{e0 + src, begin, (int)(gf - begin < BM ? gf - begin : BM)};
         }
         left -= __builtin_amdgcn_readlane(upto, GM_WAVE - 1);

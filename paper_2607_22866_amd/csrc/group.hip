@@ -274,7 +274,7 @@ struct ProductArgs {
 template <typename T, typename OUT, bool TRANS>
 __global__ __launch_bounds__(GEN_T, 2) void k_group_product_any(ProductArgs a) {
     __shared__ u32x4 lds[4 * GEN_B * BK / 8];
-    const int64_t n_row = min(count_row_tiles<GEN_B>(a.gp, a.n_groups, a.n_rows), a.max_row_tiles);
+    const int64_t n_row = count_row_tiles<GEN_B>(a.gp, a.n_groups, a.n_rows, a.max_row_tiles).full;
     const int64_t n_col = (a.n + GEN_B - 1) / GEN_B, total = n_row * n_col;
     for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
         int64_t tr, tc;
@@ -301,12 +301,17 @@ __global__ __launch_bounds__(GEN_T, 2) void k_group_product_any(ProductArgs a) {
 template <typename T, typename OUT, bool TRANS, int BP, int BQ, int WP, int WQ>
 __global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_product_fast(ProductArgs a) {
     extern __shared__ char lds_fast[];
-    const int64_t n_row = min(count_row_tiles<BP>(a.gp, a.n_groups, a.n_rows), a.max_row_tiles);
-    const int64_t n_col = (a.n + BQ - 1) / BQ, total = n_row * n_col;
+    constexpr bool HALF = BP >= 128;
+    const RowTiles n_row = count_row_tiles<BP, HALF>(a.gp, a.n_groups, a.n_rows, a.max_row_tiles);
+    const int64_t n_col = (a.n + BQ - 1) / BQ, n_full = n_row.full * n_col, total = n_full + n_row.half * n_col;
     for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
+        const bool half = HALF && b >= n_full;
         int64_t tr, tc;
-        band_tile(xcd_tile(b, total), n_row, n_col, tr, tc);
-        const RowTile t = find_row_tile<BP>(a.gp, a.n_groups, a.n_rows, tr);
+        if (half)
+            band_tile(xcd_tile(b - n_full, total - n_full), n_row.half, n_col, tr, tc);
+        else
+            band_tile(xcd_tile(b, n_full), n_row.full, n_col, tr, tc);
+        const RowTile t = find_row_tile<BP, HALF>(a.gp, a.n_groups, a.n_rows, tr, half);
         const int64_t q0 = tc * BQ;
         const int cols = (int)(a.n - q0 < BQ ? a.n - q0 : BQ);
         OUT *out = static_cast<OUT *>(a.y) + t.begin * a.ys + q0;
@@ -324,6 +329,11 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_product_fast(ProductA
         const char *w = static_cast<const char *>(a.w) + (t.group * a.wg + (TRANS ? q0 : q0 * a.ws)) * 2;
         const uint32_t wb = (uint32_t)(TRANS ? cols * 2 : ((cols - 1) * a.ws + a.k) * 2);
         const Dma q{w, wb, a.ws * 2, nullptr, 0, cols};
+        if constexpr (HALF)
+            if (half) {
+                tile_fast<T, OUT, false, TRANS, true, false, BP / 2, BQ, WP, WQ>(p, q, (int)a.k, out, a.ys, lds_fast);
+                continue;
+            }
         tile_fast<T, OUT, false, TRANS, true, false, BP, BQ, WP, WQ>(p, q, (int)a.k, out, a.ys, lds_fast);
     }
 }
@@ -351,7 +361,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_group_product_few(ProductArgs a)
     __shared__ float part[WAVES][BP][BQ + 4];
     const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16;
     const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
-    const int64_t n_row = min(count_row_tiles<BP>(a.gp, a.n_groups, a.n_rows), a.max_row_tiles);
+    const int64_t n_row = count_row_tiles<BP>(a.gp, a.n_groups, a.n_rows, a.max_row_tiles).full;
     const int64_t n_col = (a.n + BQ - 1) / BQ, total = n_row * n_col;
     const int n_k = (int)a.k, full = n_k / 64;
     for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
