@@ -55,26 +55,42 @@ GM_DEV void store_fp8x8(uint8_t *p, int valid, const float (&v)[8], float scale)
     }
 }
 
-// One scale a row and 128 columns: 16 lanes a block, eight values a lane.
+// One scale a row and 128 columns: 16 lanes a block, eight values a lane, a work
+// group 16 blocks of one row or, of rows shorter than that, several rows.
 template <typename T>
 __global__ __launch_bounds__(256) void k_quantise_rows(QuantArgs a) {
-    const int64_t blocks = (a.n_cols + SB - 1) / SB, total = a.n_stack * a.n_rows * blocks;
-    const int lane = threadIdx.x & 63;
-    for (int64_t u0 = blockIdx.x * 16ll + threadIdx.x / 64 * 4; u0 < total; u0 += gridDim.x * 16ll) {
-        const int64_t u = u0 + lane / 16;
-        const int64_t row = u / blocks, b = u - row * blocks, g = row / a.n_rows, r = row - g * a.n_rows;
-        const int64_t c0 = b * SB + lane % 16 * 8;
-        const int valid = u >= total || c0 >= a.n_cols ? 0 : a.n_cols - c0 >= 8 ? 8 : (int)(a.n_cols - c0);
-        float v[8] = {};
-        if (valid > 0) load_f32x8(static_cast<const T *>(a.x) + g * a.xg + r * a.xs + c0, valid, v);
-        uint32_t m = 0;
+    const int blocks = (int)((a.n_cols + SB - 1) / SB), wide = blocks < 16 ? blocks : 16, per = 16 / wide;
+    const int unit = threadIdx.x / 16, ur = unit / wide, ub = unit - ur * wide;
+    const int64_t rows = a.n_stack * a.n_rows;
+    for (int64_t row0 = (int64_t)blockIdx.x * per; row0 < rows; row0 += (int64_t)gridDim.x * per) {
+        const int64_t row = row0 + ur;
+        const bool mine = ur < per && row < rows;
+        const int64_t g = a.n_stack == 1 || !mine ? 0 : row / a.n_rows, r = mine ? row - g * a.n_rows : 0;
+        const T *x = static_cast<const T *>(a.x) + g * a.xg + r * a.xs;
+        for (int b0 = 0; b0 < blocks; b0 += 2 * wide) {
+            float v[2][8];
+            int valid[2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
+            for (int h = 0; h < 2; ++h) {
+                const int64_t c0 = (int64_t)(b0 + h * wide + ub) * SB + threadIdx.x % 16 * 8;
+                valid[h] = !mine || c0 >= a.n_cols ? 0 : a.n_cols - c0 >= 8 ? 8 : (int)(a.n_cols - c0);
 #pragma unroll
-        for (int d = 1; d < 16; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d, 64));
-        const float s = block_scale(m);
-        if (valid > 0) store_fp8x8(a.q + g * a.qg + r * a.qs + c0, valid, v, s);
-        if (u < total && lane % 16 == 0) a.scale[g * a.sg + r * a.ss + b] = s;
+                for (int i = 0; i < 8; ++i) v[h][i] = 0.f;
+                if (valid[h] > 0) load_f32x8(x + c0, valid[h], v[h]);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int b = b0 + h * wide + ub;
+                uint32_t m = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[h][i]));
+#pragma unroll
+                for (int d = 1; d < 16; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d, 64));
+                const float s = block_scale(m);
+                if (valid[h] > 0) store_fp8x8(a.q + g * a.qg + r * a.qs + (int64_t)b * SB + threadIdx.x % 16 * 8, valid[h], v[h], s);
+                if (mine && b < blocks && threadIdx.x % 16 == 0) a.scale[g * a.sg + r * a.ss + b] = s;
+            }
+        }
     }
 }
 
@@ -554,8 +570,8 @@ extern "C" gmagnus_status_t gmagnus_quantise_blocks(const gmagnus_dense_t *X, in
         auto launch = [&](auto v) {
             using T = decltype(v);
             if (block_rows == 1) {
-                const int64_t units = n_stack * n * scale->n_cols;
-                hipLaunchKernelGGL(k_quantise_rows<T>, dim3(grid_for(units, 16, MAX_GRID)), dim3(256), 0, s, a);
+                const int per = scale->n_cols < 16 ? (int)(16 / scale->n_cols) : 1;
+                hipLaunchKernelGGL(k_quantise_rows<T>, dim3(grid_for(n_stack * n, per, MAX_GRID)), dim3(256), 0, s, a);
             } else {
                 hipLaunchKernelGGL(k_quantise_tiles<T>, dim3(grid_for(n_stack * scale->n_rows * scale->n_cols, 1, MAX_GRID)),
                                    dim3(256), 0, s, a);
