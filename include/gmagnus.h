@@ -397,7 +397,8 @@ gmagnus_status_t gmagnus_bandwidth_probe(int32_t kind, void *dst, const void *sr
  * (group_ptr, index, slot) are trusted as the routing gives them, but numbers
  * out of range never lead to an access outside the arrays: an index outside
  * X reads as a row of zeros, bounds are clamped to the rows there are.
- * Sums are held in fp32; results are rounded once, to the output's type. */
+ * Sums are held in fp32 (8-bit operands: see there); results are rounded
+ * once, to the output's type. */
 typedef enum {
     GMAGNUS_DATA_FP32 = 0,
     GMAGNUS_DATA_BF16 = 1,
@@ -497,7 +498,9 @@ gmagnus_status_t gmagnus_quantise_blocks(const gmagnus_dense_t *X, int64_t n_sta
 /* gmagnus_group_product (W N x K) on E4M3 operands: X with a scale for each row
  * and 128 columns, W with one for each 128 rows and 128 columns, as
  * gmagnus_quantise_blocks gives them. The products of a block of 128 are
- * summed by the matrix units and its sum scaled in fp32. Y is bf16, fp16 or fp32.
+ * summed by the matrix units (16 at a time to 13 bits below the largest one's
+ * leading bit, the rest in fp32) and its sum is scaled and added in fp32. Y is
+ * bf16, fp16 or fp32.
  * One group is the plain matrix product.
  * Errors as gmagnus_group_product. */
 gmagnus_status_t gmagnus_group_product_fp8(const gmagnus_groups_t *groups, const gmagnus_dense_t *X,
