@@ -102,7 +102,7 @@ GM_DEV void group_rows(const int64_t *gp, int64_t n_groups, int64_t n_rows, int6
 // the work groups that start last have little to do. A wave counts 64 groups at
 // a time; all lanes get the same answer.
 struct RowTiles {
-    int64_t full, half;
+    uint32_t full, half;
 };
 
 template <int BM, bool HALF>
@@ -125,9 +125,10 @@ GM_DEV RowTiles count_row_tiles(const int64_t *gp, int64_t n_groups, int64_t n_r
         n += full;
         h += half;
     }
-    const int64_t full = wave_reduce_sum<int32_t>(n), half = HALF ? wave_reduce_sum<int32_t>(h) : 0;
+    const uint32_t full = wave_reduce_sum<int32_t>(n), half = HALF ? wave_reduce_sum<int32_t>(h) : 0, m = (uint32_t)most;
     // (`most`: what the rows allow, whatever group_ptr holds)
-    return RowTiles{full < most ? full : most, half < most ? half : most};
+    const uint32_t f = full < m ? full : m;
+    return RowTiles{f, half < m - f ? half : m - f};
 }
 
 struct RowTile {
@@ -138,7 +139,7 @@ struct RowTile {
 
 // Tile t of the full (`half`: of the half) ones in the order above, t below their count.
 template <int BM, bool HALF = false>
-GM_DEV RowTile find_row_tile(const int64_t *gp, int64_t n_groups, int64_t n_rows, int64_t t, bool half = false) {
+GM_DEV RowTile find_row_tile(const int64_t *gp, int64_t n_groups, int64_t n_rows, uint32_t t, bool half = false) {
     const int lane = threadIdx.x & (GM_WAVE - 1);
     int left = (int)t;
     for (int64_t e0 = 0; e0 <= n_groups; e0 += GM_WAVE) {
@@ -165,12 +166,25 @@ inline int64_t row_tiles_bound(int64_t n_groups, int64_t n_rows, int bm) {
     return n_rows / bm + (n_groups + 1 < n_rows ? n_groups + 1 : n_rows);
 }
 
+// Place of tile number b of n when each XCD gets a run of neighbours (the
+// hardware deals consecutive work groups round-robin to the 8 XCDs). 32 bits: a
+// tile's fixed work is worth counting when it has a step or two.
+GM_DEV uint32_t xcd_place(uint32_t b, uint32_t n) {
+    const uint32_t per = n / 8, rem = n % 8, x = b % 8;
+    return x * per + (x < rem ? x : rem) + b / 8;
+}
+
 // Tile (row tile, column tile) number t: bands of 8 column tiles, row tiles
 // within a band, so that the tiles in flight on one XCD share rows and columns.
-GM_DEV void band_tile(int64_t t, int64_t n_row, int64_t n_col, int64_t &row, int64_t &col) {
-    constexpr int64_t BAND = 8;
-    const int64_t band = t / (n_row * BAND), r = t - band * n_row * BAND;
-    const int64_t w = n_col - band * BAND < BAND ? n_col - band * BAND : BAND;
+GM_DEV void band_tile(uint32_t t, uint32_t n_row, uint32_t n_col, uint32_t &row, uint32_t &col) {
+    constexpr uint32_t BAND = 8;
+    if (n_col <= BAND) {
+        row = t / n_col;
+        col = t - row * n_col;
+        return;
+    }
+    const uint32_t band = t / (n_row * BAND), r = t - band * n_row * BAND;
+    const uint32_t w = n_col - band * BAND < BAND ? n_col - band * BAND : BAND;
     row = r / w;
     col = band * BAND + (r - row * w);
 }

@@ -274,13 +274,13 @@ struct ProductArgs {
 template <typename T, typename OUT, bool TRANS>
 __global__ __launch_bounds__(GEN_T, 2) void k_group_product_any(ProductArgs a) {
     __shared__ u32x4 lds[4 * GEN_B * BK / 8];
-    const int64_t n_row = count_row_tiles<GEN_B>(a.gp, a.n_groups, a.n_rows, a.max_row_tiles).full;
-    const int64_t n_col = (a.n + GEN_B - 1) / GEN_B, total = n_row * n_col;
-    for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
-        int64_t tr, tc;
-        band_tile(xcd_tile(b, total), n_row, n_col, tr, tc);
+    const uint32_t n_row = count_row_tiles<GEN_B>(a.gp, a.n_groups, a.n_rows, a.max_row_tiles).full;
+    const uint32_t n_col = (uint32_t)((a.n + GEN_B - 1) / GEN_B), total = n_row * n_col;
+    for (uint32_t b = blockIdx.x; b < total; b += gridDim.x) {
+        uint32_t tr, tc;
+        band_tile(xcd_place(b, total), n_row, n_col, tr, tc);
         const RowTile t = find_row_tile<GEN_B>(a.gp, a.n_groups, a.n_rows, tr);
-        const int64_t q0 = TRANS ? tile_start(tc, a.n, GEN_B) : tc * GEN_B;
+        const int64_t q0 = TRANS ? tile_start(tc, a.n, GEN_B) : (int64_t)tc * GEN_B;
         const int cols = (int)(a.n - q0 < GEN_B ? a.n - q0 : GEN_B);
         OUT *out = static_cast<OUT *>(a.y) + t.begin * a.ys + q0;
         if (t.group >= a.n_groups) {
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(GEN_T, 2) void k_group_product_any(ProductArgs a) {
             p.base = static_cast<const T *>(a.x) + t.begin * a.xs;
         const T *w = static_cast<const T *>(a.w) + t.group * a.wg + (TRANS ? q0 : q0 * a.ws);
         const Side q{w, a.ws, nullptr, 0, cols};
-        tile_any<T, OUT, false, TRANS, false>(p, q, (int)a.k, out, a.ys, 0, (int)(tc * GEN_B - q0), lds);
+        tile_any<T, OUT, false, TRANS, false>(p, q, (int)a.k, out, a.ys, 0, (int)((int64_t)tc * GEN_B - q0), lds);
     }
 }
 
@@ -303,16 +303,16 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_product_fast(ProductA
     extern __shared__ char lds_fast[];
     constexpr bool HALF = BP >= 128;
     const RowTiles n_row = count_row_tiles<BP, HALF>(a.gp, a.n_groups, a.n_rows, a.max_row_tiles);
-    const int64_t n_col = (a.n + BQ - 1) / BQ, n_full = n_row.full * n_col, total = n_full + n_row.half * n_col;
-    for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
+    const uint32_t n_col = (uint32_t)((a.n + BQ - 1) / BQ), n_full = n_row.full * n_col, total = n_full + n_row.half * n_col;
+    for (uint32_t b = blockIdx.x; b < total; b += gridDim.x) {
         const bool half = HALF && b >= n_full;
-        int64_t tr, tc;
+        uint32_t tr, tc;
         if (half)
-            band_tile(xcd_tile(b - n_full, total - n_full), n_row.half, n_col, tr, tc);
+            band_tile(xcd_place(b - n_full, total - n_full), n_row.half, n_col, tr, tc);
         else
-            band_tile(xcd_tile(b, n_full), n_row.full, n_col, tr, tc);
+            band_tile(xcd_place(b, n_full), n_row.full, n_col, tr, tc);
         const RowTile t = find_row_tile<BP, HALF>(a.gp, a.n_groups, a.n_rows, tr, half);
-        const int64_t q0 = tc * BQ;
+        const int64_t q0 = (int64_t)tc * BQ;
         const int cols = (int)(a.n - q0 < BQ ? a.n - q0 : BQ);
         OUT *out = static_cast<OUT *>(a.y) + t.begin * a.ys + q0;
         if (t.group >= a.n_groups) {
@@ -361,12 +361,13 @@ __global__ __launch_bounds__(64 * WAVES) void k_group_product_few(ProductArgs a)
     __shared__ float part[WAVES][BP][BQ + 4];
     const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16;
     const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
-    const int64_t n_row = count_row_tiles<BP>(a.gp, a.n_groups, a.n_rows, a.max_row_tiles).full;
-    const int64_t n_col = (a.n + BQ - 1) / BQ, total = n_row * n_col;
+    const uint32_t n_row = count_row_tiles<BP>(a.gp, a.n_groups, a.n_rows, a.max_row_tiles).full;
+    const uint32_t n_col = (uint32_t)((a.n + BQ - 1) / BQ), total = n_row * n_col;
     const int n_k = (int)a.k, full = n_k / 64;
-    for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
+    for (uint32_t b = blockIdx.x; b < total; b += gridDim.x) {
         // the row tiles of a group meet its weights one after the other
-        const int64_t tr = b % n_row, q0 = b / n_row * BQ;
+        const uint32_t tc = b / n_row, tr = b - tc * n_row;
+        const int64_t q0 = (int64_t)tc * BQ;
         const RowTile t = find_row_tile<BP>(a.gp, a.n_groups, a.n_rows, tr);
         const int cols = (int)(a.n - q0 < BQ ? a.n - q0 : BQ);
         OUT *out = static_cast<OUT *>(a.y) + t.begin * a.ys + q0;
@@ -437,36 +438,42 @@ struct OuterArgs {
     const void *dy, *x;
     void *d;
     int64_t dys, xs, ds, dg;
+    bool by_size;  // see outer_tile
 };
 
 // Tile t of the stack of gradients: its group, tile row and tile column. A tile
-// costs as much as its group has rows, so of each 64 groups the longest come
-// first and the last work groups to start have little to do; a group's tiles
-// are spread over the XCDs, neighbours together (measured on 16 groups of 16384
-// rows cut at random, 2048 x 2048, against groups in order with a run of them
-// for each XCD: see the kernels below).
-GM_DEV void outer_tile(const OuterArgs &a, int64_t t, int64_t n_row, int64_t n_col, int64_t &e, int64_t &tr, int64_t &tc) {
-    const int64_t per = n_row * n_col, place = t / per, e0 = place / GM_WAVE * GM_WAVE;
-    const int lane = threadIdx.x & 63, want = (int)(place - e0);
-    int64_t b = 0, f = -1;
-    if (e0 + lane < a.n_groups) group_rows(a.gp, a.n_groups, a.n_rows, e0 + lane, b, f);
-    const int size = (int)(f - b);  // (lanes past the last group: -1, after all others)
-    int rank = 0;
-    for (int o = 0; o < GM_WAVE; ++o) {
-        const int other = __builtin_amdgcn_readlane(size, o);
-        rank += other > size || (other == size && o < lane);
+// costs as much as its group has rows, so where the groups are long (by_size) of
+// each 64 the longest come first, and the last work groups to start have little
+// to do; a group's tiles are spread over the XCDs, neighbours together. (16
+// groups of 16384 rows cut at random, 2048 x 2048: 179 us; groups in order with a
+// run of tiles for each XCD: 271 us. Ordering costs a tile about a microsecond.)
+GM_DEV void outer_tile(const OuterArgs &a, uint32_t t, uint32_t n_row, uint32_t n_col, uint32_t &e, uint32_t &tr, uint32_t &tc) {
+    const uint32_t per = n_row * n_col, place = t / per;
+    e = place;
+    if (a.by_size) {
+        const uint32_t e0 = place / GM_WAVE * GM_WAVE;
+        const int lane = threadIdx.x & 63, want = (int)(place - e0);
+        int64_t b = 0, f = -1;
+        if (e0 + lane < a.n_groups) group_rows(a.gp, a.n_groups, a.n_rows, e0 + lane, b, f);
+        const int size = (int)(f - b);  // (lanes past the last group: -1, after all others)
+        int rank = 0;
+        for (int o = 0; o < GM_WAVE; ++o) {
+            const int other = __builtin_amdgcn_readlane(size, o);
+            rank += other > size || (other == size && o < lane);
+        }
+        e = e0 + __ffsll((unsigned long long)ballot(rank == want)) - 1;
     }
-    e = e0 + __ffsll((unsigned long long)ballot(rank == want)) - 1;
-    band_tile(xcd_tile(t - place * per, per), n_row, n_col, tr, tc);
+    band_tile(xcd_place(t - place * per, per), n_row, n_col, tr, tc);
 }
 
 template <typename T, typename OUT, bool IDX>
 __global__ __launch_bounds__(GEN_T, 2) void k_group_outer_any(OuterArgs a) {
     __shared__ u32x4 lds[4 * GEN_B * BK / 8];
-    const int64_t n_row = (a.n + GEN_B - 1) / GEN_B, n_col = (a.k + GEN_B - 1) / GEN_B;
-    const int64_t per = n_row * n_col, total = per * a.n_groups;
-    for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
-        int64_t e, tr, tc, begin, end;
+    const uint32_t n_row = (uint32_t)((a.n + GEN_B - 1) / GEN_B), n_col = (uint32_t)((a.k + GEN_B - 1) / GEN_B);
+    const uint32_t total = n_row * n_col * (uint32_t)a.n_groups;
+    for (uint32_t b = blockIdx.x; b < total; b += gridDim.x) {
+        uint32_t e, tr, tc;
+        int64_t begin, end;
         outer_tile(a, b, n_row, n_col, e, tr, tc);
         group_rows(a.gp, a.n_groups, a.n_rows, e, begin, end);
         const int64_t p0 = tile_start(tr, a.n, GEN_B), q0 = tile_start(tc, a.k, GEN_B);
@@ -480,7 +487,7 @@ __global__ __launch_bounds__(GEN_T, 2) void k_group_outer_any(OuterArgs a) {
             q.base = static_cast<const T *>(a.x) + begin * a.xs + q0;
         }
         OUT *out = static_cast<OUT *>(a.d) + e * a.dg + p0 * a.ds + q0;
-        tile_any<T, OUT, true, true, IDX>(p, q, (int)(end - begin), out, a.ds, (int)(tr * GEN_B - p0), (int)(tc * GEN_B - q0), lds);
+        tile_any<T, OUT, true, true, IDX>(p, q, (int)(end - begin), out, a.ds, (int)((int64_t)tr * GEN_B - p0), (int)((int64_t)tc * GEN_B - q0), lds);
     }
 }
 
@@ -499,13 +506,14 @@ void with_elem(int32_t type, int32_t out, F &&f) {
 template <typename T, typename OUT, bool IDX, int BP, int BQ, int WP, int WQ>
 __global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_outer_fast(OuterArgs a) {
     extern __shared__ char lds_fast[];
-    const int64_t n_row = (a.n + BP - 1) / BP, n_col = (a.k + BQ - 1) / BQ;
-    const int64_t per = n_row * n_col, total = per * a.n_groups;
-    for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
-        int64_t e, tr, tc, begin, end;
+    const uint32_t n_row = (uint32_t)((a.n + BP - 1) / BP), n_col = (uint32_t)((a.k + BQ - 1) / BQ);
+    const uint32_t total = n_row * n_col * (uint32_t)a.n_groups;
+    for (uint32_t b = blockIdx.x; b < total; b += gridDim.x) {
+        uint32_t e, tr, tc;
+        int64_t begin, end;
         outer_tile(a, b, n_row, n_col, e, tr, tc);
         group_rows(a.gp, a.n_groups, a.n_rows, e, begin, end);
-        const int64_t p0 = tr * BP, q0 = tc * BQ;
+        const int64_t p0 = (int64_t)tr * BP, q0 = (int64_t)tc * BQ;
         const int pv = (int)(a.n - p0 < BP ? a.n - p0 : BP), qv = (int)(a.k - q0 < BQ ? a.k - q0 : BQ);
         const Dma p{static_cast<const char *>(a.dy) + (begin * a.dys + p0) * 2, (uint32_t)(pv * 2), a.dys * 2, nullptr, 0, pv};
         Dma q{static_cast<const char *>(a.x) + q0 * 2, (uint32_t)(qv * 2), a.xs * 2, nullptr, a.n_x, qv};
@@ -628,7 +636,8 @@ extern "C" gmagnus_status_t gmagnus_group_outer(const gmagnus_groups_t *groups, 
         GM_REQUIRE(groups->n_groups <= 1 || D->stack_stride >= (n - 1) * D->row_stride + k, GMAGNUS_ERROR_INVALID_VALUE,
                    "matrices of D overlap");
         const OuterArgs a{groups->group_ptr, groups->index, groups->n_groups, groups->n_rows, X->n_rows, n, k,
-                          DY->data, X->data, D->data, DY->row_stride, X->row_stride, D->row_stride, D->stack_stride};
+                          DY->data, X->data, D->data, DY->row_stride, X->row_stride, D->row_stride, D->stack_stride,
+                          groups->n_rows / groups->n_groups >= 256};
         hipStream_t s = (hipStream_t)hip_stream;
         const bool fast = fast_side(a.dy, a.dys, 0, n, BK) && fast_side(a.x, a.xs, 0, k, a.index ? a.n_x : BK);
         const bool big = big_tiles(n, k, a.n_groups);
@@ -637,7 +646,8 @@ extern "C" gmagnus_status_t gmagnus_group_outer(const gmagnus_groups_t *groups, 
             using O = decltype(o);
             auto launch = [&](auto kernel, int b, int threads, int lds) {
                 const int64_t tiles = (n + b - 1) / b * ((k + b - 1) / b);
-                launch_fast(kernel, tiles > MAX_GRID / a.n_groups ? MAX_GRID : tiles * a.n_groups, threads, lds, a, s);
+                GM_REQUIRE(tiles < INT32_MAX / a.n_groups, GMAGNUS_ERROR_UNSUPPORTED, "2^31 tiles or more");
+                launch_fast(kernel, tiles * a.n_groups, threads, lds, a, s);
             };
             auto go = [&](auto idx) {
                 constexpr bool IX = decltype(idx)::value;

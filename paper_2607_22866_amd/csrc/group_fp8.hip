@@ -189,13 +189,13 @@ __global__ __launch_bounds__(GEN_T, 2) void k_group_product_fp8_any(Fp8Args a) {
     u32x4 *lp = lds, *lq = lds + GEN_B * 8;
     const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16, wv = threadIdx.x / 64;
     const int p0 = wv / 2 * 64, q0 = wv % 2 * 64;
-    const int64_t n_row = count_row_tiles<GEN_B>(a.gp, a.n_groups, a.n_rows, a.max_row_tiles).full;
-    const int64_t n_col = (a.n + GEN_B - 1) / GEN_B, total = n_row * n_col;
-    for (int64_t blk = blockIdx.x; blk < total; blk += gridDim.x) {
-        int64_t tr, tc;
-        band_tile(xcd_tile(blk, total), n_row, n_col, tr, tc);
+    const uint32_t n_row = count_row_tiles<GEN_B>(a.gp, a.n_groups, a.n_rows, a.max_row_tiles).full;
+    const uint32_t n_col = (uint32_t)((a.n + GEN_B - 1) / GEN_B), total = n_row * n_col;
+    for (uint32_t blk = blockIdx.x; blk < total; blk += gridDim.x) {
+        uint32_t tr, tc;
+        band_tile(xcd_place(blk, total), n_row, n_col, tr, tc);
         const RowTile t = find_row_tile<GEN_B>(a.gp, a.n_groups, a.n_rows, tr);
-        const int64_t n0 = tc * GEN_B;
+        const int64_t n0 = (int64_t)tc * GEN_B;
         const int cols = (int)(a.n - n0 < GEN_B ? a.n - n0 : GEN_B);
         OUT *out = static_cast<OUT *>(a.y) + t.begin * a.ys + n0;
         if (t.group >= a.n_groups) {
@@ -412,16 +412,16 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_product_fp8_fast(Fp8A
     extern __shared__ char lds_fast[];
     constexpr bool HALF = BP >= 128;
     const RowTiles n_row = count_row_tiles<BP, HALF>(a.gp, a.n_groups, a.n_rows, a.max_row_tiles);
-    const int64_t n_col = (a.n + BQ - 1) / BQ, n_full = n_row.full * n_col, total = n_full + n_row.half * n_col;
-    for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
+    const uint32_t n_col = (uint32_t)((a.n + BQ - 1) / BQ), n_full = n_row.full * n_col, total = n_full + n_row.half * n_col;
+    for (uint32_t b = blockIdx.x; b < total; b += gridDim.x) {
         const bool half = HALF && b >= n_full;
-        int64_t tr, tc;
+        uint32_t tr, tc;
         if (half)
-            band_tile(xcd_tile(b - n_full, total - n_full), n_row.half, n_col, tr, tc);
+            band_tile(xcd_place(b - n_full, total - n_full), n_row.half, n_col, tr, tc);
         else
-            band_tile(xcd_tile(b, n_full), n_row.full, n_col, tr, tc);
+            band_tile(xcd_place(b, n_full), n_row.full, n_col, tr, tc);
         const RowTile t = find_row_tile<BP, HALF>(a.gp, a.n_groups, a.n_rows, tr, half);
-        const int64_t n0 = tc * BQ;
+        const int64_t n0 = (int64_t)tc * BQ;
         const int cols = (int)(a.n - n0 < BQ ? a.n - n0 : BQ);
         if (t.group >= a.n_groups) {
             zero_tile(static_cast<OUT *>(a.y) + t.begin * a.ys + n0, a.ys, t.rows, cols);
@@ -448,11 +448,12 @@ __global__ __launch_bounds__(64 * WAVES) void k_group_product_fp8_few(Fp8Args a)
     __shared__ float part[WAVES][BP][BQ + 4];
     const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16;
     const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
-    const int64_t n_row = count_row_tiles<BP>(a.gp, a.n_groups, a.n_rows, a.max_row_tiles).full;
-    const int64_t n_col = (a.n + BQ - 1) / BQ, total = n_row * n_col;
+    const uint32_t n_row = count_row_tiles<BP>(a.gp, a.n_groups, a.n_rows, a.max_row_tiles).full;
+    const uint32_t n_col = (uint32_t)((a.n + BQ - 1) / BQ), total = n_row * n_col;
     const int n_k = (int)a.k, full = n_k / SB;
-    for (int64_t b = blockIdx.x; b < total; b += gridDim.x) {
-        const int64_t tr = b % n_row, q0 = b / n_row * BQ;
+    for (uint32_t b = blockIdx.x; b < total; b += gridDim.x) {
+        const uint32_t tc = b / n_row, tr = b - tc * n_row;
+        const int64_t q0 = (int64_t)tc * BQ;
         const RowTile t = find_row_tile<BP>(a.gp, a.n_groups, a.n_rows, tr);
         const int cols = (int)(a.n - q0 < BQ ? a.n - q0 : BQ);
         OUT *out = static_cast<OUT *>(a.y) + t.begin * a.ys + q0;

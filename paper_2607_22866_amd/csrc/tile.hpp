@@ -180,6 +180,7 @@ constexpr int fast_bytes(int bp, int bq) { return 2 * (bp + bq) * BK * 2; }
 
 template <typename K, typename A>
 void launch_fast(K kernel, int64_t tiles, int threads, int lds, const A &a, hipStream_t s) {
+    GM_REQUIRE(tiles < INT32_MAX, GMAGNUS_ERROR_UNSUPPORTED, "2^31 tiles or more");
     if (lds > 0) allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles < MAX_GRID ? tiles : MAX_GRID)), dim3(threads), lds, s, a);
 }

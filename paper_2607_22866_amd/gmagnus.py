@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional
 
@@ -179,8 +180,9 @@ def load(path: str = LIB_PATH):
     lib.gmagnus_bandwidth_probe.argtypes = [ctypes.c_int32, P, P, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, P,
                                             ctypes.POINTER(ctypes.c_double)]
     lib.gmagnus_bandwidth_probe.restype = ctypes.c_int
-    D, G, I64, I32 = ctypes.POINTER(DenseDesc), ctypes.POINTER(GroupsDesc), ctypes.c_int64, ctypes.c_int32
-    R = ctypes.POINTER(RoutingDesc)
+    # descriptors of the routed expert products: a structure's address, or its bytes (packed in a third of the time)
+    D = G = R = ctypes.c_void_p
+    I64, I32 = ctypes.c_int64, ctypes.c_int32
     lib.gmagnus_route_workspace_bytes.argtypes = [I64, I64, I64]
     lib.gmagnus_route_workspace_bytes.restype = ctypes.c_int64
     lib.gmagnus_route.argtypes = [D, I64, I32, R, P, I64, P]
@@ -490,9 +492,15 @@ def _check_device(t, dev: int, name: str):
         raise ValueError("%s must be a CUDA tensor on cuda:%d" % (name, dev))
 
 
-def _dense(t: torch.Tensor, dev: int, name: str, dims: int = 2) -> DenseDesc:
+_pack_dense = struct.Struct("@Pqqqqi4x").pack  # DenseDesc
+_pack_groups = struct.Struct("@qqPP").pack      # GroupsDesc
+_pack_routing = struct.Struct("@7P").pack       # RoutingDesc
+
+
+def _dense(t: torch.Tensor, dev: int, name: str, dims: int = 2) -> bytes:
     """Descriptor of a matrix (dims 2) or a stack of them (dims 3) whose columns are contiguous."""
-    _check_device(t, dev, name)
+    if not isinstance(t, torch.Tensor) or t.get_device() != dev:
+        raise ValueError("%s must be a CUDA tensor on cuda:%d" % (name, dev))
     st, shape = t.stride(), t.shape
     if len(st) != dims:
         raise ValueError("%s must have %d dimensions" % (name, dims))
@@ -505,7 +513,7 @@ def _dense(t: torch.Tensor, dev: int, name: str, dims: int = 2) -> DenseDesc:
     row = st[-2]
     if n_rows <= 1 and row < n_cols:
         row = n_cols
-    return DenseDesc(t.data_ptr(), n_rows, n_cols, row, st[0] if dims == 3 else 0, kind)
+    return _pack_dense(t.data_ptr(), n_rows, n_cols, row, st[0] if dims == 3 else 0, kind)
 
 
 def _array(t: torch.Tensor, dev: int, name: str, dtype, numel: int) -> int:
@@ -559,8 +567,8 @@ class Routing:
     def arrays(self):
         return (self.row_ptr, self.expert, self.weight, self.group_ptr, self.token, self.slot, self.group_weight)
 
-    def _desc(self) -> RoutingDesc:
-        return RoutingDesc(self.row_ptr.data_ptr(), self.expert.data_ptr(), self.weight.data_ptr(),
+    def _desc(self) -> bytes:
+        return _pack_routing(self.row_ptr.data_ptr(), self.expert.data_ptr(), self.weight.data_ptr(),
                            self.group_ptr.data_ptr(), self.token.data_ptr(), self.slot.data_ptr(),
                            self.group_weight.data_ptr())
 
@@ -581,7 +589,7 @@ def route(logits: torch.Tensor, top_k: int, normalise: bool = True) -> Routing:
     weight, group_weight = torch.empty((2, n), dtype=torch.float32, device=device).unbind(0)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     r = Routing(t, e, top_k, bool(normalise), row_ptr, expert, weight, group_ptr, token, slot, group_weight)
-    _check(lib.gmagnus_route(ctypes.byref(d), top_k, int(r.normalise), ctypes.byref(r._desc()), ws.data_ptr(), nbytes,
+    _check(lib.gmagnus_route(d, top_k, int(r.normalise), r._desc(), ws.data_ptr(), nbytes,
                              _raw_stream(dev)))
     return r
 
@@ -598,18 +606,18 @@ def route_backward(logits: torch.Tensor, routing: Routing, d_weight: torch.Tenso
     g = _array(d_weight, dev, "d_weight", torch.float32, routing.n_tokens * routing.top_k)
     out = _out(out, tuple(logits.shape), logits.dtype, logits, "out")
     o = _dense(out, dev, "out")
-    _check(load().gmagnus_route_backward(ctypes.byref(d), routing.top_k, int(routing.normalise),
-                                         ctypes.byref(routing._desc()), g, ctypes.byref(o), _raw_stream(dev)))
+    _check(load().gmagnus_route_backward(d, routing.top_k, int(routing.normalise),
+                                         routing._desc(), g, o, _raw_stream(dev)))
     return out
 
 
-def _groups(group_ptr, index, n_rows: int, dev: int) -> GroupsDesc:
+def _groups(group_ptr, index, n_rows: int, dev: int) -> bytes:
     if not isinstance(group_ptr, torch.Tensor) or group_ptr.numel() < 2:
         raise ValueError("group_ptr must be a tensor of at least two entries")
     n = group_ptr.numel()
     gp = _array(group_ptr, dev, "group_ptr", torch.int64, n)
-    ix = None if index is None else _array(index, dev, "index", torch.int32, n_rows)
-    return GroupsDesc(n - 1, n_rows, gp, ix)
+    ix = 0 if index is None else _array(index, dev, "index", torch.int32, n_rows)
+    return _pack_groups(n - 1, n_rows, gp, ix)
 
 
 @_on_stream
@@ -620,14 +628,14 @@ def group_product(x: torch.Tensor, w: torch.Tensor, group_ptr: torch.Tensor, ind
     bfloat16 or float16, sums in fp32; out_dtype: the inputs' type or float32."""
     dev = _device_of(x, "x")
     dx, dw = _dense(x, dev, "x"), _dense(w, dev, "w", 3)
-    n_rows = dx.n_rows if index is None else index.numel()
+    n_rows = x.shape[0] if index is None else index.numel()
     gd = _groups(group_ptr, index, n_rows, dev)
-    if w.shape[0] != gd.n_groups:
+    if w.shape[0] != group_ptr.numel() - 1:
         raise ValueError("w must have one matrix a group")
-    out = _out(out, (n_rows, dw.n_cols if transposed else dw.n_rows), out_dtype or x.dtype, x, "out")
+    out = _out(out, (n_rows, w.shape[2 if transposed else 1]), out_dtype or x.dtype, x, "out")
     dy = _dense(out, dev, "out")
-    _check(load().gmagnus_group_product(ctypes.byref(gd), ctypes.byref(dx), ctypes.byref(dw), int(transposed),
-                                        ctypes.byref(dy), _raw_stream(dev)))
+    _check(load().gmagnus_group_product(gd, dx, dw, int(transposed),
+                                        dy, _raw_stream(dev)))
     return out
 
 
@@ -637,10 +645,10 @@ def group_outer(d_y: torch.Tensor, x: torch.Tensor, group_ptr: torch.Tensor, ind
     """Gradient of group_product's w: for every group e the sum of d_y[r].T @ x[index[r]] over its rows."""
     dev = _device_of(d_y, "d_y")
     ddy, dx = _dense(d_y, dev, "d_y"), _dense(x, dev, "x")
-    gd = _groups(group_ptr, index, ddy.n_rows, dev)
-    out = _out(out, (gd.n_groups, ddy.n_cols, dx.n_cols), out_dtype or x.dtype, x, "out")
+    gd = _groups(group_ptr, index, d_y.shape[0], dev)
+    out = _out(out, (group_ptr.numel() - 1, d_y.shape[1], x.shape[1]), out_dtype or x.dtype, x, "out")
     dd = _dense(out, dev, "out", 3)
-    _check(load().gmagnus_group_outer(ctypes.byref(gd), ctypes.byref(ddy), ctypes.byref(dx), ctypes.byref(dd),
+    _check(load().gmagnus_group_outer(gd, ddy, dx, dd,
                                       _raw_stream(dev)))
     return out
 
@@ -655,11 +663,11 @@ def quantise_blocks(x: torch.Tensor, block_rows: int = 1):
     if block_rows not in (1, SCALE_BLOCK):
         raise ValueError("block_rows must be 1 or %d" % SCALE_BLOCK)
     q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
-    scale = torch.empty(tuple(x.shape[:-2]) + (-(-dx.n_rows // block_rows), -(-dx.n_cols // SCALE_BLOCK)),
+    scale = torch.empty(tuple(x.shape[:-2]) + (-(-x.shape[-2] // block_rows), -(-x.shape[-1] // SCALE_BLOCK)),
                         dtype=torch.float32, device=x.device)
     dq, ds = _dense(q, dev, "q", dims), _dense(scale, dev, "scale", dims)
-    _check(load().gmagnus_quantise_blocks(ctypes.byref(dx), x.shape[0] if dims == 3 else 1, block_rows,
-                                          ctypes.byref(dq), ctypes.byref(ds), _raw_stream(dev)))
+    _check(load().gmagnus_quantise_blocks(dx, x.shape[0] if dims == 3 else 1, block_rows,
+                                          dq, ds, _raw_stream(dev)))
     return q, scale
 
 
@@ -672,14 +680,14 @@ def group_product_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w
     dev = _device_of(x, "x")
     dx, dxs = _dense(x, dev, "x"), _dense(x_scale, dev, "x_scale")
     dw, dws = _dense(w, dev, "w", 3), _dense(w_scale, dev, "w_scale", 3)
-    n_rows = dx.n_rows if index is None else index.numel()
+    n_rows = x.shape[0] if index is None else index.numel()
     gd = _groups(group_ptr, index, n_rows, dev)
-    if w.shape[0] != gd.n_groups or w_scale.shape[0] != gd.n_groups:
+    if not w.shape[0] == w_scale.shape[0] == group_ptr.numel() - 1:
         raise ValueError("w and w_scale must have one matrix a group")
-    out = _out(out, (n_rows, dw.n_rows), out_dtype, x, "out")
+    out = _out(out, (n_rows, w.shape[1]), out_dtype, x, "out")
     dy = _dense(out, dev, "out")
-    _check(load().gmagnus_group_product_fp8(ctypes.byref(gd), ctypes.byref(dx), ctypes.byref(dxs), ctypes.byref(dw),
-                                            ctypes.byref(dws), ctypes.byref(dy), _raw_stream(dev)))
+    _check(load().gmagnus_group_product_fp8(gd, dx, dxs, dw,
+                                            dws, dy, _raw_stream(dev)))
     return out
 
 
@@ -699,9 +707,9 @@ def combine(y: torch.Tensor, row_ptr: torch.Tensor, slot: torch.Tensor, weight: 
     dev = _device_of(y, "y")
     d = _dense(y, dev, "y")
     rp, sl, w, n = _combine_args(row_ptr, slot, weight, dev)
-    out = _out(out, (row_ptr.numel() - 1, d.n_cols), y.dtype, y, "out")
+    out = _out(out, (row_ptr.numel() - 1, y.shape[1]), y.dtype, y, "out")
     o = _dense(out, dev, "out")
-    _check(load().gmagnus_combine(rp, sl, w, n, ctypes.byref(d), ctypes.byref(o), _raw_stream(dev)))
+    _check(load().gmagnus_combine(rp, sl, w, n, d, o, _raw_stream(dev)))
     return out
 
 
@@ -713,14 +721,14 @@ def combine_backward(y: Optional[torch.Tensor], row_ptr: torch.Tensor, slot: tor
     dev = _device_of(d_out, "d_out")
     do = _dense(d_out, dev, "d_out")
     rp, sl, w, n = _combine_args(row_ptr, slot, weight, dev)
-    if row_ptr.numel() - 1 != do.n_rows:
+    if row_ptr.numel() - 1 != d_out.shape[0]:
         raise ValueError("d_out must have a row a token")
     if y is None and n_rows is None:
         raise ValueError("n_rows is required without y")
     dy = None if y is None else _dense(y, dev, "y")
-    d_y = torch.empty((n_rows if y is None else dy.n_rows, do.n_cols), dtype=d_out.dtype, device=d_out.device)
+    d_y = torch.empty((n_rows if y is None else y.shape[0], d_out.shape[1]), dtype=d_out.dtype, device=d_out.device)
     d_w = None if y is None else torch.empty(n, dtype=torch.float32, device=d_out.device)
-    _check(load().gmagnus_combine_backward(rp, sl, w, n, None if dy is None else ctypes.byref(dy), ctypes.byref(do),
-                                           ctypes.byref(_dense(d_y, dev, "d_y")),
+    _check(load().gmagnus_combine_backward(rp, sl, w, n, None if dy is None else dy, do,
+                                           _dense(d_y, dev, "d_y"),
                                            None if d_w is None else d_w.data_ptr(), _raw_stream(dev)))
     return d_y, d_w
