@@ -178,7 +178,7 @@ GM_DEV void tile_fast(const Dma &p, const Dma &q, int n_k, OUT *out, int64_t out
     constexpr int THREADS = 64 * WP * WQ, MP = BP / WP, MQ = BQ / WQ, NP = MP / 32, NQ = MQ / 16;
     constexpr int PB = BP * BK * 2, QB = BQ * BK * 2;
     char *lp = lds, *lq = lds + 2 * PB;
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
+    const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
     const int p0 = w / WQ * MP, q0 = w % WQ * MQ;
     Feed<PK, PI, BP, THREADS> fp;
     Feed<QK, QI, BQ, THREADS> fq;
@@ -248,17 +248,8 @@ GM_DEV void tile_fast(const Dma &p, const Dma &q, int n_k, OUT *out, int64_t out
         fp.fetch_ids(p, (s + 3) * BK, n_k);
     }
     wait_and_barrier();  // (no load may be on its way to LDS when the work group ends)
-#pragma unroll
-    for (int i = 0; i < 2 * NP; ++i) {
-        const int r = p0 + 16 * i + lane % 16;
-        if (r < p.valid) {
-#pragma unroll
-            for (int j = 0; j < NQ; ++j) {
-                const int c = q0 + 16 * j + lane / 16 * 4;
-                store4(out + r * out_stride + c, acc[i / NP][i % NP][j], q.valid - c);
-            }
-        }
-    }
+    store_tile<OUT, BP, BQ, 2 * NP, NQ, THREADS>(out, out_stride, p.valid, q.valid, p0, q0, lds,
+                                                 [&](int i, int j) { return acc[i / NP][i % NP][j]; });
 }
 
 struct ProductArgs {

@@ -394,17 +394,7 @@ GM_DEV void tile_fp8_fast(const Fp8Args &a, const RowTile &t, int64_t n0, int co
     }
     wait_and_barrier();  // (no load may be on its way to LDS when the work group ends)
     OUT *out = static_cast<OUT *>(a.y) + t.begin * a.ys + n0;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int r = p0 + 16 * i + i16;
-        if (r < t.rows) {
-#pragma unroll
-            for (int j = 0; j < NQ; ++j) {
-                const int c = q0 + 16 * j + lane / 16 * 4;
-                store4(out + r * a.ys + c, acc[i][j], cols - c);
-            }
-        }
-    }
+    store_tile<OUT, BP, BQ, NP, NQ, THREADS>(out, a.ys, t.rows, cols, p0, q0, lds, [&](int i, int j) { return acc[i][j]; });
 }
 
 template <typename OUT, int BP, int BQ, int WP, int WQ>
