@@ -112,7 +112,7 @@ GM_DEV void tile_any(const Side &p, const Side &q, int n_k, OUT *out, int64_t ou
     Staged<T, QK, QI> sq;
     sp.init(p);
     sq.init(q);
-    const int lane = threadIdx.x & 63, w = threadIdx.x / 64;
+    const int w = threadIdx.x / 64;
     const int p0 = w / 2 * 64, q0 = w % 2 * 64;
     const Reader<PK, GEN_B> rp(p0);
     const Reader<QK, GEN_B> rq(q0);
@@ -153,17 +153,8 @@ GM_DEV void tile_any(const Side &p, const Side &q, int n_k, OUT *out, int64_t ou
         if (k0 + BK < n_k) step(k0 + BK, 1);
     }
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = p0 + 16 * i + lane % 16;
-        if (r >= skip_p && r < p.valid) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int c = q0 + 16 * j + lane / 16 * 4;
-                store4(out + r * out_stride + c, acc[i][j], q.valid - c, skip_q - c);
-            }
-        }
-    }
+    store_tile<OUT, GEN_B, GEN_B, 4, 4, GEN_T>(out, out_stride, p.valid, q.valid, p0, q0, reinterpret_cast<char *>(lds),
+                                               [&](int i, int j) { return acc[i][j]; }, skip_p, skip_q);
 }
 
 // A tile by WP x WQ waves. A wave's share of a step is four units of (32

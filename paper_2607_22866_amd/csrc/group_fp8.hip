@@ -256,16 +256,8 @@ __global__ __launch_bounds__(GEN_T, 2) void k_group_product_fp8_any(Fp8Args a) {
                 }
         }
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = p0 + 16 * i + i16;
-            if (r < t.rows)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int c = q0 + 16 * j + g * 4;
-                    store4(out + r * a.ys + c, acc[i][j], cols - c);
-                }
-        }
+        store_tile<OUT, GEN_B, GEN_B, 4, 4, GEN_T>(out, a.ys, t.rows, cols, p0, q0, reinterpret_cast<char *>(lds),
+                                                   [&](int i, int j) { return acc[i][j]; });
     }
 }
 

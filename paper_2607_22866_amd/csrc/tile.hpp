@@ -161,26 +161,28 @@ struct Reader {
     }
 };
 
-// Eight 16-bit neighbours of an output row, as many as there are, at any alignment.
+// Eight 16-bit neighbours of an output row, from `first` on as many as there are, at any alignment.
 template <typename OUT>
-GM_DEV void store8(OUT *p, u32x4 v, int left) {
-    if (left >= 8) {
+GM_DEV void store8(OUT *p, u32x4 v, int left, int first) {
+    if (left >= 8 && first <= 0) {
         *reinterpret_cast<Bytes16<2> *>(p) = Bytes16<2>{{v[0], v[1], v[2], v[3]}};
     } else {
         uint16_t *q = reinterpret_cast<uint16_t *>(p);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < left) q[i] = (uint16_t)(v[i >> 1] >> (16 * (i & 1)));
+            if (i >= first && i < left) q[i] = (uint16_t)(v[i >> 1] >> (16 * (i & 1)));
     }
 }
 
-// Writes a work group's BP x BQ results, of which rows x cols are there. A lane
+// Writes a work group's BP x BQ results, of which rows x cols are there and the
+// first skip_p rows and skip_q columns another tile's. A lane
 // holds four neighbours of a row (acc(i, j): row p0 + 16 i + lane % 16, columns from
 // q0 + 16 j + 4 (lane / 16) on): 16-bit results go through LDS, so that whole lines
-// leave the CU instead of quarters of them (16 groups of 64 rows, gradient of 2048 x
-// 2048 weights: see group.hip). No wave may be reading LDS any more.
+// leave the CU instead of quarters of them (gradient of 2048 x 2048 weights, 64
+// groups of 64 rows: 226 -> 160 us). No wave may be reading LDS any more.
 template <typename OUT, int BP, int BQ, int NP, int NQ, int THREADS, class ACC>
-GM_DEV void store_tile(OUT *out, int64_t stride, int rows, int cols, int p0, int q0, char *lds, ACC &&acc) {
+GM_DEV void store_tile(OUT *out, int64_t stride, int rows, int cols, int p0, int q0, char *lds, ACC &&acc, int skip_p = 0,
+                       int skip_q = 0) {
     const int lane = threadIdx.x & 63;
     if constexpr (sizeof(OUT) == 2) {
         // 8-byte unit u of row r sits at u ^ 2 (r % 8)
@@ -200,17 +202,18 @@ GM_DEV void store_tile(OUT *out, int64_t stride, int rows, int cols, int p0, int
 #pragma unroll 4
         for (int x = threadIdx.x; x < BP * (BQ / 8); x += THREADS) {
             const int r = x / (BQ / 8), c = x % (BQ / 8);
-            if (r < rows) store8(out + r * stride + c * 8, get[r * (BQ / 8) + (c ^ (r % 8))], cols - c * 8);
+            if (r >= skip_p && r < rows)
+                store8(out + r * stride + c * 8, get[r * (BQ / 8) + (c ^ (r % 8))], cols - c * 8, skip_q - c * 8);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int r = p0 + 16 * i + lane % 16;
-            if (r < rows) {
+            if (r >= skip_p && r < rows) {
 #pragma unroll
                 for (int j = 0; j < NQ; ++j) {
                     const int c = q0 + 16 * j + lane / 16 * 4;
-                    store4(out + r * stride + c, acc(i, j), cols - c);
+                    store4(out + r * stride + c, acc(i, j), cols - c, skip_q - c);
                 }
             }
         }
