@@ -512,27 +512,37 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_outer_fast(OuterArgs 
 
 // The kernel of a product. The host knows the groups' mean size only; every
 // kernel is right for any sizes.
-enum class Shape { FEW16, FEW64, ANY, T32, T64, T128, T256 };
+enum class Shape { FEW16, FEW64, ANY, T32, T64, T256 };
 
 Shape product_shape(const ProductArgs &a, bool transposed) {
     const int64_t mean = (a.n_rows + a.n_groups - 1) / a.n_groups, groups = a.n_groups < a.n_rows ? a.n_groups : a.n_rows;
     const bool fast = fast_side(a.x, a.xs, 0, a.k, a.index ? a.n_x : 256) &&
                       fast_side(a.w, a.ws, a.n_groups > 1 ? a.wg : 0, transposed ? a.n : a.k, 256);
     // Up to 16 rows a group the weights' bytes are all there is. 64 columns a work
-    // group (64 groups of 1 to 2 rows, 2048 x 2048: 79 us, 32 x 128 tiles 98) unless
-    // that leaves CUs without one, then 16 (one row, 4096 x 4096: 12.5 us against 23).
-    // Rows that are not aligned are slower that way (2047 wide: 121 us, staged tiles 61).
+    // group (64 groups, 2048 x 2048, of 1, 4 and 16 rows: 84, 104 and 148 us; tiles of
+    // 32 x 128 109, 140 and 165; of 24 rows 179 against 153) unless that leaves CUs
+    // without one, then 16 (4 groups of 1 row: 12.6 against 13.9). Rows that are not
+    // aligned are slower that way (2047 wide, 1 row: 121 us, staged tiles 61).
     if (!transposed && mean <= 16) {
         if (groups * ((a.n + 63) / 64) < 256) return Shape::FEW16;
         if (fast) return Shape::FEW64;
     }
     if (!fast) return Shape::ANY;
-    // Tiles as high as the groups: 64 groups, 2048 x 2048, of 32 rows 146 us (64-row
-    // tiles 171, 128-row 161), of 125 rows 203 (179, 160); 40 groups of 50 rows, 776 x
-    // 1296, 26.9 (24.1, 25.7).
-    if (mean <= 40) return Shape::T32;
-    if (mean <= 96) return Shape::T64;
-    return big_tiles(mean, a.n, a.n_groups) ? Shape::T256 : Shape::T128;
+    // Tiles of 32 rows or of 64 by the groups' height: of 48 rows 135 against 150 us, of
+    // 64 rows 151 / 175, of 96 rows 178 / 151; transposed 24 rows 116 / 123, 48 rows 132 / 118.
+    if (mean <= (transposed ? 32 : 64)) return Shape::T32;
+    return big_product_tiles(mean, a.n, groups) ? Shape::T256 : Shape::T64;
+}
+
+// Whether a gradient's tiles are 256 x 256 rather than 128 x 128. A tile takes as
+// long as its group has rows, so there have to be several a CU to even that out,
+// unless there is one group: 64 groups of 256 rows, 2048 x 2048 (4096 tiles), 285
+// against 376 us, 768 x 1024 (768 tiles) 59 / 74; 16 groups of 1024 rows, 1024 x 1024
+// (256 tiles), 107 / 74; one group of 1024 rows, 4096 x 4096 (256 tiles), 37 / 44, 2048
+// x 2048 (64 tiles) 29 / 18. And not where padding grows by more than a third.
+bool big_outer_tiles(int64_t n, int64_t k, int64_t n_groups) {
+    const int64_t tiles = (n + 255) / 256 * ((k + 255) / 256), small = (n + 127) / 128 * ((k + 127) / 128);
+    return tiles * n_groups >= (n_groups == 1 ? 192 : 512) && 3 * 4 * tiles <= 4 * small;
 }
 
 }  // namespace
@@ -577,8 +587,6 @@ extern "C" gmagnus_status_t gmagnus_group_product(const gmagnus_groups_t *groups
                     launch(k_group_product_fast<T, O, TR, 32, 128, 1, 4>, 32, 128, 256, fast_bytes(32, 128));
                 else if (shape == Shape::T64)
                     launch(k_group_product_fast<T, O, TR, 64, 128, 2, 2>, 64, 128, 256, fast_bytes(64, 128));
-                else if (shape == Shape::T128)
-                    launch(k_group_product_fast<T, O, TR, 128, 128, 2, 2>, 128, 128, 256, fast_bytes(128, 128));
                 else
                     launch(k_group_product_fast<T, O, TR, 256, 256, 2, 4>, 256, 256, 512, fast_bytes(256, 256));
             };
@@ -622,7 +630,7 @@ extern "C" gmagnus_status_t gmagnus_group_outer(const gmagnus_groups_t *groups, 
                           groups->n_rows / groups->n_groups >= 256};
         hipStream_t s = (hipStream_t)hip_stream;
         const bool fast = fast_side(a.dy, a.dys, 0, n, BK) && fast_side(a.x, a.xs, 0, k, a.index ? a.n_x : BK);
-        const bool big = big_tiles(n, k, a.n_groups);
+        const bool big = big_outer_tiles(n, k, a.n_groups);
         with_elem(X->data_type, D->data_type, [&](auto t, auto o) {
             using T = decltype(t);
             using O = decltype(o);

@@ -506,9 +506,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_group_product_fp8_few(Fp8Args a)
     }
 }
 
-// The kernel of a product, as for 16 bits (group.hip). Without a fast layout
-// only one tile is there.
-enum class Shape { FEW16, FEW64, ANY, T32, T64, T128, T256 };
+// The kernel of a product, as for 16 bits (group.hip).
+enum class Shape { FEW16, FEW64, ANY, T32, T64, T256 };
 
 Shape fp8_shape(const Fp8Args &a) {
     const int64_t mean = (a.n_rows + a.n_groups - 1) / a.n_groups, groups = a.n_groups < a.n_rows ? a.n_groups : a.n_rows;
@@ -516,17 +515,18 @@ Shape fp8_shape(const Fp8Args &a) {
     const bool fast = fast_side(a.x, a.xs, 0, a.k, a.index ? a.n_x : 256, 1) &&
                       fast_side(a.w, a.ws, a.n_groups > 1 ? a.wg : 0, a.k, 256, 1) &&
                       (a.n_x * a.sxs + kb) * 4 < (int64_t)NOWHERE && (2 * a.sws + kb) * 4 < (int64_t)NOWHERE;
-    // (64 groups, 2048 x 4096, of 1 row: 79 us with 64 columns a work group, 106 with
-    // 32 x 128 tiles; of 31 rows: 32-row tiles 141, 64-row 173, 128-row 162; one row, 4096
-    // x 4096: 13.4 with 16 columns, 15.0 with 64)
-    if (mean <= 16) {
+    // 64 groups, 2048 x 4096: of 1, 4 and 16 rows 64 columns a work group 107, 134 and
+    // 192 us, tiles of 32 x 128 112, 170 and 158; one row, 4096 x 4096: 13.4 with 16
+    // columns, 15.0 with 64
+    if (mean <= 8) {
         if (groups * ((a.n + 63) / 64) < 256) return Shape::FEW16;
         if (fast) return Shape::FEW64;
     }
     if (!fast) return Shape::ANY;
-    if (mean <= 40) return Shape::T32;
-    if (mean <= 96) return Shape::T64;
-    return big_tiles(mean, a.n, a.n_groups) ? Shape::T256 : Shape::T128;
+    // of 24 rows tiles of 32 rows 137, of 64 155; of 48 rows 151 / 139, of 96 208 / 167
+    if (mean <= 32) return Shape::T32;
+    // of 96 rows 256 x 256 tiles 172 against 167, of 128 179 / 198, of 512 368 / 497
+    return big_product_tiles(mean, a.n, groups) ? Shape::T256 : Shape::T64;
 }
 
 }  // namespace
@@ -614,7 +614,6 @@ extern "C" gmagnus_status_t gmagnus_group_product_fp8(const gmagnus_groups_t *gr
             case Shape::ANY: return go(k_group_product_fp8_any<O>, GEN_B, GEN_B, GEN_T, 0);
             case Shape::T32: return go(k_group_product_fp8_fast<O, 32, 128, 1, 4>, 32, 128, 256, fast_lds<32, 128>());
             case Shape::T64: return go(k_group_product_fp8_fast<O, 64, 128, 2, 2>, 64, 128, 256, fast_lds<64, 128>());
-            case Shape::T128: return go(k_group_product_fp8_fast<O, 128, 128, 2, 2>, 128, 128, 256, fast_lds<128, 128>());
             case Shape::T256: return go(k_group_product_fp8_fast<O, 256, 256, 2, 4>, 256, 256, 512, fast_lds<256, 256>());
             }
         };

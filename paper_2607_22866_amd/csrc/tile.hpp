@@ -226,12 +226,15 @@ inline bool fast_side(const void *p, int64_t stride, int64_t stack, int64_t axis
     return aligned16(p, stride, stack, size) && axis * size % 16 == 0 && (rows * stride + axis) * size < (int64_t)NOWHERE;
 }
 
-// 256 x 256 tiles (one work group a CU, the fewest bytes a product) where about as
-// many as CUs come out of `n_groups` outputs of m x n and rows are not mostly
-// padding, else 128 x 128 (two a CU).
-inline bool big_tiles(int64_t m, int64_t n, int64_t n_groups) {
-    const int64_t tiles = (m + 255) / 256 * ((n + 255) / 256);
-    return m >= 384 && (tiles >= 192 || tiles * n_groups >= 192);
+// Whether a product of `groups` groups of `mean` rows and n columns takes 256 x
+// 256 tiles (one work group a CU, the fewest bytes a product) rather than 64 x 128
+// (three a CU): at 64 groups, 2048 x 2048, bf16, of 96 rows 166 against 151 us, 128
+// rows 175 / 177, 192 rows 192 / 202, 512 rows 331 / 418; where they leave CUs
+// without one, 8 groups of 512 rows, 1024 x 1024 (64 tiles), 26.7 / 19.1, of 1024
+// rows (128 tiles) 28.5 / 30.7; and not where the columns' padding grows by more than a third.
+inline bool big_product_tiles(int64_t mean, int64_t n, int64_t groups) {
+    const int64_t cols = (n + 255) / 256;
+    return mean >= 128 && (mean + 255) / 256 * cols * groups >= 128 && 3 * 2 * cols <= 4 * ((n + 127) / 128);
 }
 
 // LDS of two buffers of tiles of bp and bq rows.

@@ -162,3 +162,17 @@ def test_large_tiles_do_not_leak(g):
     assert bool(torch.isfinite(y).all())
     d = g.group_outer(y, x[:, :k], gp)
     assert bool(torch.isnan(d[14]).all()) and bool(torch.isfinite(d[:14]).all()) and bool(torch.isfinite(d[15:]).all())
+
+
+@pytest.mark.parametrize("n,k", [(64, 72), (136, 264), (77, 61)])
+def test_outer_of_many_long_groups(g, n, k):
+    # more than 64 groups, long ones: every 64 are taken in the order of their sizes
+    sizes = [260 + 7 * (i % 11) for i in range(64)] + [0, 900, 1, 300, 300]
+    rows = sum(sizes)
+    gp = offsets(sizes)
+    x, d_y = rand((rows, k), torch.bfloat16, 1), rand((rows, n), torch.bfloat16, 2)
+    d = g.group_outer(d_y, x, gp, out_dtype=torch.float32)
+    b = gp.tolist()
+    for e, size in enumerate(sizes):
+        m, r = d_y[b[e]:b[e + 1]].double().t().contiguous(), x[b[e]:b[e + 1]].double()
+        within(d[e], m @ r, m.abs() @ r.abs(), size, torch.float32)
