@@ -301,15 +301,15 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_product_fast(ProductA
             zero_tile(out, a.ys, t.rows, cols);
             continue;
         }
-        Dma p{static_cast<const char *>(a.x), (uint32_t)(((a.n_x - 1) * a.xs + a.k) * 2), a.xs * 2, nullptr, a.n_x, t.rows};
+        Dma p{static_cast<const char *>(a.x), span(a.n_x, a.xs * 2, a.k * 2), a.xs * 2, nullptr, a.n_x, t.rows};
         if (a.index) {
             p.index = a.index + t.begin;
         } else {
             p.base += t.begin * p.stride;
-            p.records = (uint32_t)((t.rows - 1) * p.stride + a.k * 2);
+            p.records = span(t.rows, p.stride, a.k * 2);
         }
         const char *w = static_cast<const char *>(a.w) + (t.group * a.wg + (TRANS ? q0 : q0 * a.ws)) * 2;
-        const uint32_t wb = (uint32_t)(TRANS ? cols * 2 : ((cols - 1) * a.ws + a.k) * 2);
+        const uint32_t wb = TRANS ? (uint32_t)cols * 2 : span(cols, a.ws * 2, a.k * 2);
         const Dma q{w, wb, a.ws * 2, nullptr, 0, cols};
         if constexpr (HALF)
             if (half) {
@@ -501,7 +501,7 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_outer_fast(OuterArgs 
         Dma q{static_cast<const char *>(a.x) + q0 * 2, (uint32_t)(qv * 2), a.xs * 2, nullptr, a.n_x, qv};
         if constexpr (IDX) {
             q.index = a.index + begin;
-            q.records = (uint32_t)((a.n_x - 1) * q.stride + qv * 2);
+            q.records = span(a.n_x, q.stride, qv * 2);
         } else {
             q.base += begin * q.stride;
         }

@@ -279,14 +279,14 @@ GM_DEV void tile_fp8_fast(const Fp8Args &a, const RowTile &t, int64_t n0, int co
     float *ls = reinterpret_cast<float *>(lds + 2 * PB + 2 * QB);
     const int lane = threadIdx.x & 63, i16 = lane % 16, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
     const int p0 = w / WQ * MP, q0 = w % WQ * MQ;
-    Dma p{reinterpret_cast<const char *>(a.x), (uint32_t)((a.n_x - 1) * a.xs + a.k), a.xs, nullptr, a.n_x, t.rows};
+    Dma p{reinterpret_cast<const char *>(a.x), span(a.n_x, a.xs, a.k), a.xs, nullptr, a.n_x, t.rows};
     if (a.index) {
         p.index = a.index + t.begin;
     } else {
         p.base += t.begin * a.xs;
-        p.records = (uint32_t)((t.rows - 1) * a.xs + a.k);
+        p.records = span(t.rows, a.xs, a.k);
     }
-    const Dma q{reinterpret_cast<const char *>(a.w) + t.group * a.wg + n0 * a.ws, (uint32_t)((cols - 1) * a.ws + a.k), a.ws,
+    const Dma q{reinterpret_cast<const char *>(a.w) + t.group * a.wg + n0 * a.ws, span(cols, a.ws, a.k), a.ws,
                 nullptr, 0, cols};
     // The step's scales come as single values: a row's to each thread of the first
     // RW waves, the column blocks' to the next waves (which repeat each other:
@@ -297,7 +297,7 @@ GM_DEV void tile_fp8_fast(const Fp8Args &a, const RowTile &t, int64_t n0, int co
     const bool row_wave = w < RW;
     const float *s_base = row_wave ? a.sx : a.sw + t.group * a.swg + n0 / SB * a.sws;
     const int s_blocks = (cols + SB - 1) / SB;
-    const uint32_t s_records = (uint32_t)(((row_wave ? a.n_x - 1 : s_blocks - 1) * (row_wave ? a.sxs : a.sws) + kb) * 4);
+    const uint32_t s_records = row_wave ? span(a.n_x, a.sxs * 4, kb * 4) : span(s_blocks, a.sws * 4, kb * 4);
     uint32_t sat = NOWHERE;
     if (row_wave && (int)threadIdx.x < t.rows) {
         const int64_t r = a.index ? a.index[t.begin + threadIdx.x] : t.begin + threadIdx.x;

@@ -36,6 +36,9 @@ struct Dma {
 
 constexpr uint32_t NOWHERE = 0x80000000u;  // beyond any operand's bytes: reads as zeros
 
+// Bytes from the first of `rows` rows to the last one's end.
+GM_DEV uint32_t span(int64_t rows, int64_t stride, int64_t row) { return rows > 0 ? (uint32_t)((rows - 1) * stride + row) : 0u; }
+
 // Lane l's BYTES (16 or 4) at base + soff + v go to LDS at `to` + BYTES l; zeros where v is not
 // below `records`. An instruction without results: the compiler, which would
 // wait for it before every transposing read of LDS, counts no load, and

@@ -176,3 +176,21 @@ def test_outer_of_many_long_groups(g, n, k):
     for e, size in enumerate(sizes):
         m, r = d_y[b[e]:b[e + 1]].double().t().contiguous(), x[b[e]:b[e + 1]].double()
         within(d[e], m @ r, m.abs() @ r.abs(), size, torch.float32)
+
+
+@pytest.mark.parametrize("rows", [[1, 2], [30, 500], [1500, 900]])
+@pytest.mark.parametrize("n,k", [(136, 72), (1536, 128), (61, 45)])
+def test_index_into_no_rows(g, rows, n, k):
+    # X without a row: whatever the index holds, every result is zero
+    total, gp = sum(rows), offsets(rows)
+    index = torch.randint(-2, 3, (total,), dtype=torch.int32, device="cuda")
+    for pad in (0, 8):
+        x = torch.empty((0, k + pad), dtype=torch.bfloat16, device="cuda")[:, :k]
+        y = g.group_product(x, rand((2, n, k), torch.bfloat16, 1), gp, index=index)
+        assert y.shape == (total, n) and not y.any()
+        assert not g.group_product(x, rand((2, k, n), torch.bfloat16, 2), gp, index=index, transposed=True).any()
+        assert not g.group_outer(rand((total, n), torch.bfloat16, 3), x, gp, index=index).any()
+        q = torch.empty((0, k + 16 * pad), dtype=torch.float8_e4m3fn, device="cuda")[:, :k]
+        wq, ws = g.quantise_blocks(rand((2, n, k), torch.float32, 4), 128)
+        s = torch.empty((0, -(-k // 128) + pad), device="cuda")[:, :-(-k // 128)]
+        assert not g.group_product_fp8(q, s, wq, ws, gp, index=index).any()
