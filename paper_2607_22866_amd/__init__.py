@@ -1,4 +1,5 @@
-"""MI355X (gfx950) SpGEMM C = A*B on CSR with the gMAGNUS heavy-row method.
+"""MI355X (gfx950) SpGEMM C = A*B on CSR with the gMAGNUS heavy-row method, and
+the products that a sparse routing matrix selects (layers of experts).
 
 The compute lives in libgmagnus.so (HIP kernels behind the C ABI declared in
 include/gmagnus.h); :mod:`paper_2607_22866_amd.gmagnus` is its ctypes binding.

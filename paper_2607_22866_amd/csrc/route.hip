@@ -320,7 +320,8 @@ struct RouteBackArgs {
 };
 
 // A wave a token. Lane l holds experts l, l + 64, ...; the entries' gradients (and
-// weights) reach their lanes through LDS.
+// weights) reach their lanes through LDS. Bound by the latency of three dependent
+// loads: 16384 tokens, 256 experts, top_k 8, bf16 10 us (17 MB).
 template <typename T, int V>
 __global__ __launch_bounds__(256) void k_route_backward(RouteBackArgs a) {
     __shared__ float grad[4][V * 64], prob[4][V * 64];
@@ -437,7 +438,8 @@ GM_DEV int64_t wave_number() {
     return __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)) + (int64_t)blockIdx.x * (blockDim.x / 64);
 }
 
-// A wave: one token's CHUNK columns.
+// A wave: one token's CHUNK columns. Bound by its bytes: 8192 tokens of 4 rows of
+// 4096 bf16 78 us, 4.3 TB/s (two entries' rows at once gained nothing: 83 us).
 template <typename T>
 __global__ __launch_bounds__(256) void k_combine(CombineArgs a) {
     const int lane = threadIdx.x & 63;
@@ -461,7 +463,8 @@ __global__ __launch_bounds__(256) void k_combine(CombineArgs a) {
     }
 }
 
-// A wave: one entry's row of Y with its token's row of the sum's gradient.
+// A wave: one entry's row of Y with its token's row of the sum's gradient, read
+// once from memory and top_k - 1 times from L2. The same sizes: 115-120 us, 5.1 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void k_combine_backward(CombineArgs a) {
     const int lane = threadIdx.x & 63;

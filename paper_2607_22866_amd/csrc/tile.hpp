@@ -42,7 +42,8 @@ GM_DEV uint32_t span(int64_t rows, int64_t stride, int64_t row) { return rows > 
 // Lane l's BYTES (16 or 4) at base + soff + v go to LDS at `to` + BYTES l; zeros where v is not
 // below `records`. An instruction without results: the compiler, which would
 // wait for it before every transposing read of LDS, counts no load, and
-// wait_and_barrier() is what waits.
+// wait_and_barrier() is what waits. (M0 is set and used inside; the compiler,
+// which reserves it, does the same for each of its own uses.)
 template <int BYTES = 16>
 GM_DEV void load_to_lds(const void *base, uint32_t records, uint32_t v, uint32_t soff, void *to) {
     typedef __attribute__((address_space(3))) char lds_char;
