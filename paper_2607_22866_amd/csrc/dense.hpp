@@ -202,7 +202,7 @@ inline void check_dense(const gmagnus_dense_t *m, const char *name, int64_t n_ro
     GM_REQUIRE(m->n_rows == n_rows && m->n_cols == n_cols, GMAGNUS_ERROR_INVALID_VALUE,
                s + " is " + std::to_string(m->n_rows) + " x " + std::to_string(m->n_cols) + ", expected " +
                    std::to_string(n_rows) + " x " + std::to_string(n_cols));
-    GM_REQUIRE(n_rows <= 1 || m->row_stride >= n_cols, GMAGNUS_ERROR_INVALID_VALUE, "row stride of " + s + " below its columns");
+    GM_REQUIRE(n_rows == 0 || m->row_stride >= n_cols, GMAGNUS_ERROR_INVALID_VALUE, "row stride of " + s + " below its columns");
     GM_REQUIRE(n_stack <= 1 || n_rows == 0 || m->stack_stride >= 0, GMAGNUS_ERROR_INVALID_VALUE, "negative stack stride of " + s);
     GM_REQUIRE(m->data != nullptr || n_rows == 0 || n_cols == 0 || n_stack == 0, GMAGNUS_ERROR_INVALID_VALUE,
                "NULL data of " + s);

@@ -555,6 +555,9 @@ extern "C" gmagnus_status_t gmagnus_quantise_blocks(const gmagnus_dense_t *X, in
                        scale->data_type == GMAGNUS_DATA_FP32,
                    GMAGNUS_ERROR_INVALID_VALUE, "X must be fp32, bf16 or fp16, Q E4M3, scale fp32");
         if (n == 0 || n_stack == 0) return;
+        for (const gmagnus_dense_t *m : {Q, scale})
+            GM_REQUIRE(n_stack == 1 || m->stack_stride >= (m->n_rows - 1) * m->row_stride + m->n_cols,
+                       GMAGNUS_ERROR_INVALID_VALUE, "matrices of Q or of scale overlap");
         const QuantArgs a{X->data, (uint8_t *)Q->data, (float *)scale->data, n, k, X->row_stride, X->stack_stride,
                           Q->row_stride, Q->stack_stride, scale->row_stride, scale->stack_stride, n_stack};
         hipStream_t s = (hipStream_t)hip_stream;

@@ -156,3 +156,20 @@ def test_binding_refuses_host_tensors(lib):
                  lambda: gm.combine_backward(x, gp, gp.int(), None, x)):
         with pytest.raises(ValueError, match="CUDA tensor"):
             call()
+
+
+@pytest.mark.parametrize("stride", [0, -24, 23])
+def test_single_rows_need_their_stride(lib, stride):
+    # (a gradient's rows are the reduction: rows past the last are told apart by the stride, also past a single one)
+    g, x, d = groups(n_rows=1), dense(1, 16), dense(24, 16)
+    assert lib.gmagnus_group_outer(ref(g), ref(dense(1, 24, stride=stride)), ref(x), ref(d), None) == INVALID
+    assert b"row stride" in lib.gmagnus_last_error()
+
+
+@pytest.mark.parametrize("kw", [dict(q=dense(5, 200, FP8, stack=999)), dict(q=dense(5, 200, FP8, stride=208, stack=1031)),
+                                dict(scale=dense(5, 2, F32, stack=0))])
+def test_quantised_stacks_do_not_overlap(lib, kw):
+    a = dict(q=dense(5, 200, FP8), scale=dense(5, 2, F32))
+    a.update(kw)
+    assert lib.gmagnus_quantise_blocks(ref(dense(5, 200)), 3, 1, ref(a["q"]), ref(a["scale"]), None) == INVALID
+    assert b"overlap" in lib.gmagnus_last_error()
