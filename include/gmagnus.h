@@ -396,7 +396,8 @@ gmagnus_status_t gmagnus_bandwidth_probe(int32_t kind, void *dst, const void *sr
  * back, so they may be captured into a HIP graph. Device arrays of sizes
  * (group_ptr, index, slot) are trusted as the routing gives them, but numbers
  * out of range never lead to an access outside the arrays: an index outside
- * X reads as a row of zeros, bounds are clamped to the rows there are.
+ * X reads as a row of zeros (against weights that are infinite or NaN its
+ * results are zeros or NaN), bounds are clamped to the rows there are.
  * Sums are held in fp32 (8-bit operands: see there); results are rounded
  * once, to the output's type. */
 typedef enum {
