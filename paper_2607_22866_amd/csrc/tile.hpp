@@ -39,26 +39,29 @@ constexpr uint32_t NOWHERE = 0x80000000u;  // beyond any operand's bytes: reads 
 // Bytes from the first of `rows` rows to the last one's end.
 GM_DEV uint32_t span(int64_t rows, int64_t stride, int64_t row) { return rows > 0 ? (uint32_t)((rows - 1) * stride + row) : 0u; }
 
-// Lane l's BYTES (16 or 4) at base + soff + v go to LDS at `to` + BYTES l; zeros where v is not
-// below `records`. An instruction without results: the compiler, which would
+// Lane l's BYTES (16 or 4) at base + v go to LDS at `to` + BYTES l; zeros where v is not
+// below `records`, and nothing is read there. The instruction's scalar offset is
+// always 0 (it does not take part in that check as v does): a step along
+// contiguous elements moves the base and shortens the records. An instruction
+// without results: the compiler, which would
 // wait for it before every transposing read of LDS, counts no load, and
 // wait_and_barrier() is what waits. (M0 is set and used inside; the compiler,
 // which reserves it, does the same for each of its own uses.)
 template <int BYTES = 16>
-GM_DEV void load_to_lds(const void *base, uint32_t records, uint32_t v, uint32_t soff, void *to) {
+GM_DEV void load_to_lds(const void *base, uint32_t records, uint32_t v, void *to) {
     typedef __attribute__((address_space(3))) char lds_char;
     const uint64_t b = (uint64_t)base;
     const u32x4 rsrc = {(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, records, 0x00027000u};
     const uint32_t m0 = (uint32_t)(uintptr_t)(lds_char *)to;
     if constexpr (BYTES == 16)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                      :
-                     : "s"(m0), "v"(v), "s"(rsrc), "s"(soff)
+                     : "s"(m0), "v"(v), "s"(rsrc)
                      : "memory");
     else
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
                      :
-                     : "s"(m0), "v"(v), "s"(rsrc), "s"(soff)
+                     : "s"(m0), "v"(v), "s"(rsrc)
                      : "memory");
 }
 
@@ -110,7 +113,7 @@ struct Feed {
     // load i of step k0 (past n_k: zeros)
     GM_DEV void issue(const Dma &d, char *lds, int k0, int n_k, int i) {
         const char *base = d.base;
-        uint32_t records = d.records, soff = 0, v = at[i];
+        uint32_t records = d.records, v = at[i];
         if constexpr (KROWS && IDX) {
             const bool ok = ids[i] >= 0 && ids[i] < (int)d.n_mem && v != NOWHERE;
             v = ok ? v + (uint32_t)ids[i] * (uint32_t)d.stride : NOWHERE;
@@ -120,10 +123,13 @@ struct Feed {
             base += k0 * d.stride;
             records = rows > 0 ? (uint32_t)((rows - 1) * d.stride) + d.records : 0u;
         } else {
-            soff = (uint32_t)k0 * 2;
+            // (an operand has whole rows of n_k elements, or none)
+            const uint32_t past = (uint32_t)k0 * 2;
+            base += past;
+            records = k0 < (records ? n_k : 0) ? records - past : 0u;
             v = elem_of(i) < n_k - k0 ? v : NOWHERE;
         }
-        load_to_lds(base, records, v, soff, lds + (wave() * L + i) * 1024);
+        load_to_lds(base, records, v, lds + (wave() * L + i) * 1024);
     }
 };
 
