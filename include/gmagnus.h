@@ -472,7 +472,7 @@ typedef struct {
  * and W is a stack of K x N. Rows of Y past the last group are set to zero.
  * X and W have one type, bf16 or fp16; Y has it too, or fp32.
  * Errors: INVALID_VALUE (NULL, shapes, strides, types), UNSUPPORTED (n_rows
- * or a side of a matrix >= 2^31), HIP. */
+ * or a column count above 2^31 - 1025, n_groups or rows of X above 2^31 - 2), HIP. */
 gmagnus_status_t gmagnus_group_product(const gmagnus_groups_t *groups, const gmagnus_dense_t *X,
                                        const gmagnus_dense_t *W, int32_t transposed, const gmagnus_dense_t *Y,
                                        void *hip_stream);

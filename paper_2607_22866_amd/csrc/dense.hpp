@@ -259,16 +259,22 @@ GM_DEV void zero_tile(OUT *out, int64_t stride, int rows, int cols) {
 // Work groups of a launch: the kernels' loops take what exceeds this.
 constexpr int64_t MAX_GRID = 1 << 22;
 
+// Grouped rows and sides of matrices. The kernels count rows of a group, and
+// elements of the reduction, in 32 bits, and go past their end by a few steps
+// (384 elements) and round up to tiles (256 rows) before they compare.
+constexpr int64_t MAX_SIDE = (int64_t(1) << 31) - 1025;
+
 inline void check_groups(const gmagnus_groups_t *g) {
     GM_REQUIRE(g != nullptr, GMAGNUS_ERROR_INVALID_VALUE, "NULL groups");
     GM_REQUIRE(g->n_groups >= 1 && g->n_rows >= 0, GMAGNUS_ERROR_INVALID_VALUE, "groups: n_groups must be positive, n_rows not negative");
     GM_REQUIRE(g->group_ptr != nullptr, GMAGNUS_ERROR_INVALID_VALUE, "groups: NULL group_ptr");
-    GM_REQUIRE(g->n_rows < INT32_MAX && g->n_groups < INT32_MAX, GMAGNUS_ERROR_UNSUPPORTED, "groups: more than 2^31 - 2 rows or groups");
+    GM_REQUIRE(g->n_rows <= MAX_SIDE && g->n_groups < INT32_MAX, GMAGNUS_ERROR_UNSUPPORTED,
+               "groups: more than 2^31 - 1025 rows or 2^31 - 2 groups");
 }
 
 inline void check_side(int64_t n, const char *what) {
     GM_REQUIRE(n >= 1, GMAGNUS_ERROR_INVALID_VALUE, std::string(what) + " must be positive");
-    GM_REQUIRE(n < INT32_MAX, GMAGNUS_ERROR_UNSUPPORTED, std::string(what) + " beyond 2^31 - 2");
+    GM_REQUIRE(n <= MAX_SIDE, GMAGNUS_ERROR_UNSUPPORTED, std::string(what) + " beyond 2^31 - 1025");
 }
 
 // 16-byte aligned rows (and matrices of a stack).
