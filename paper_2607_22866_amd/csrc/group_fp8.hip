@@ -331,7 +331,7 @@ GM_DEV void tile_fp8_fast(const Fp8Args &a, const RowTile &t, int64_t n0, int co
         for (int h = 0; h < 2; ++h) b[j][h] = rq.get(lq + (s & 1) * QB, h, j);
     };
     auto feed_scales = [&](int s) {  // (past the last block: zeros, nothing is read)
-        load_to_lds<4>(s_base + s, s < (s_records ? kb : 0) ? s_records - (uint32_t)s * 4 : 0u, sat,
+        load_to_lds<4>(s_base, s_records, s < kb ? sat + (uint32_t)s * 4 : NOWHERE,
                        ls + (s & 1) * SR + (row_wave ? w : RW) * 64);
     };
     auto read_sq = [&](int s) { return ls[(s & 1) * SR + RW * 64 + q0 / SB]; };

@@ -41,12 +41,11 @@ GM_DEV uint32_t span(int64_t rows, int64_t stride, int64_t row) { return rows > 
 
 // Lane l's BYTES (16 or 4) at base + v go to LDS at `to` + BYTES l; zeros where v is not
 // below `records`, and nothing is read there. The instruction's scalar offset is
-// always 0 (it does not take part in that check as v does): a step along
-// contiguous elements moves the base and shortens the records. An instruction
-// without results: the compiler, which would
-// wait for it before every transposing read of LDS, counts no load, and
-// wait_and_barrier() is what waits. (M0 is set and used inside; the compiler,
-// which reserves it, does the same for each of its own uses.)
+// always 0: it does not take part in that check as v does. An instruction without
+// results: the compiler, which would wait for it before every transposing read
+// of LDS, counts no load, and wait_and_barrier() is what waits. (M0 is set and
+// used inside; the compiler, which reserves it, does the same for each of its
+// own uses.)
 template <int BYTES = 16>
 GM_DEV void load_to_lds(const void *base, uint32_t records, uint32_t v, void *to) {
     typedef __attribute__((address_space(3))) char lds_char;
@@ -123,11 +122,7 @@ struct Feed {
             base += k0 * d.stride;
             records = rows > 0 ? (uint32_t)((rows - 1) * d.stride) + d.records : 0u;
         } else {
-            // (an operand has whole rows of n_k elements, or none)
-            const uint32_t past = (uint32_t)k0 * 2;
-            base += past;
-            records = k0 < (records ? n_k : 0) ? records - past : 0u;
-            v = elem_of(i) < n_k - k0 ? v : NOWHERE;
+            v = elem_of(i) < n_k - k0 ? v + (uint32_t)k0 * 2 : NOWHERE;
         }
         load_to_lds(base, records, v, lds + (wave() * L + i) * 1024);
     }
