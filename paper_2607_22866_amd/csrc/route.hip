@@ -319,6 +319,8 @@ struct RouteBackArgs {
     const float *weight, *d_weight;
 };
 
+constexpr uint32_t NOT_CHOSEN = 0xffffffffu;  // as a weight: a NaN that no arithmetic gives
+
 // A wave a token. Lane l holds experts l, l + 64, ...; the entries' gradients (and
 // weights) reach their lanes through LDS. Bound by the latency of three dependent
 // loads: 16384 tokens, 256 experts, top_k 8, bf16 10 us (17 MB).
@@ -339,7 +341,7 @@ __global__ __launch_bounds__(256) void k_route_backward(RouteBackArgs a) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             grad[w][j * 64 + lane] = 0.f;
-            if (a.normalise) prob[w][j * 64 + lane] = 0.f;
+            if (a.normalise) prob[w][j * 64 + lane] = __uint_as_float(NOT_CHOSEN);
         }
         wave_lds_fence();
         float dot = 0.f;
@@ -355,9 +357,13 @@ __global__ __launch_bounds__(256) void k_route_backward(RouteBackArgs a) {
         wave_lds_fence();
         dot = wave_sum(dot);
         float p[V];
+        bool there[V];  // the logit has a part in the softmax: the others' gradient is zero whatever the sum holds
         if (a.normalise) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) p[j] = prob[w][j * 64 + lane];
+            for (int j = 0; j < V; ++j) {
+                p[j] = prob[w][j * 64 + lane];
+                there[j] = __float_as_uint(p[j]) != NOT_CHOSEN;
+            }
         } else {
             uint32_t key[V], m = 0;
 #pragma unroll
@@ -374,13 +380,16 @@ __global__ __launch_bounds__(256) void k_route_backward(RouteBackArgs a) {
             }
             const float scale = 1.f / wave_sum(sum);
 #pragma unroll
-            for (int j = 0; j < V; ++j) p[j] = key[j] ? p[j] * scale : 0.f;
+            for (int j = 0; j < V; ++j) {
+                p[j] *= scale;
+                there[j] = key[j] != 0;
+            }
         }
         T *out = static_cast<T *>(a.d_logits) + t * a.d_stride;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const int e = j * 64 + lane;
-            if (e < a.n_experts) out[e] = (T)(p[j] * (grad[w][e] - dot));
+            if (e < a.n_experts) out[e] = there[j] ? (T)(p[j] * (grad[w][e] - dot)) : (T)0.f;
         }
         wave_lds_fence();
     }
