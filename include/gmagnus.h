@@ -469,7 +469,9 @@ typedef struct {
 
 /* Y[r,:] = X[index[r],:] * W_e^T for every row r of every group e, W a stack of
  * n_groups matrices N x K; with transposed = 1, Y[r,:] = X[index[r],:] * W_e
- * and W is a stack of K x N. Rows of Y past the last group are set to zero.
+ * and W is a stack of K x N. Rows of Y before the first group and past the last
+ * one are set to zero (group_ptr may be a part of a routing's, for some of its
+ * experts).
  * X and W have one type, bf16 or fp16; Y has it too, or fp32.
  * Errors: INVALID_VALUE (NULL, shapes, strides, types), UNSUPPORTED (n_rows
  * or a column count above 2^31 - 1025, n_groups or rows of X above 2^31 - 2), HIP. */

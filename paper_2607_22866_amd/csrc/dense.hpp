@@ -89,15 +89,17 @@ GM_DEV f32x4 mfma_16x16x32(u32x4 a, u32x4 b, f32x4 c, _Float16) {
 }
 
 // Rows [begin, end) of ragged group e, clamped to the rows there are; group
-// n_groups is what lies past the last one.
+// n_groups is what lies past the last one, n_groups + 1 what lies before the first.
 GM_DEV void group_rows(const int64_t *gp, int64_t n_groups, int64_t n_rows, int64_t e, int64_t &begin, int64_t &end) {
-    const int64_t b = gp[e], f = e < n_groups ? gp[e + 1] : n_rows;
+    int64_t b = gp[e <= n_groups ? e : 0], f = gp[e < n_groups ? e + 1 : 0];
+    b = e <= n_groups ? b : 0;
+    f = e == n_groups ? n_rows : f;
     begin = b < 0 ? 0 : b > n_rows ? n_rows : b;
     end = f < begin ? begin : f > n_rows ? n_rows : f;
 }
 
 // Row tiles of at most BM rows, group after group, the rows past the last group
-// as one more. With HALF a group's last tile of at most BM / 2 rows is a tile of
+// and those before the first as two more. With HALF a group's last tile of at most BM / 2 rows is a tile of
 // that height, and those come after all others: less padding is computed, and
 // the work groups that start last have little to do. A wave counts 64 groups at
 // a time; all lanes get the same answer.
@@ -108,7 +110,7 @@ struct RowTiles {
 template <int BM, bool HALF>
 GM_DEV void tiles_of(const int64_t *gp, int64_t n_groups, int64_t n_rows, int64_t e, int64_t &b, int64_t &f, int &full, int &half) {
     b = f = 0;
-    if (e <= n_groups) group_rows(gp, n_groups, n_rows, e, b, f);
+    if (e <= n_groups + 1) group_rows(gp, n_groups, n_rows, e, b, f);
     const int rows = (int)(f - b), rem = rows % BM;
     half = HALF && e < n_groups && rem > 0 && rem <= BM / 2;
     full = (rows + BM - 1) / BM - half;
@@ -118,7 +120,7 @@ template <int BM, bool HALF = false>
 GM_DEV RowTiles count_row_tiles(const int64_t *gp, int64_t n_groups, int64_t n_rows, int64_t most) {
     const int lane = threadIdx.x & (GM_WAVE - 1);
     int n = 0, h = 0;
-    for (int64_t e = lane; e <= n_groups; e += GM_WAVE) {
+    for (int64_t e = lane; e <= n_groups + 1; e += GM_WAVE) {
         int64_t b, f;
         int full, half;
         tiles_of<BM, HALF>(gp, n_groups, n_rows, e, b, f, full, half);
@@ -132,7 +134,7 @@ GM_DEV RowTiles count_row_tiles(const int64_t *gp, int64_t n_groups, int64_t n_r
 }
 
 struct RowTile {
-    int64_t group;  // n_groups: rows past the last group
+    int64_t group;  // n_groups or above: rows of no group
     int64_t begin;  // first row
     int rows;       // at most BM, a half tile's at most BM / 2
 };
@@ -142,7 +144,7 @@ template <int BM, bool HALF = false>
 GM_DEV RowTile find_row_tile(const int64_t *gp, int64_t n_groups, int64_t n_rows, uint32_t t, bool half = false) {
     const int lane = threadIdx.x & (GM_WAVE - 1);
     int left = (int)t;
-    for (int64_t e0 = 0; e0 <= n_groups; e0 += GM_WAVE) {
+    for (int64_t e0 = 0; e0 <= n_groups + 1; e0 += GM_WAVE) {
         int64_t b, f;
         int n, h;
         tiles_of<BM, HALF>(gp, n_groups, n_rows, e0 + lane, b, f, n, h);
@@ -163,7 +165,7 @@ GM_DEV RowTile find_row_tile(const int64_t *gp, int64_t n_groups, int64_t n_rows
 
 // Upper bound of count_row_tiles on the host, which does not know the groups.
 inline int64_t row_tiles_bound(int64_t n_groups, int64_t n_rows, int bm) {
-    return n_rows / bm + (n_groups + 1 < n_rows ? n_groups + 1 : n_rows);
+    return n_rows / bm + (n_groups + 2 < n_rows ? n_groups + 2 : n_rows);
 }
 
 // Place of tile number b of n when each XCD gets a run of neighbours (the

@@ -628,8 +628,8 @@ def _groups(group_ptr, index, n_rows: int, dev: int) -> bytes:
 def group_product(x: torch.Tensor, w: torch.Tensor, group_ptr: torch.Tensor, index: Optional[torch.Tensor] = None,
                   transposed: bool = False, out_dtype=None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y[r] = x[index[r]] @ w[e].T (transposed: @ w[e]) for every row r of every
-    group e, group_ptr[e] <= r < group_ptr[e + 1]. index None: x's own rows.
-    bfloat16 or float16, sums in fp32; out_dtype: the inputs' type or float32."""
+    group e, group_ptr[e] <= r < group_ptr[e + 1], zeros for rows of no group. index
+    None: x's own rows. bfloat16 or float16, sums in fp32; out_dtype: the inputs' type or float32."""
     dev = _device_of(x, "x")
     dx, dw = _dense(x, dev, "x"), _dense(w, dev, "w", 3)
     n_rows = x.shape[0] if index is None else index.numel()

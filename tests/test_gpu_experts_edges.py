@@ -56,3 +56,31 @@ def test_route_backward_masked_logits_get_zero(g, bad, normalise, e):
     r = g.route(l, k, normalise=normalise)
     out = g.route_backward(l, r, torch.ones(t * k, device="cuda"))
     assert not out[:, 4:6].any() and not out[:, 7].any() and out[rows[2:]].isfinite().all()
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("mean", [3, 30, 100, 300])
+@pytest.mark.parametrize("experts", [8, 62, 63, 64, 130])
+def test_some_of_a_routings_experts(g, transposed, mean, experts):
+    # a part of group_ptr with its experts' weights: the other experts' rows are zeros, before and behind
+    r = g.route(rand((mean * experts // 2, experts + 7), torch.float32, 1), 2)
+    rows = r.token.numel()
+    for n, k in ((136, 72), (45, 67)) if experts > 8 else ((136, 72), (45, 67), (2048, 128)):
+        x = rand((r.n_tokens, k), torch.bfloat16, 2)
+        w = rand((experts,) + ((k, n) if transposed else (n, k)), torch.bfloat16, 3, k ** -0.5)
+        gp = r.group_ptr[4:4 + experts + 1]
+        y = g.group_product(x, w, gp, index=r.token, transposed=transposed,
+                            out=torch.full((rows, n), float("nan"), dtype=torch.bfloat16, device="cuda"))
+        b, f = int(gp[0]), int(gp[-1])
+        assert 0 < b < f < rows and not y[:b].any() and not y[f:].any()
+        whole = g.group_product(x, w, gp - b, index=r.token[b:f].contiguous(), transposed=transposed)
+        # (sums in another order where another tile is taken)
+        limit = 2.0 ** -7 * whole.double().abs() + (k + 8) * 2.0 ** -22 * float(x.abs().max()) * float(w.abs().max()) * k
+        assert bool(((y[b:f].double() - whole.double()).abs() <= limit).all())
+        if not transposed:
+            q, s = g.quantise_blocks(x)
+            wq, ws = g.quantise_blocks(w, 128)
+            y = g.group_product_fp8(q, s, wq, ws, gp, index=r.token,
+                                    out=torch.full((rows, n), float("nan"), dtype=torch.bfloat16, device="cuda"))
+            assert not y[:b].any() and not y[f:].any() and y[b:f].isfinite().all()
+            assert y[b:f].any(1).all()
