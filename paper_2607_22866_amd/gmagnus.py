@@ -456,6 +456,9 @@ def release_cache():
 
 
 # ------------------------------------------------------------ routed expert products
+# Gradients are calls (route_backward, group_product, group_outer, combine_backward).
+# Autograd does not make them: differentiating a result with respect to an input
+# raises. Results written to a given `out` are not part of any graph.
 _raw_stream = torch._C._cuda_getCurrentRawStream  # the current stream's handle (a tenth of current_stream()'s time)
 
 
@@ -531,6 +534,30 @@ def _out(out, shape, dtype, like, name):
     return out
 
 
+class _NoFormula(torch.autograd.Function):
+    """Puts a result into the graph of its inputs, as a node that raises when it is differentiated."""
+
+    @staticmethod
+    def forward(ctx, message, result, *inputs):
+        ctx.message = message
+        ctx.mark_dirty(result)
+        return result
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError(ctx.message)
+
+
+def _no_formula(call: str, gradients: str, results, *inputs):
+    """The gradients are calls of their own, which autograd does not make: where it would differentiate the results
+    with respect to an input it raises, instead of leaving the input without its gradient."""
+    inputs = [t for t in inputs if t is not None and t.requires_grad]
+    if inputs and torch.is_grad_enabled():
+        message = "gmagnus.%s has no autograd formula: %s" % (call, gradients)
+        for t in results:
+            _NoFormula.apply(message, t, *inputs)
+
+
 @dataclass
 class Routing:
     """The routing matrix (tokens x experts) as device arrays in both orders. Arrays
@@ -595,6 +622,8 @@ def route(logits: torch.Tensor, top_k: int, normalise: bool = True) -> Routing:
     r = Routing(t, e, top_k, bool(normalise), row_ptr, expert, weight, group_ptr, token, slot, group_weight)
     _check(lib.gmagnus_route(d, top_k, int(r.normalise), r._desc(), ws.data_ptr(), nbytes,
                              _raw_stream(dev)))
+    if logits.requires_grad:
+        _no_formula("route", "the gradient of its logits is route_backward", (weight, group_weight), logits)
     return r
 
 
@@ -636,11 +665,13 @@ def group_product(x: torch.Tensor, w: torch.Tensor, group_ptr: torch.Tensor, ind
     gd = _groups(group_ptr, index, n_rows, dev)
     if w.shape[0] != group_ptr.numel() - 1:
         raise ValueError("w must have one matrix a group")
-    out = _out(out, (n_rows, w.shape[2 if transposed else 1]), out_dtype or x.dtype, x, "out")
-    dy = _dense(out, dev, "out")
+    y = _out(out, (n_rows, w.shape[2 if transposed else 1]), out_dtype or x.dtype, x, "out")
+    dy = _dense(y, dev, "out")
     _check(load().gmagnus_group_product(gd, dx, dw, int(transposed),
                                         dy, _raw_stream(dev)))
-    return out
+    if out is None and (x.requires_grad or w.requires_grad):
+        _no_formula("group_product", "its gradients are group_product with the other order of w, and group_outer", (y,), x, w)
+    return y
 
 
 @_on_stream
@@ -672,6 +703,8 @@ def quantise_blocks(x: torch.Tensor, block_rows: int = 1):
     dq, ds = _dense(q, dev, "q", dims), _dense(scale, dev, "scale", dims)
     _check(load().gmagnus_quantise_blocks(dx, x.shape[0] if dims == 3 else 1, block_rows,
                                           dq, ds, _raw_stream(dev)))
+    if x.requires_grad:
+        _no_formula("quantise_blocks", "it rounds", (q, scale), x)
     return q, scale
 
 
@@ -688,11 +721,13 @@ def group_product_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w
     gd = _groups(group_ptr, index, n_rows, dev)
     if not w.shape[0] == w_scale.shape[0] == group_ptr.numel() - 1:
         raise ValueError("w and w_scale must have one matrix a group")
-    out = _out(out, (n_rows, w.shape[1]), out_dtype, x, "out")
-    dy = _dense(out, dev, "out")
+    y = _out(out, (n_rows, w.shape[1]), out_dtype, x, "out")
+    dy = _dense(y, dev, "out")
     _check(load().gmagnus_group_product_fp8(gd, dx, dxs, dw,
                                             dws, dy, _raw_stream(dev)))
-    return out
+    if out is None and (x.requires_grad or x_scale.requires_grad or w.requires_grad or w_scale.requires_grad):
+        _no_formula("group_product_fp8", "it is for serving", (y,), x, x_scale, w, w_scale)
+    return y
 
 
 def _combine_args(row_ptr, slot, weight, dev: int):
@@ -711,10 +746,12 @@ def combine(y: torch.Tensor, row_ptr: torch.Tensor, slot: torch.Tensor, weight: 
     dev = _device_of(y, "y")
     d = _dense(y, dev, "y")
     rp, sl, w, n = _combine_args(row_ptr, slot, weight, dev)
-    out = _out(out, (row_ptr.numel() - 1, y.shape[1]), y.dtype, y, "out")
-    o = _dense(out, dev, "out")
+    sums = _out(out, (row_ptr.numel() - 1, y.shape[1]), y.dtype, y, "out")
+    o = _dense(sums, dev, "out")
     _check(load().gmagnus_combine(rp, sl, w, n, d, o, _raw_stream(dev)))
-    return out
+    if out is None and (y.requires_grad or (weight is not None and weight.requires_grad)):
+        _no_formula("combine", "its gradients are combine_backward", (sums,), y, weight)
+    return sums
 
 
 @_on_stream
