@@ -608,8 +608,8 @@ def route(logits: torch.Tensor, top_k: int, normalise: bool = True) -> Routing:
     d = _dense(logits, dev, "logits")
     t, e = logits.shape
     lib = load()
-    n = t * top_k if top_k > 0 else 0
     nbytes = lib.gmagnus_route_workspace_bytes(t, e, top_k)
+    n = t * top_k if nbytes else 0  # (sizes that are refused below have no workspace)
     device = logits.device
     row_ptr, group_ptr = torch.empty(t + e + 2, dtype=torch.int64, device=device).split((t + 1, e + 1))
     # one block for the entries' arrays, a small workspace in front of them (every tensor made costs 1.5 us)

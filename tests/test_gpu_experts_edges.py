@@ -84,3 +84,11 @@ def test_some_of_a_routings_experts(g, transposed, mean, experts):
                                     out=torch.full((rows, n), float("nan"), dtype=torch.bfloat16, device="cuda"))
             assert not y[:b].any() and not y[f:].any() and y[b:f].isfinite().all()
             assert y[b:f].any(1).all()
+
+
+def test_route_refuses_a_top_k_beyond_any_memory(g):
+    # refused with a status, before arrays of that many entries are asked for
+    for top_k in (9, 1 << 20, 1 << 40):
+        with pytest.raises(g.GmagnusError) as e:
+            g.route(rand((4096, 8), torch.float32, 1), top_k)
+        assert e.value.status == 1
