@@ -635,8 +635,11 @@ def route_backward(logits: torch.Tensor, routing: Routing, d_weight: torch.Tenso
     d = _dense(logits, dev, "logits")
     if tuple(logits.shape) != (routing.n_tokens, routing.n_experts):
         raise ValueError("logits must have the routing's shape")
-    _check_device(routing.row_ptr, dev, "routing")
-    g = _array(d_weight, dev, "d_weight", torch.float32, routing.n_tokens * routing.top_k)
+    n = routing.n_tokens * routing.top_k
+    _array(routing.row_ptr, dev, "routing.row_ptr", torch.int64, routing.n_tokens + 1)
+    _array(routing.expert, dev, "routing.expert", torch.int32, n)
+    _array(routing.weight, dev, "routing.weight", torch.float32, n)
+    g = _array(d_weight, dev, "d_weight", torch.float32, n)
     out = _out(out, tuple(logits.shape), logits.dtype, logits, "out")
     o = _dense(out, dev, "out")
     _check(load().gmagnus_route_backward(d, routing.top_k, int(routing.normalise),

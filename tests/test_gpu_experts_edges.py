@@ -1,6 +1,8 @@
 """Calls of the routed expert products at the edges of what they accept, against
 64-bit forms: infinities and NaN that reach a sum, parts of a routing, scales
 near the ends of fp32."""
+import dataclasses
+
 import numpy as np
 import pytest
 
@@ -92,3 +94,15 @@ def test_route_refuses_a_top_k_beyond_any_memory(g):
         with pytest.raises(g.GmagnusError) as e:
             g.route(rand((4096, 8), torch.float32, 1), top_k)
         assert e.value.status == 1
+
+
+@pytest.mark.parametrize("name,change", [("row_ptr", lambda a: a[:-1]), ("row_ptr", lambda a: a.int()), ("expert", lambda a: a[:-1]),
+                                         ("expert", lambda a: a.long()), ("weight", lambda a: a[::2]), ("weight", lambda a: a.half()),
+                                         ("weight", lambda a: a.cpu())])
+def test_route_backward_refuses_a_routings_arrays(g, name, change):
+    # the arrays of a routing that a program put together itself are checked like any other array
+    l = rand((20, 8), torch.float32, 1)
+    r = g.route(l, 2)
+    bad = dataclasses.replace(r, **{name: change(getattr(r, name))})
+    with pytest.raises(ValueError, match="routing." + name):
+        g.route_backward(l, bad, torch.ones(40, device="cuda"))
