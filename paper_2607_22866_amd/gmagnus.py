@@ -716,7 +716,8 @@ def group_product_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w
                       group_ptr: torch.Tensor, index: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """group_product of float8_e4m3fn operands with the scales quantise_blocks gives
-    (x: block_rows 1, w: block_rows 128). One group is the plain product."""
+    (x: block_rows 1, w: block_rows 128). One group is the plain product. A block's two
+    scales are multiplied first: their product has to be a normal float32 number."""
     dev = _device_of(x, "x")
     dx, dxs = _dense(x, dev, "x"), _dense(x_scale, dev, "x_scale")
     dw, dws = _dense(w, dev, "w", 3), _dense(w_scale, dev, "w_scale", 3)

@@ -106,3 +106,33 @@ def test_route_backward_refuses_a_routings_arrays(g, name, change):
     bad = dataclasses.replace(r, **{name: change(getattr(r, name))})
     with pytest.raises(ValueError, match="routing." + name):
         g.route_backward(l, bad, torch.ones(40, device="cuda"))
+
+
+def fp8(v):
+    return v.to(torch.float8_e4m3fn)
+
+
+# groups, rows of each, columns, reduction: a work group's 16 rows with 16 and with 64 columns, any alignment, 32, 64 and 256 rows
+FP8_SHAPES = [(2, 3, 72, 400), (64, 5, 520, 272), (3, 40, 130, 333), (8, 30, 136, 528), (4, 100, 264, 144), (16, 140, 2048, 272)]
+
+
+@pytest.mark.parametrize("e,rows,n,k", FP8_SHAPES)
+@pytest.mark.parametrize("x_exp,w_exp", [(-63, -63), (-126, 0), (0, -126), (-100, -20), (63, 64), (100, 27), (8, 119)])
+def test_fp8_scales_to_the_ends_of_their_product(g, e, rows, n, k, x_exp, w_exp):
+    # a block's two scales multiply to between 2^-126 and 2^128: small values meet the large ones, so that sums stay in fp32
+    top = 448.0 if x_exp + w_exp < 0 else 2.0 ** -6
+    q = fp8(rand((e * rows, k), torch.float32, 1).clamp(-1, 1) * top)
+    wq = fp8(rand((e, n, k), torch.float32, 2).clamp(-1, 1) * top)
+    kb, nb = -(-k // 128), -(-n // 128)
+    mant = lambda shape, seed: 1 + torch.rand(shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed)) * 0.4
+    s, ws = mant((e * rows, kb), 3) * 2.0 ** x_exp, mant((e, nb, kb), 4) * 2.0 ** w_exp
+    q[1, :128] = 0                      # a block whose sum is zero
+    y = g.group_product_fp8(q, s, wq, ws, offsets([rows] * e), out_dtype=torch.float32)
+    up, down = torch.arange(k, device="cuda") // 128, torch.arange(n, device="cuda") // 128
+    xv = (q.double() * s.double()[:, up]).reshape(e, rows, k)
+    wv = (wq.double() * ws.double()[:, down][:, :, up]).transpose(1, 2).contiguous()
+    want, mag = xv @ wv, xv.abs() @ wv.abs()
+    # 16 products at a time are cut 13 bits below the largest: 16 * 2^-13 of it, at most of the sum of magnitudes
+    limit = er.U["float32"] * want.abs() + er.TINY["float32"] + ((k + 8) * 2.0 ** -23 + 2.0 ** -9) * mag
+    assert y.isfinite().all()
+    assert bool(((y.double().reshape(want.shape) - want).abs() <= limit).all())
