@@ -464,7 +464,7 @@ typedef struct {
     int64_t n_groups;
     int64_t n_rows;           /* grouped rows the arrays have room for */
     const int64_t *group_ptr; /* device, n_groups + 1 */
-    const int32_t *index;     /* device, n_rows, or NULL */
+    const int32_t *index;     /* device, n_rows, or NULL (X then has n_rows rows; any number if n_rows is 0) */
 } gmagnus_groups_t;
 
 /* Y[r,:] = X[index[r],:] * W_e^T for every row r of every group e, W a stack of

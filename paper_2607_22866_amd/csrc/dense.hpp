@@ -274,6 +274,10 @@ inline void check_groups(const gmagnus_groups_t *g) {
                "groups: more than 2^31 - 1025 rows or 2^31 - 2 groups");
 }
 
+// Rows that X has to have: its own with an index (and without grouped rows, where
+// an empty index may be NULL), one for each grouped row otherwise.
+inline int64_t x_rows(const gmagnus_groups_t &g, const gmagnus_dense_t &X) { return g.index || g.n_rows == 0 ? X.n_rows : g.n_rows; }
+
 inline void check_side(int64_t n, const char *what) {
     GM_REQUIRE(n >= 1, GMAGNUS_ERROR_INVALID_VALUE, std::string(what) + " must be positive");
     GM_REQUIRE(n <= MAX_SIDE, GMAGNUS_ERROR_UNSUPPORTED, std::string(what) + " beyond 2^31 - 1025");

@@ -567,7 +567,7 @@ extern "C" gmagnus_status_t gmagnus_group_product(const gmagnus_groups_t *groups
         const int64_t k = X->n_cols, n = Y->n_cols;
         check_side(k, "columns of X");
         check_side(n, "columns of Y");
-        check_dense(X, "X", groups->index ? X->n_rows : groups->n_rows, k);
+        check_dense(X, "X", x_rows(*groups, *X), k);
         check_dense(Y, "Y", groups->n_rows, n);
         check_dense(W, "W", transposed ? k : n, transposed ? n : k, groups->n_groups);
         GM_REQUIRE(X->n_rows >= 0 && X->n_rows < INT32_MAX, GMAGNUS_ERROR_UNSUPPORTED, "rows of X beyond 2^31 - 2");
@@ -623,7 +623,7 @@ extern "C" gmagnus_status_t gmagnus_group_outer(const gmagnus_groups_t *groups, 
         check_side(n, "columns of DY");
         check_side(k, "columns of X");
         check_dense(DY, "DY", groups->n_rows, n);
-        check_dense(X, "X", groups->index ? X->n_rows : groups->n_rows, k);
+        check_dense(X, "X", x_rows(*groups, *X), k);
         check_dense(D, "D", n, k, groups->n_groups);
         GM_REQUIRE(X->n_rows >= 0 && X->n_rows < INT32_MAX, GMAGNUS_ERROR_UNSUPPORTED, "rows of X beyond 2^31 - 2");
         GM_REQUIRE(is_16bit(X->data_type) && DY->data_type == X->data_type, GMAGNUS_ERROR_INVALID_VALUE,

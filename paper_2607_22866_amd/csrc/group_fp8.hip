@@ -592,7 +592,7 @@ extern "C" gmagnus_status_t gmagnus_group_product_fp8(const gmagnus_groups_t *gr
         const int64_t k = X->n_cols, n = Y->n_cols;
         check_side(k, "columns of X");
         check_side(n, "columns of Y");
-        const int64_t n_x = groups->index ? X->n_rows : groups->n_rows, kb = (k + SB - 1) / SB;
+        const int64_t n_x = x_rows(*groups, *X), kb = (k + SB - 1) / SB;
         check_dense(X, "X", n_x, k);
         check_dense(X_scale, "X_scale", n_x, kb);
         check_dense(Y, "Y", groups->n_rows, n);

@@ -136,3 +136,23 @@ def test_fp8_scales_to_the_ends_of_their_product(g, e, rows, n, k, x_exp, w_exp)
     limit = er.U["float32"] * want.abs() + er.TINY["float32"] + ((k + 8) * 2.0 ** -23 + 2.0 ** -9) * mag
     assert y.isfinite().all()
     assert bool(((y.double().reshape(want.shape) - want).abs() <= limit).all())
+
+
+def test_no_grouped_rows(g):
+    # an empty index into an X with rows (no token chose any of these experts): empty results, zero gradients
+    x, w = rand((9, 64), torch.bfloat16, 1), rand((3, 72, 64), torch.bfloat16, 2)
+    gp, none = offsets([0, 0, 0]), torch.empty(0, dtype=torch.int32, device="cuda")
+    assert g.group_product(x, w, gp, index=none).shape == (0, 72)
+    assert g.group_product(rand((9, 72), torch.bfloat16, 1), w, gp, index=none, transposed=True).shape == (0, 64)
+    d = g.group_outer(torch.empty((0, 72), dtype=torch.bfloat16, device="cuda"), x, gp, index=none,
+                      out=torch.full((3, 72, 64), float("nan"), dtype=torch.bfloat16, device="cuda"))
+    assert not d.any()
+    q, s = g.quantise_blocks(x)
+    wq, ws = g.quantise_blocks(w, 128)
+    assert g.group_product_fp8(q, s, wq, ws, gp, index=none).shape == (0, 72)
+    # and their sums
+    y = g.combine(torch.empty((0, 72), dtype=torch.bfloat16, device="cuda"), torch.zeros(6, dtype=torch.int64, device="cuda"), none)
+    assert y.shape == (5, 72) and not y.any()
+    d_y, d_w = g.combine_backward(torch.empty((0, 72), dtype=torch.bfloat16, device="cuda"),
+                                  torch.zeros(6, dtype=torch.int64, device="cuda"), none, None, y)
+    assert d_y.shape == (0, 72) and d_w.shape == (0,)
