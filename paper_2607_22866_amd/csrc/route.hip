@@ -39,9 +39,17 @@ GM_DEV float key_value(uint32_t k) {
         return to_f32(__builtin_bit_cast(T, (uint16_t)(k >> 15 ? k & 0x7fffu : ~k)));
 }
 
-// e^x for x <= 0, by the hardware's power of two: a few units more off than expf
-// and, like the rounding of x itself, by |x| units of 2^-24.
-GM_DEV float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+// e^x for x <= 0, by the hardware's power of two: what x log2(e) loses when it is
+// rounded (|x| units of 2^-24 of the result) is multiplied in afterwards, so that a few
+// units are off at any x. (From -200 on down the result is zero, for NaN too: an
+// infinite logit, whose difference to itself that is, has a sum of zero and NaN weights.)
+GM_DEV float exp_neg(float x) {
+    constexpr float L = 0x1.715476p+0f, L_REST = 0x1.4ae0cp-26f, LN2 = 0x1.62e43p-1f;
+    const float y = __builtin_amdgcn_fmed3f(x, -200.f, 0.f), t = y * L;
+    const float rest = __builtin_fmaf(y, L_REST, __builtin_fmaf(y, L, -t));
+    const float r = __builtin_amdgcn_exp2f(t);
+    return __builtin_fmaf(r * LN2, rest, r);
+}
 
 GM_DEV uint32_t wave_max(uint32_t x) {
 #define GM_STEP(ctrl, rows) \

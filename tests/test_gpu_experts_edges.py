@@ -156,3 +156,28 @@ def test_no_grouped_rows(g):
     d_y, d_w = g.combine_backward(torch.empty((0, 72), dtype=torch.bfloat16, device="cuda"),
                                   torch.zeros(6, dtype=torch.int64, device="cuda"), none, None, y)
     assert d_y.shape == (0, 72) and d_w.shape == (0,)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("normalise", [True, False])
+def test_route_weights_of_widely_spread_logits(g, dtype, normalise):
+    # logits whose differences are exact in fp32 (multiples of 1/8): the weights are good to a few units however small they are
+    t, e = 500, 4
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    l = (torch.randint(0, 84 * 8, (t, e), device="cuda", generator=gen).float() / 8 - 40).to(dtype)
+    l[0] = torch.tensor([torch.finfo(dtype).min, 3.0, -float("inf"), 3.0])
+    r = g.route(l, e, normalise=normalise)
+    want = torch.softmax(l.double(), 1)
+    got = torch.zeros(t, e, dtype=torch.float64, device="cuda")
+    row = torch.repeat_interleave(torch.arange(t, device="cuda"), r.row_ptr[1:] - r.row_ptr[:-1])
+    got[row, r.expert[:row.numel()].long()] = r.weight[:row.numel()].double()
+    assert got[0].tolist() == [0.0, 0.5, 0.0, 0.5]
+    # units of 2^-24: e^x 5, the sum of 4 terms 4, its reciprocal 3, the product 1
+    assert bool(((got - want).abs() <= 13 * 2.0 ** -24 * want + 1e-37).all())
+    d = rand((t * e,), torch.float32, 2)
+    d64 = torch.zeros_like(got)
+    d64[row, r.expert[:row.numel()].long()] = d[:row.numel()].double()
+    grad = want * (d64 - (want * d64).sum(1, keepdim=True))
+    mag = want * (d64.abs() + (want * d64.abs()).sum(1, keepdim=True))
+    limit = er.U[str(dtype).replace("torch.", "")] * grad.abs() + er.TINY[str(dtype).replace("torch.", "")] + 40 * 2.0 ** -24 * mag + 1e-37
+    assert bool(((g.route_backward(l, r, d).double() - grad).abs() <= limit).all())
