@@ -459,7 +459,8 @@ def release_cache():
 # Gradients are calls (route_backward, group_product, group_outer, combine_backward).
 # Autograd does not make them: differentiating a result with respect to an input
 # raises. Results written to a given `out` are not part of any graph.
-_raw_stream = torch._C._cuda_getCurrentRawStream  # the current stream's handle (a tenth of current_stream()'s time)
+# the current stream's handle, in a tenth of current_stream()'s time (a torch without GPU support does not have it)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _on_stream(f):
