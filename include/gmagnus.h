@@ -399,7 +399,7 @@ gmagnus_status_t gmagnus_bandwidth_probe(int32_t kind, void *dst, const void *sr
  * X reads as a row of zeros (against weights that are infinite or NaN its
  * results are zeros or NaN), bounds are clamped to the rows there are.
  * Sums are held in fp32 (8-bit operands: see there); results are rounded
- * once, to the output's type. */
+ * once, to the output's type. Outputs may not overlap inputs. */
 typedef enum {
     GMAGNUS_DATA_FP32 = 0,
     GMAGNUS_DATA_BF16 = 1,
@@ -521,9 +521,13 @@ gmagnus_status_t gmagnus_combine(const int64_t *row_ptr, const int32_t *slot, co
 
 /* Gradients of gmagnus_combine: D_Y[slot[j],:] = weight[j] * D_OUT[t,:] and
  * d_weight[j] = sum of Y[slot[j],:] * D_OUT[t,:] (fp32). Rows of D_Y past the
- * last entry and places of d_weight past it are set to zero (the slots of a
- * routing are a permutation of the rows before it). weight NULL means 1;
- * d_weight (and then Y) or D_Y may be NULL where it is not wanted.
+ * last entry and places of d_weight past it are set to zero. The rows before it
+ * have to be named by one slot each, as those of a whole routing are: row_ptr
+ * begins with 0, a row that two slots name holds either's gradient, and a row
+ * that none names is not written. (A slot outside D_Y is passed over, so a part
+ * of the experts, whose rows are D_Y's, needs no more than its slots counted from
+ * its first row on.) weight NULL means 1; d_weight (and then Y) or D_Y may be NULL
+ * where it is not wanted.
  * Errors as gmagnus_combine. */
 gmagnus_status_t gmagnus_combine_backward(const int64_t *row_ptr, const int32_t *slot, const float *weight,
                                           int64_t n_entries, const gmagnus_dense_t *Y, const gmagnus_dense_t *D_OUT,

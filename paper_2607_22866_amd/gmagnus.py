@@ -762,8 +762,9 @@ def combine(y: torch.Tensor, row_ptr: torch.Tensor, slot: torch.Tensor, weight: 
 @_on_stream
 def combine_backward(y: Optional[torch.Tensor], row_ptr: torch.Tensor, slot: torch.Tensor,
                      weight: Optional[torch.Tensor], d_out: torch.Tensor, n_rows: Optional[int] = None):
-    """(gradient of y, gradient of weight) of combine. y None (with n_rows, the rows
-    of y): the weights' gradient is not wanted and None."""
+    """(gradient of y, gradient of weight) of combine for a whole routing (row_ptr[0] is
+    0, each row of y before row_ptr[-1] is named by one slot). y None (with n_rows, the
+    rows of y): the weights' gradient is not wanted and None."""
     dev = _device_of(d_out, "d_out")
     do = _dense(d_out, dev, "d_out")
     rp, sl, w, n = _combine_args(row_ptr, slot, weight, dev)

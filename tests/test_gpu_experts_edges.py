@@ -181,3 +181,18 @@ def test_route_weights_of_widely_spread_logits(g, dtype, normalise):
     mag = want * (d64.abs() + (want * d64.abs()).sum(1, keepdim=True))
     limit = er.U[str(dtype).replace("torch.", "")] * grad.abs() + er.TINY[str(dtype).replace("torch.", "")] + 40 * 2.0 ** -24 * mag + 1e-37
     assert bool(((g.route_backward(l, r, d).double() - grad).abs() <= limit).all())
+
+
+@pytest.mark.parametrize("t,e,k,n", [(50, 12, 3, 40), (400, 70, 2, 520)])
+def test_combine_of_some_experts_rows(g, t, e, k, n):
+    # the rows of experts 4 .. e - 3 only, slots counted from the first of them: the others add nothing and get no gradient
+    r = g.route(rand((t, e), torch.float32, 1), k)
+    b, f = int(r.group_ptr[4]), int(r.group_ptr[e - 3])
+    y, d_out = rand((t * k, n), torch.bfloat16, 2), rand((t, n), torch.bfloat16, 3)
+    here = torch.zeros_like(y)
+    here[b:f] = y[b:f]
+    slot = r.slot - b
+    assert torch.equal(g.combine(y[b:f], r.row_ptr, slot, r.weight), g.combine(here, r.row_ptr, r.slot, r.weight))
+    d_y, d_w = g.combine_backward(y[b:f], r.row_ptr, slot, r.weight, d_out)
+    want_y, want_w = g.combine_backward(here, r.row_ptr, r.slot, r.weight, d_out)
+    assert torch.equal(d_y, want_y[b:f]) and torch.equal(d_w, want_w)
