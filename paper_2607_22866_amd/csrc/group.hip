@@ -20,7 +20,7 @@ namespace {
 // waves of 64 x 64. Two steps' loads are in flight in registers while a third
 // step's tile is multiplied from one of two LDS buffers; bound by that staging
 // (loads that cross lines, LDS writes). One group of 4001 x 4001 x 4001, fp16: 700
-// TFLOP/s, transposed 740, gradient 594.
+// TFLOP/s, transposed 730, gradient 690.
 constexpr int GEN_B = 128, GEN_T = 256;
 
 // IDX: k as rows, their numbers by an index.
@@ -160,9 +160,10 @@ GM_DEV void tile_any(const Side &p, const Side &q, int n_k, OUT *out, int64_t ou
 }
 
 // A tile by WP x WQ waves; bound by the matrix units' power and, in small groups,
-// by the weights' bytes. One group of 8192 x 8192 x 8192, bf16: 1265-1320 TFLOP/s
-// (weights n x k), 1357-1405 (k x n), gradient 1345-1430; 32 groups of 1024 rows,
-// 2048 x 4096, 1090, gradient 845. 256 x 256 tiles move the fewest bytes a product
+// by the weights' bytes. One group of 8192 x 8192 x 8192, bf16: 1265-1440 TFLOP/s from
+// card to card (weights n x k), 1357-1460 (k x n), gradient 1345-1465, on operands of
+// zeros, which draw less power, 1655, 1700 and 1810; 32 groups of 1024 rows, 2048 x
+// 4096, 1090-1130 (with one matrix of weights for all 1360), gradient 845-965. 256 x 256 tiles move the fewest bytes a product
 // that registers hold sums for (128 a lane). A wave's share of a step is four units of (32
 // reduction elements, half of its p rows); a unit's fragments are read from LDS
 // while the one before is multiplied. The barrier stands before a step's last
@@ -333,8 +334,8 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_product_fast(ProductA
 // of 64 reduction elements, FEW_U blocks' loads in flight each, and their sums
 // are joined in LDS in the waves' order. A lane's 16 bytes of a row (chunks g
 // and g + 4 of the block, the same for both operands) lie next to its
-// neighbours'. 64 groups of 1 row, 2048 x 2048, bf16: 84 us (4.3 TB/s of weights);
-// one row, 4096 x 4096: 12.5 us with the call.
+// neighbours'. 64 groups of 1 row, 2048 x 2048, bf16: 112 us (4.8 TB/s of weights);
+// one row, 4096 x 4096: 11 us with the call.
 constexpr int FEW_U = 4;
 
 // Row of X that the tile's row r stands for, -1 if there is none.
@@ -433,9 +434,12 @@ struct OuterArgs {
 // Tile t of the stack of gradients: its group, tile row and tile column. A tile
 // costs as much as its group has rows, so where the groups are long (by_size) of
 // each 64 the longest come first, and the last work groups to start have little
-// to do; a group's tiles are spread over the XCDs, neighbours together. (16
-// groups of 16384 rows cut at random, 2048 x 2048: 179 us; groups in order with a
-// run of tiles for each XCD: 271 us. Ordering costs a tile about a microsecond.)
+// to do; a group's tiles are spread over the XCDs, neighbours together. In order
+// against by size, 16 groups of 1024 rows on the average, 2048 x 2048, bf16: equal
+// groups 129 / 135 us, half of the rows in the last group 213 / 169, sizes that fall
+// off exponentially 156 / 134; of 256 rows 62 / 70, 81 / 69, 64 / 63; 64 groups of 256
+// rows 248 / 272, 378 / 303, 258 / 282. Ordering costs a tile one to two microseconds,
+// so shorter groups are taken as they come (64 groups of 128 equal ones 192 / 219).
 GM_DEV void outer_tile(const OuterArgs &a, uint32_t t, uint32_t n_row, uint32_t n_col, uint32_t &e, uint32_t &tr, uint32_t &tc) {
     const uint32_t per = n_row * n_col, place = t / per;
     e = place;
@@ -526,27 +530,32 @@ Shape product_shape(const ProductArgs &a, bool transposed) {
     const bool fast = fast_side(a.x, a.xs, 0, a.k, a.index ? a.n_x : 256) &&
                       fast_side(a.w, a.ws, a.n_groups > 1 ? a.wg : 0, transposed ? a.n : a.k, 256);
     // Up to 16 rows a group the weights' bytes are all there is. 64 columns a work
-    // group (64 groups, 2048 x 2048, of 1, 4 and 16 rows: 84, 104 and 148 us; tiles of
-    // 32 x 128 109, 140 and 165; of 24 rows 179 against 153) unless that leaves CUs
-    // without one, then 16 (4 groups of 1 row: 12.6 against 13.9). Rows that are not
-    // aligned are slower that way (2047 wide, 1 row: 121 us, staged tiles 61).
+    // group (64 groups, 2048 x 2048, sizes as chance deals them, of 1, 4 and 16 rows on
+    // the average: 80, 111 and 142 us; tiles of 32 x 128 84, 149 and 156; of 24 rows 180
+    // against 172) unless that leaves CUs without one, then 16 (4 groups of 1 row: 10.9
+    // against 12.9). Rows that are not aligned are slower with 64 (64 groups of 1 row,
+    // 2047 x 2047: 194 us, staged tiles 101), not with 16 (4 groups: 29 / 37). Where one
+    // group has all the rows its weights are read for every 16 of them, from the
+    // caches: mean 16, 77 against 24 us with tiles of 32 x 128.
     if (!transposed && mean <= 16) {
         if (groups * ((a.n + 63) / 64) < 256) return Shape::FEW16;
         if (fast) return Shape::FEW64;
     }
     if (!fast) return Shape::ANY;
-    // Tiles of 32 rows or of 64 by the groups' height: of 48 rows 135 against 150 us, of
-    // 64 rows 151 / 175, of 96 rows 178 / 151; transposed 24 rows 116 / 123, 48 rows 132 / 118.
+    // Tiles of 32 rows or of 64 by the groups' height: of 48 rows 130 against 177 us, of
+    // 64 rows 143 / 151, of 96 rows 169 / 152 (all rows in one of the groups, mean 64: 58 /
+    // 50); transposed 24 rows 122 / 125, 32 rows 116 / 127, and of 48 rows still 128 / 133.
     if (mean <= (transposed ? 32 : 64)) return Shape::T32;
     return big_product_tiles(mean, a.n, groups) ? Shape::T256 : Shape::T64;
 }
 
 // Whether a gradient's tiles are 256 x 256 rather than 128 x 128. A tile takes as
 // long as its group has rows, so there have to be several a CU to even that out,
-// unless there is one group: 64 groups of 256 rows, 2048 x 2048 (4096 tiles), 285
-// against 376 us, 768 x 1024 (768 tiles) 59 / 74; 16 groups of 1024 rows, 1024 x 1024
-// (256 tiles), 107 / 74; one group of 1024 rows, 4096 x 4096 (256 tiles), 37 / 44, 2048
-// x 2048 (64 tiles) 29 / 18. And not where padding grows by more than a third.
+// unless there is one group. Equal groups, then rows cut at random: 64 groups of 256
+// rows on the average, 2048 x 2048 (4096 tiles), 289 against 407 us and 281 / 373, 768 x
+// 1024 (768 tiles) 57 / 76 and 52 / 73; 16 groups of 1024 rows, 1024 x 1024 (256 tiles),
+// 40 / 56 and 74 / 58; one group of 1024 rows, 4096 x 4096 (256 tiles), 35 / 41, 2048 x
+// 2048 (64 tiles) 27 / 16. And not where padding grows by more than a third.
 bool big_outer_tiles(int64_t n, int64_t k, int64_t n_groups) {
     const int64_t tiles = (n + 255) / 256 * ((k + 255) / 256), small = (n + 127) / 128 * ((k + 127) / 128);
     return tiles * n_groups >= (n_groups == 1 ? 192 : 512) && 3 * 4 * tiles <= 4 * small;

@@ -61,7 +61,7 @@ GM_DEV void store_fp8x8(uint8_t *p, int valid, const float (&v)[8], float scale)
 
 // One scale a row and 128 columns: 16 lanes a block, eight values a lane, a work
 // group 16 blocks of one row or, of rows shorter than that, several rows. Bound by
-// its bytes: 8192 x 8192 bf16 48 us, 4.2 TB/s; 16384 x 4096 28 us.
+// its bytes: 8192 x 8192 bf16 42-48 us, 4.2-4.8 TB/s; 16384 x 4096 45-47 us.
 template <typename T>
 __global__ __launch_bounds__(256) void k_quantise_rows(QuantArgs a) {
     const int blocks = (int)((a.n_cols + SB - 1) / SB), wide = blocks < 16 ? blocks : 16, per = 16 / wide;
@@ -99,7 +99,10 @@ __global__ __launch_bounds__(256) void k_quantise_rows(QuantArgs a) {
     }
 }
 
-// One scale for 128 x 128 values: a work group a block, kept in registers.
+// One scale for 128 x 128 values: a work group a block, kept in registers. Bound by
+// its bytes in bf16 (8192 x 8192 42 us, 4.7 TB/s; 16 x 4096 x 4096 160 us, 5.0); in
+// fp32, where a lane's 32 bytes are two loads, at half that (145 us, 2.3 TB/s; 523 us,
+// 2.6).
 template <typename T>
 __global__ __launch_bounds__(256) void k_quantise_tiles(QuantArgs a) {
     __shared__ uint32_t part[4];
@@ -181,7 +184,9 @@ GM_DEV u32x4 load16(const uint8_t *p, int64_t valid) {
 // Any alignment: tiles of 128 x 128 staged through registers, four waves of
 // 64 x 64. LDS rows are one block of 128 bytes; chunk c of row r sits at
 // c ^ (r / 2 % 8). A lane's 32 reduction bytes are chunks g and g + 4 of its row,
-// the same for both operands (the order within a block does not matter).
+// the same for both operands (the order within a block does not matter). One
+// buffer, one step's loads in flight: one group of 4001 x 4001 x 4001 177 us, 720
+// TFLOP/s; 16 groups of 1024 rows, 2047 x 2047, 197 us, 700.
 constexpr int GEN_B = 128, GEN_T = 256;
 
 template <typename OUT>
@@ -266,10 +271,10 @@ __global__ __launch_bounds__(GEN_T, 2) void k_group_product_fp8_any(Fp8Args a) {
 // them (tile.hpp): a step is one block of 128 bytes a row. A wave takes its p
 // rows 16 at a time against its 64 q columns. What the matrix units return for
 // a block goes into the fp32 sums with the row's scale times the column
-// block's, on the vector units while the other wave of the SIMD multiplies. One
-// group of 8192 x 8192 x 8192: 2000 TFLOP/s (of zeros, which draw less power, 2680);
-// 16 groups of 1024 rows, 4096 x 4096, 1720. The
-// scales of X's rows come with their tile, 64 rows by each of the first waves.
+// block's, on the vector units while the other wave of the SIMD multiplies; the
+// matrix units are busy half of the cycles (4096 x 4096 x 4096). One group of 8192 x
+// 8192 x 8192: 2000-2300 TFLOP/s from card to card (of zeros, which draw less power,
+// 2700); 16 groups of 1024 rows, 4096 x 4096, 1720-1920. The scales of X's rows come with their tile, 64 rows by each of the first waves.
 template <int BP, int BQ>
 constexpr int fast_lds() { return 2 * ((BP + BQ) * SB + ((BP + 63) / 64 * 64 + 64) * 4); }
 
@@ -423,8 +428,8 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void k_group_product_fp8_fast(Fp8A
 }
 
 // Groups of a few rows: the weights' bytes are the bound, and go straight into the
-// matrix unit's registers, any alignment (64 groups of 1 row, 2048 x 4096: 107 us,
-// 4 rows 134; 3.4-4.0 TB/s of weights). A work group takes 16 rows of a group and 16 NT
+// matrix unit's registers, any alignment (64 groups of 1 row, 2048 x 4096: 144 us,
+// 4 rows 146; 3.7 TB/s of weights). A work group takes 16 rows of a group and 16 NT
 // columns, its waves take turns at blocks of 128, FEW_U blocks' loads in flight
 // each, and their sums are joined in LDS in the waves' order.
 constexpr int FEW_U = 4;
@@ -520,17 +525,19 @@ Shape fp8_shape(const Fp8Args &a) {
     const bool fast = fast_side(a.x, a.xs, 0, a.k, a.index ? a.n_x : 256, 1) &&
                       fast_side(a.w, a.ws, a.n_groups > 1 ? a.wg : 0, a.k, 256, 1) &&
                       (a.n_x * a.sxs + kb) * 4 < (int64_t)NOWHERE && (2 * a.sws + kb) * 4 < (int64_t)NOWHERE;
-    // 64 groups, 2048 x 4096: of 1, 4 and 16 rows 64 columns a work group 107, 134 and
-    // 192 us, tiles of 32 x 128 112, 170 and 158; one row, 4096 x 4096: 13.4 with 16
-    // columns, 15.0 with 64
+    // 64 groups, 2048 x 4096, sizes as chance deals them: of 1, 4, 8 and 16 rows 64
+    // columns a work group 103, 141, 156 and 181 us, tiles of 32 x 128 88, 173, 176 and
+    // 177 (all rows in one of the groups, mean 8: 60 / 26); one row, 4096 x 4096: 11.7
+    // with 16 columns, 13.8 with 64; 4 groups of 1 row, 2047 x 2047 (not aligned): 19.4,
+    // staged tiles 27.4
     if (mean <= 8) {
         if (groups * ((a.n + 63) / 64) < 256) return Shape::FEW16;
         if (fast) return Shape::FEW64;
     }
     if (!fast) return Shape::ANY;
-    // of 24 rows tiles of 32 rows 137, of 64 155; of 48 rows 151 / 139, of 96 208 / 167
+    // of 24 rows tiles of 32 rows 172, of 64 178; of 32 rows 137 / 176, of 96 206 / 162 (and of 48 still 148 / 173)
     if (mean <= 32) return Shape::T32;
-    // of 96 rows 256 x 256 tiles 172 against 167, of 128 179 / 198, of 512 368 / 497
+    // of 96 rows 256 x 256 tiles 142 against 162, of 128 151 / 200, of 512 370 / 510
     return big_product_tiles(mean, a.n, groups) ? Shape::T256 : Shape::T64;
 }
 

@@ -233,10 +233,13 @@ inline bool fast_side(const void *p, int64_t stride, int64_t stack, int64_t axis
 
 // Whether a product of `groups` groups of `mean` rows and n columns takes 256 x
 // 256 tiles (one work group a CU, the fewest bytes a product) rather than 64 x 128
-// (three a CU): at 64 groups, 2048 x 2048, bf16, of 96 rows 166 against 151 us, 128
-// rows 175 / 177, 192 rows 192 / 202, 512 rows 331 / 418; where they leave CUs
-// without one, 8 groups of 512 rows, 1024 x 1024 (64 tiles), 26.7 / 19.1, of 1024
-// rows (128 tiles) 28.5 / 30.7; and not where the columns' padding grows by more than a third.
+// (three a CU). 64 groups, 2048 x 2048, bf16, sizes as chance deals them: of 128
+// rows on the average 150 against 177 us, 192 rows 153 / 207, 512 rows 332 / 415, and
+// already of 96 rows 142 / 152 (of 64 rows, equal groups, 139 against 133 with 32 x
+// 128); all rows in one of the groups: mean 128 55 / 79, 256 104 / 156. Where they
+// leave CUs without one: 8 groups of 512 rows, 1024 x 1024 (64 tiles), 24.5 / 17.7, of
+// 1024 rows (128 tiles) 26.5 / 30.2; and not where the columns' padding grows by more
+// than a third.
 inline bool big_product_tiles(int64_t mean, int64_t n, int64_t groups) {
     const int64_t cols = (n + 255) / 256;
     return mean >= 128 && (mean + 255) / 256 * cols * groups >= 128 && 3 * 2 * cols <= 4 * ((n + 127) / 128);
