@@ -404,7 +404,8 @@ typedef enum {
     GMAGNUS_DATA_FP32 = 0,
     GMAGNUS_DATA_BF16 = 1,
     GMAGNUS_DATA_FP16 = 2,
-    GMAGNUS_DATA_FP8_E4M3 = 3 /* OCP E4M3: no infinities, largest finite value 448 */
+    GMAGNUS_DATA_FP8_E4M3 = 3, /* OCP E4M3: no infinities, largest finite value 448 */
+    GMAGNUS_DATA_INT8 = 4      /* where a call names it */
 } gmagnus_data_type_t;
 
 /* A row-major matrix, or a stack of them (one per group, stack_stride elements
@@ -532,6 +533,58 @@ gmagnus_status_t gmagnus_combine(const int64_t *row_ptr, const int32_t *slot, co
 gmagnus_status_t gmagnus_combine_backward(const int64_t *row_ptr, const int32_t *slot, const float *weight,
                                           int64_t n_entries, const gmagnus_dense_t *Y, const gmagnus_dense_t *D_OUT,
                                           const gmagnus_dense_t *D_Y, float *d_weight, void *hip_stream);
+
+/* What a layer of experts does to its rows around the products, with the results in
+ * the rows' type, in 8 bits with scales, or both. An 8-bit result Q has its scales
+ * (fp32) beside it: E4M3 as gmagnus_quantise_blocks with block_rows 1 gives them
+ * (scale n_rows x ceil(n_cols / 128)), int8 as gmagnus_quantise_rows does (scale 1 x
+ * n_rows); it is rounded from the fp32 result, not from the one in the rows' type.
+ * Q and scale, or Y, may be NULL where that result is not wanted. */
+
+/* TOTAL = X + residual, rounded to their type, and Y = TOTAL * weight / sqrt(mean of a
+ * row's squares + eps), of TOTAL as its type holds it; without a residual (NULL, as
+ * total then) TOTAL is X. X, residual, total and Y have one type, fp32, bf16 or fp16;
+ * weight is 1 x n_cols of that type or fp32, NULL: ones. Squares are summed in fp32:
+ * rows with values beyond 1e18 overflow there, and are zeros.
+ * Errors: INVALID_VALUE, UNSUPPORTED (2^31 - 1 rows or more, columns above 2^31 -
+ * 1025), HIP. */
+gmagnus_status_t gmagnus_rms_norm(const gmagnus_dense_t *X, const gmagnus_dense_t *residual,
+                                  const gmagnus_dense_t *weight, double eps, const gmagnus_dense_t *total,
+                                  const gmagnus_dense_t *Y, const gmagnus_dense_t *Q, const gmagnus_dense_t *scale,
+                                  void *hip_stream);
+
+/* Device bytes gmagnus_rms_norm_backward needs as workspace (host-only; 0 for sizes it refuses). */
+int64_t gmagnus_rms_norm_backward_workspace_bytes(int64_t n_rows, int64_t n_cols);
+
+/* Gradients of gmagnus_rms_norm from TOTAL (X without a residual) and Y's gradient D_Y:
+ * D_X, which is X's and the residual's alike, with TOTAL's own gradient D_TOTAL added
+ * (NULL: none), and d_weight (fp32, n_cols; NULL where it is not wanted), summed over
+ * the rows in an order that is the same in every run. The workspace is the call's
+ * until it has run. Errors as gmagnus_rms_norm. */
+gmagnus_status_t gmagnus_rms_norm_backward(const gmagnus_dense_t *TOTAL, const gmagnus_dense_t *weight, double eps,
+                                           const gmagnus_dense_t *D_Y, const gmagnus_dense_t *D_TOTAL,
+                                           const gmagnus_dense_t *D_X, float *d_weight, void *workspace,
+                                           int64_t workspace_bytes, void *hip_stream);
+
+/* Y = silu(G) * U for rows H = [G | U] of twice Y's columns, silu(g) = g / (1 + e^-g): the
+ * gate between the two products of an expert. (An infinite G gives what that formula
+ * gives in IEEE arithmetic as g * sigma(g): infinities, NaN for -inf and for 0 * inf.)
+ * Errors as gmagnus_rms_norm. */
+gmagnus_status_t gmagnus_gate(const gmagnus_dense_t *H, const gmagnus_dense_t *Y, const gmagnus_dense_t *Q,
+                              const gmagnus_dense_t *scale, void *hip_stream);
+
+/* Gradient D_H = [d_G | d_U] of gmagnus_gate from Y's gradient D_A. H, D_A and D_H have
+ * one type. Errors as gmagnus_rms_norm. */
+gmagnus_status_t gmagnus_gate_backward(const gmagnus_dense_t *H, const gmagnus_dense_t *D_A, const gmagnus_dense_t *D_H,
+                                       void *hip_stream);
+
+/* Q = X / scale rounded to int8 (-127 .. 127, ties to even), one scale for each row: its
+ * largest magnitude / 127, at least 2^-126. X is fp32, bf16 or fp16, a matrix or a stack
+ * of n_stack; Q has its shape, and scale (fp32) is n_stack x n_rows. A NaN makes its
+ * row's scale NaN, an infinity makes it infinite (and its integers 0, the row NaN).
+ * Errors as gmagnus_rms_norm. */
+gmagnus_status_t gmagnus_quantise_rows(const gmagnus_dense_t *X, int64_t n_stack, const gmagnus_dense_t *Q,
+                                       const gmagnus_dense_t *scale, void *hip_stream);
 
 /* Frees device blocks cached by the library's allocator (no plan may be alive). */
 void gmagnus_release_cache(void);

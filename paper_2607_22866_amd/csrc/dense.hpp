@@ -81,6 +81,58 @@ GM_DEV void load_f32x8(const T *p, int valid, float (&v)[8]) {
     }
 }
 
+// Eight values rounded to T, of which `valid` are there, at any alignment.
+template <typename T>
+GM_DEV void store_f32(T *p, int valid, const float (&v)[8]) {
+    if (valid >= 8) {
+        if constexpr (sizeof(T) == 4) {
+            Bytes16<4> b0, b1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                b0.v[i] = __float_as_uint(v[i]);
+                b1.v[i] = __float_as_uint(v[4 + i]);
+            }
+            reinterpret_cast<Bytes16<4> *>(p)[0] = b0;
+            reinterpret_cast<Bytes16<4> *>(p)[1] = b1;
+        } else {
+            Bytes16<2> b;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) b.v[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
+            *reinterpret_cast<Bytes16<2> *>(p) = b;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < valid) p[i] = (T)v[i];
+    }
+}
+
+// e^x for x <= 0, by the hardware's power of two: what x log2(e) loses when it is
+// rounded (|x| units of 2^-24 of the result) is multiplied in afterwards, so that a few
+// units are off at any x. (From -200 on down the result is zero, for NaN too: an
+// infinite logit, whose difference to itself that is, has a sum of zero and NaN weights.)
+GM_DEV float exp_neg(float x) {
+    constexpr float L = 0x1.715476p+0f, L_REST = 0x1.4ae0cp-26f, LN2 = 0x1.62e43p-1f;
+    const float y = __builtin_amdgcn_fmed3f(x, -200.f, 0.f), t = y * L;
+    const float rest = __builtin_fmaf(y, L_REST, __builtin_fmaf(y, L, -t));
+    const float r = __builtin_amdgcn_exp2f(t);
+    return __builtin_fmaf(r * LN2, rest, r);
+}
+
+GM_DEV uint32_t wave_max(uint32_t x) {
+#define GM_STEP(ctrl, rows) \
+    { const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false); x = x > y ? x : y; }
+    GM_STEP(0x111, 0xf) GM_STEP(0x112, 0xf) GM_STEP(0x114, 0xf) GM_STEP(0x118, 0xf) GM_STEP(0x142, 0xa) GM_STEP(0x143, 0xc)
+#undef GM_STEP
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, GM_WAVE - 1);
+}
+GM_DEV float wave_sum(float x) {
+#define GM_STEP(ctrl, rows) x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), ctrl, rows, 0xf, false));
+    GM_STEP(0x111, 0xf) GM_STEP(0x112, 0xf) GM_STEP(0x114, 0xf) GM_STEP(0x118, 0xf) GM_STEP(0x142, 0xa) GM_STEP(0x143, 0xc)
+#undef GM_STEP
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), GM_WAVE - 1));
+}
+
 GM_DEV f32x4 mfma_16x16x32(u32x4 a, u32x4 b, f32x4 c, __bf16) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
@@ -191,15 +243,29 @@ GM_DEV void band_tile(uint32_t t, uint32_t n_row, uint32_t n_col, uint32_t &row,
     col = band * BAND + (r - row * w);
 }
 
-inline int data_size(int32_t type) {
-    return type == GMAGNUS_DATA_FP32 ? 4 : type == GMAGNUS_DATA_FP8_E4M3 ? 1 : 2;
+// f(T{}) for a type of fp32, bf16 or fp16.
+template <class F>
+inline void with_float(int32_t type, F &&f) {
+    if (type == GMAGNUS_DATA_BF16)
+        f(__bf16{});
+    else if (type == GMAGNUS_DATA_FP16)
+        f(_Float16{});
+    else
+        f(float{});
 }
 
-// Common checks of a dense operand of an entry point.
-inline void check_dense(const gmagnus_dense_t *m, const char *name, int64_t n_rows, int64_t n_cols, int64_t n_stack = 1) {
+inline int data_size(int32_t type) {
+    return type == GMAGNUS_DATA_FP32 ? 4 : type == GMAGNUS_DATA_FP8_E4M3 || type == GMAGNUS_DATA_INT8 ? 1 : 2;
+}
+
+inline bool is_float(int32_t type) { return type == GMAGNUS_DATA_FP32 || type == GMAGNUS_DATA_BF16 || type == GMAGNUS_DATA_FP16; }
+
+// Common checks of a dense operand of an entry point (`last`: the last of the types it may have).
+inline void check_dense(const gmagnus_dense_t *m, const char *name, int64_t n_rows, int64_t n_cols, int64_t n_stack = 1,
+                        int32_t last = GMAGNUS_DATA_FP8_E4M3) {
     const std::string s(name);
     GM_REQUIRE(m != nullptr, GMAGNUS_ERROR_INVALID_VALUE, "NULL " + s);
-    GM_REQUIRE(m->data_type >= GMAGNUS_DATA_FP32 && m->data_type <= GMAGNUS_DATA_FP8_E4M3, GMAGNUS_ERROR_INVALID_VALUE,
+    GM_REQUIRE(m->data_type >= GMAGNUS_DATA_FP32 && m->data_type <= last, GMAGNUS_ERROR_INVALID_VALUE,
                "unknown data type of " + s);
     GM_REQUIRE(m->n_rows == n_rows && m->n_cols == n_cols, GMAGNUS_ERROR_INVALID_VALUE,
                s + " is " + std::to_string(m->n_rows) + " x " + std::to_string(m->n_cols) + ", expected " +

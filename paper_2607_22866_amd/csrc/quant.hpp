@@ -1,0 +1,73 @@
+// Values in 8 bits with a scale: E4M3 in blocks of 128, and integers by rows.
+#pragma once
+
+#include "dense.hpp"
+
+namespace gm {
+
+constexpr int SB = GMAGNUS_SCALE_BLOCK;
+constexpr float FP8_MAX = 448.f;
+constexpr float SCALE_MIN = 0x1p-126f;
+constexpr float INT8_MAX_F = 127.f;
+
+// Magnitudes compare as their bits, NaN above infinity above the rest.
+GM_DEV uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+GM_DEV float block_scale(uint32_t most) {
+    const float s = __uint_as_float(most) / FP8_MAX;
+    return s < SCALE_MIN ? SCALE_MIN : s;  // (a NaN stays)
+}
+
+GM_DEV float to_range(float x, float scale) {
+    const float v = x / scale;
+    return v > FP8_MAX ? FP8_MAX : v < -FP8_MAX ? -FP8_MAX : v;
+}
+
+GM_DEV uint32_t pack_fp8(float a, float b, float c, float d) {
+    int v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
+}
+
+// Eight bytes, of which `valid` are there, at any alignment.
+GM_DEV void store_bytes8(uint8_t *p, int valid, const uint32_t (&w)[2]) {
+    if (valid >= 8) {
+        struct Bytes8 {
+            uint32_t v[2] __attribute__((packed, aligned(1)));
+        };
+        *reinterpret_cast<Bytes8 *>(p) = Bytes8{{w[0], w[1]}};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < valid) p[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+    }
+}
+
+GM_DEV void store_fp8x8(uint8_t *p, int valid, const float (&v)[8], float scale) {
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = to_range(v[i], scale);
+    const uint32_t w[2] = {pack_fp8(r[0], r[1], r[2], r[3]), pack_fp8(r[4], r[5], r[6], r[7])};
+    store_bytes8(p, valid, w);
+}
+
+// The scale of a row of 8-bit integers.
+GM_DEV float row_scale(uint32_t most) {
+    const float s = __uint_as_float(most) / INT8_MAX_F;
+    return s < SCALE_MIN ? SCALE_MIN : s;  // (a NaN stays)
+}
+
+// x / scale to the nearest integer, ties to even, at most 127 in magnitude; a NaN as 0.
+GM_DEV uint32_t to_int8(float x, float scale) {
+    const float v = __builtin_rintf(x / scale);
+    const float c = v > INT8_MAX_F ? INT8_MAX_F : v < -INT8_MAX_F ? -INT8_MAX_F : v == v ? v : 0.f;
+    return (uint32_t)(int)c & 0xffu;
+}
+
+GM_DEV void store_int8x8(uint8_t *p, int valid, const float (&v)[8], float scale) {
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i >> 2] |= to_int8(v[i], scale) << (8 * (i & 3));
+    store_bytes8(p, valid, w);
+}
+
+}  // namespace gm

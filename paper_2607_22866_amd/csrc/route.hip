@@ -39,32 +39,6 @@ GM_DEV float key_value(uint32_t k) {
         return to_f32(__builtin_bit_cast(T, (uint16_t)(k >> 15 ? k & 0x7fffu : ~k)));
 }
 
-// e^x for x <= 0, by the hardware's power of two: what x log2(e) loses when it is
-// rounded (|x| units of 2^-24 of the result) is multiplied in afterwards, so that a few
-// units are off at any x. (From -200 on down the result is zero, for NaN too: an
-// infinite logit, whose difference to itself that is, has a sum of zero and NaN weights.)
-GM_DEV float exp_neg(float x) {
-    constexpr float L = 0x1.715476p+0f, L_REST = 0x1.4ae0cp-26f, LN2 = 0x1.62e43p-1f;
-    const float y = __builtin_amdgcn_fmed3f(x, -200.f, 0.f), t = y * L;
-    const float rest = __builtin_fmaf(y, L_REST, __builtin_fmaf(y, L, -t));
-    const float r = __builtin_amdgcn_exp2f(t);
-    return __builtin_fmaf(r * LN2, rest, r);
-}
-
-GM_DEV uint32_t wave_max(uint32_t x) {
-#define GM_STEP(ctrl, rows) \
-    { const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false); x = x > y ? x : y; }
-    GM_STEP(0x111, 0xf) GM_STEP(0x112, 0xf) GM_STEP(0x114, 0xf) GM_STEP(0x118, 0xf) GM_STEP(0x142, 0xa) GM_STEP(0x143, 0xc)
-#undef GM_STEP
-    return (uint32_t)__builtin_amdgcn_readlane((int)x, GM_WAVE - 1);
-}
-GM_DEV float wave_sum(float x) {
-#define GM_STEP(ctrl, rows) x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), ctrl, rows, 0xf, false));
-    GM_STEP(0x111, 0xf) GM_STEP(0x112, 0xf) GM_STEP(0x114, 0xf) GM_STEP(0x118, 0xf) GM_STEP(0x142, 0xa) GM_STEP(0x143, 0xc)
-#undef GM_STEP
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), GM_WAVE - 1));
-}
-
 struct RouteArgs {
     const void *logits;
     int64_t n_tokens, stride;
@@ -419,31 +393,6 @@ struct CombineArgs {
 
 constexpr int LANE_N = 8, CHUNK = LANE_N * GM_WAVE;  // columns of a lane, of a wave's step
 
-template <typename T>
-GM_DEV void store_f32(T *p, int valid, const float (&v)[LANE_N]) {
-    if (valid >= LANE_N) {
-        if constexpr (sizeof(T) == 4) {
-            Bytes16<4> b0, b1;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                b0.v[i] = __float_as_uint(v[i]);
-                b1.v[i] = __float_as_uint(v[4 + i]);
-            }
-            reinterpret_cast<Bytes16<4> *>(p)[0] = b0;
-            reinterpret_cast<Bytes16<4> *>(p)[1] = b1;
-        } else {
-            Bytes16<2> b;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) b.v[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
-            *reinterpret_cast<Bytes16<2> *>(p) = b;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < LANE_N; ++i)
-            if (i < valid) p[i] = (T)v[i];
-    }
-}
-
 GM_DEV void entry_range(const CombineArgs &a, int64_t t, int64_t &b, int64_t &f) {
     b = a.row_ptr[t];
     f = a.row_ptr[t + 1];
@@ -530,16 +479,6 @@ __global__ __launch_bounds__(256) void k_combine_backward(CombineArgs a) {
 }
 
 // ------------------------------------------------------------------ host side
-template <class F>
-void with_float(int32_t type, F &&f) {
-    if (type == GMAGNUS_DATA_BF16)
-        f(__bf16{});
-    else if (type == GMAGNUS_DATA_FP16)
-        f(_Float16{});
-    else
-        f(float{});
-}
-
 // f(T{}, V{}): the logits' type, and how many of a row's e experts a lane holds.
 template <class F>
 void with_logits(int32_t type, int64_t e, F &&f) {

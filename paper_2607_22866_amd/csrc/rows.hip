@@ -1,0 +1,753 @@
+// What a layer of experts does to whole rows around its products: the root-mean-
+// square norm with the residual's addition, the gate of a pair of columns, and
+// the rounding of rows to 8-bit integers; each result in the rows' type, in 8 bits with
+// scales, or both; and the gradients of the first two.
+//   h = x + residual (rounded to its type),  y = h w / sqrt(mean(h^2) + eps)
+//   a = silu(g) u for rows [g | u],          silu(g) = g / (1 + e^-g)
+// All of it is bound by its bytes, so a row is read once and held in registers until
+// what is needed of the whole row is known: eight columns of a piece to a lane, CH
+// pieces, by one wave or by the W waves of a work group. Rows longer than that are
+// read again for each thing to be known.
+#include "quant.hpp"
+
+namespace gm {
+namespace {
+
+enum class Op { NORM, GATE, COPY };
+enum { IN_TYPE = 0, E4M3 = 1, INTEGER = 2 };  // the 8-bit result
+
+struct RowArgs {
+    const void *x, *r, *w;  // rows (of the gate: pairs), residual, weight; the latter two may be null
+    void *total, *y;        // may be null
+    uint8_t *q;
+    float *scale;
+    int64_t n_rows, n, xs, rs, ts, ys, qs, ss;
+    int64_t stack_rows, xg, qg, sg;  // rows of each matrix of a stack, strides between those
+    float eps;
+    int format;
+    bool w32;
+};
+
+template <int ROR>
+GM_DEV uint32_t max_with_ror(uint32_t x) {
+    const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x120 + ROR, 0xf, 0xf, false);
+    return x > y ? x : y;
+}
+// The largest of 16 neighbouring lanes', in all of them.
+GM_DEV uint32_t max16(uint32_t x) { return max_with_ror<1>(max_with_ror<2>(max_with_ror<4>(max_with_ror<8>(x)))); }
+
+// Sums and maxima over the W waves of a row. Two sets of places: a set is written again
+// behind the barrier of the next one, when all have read it.
+template <int W>
+struct Join {
+    float (*part)[W];
+    int turn = 0;
+    GM_DEV float sum(float x) {
+        x = wave_sum(x);
+        if constexpr (W > 1) {
+            float *p = part[turn];
+            turn ^= 1;
+            if ((threadIdx.x & 63) == 0) p[threadIdx.x / 64] = x;
+            __syncthreads();
+            x = p[0];
+#pragma unroll
+            for (int i = 1; i < W; ++i) x += p[i];
+        }
+        return x;
+    }
+    GM_DEV uint32_t most(uint32_t x) {
+        x = wave_max(x);
+        if constexpr (W > 1) {
+            float *p = part[turn];
+            turn ^= 1;
+            if ((threadIdx.x & 63) == 0) p[threadIdx.x / 64] = __uint_as_float(x);
+            __syncthreads();
+            x = 0;
+#pragma unroll
+            for (int i = 0; i < W; ++i) x = max(x, __float_as_uint(p[i]));
+        }
+        return x;
+    }
+};
+
+GM_DEV int columns_left(int64_t n, int64_t c) { return n - c >= 8 ? 8 : n > c ? (int)(n - c) : 0; }
+
+// Eight columns, of which `valid` are there. WHOLE: all or none are, which leaves out what
+// cut pieces take (the norm of 4096 bf16 columns 102 -> 84 registers).
+template <bool WHOLE, typename T>
+GM_DEV void load(const T *p, int valid, float (&v)[8]) {
+    if constexpr (WHOLE) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.f;
+        if (valid > 0) load_f32x8(p, 8, v);
+    } else {
+        load_f32x8(p, valid, v);
+    }
+}
+template <bool WHOLE, typename T>
+GM_DEV void store(T *p, int valid, const float (&v)[8]) {
+    if constexpr (WHOLE) {
+        if (valid > 0) store_f32(p, 8, v);
+    } else {
+        store_f32(p, valid, v);
+    }
+}
+
+// Of a weight of type T, or float32 (w32); null: ones.
+template <bool WHOLE, typename T>
+GM_DEV void load_weight(const void *w, bool w32, int64_t c, int valid, float (&v)[8]) {
+    if (!w) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 1.f;
+    } else if (w32) {
+        load<WHOLE>(static_cast<const float *>(w) + c, valid, v);
+    } else {
+        load<WHOLE>(static_cast<const T *>(w) + c, valid, v);
+    }
+}
+
+// sigma(g) and 1 - sigma(g), each to a few units however small.
+GM_DEV void sigmoid(float g, float &s, float &rest) {
+    const float z = exp_neg(-fabsf(g)), big = 1.f / (1.f + z), small = z * big;
+    s = g >= 0.f ? big : small;
+    rest = g >= 0.f ? small : big;
+}
+
+// Where row number `row` of a stack lies.
+struct Place {
+    int64_t g, r;
+    GM_DEV Place(const RowArgs &a, int64_t row) {
+        g = a.stack_rows == a.n_rows ? 0 : row / a.stack_rows;
+        r = row - g * a.stack_rows;
+    }
+};
+
+// Eight columns of what comes before anything is known of the row: the gate's and
+// a copy's results, the norm's h (which goes to `total`).
+template <Op OP, bool WHOLE, typename T>
+GM_DEV void load_piece(const RowArgs &a, const T *x, int64_t row, int64_t c, int valid, bool store_total, float (&v)[8]) {
+    load<WHOLE>(x + c, valid, v);
+    if constexpr (OP == Op::GATE) {
+        float u[8];
+        load<WHOLE>(x + a.n + c, valid, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float s, rest;
+            sigmoid(v[i], s, rest);
+            v[i] = v[i] * s * u[i];
+        }
+    }
+    if constexpr (OP == Op::NORM) {
+        if (a.r) {
+            float u[8];
+            load<WHOLE>(static_cast<const T *>(a.r) + row * a.rs + c, valid, u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = to_f32((T)(v[i] + u[i]));
+            if (store_total) store<WHOLE>(static_cast<T *>(a.total) + row * a.ts + c, valid, v);
+        }
+    }
+}
+
+// Eight columns of the results; E4M3: 16 lanes hold a block of 128.
+template <bool WHOLE, typename T>
+GM_DEV void store_piece(const RowArgs &a, const Place &at, int64_t row, int64_t c, int valid, const float (&v)[8], float scale) {
+    if (a.y) store<WHOLE>(static_cast<T *>(a.y) + row * a.ys + c, valid, v);
+    uint8_t *q = a.q + at.g * a.qg + at.r * a.qs + c;
+    if (a.format == E4M3) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
+        const float s = block_scale(max16(m));
+        if (valid > 0) {
+            store_fp8x8(q, WHOLE ? 8 : valid, v, s);
+            if (threadIdx.x % 16 == 0) a.scale[row * a.ss + c / SB] = s;
+        }
+    } else if (a.format == INTEGER) {
+        if (valid > 0) store_int8x8(q, WHOLE ? 8 : valid, v, scale);
+    }
+}
+
+template <Op OP, typename T, int W, int CH, bool WHOLE>
+__global__ __launch_bounds__(W > 4 ? 64 * W : 256) void k_rows(RowArgs a) {
+    constexpr int PER = W == 1 ? 4 : 1;  // rows of a work group
+    __shared__ float part[2][W];
+    Join<W> join{part};
+    const int t = W == 1 ? threadIdx.x % 64 : threadIdx.x;
+    int valid[CH];
+    float w[OP == Op::NORM ? CH : 1][8];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int64_t c = (j * W * 64 + t) * 8;
+        valid[j] = columns_left(a.n, c);
+        if constexpr (OP == Op::NORM) load_weight<WHOLE, T>(a.w, a.w32, c, valid[j], w[j]);
+    }
+    for (int64_t row = (int64_t)blockIdx.x * PER + (W == 1 ? threadIdx.x / 64 : 0); row < a.n_rows; row += (int64_t)gridDim.x * PER) {
+        const Place at(a, row);
+        const T *x = static_cast<const T *>(a.x) + at.g * a.xg + at.r * a.xs;
+        float v[CH][8];
+#pragma unroll
+        for (int j = 0; j < CH; ++j) load_piece<OP, WHOLE>(a, x, row, (j * W * 64 + t) * 8, valid[j], true, v[j]);
+        if constexpr (OP == Op::NORM) {
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s += v[j][i] * v[j][i];
+            const float r = 1.f / sqrtf(join.sum(s) / (float)a.n + a.eps);
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[j][i] = i < valid[j] ? v[j][i] * r * w[j][i] : 0.f;
+        }
+        float scale = 0.f;
+        if (a.format == INTEGER) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[j][i]));
+            scale = row_scale(join.most(m));
+            if (t == 0) a.scale[at.g * a.sg + at.r] = scale;
+        }
+#pragma unroll
+        for (int j = 0; j < CH; ++j) store_piece<WHOLE, T>(a, at, row, (j * W * 64 + t) * 8, valid[j], v[j], scale);
+    }
+}
+
+// Rows of any length: what is to be known of a row is found in passes of their own.
+constexpr int LONG_W = 16;
+
+template <Op OP, typename T, bool WHOLE>
+__global__ __launch_bounds__(64 * LONG_W) void k_rows_long(RowArgs a) {
+    __shared__ float part[2][LONG_W];
+    Join<LONG_W> join{part};
+    constexpr int64_t STEP = 64 * LONG_W * 8;
+    for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
+        const Place at(a, row);
+        const T *x = static_cast<const T *>(a.x) + at.g * a.xg + at.r * a.xs;
+        float v[8], w[8], r = 0.f, scale = 0.f;
+        if constexpr (OP == Op::NORM) {
+            float s = 0.f;
+            for (int64_t c0 = 0; c0 < a.n; c0 += STEP) {
+                const int64_t c = c0 + threadIdx.x * 8;
+                load_piece<OP, WHOLE>(a, x, row, c, columns_left(a.n, c), true, v);
+                float p = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p += v[i] * v[i];
+                s += p;
+            }
+            r = 1.f / sqrtf(join.sum(s) / (float)a.n + a.eps);
+        }
+        auto piece = [&](int64_t c, int valid) {
+            load_piece<OP, WHOLE>(a, x, row, c, valid, false, v);
+            if constexpr (OP == Op::NORM) {
+                load_weight<WHOLE, T>(a.w, a.w32, c, valid, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = i < valid ? v[i] * r * w[i] : 0.f;
+            }
+        };
+        if (a.format == INTEGER) {
+            uint32_t m = 0;
+            for (int64_t c0 = 0; c0 < a.n; c0 += STEP) {
+                const int64_t c = c0 + threadIdx.x * 8;
+                piece(c, columns_left(a.n, c));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
+            }
+            scale = row_scale(join.most(m));
+            if (threadIdx.x == 0) a.scale[at.g * a.sg + at.r] = scale;
+        }
+        for (int64_t c0 = 0; c0 < a.n; c0 += STEP) {
+            const int64_t c = c0 + threadIdx.x * 8;
+            const int valid = columns_left(a.n, c);
+            piece(c, valid);
+            store_piece<WHOLE, T>(a, at, row, c, valid, v, scale);
+        }
+    }
+}
+
+// ------------------------------------------------------------ norm's gradients
+// With r = 1 / sqrt(mean(h^2) + eps), g = d_y w and c = mean(g h) r^2:
+//   d_h = r (g - h c) + d_total,   d_w = sum over rows of d_y h r
+// A work group takes rows in turns and holds its share of d_w in registers; the
+// shares are added in their order by a second kernel, so results do not change from
+// run to run.
+struct NormBackArgs {
+    const void *h, *w, *d_y, *d_total;
+    void *d_h;
+    float *share;    // [units][n], null: d_w is not wanted
+    float *of_row;   // long rows: r and c
+    int64_t n_rows, n, hs, ds, ts, os;
+    float eps;
+    bool w32;
+};
+
+template <typename T, int W, int CH, bool WHOLE>
+__global__ __launch_bounds__(W > 4 ? 64 * W : 256) void k_norm_backward(NormBackArgs a) {
+    constexpr int PER = W == 1 ? 4 : 1;
+    __shared__ float part[2][W];
+    __shared__ float whole[W == 1 ? CH * 512 : 1];
+    Join<W> join{part};
+    const int t = W == 1 ? threadIdx.x % 64 : threadIdx.x;
+    int valid[CH];
+    float w[CH][8], share[CH][8] = {};
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int64_t c = (j * W * 64 + t) * 8;
+        valid[j] = columns_left(a.n, c);
+        load_weight<WHOLE, T>(a.w, a.w32, c, valid[j], w[j]);
+    }
+    for (int64_t row = (int64_t)blockIdx.x * PER + (W == 1 ? threadIdx.x / 64 : 0); row < a.n_rows; row += (int64_t)gridDim.x * PER) {
+        float h[CH][8], d[CH][8], square = 0.f, dot = 0.f;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int64_t c = (j * W * 64 + t) * 8;
+            load<WHOLE>(static_cast<const T *>(a.h) + row * a.hs + c, valid[j], h[j]);
+            load<WHOLE>(static_cast<const T *>(a.d_y) + row * a.ds + c, valid[j], d[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                square += h[j][i] * h[j][i];
+                dot += d[j][i] * w[j][i] * h[j][i];
+            }
+        square = join.sum(square);
+        dot = join.sum(dot);
+        const float r = 1.f / sqrtf(square / (float)a.n + a.eps), c = r * (dot / (float)a.n) * r;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int64_t col = (j * W * 64 + t) * 8;
+            float o[8] = {};
+            if (a.d_total) load<WHOLE>(static_cast<const T *>(a.d_total) + row * a.ts + col, valid[j], o);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                share[j][i] += d[j][i] * (h[j][i] * r);
+                o[i] += r * (d[j][i] * w[j][i] - h[j][i] * c);
+            }
+            store<WHOLE>(static_cast<T *>(a.d_h) + row * a.os + col, valid[j], o);
+        }
+    }
+    if (!a.share) return;
+    if constexpr (W == 1) {  // the four waves' shares
+        for (int v = 0; v < 4; ++v) {
+            if ((int)threadIdx.x / 64 == v)
+#pragma unroll
+                for (int j = 0; j < CH; ++j)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float *p = &whole[i * (CH * 64) + j * 64 + t];
+                        *p = v ? *p + share[j][i] : share[j][i];
+                    }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < CH * 512; c += 256)
+            if (c < a.n) a.share[blockIdx.x * a.n + c] = whole[c % 8 * (CH * 64) + c / 8];
+    } else {
+#pragma unroll
+        for (int j = 0; j < CH; ++j) store<WHOLE>(a.share + blockIdx.x * a.n + (j * W * 64 + t) * 8, valid[j], share[j]);
+    }
+}
+
+// d_w from the units' shares: 64 columns a work group, a wave every 16th unit.
+__global__ __launch_bounds__(1024) void k_add_shares(const float *share, int64_t n, int units, float *out) {
+    __shared__ float part[16][64];
+    const int x = threadIdx.x % 64, w = threadIdx.x / 64;
+    for (int64_t c0 = (int64_t)blockIdx.x * 64; c0 < n; c0 += (int64_t)gridDim.x * 64) {
+        const int64_t c = c0 + x;
+        float s = 0.f;
+        if (c < n)
+#pragma unroll 8
+            for (int u = w; u < units; u += 16) s += share[u * n + c];
+        part[w][x] = s;
+        __syncthreads();
+        if (w == 0 && c < n) {
+#pragma unroll
+            for (int i = 1; i < 16; ++i) s += part[i][x];
+            out[c] = s;
+        }
+        __syncthreads();
+    }
+}
+
+// Rows of any length: r and c of each row, then the columns 512 at a time.
+template <typename T, bool WHOLE>
+__global__ __launch_bounds__(64 * LONG_W) void k_norm_backward_rows(NormBackArgs a) {
+    __shared__ float part[2][LONG_W];
+    Join<LONG_W> join{part};
+    for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
+        float square = 0.f, dot = 0.f;
+        for (int64_t c0 = 0; c0 < a.n; c0 += 64 * LONG_W * 8) {
+            const int64_t c = c0 + threadIdx.x * 8;
+            const int valid = columns_left(a.n, c);
+            float h[8], d[8], w[8], p = 0.f, q = 0.f;
+            load<WHOLE>(static_cast<const T *>(a.h) + row * a.hs + c, valid, h);
+            load<WHOLE>(static_cast<const T *>(a.d_y) + row * a.ds + c, valid, d);
+            load_weight<WHOLE, T>(a.w, a.w32, c, valid, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                p += h[i] * h[i];
+                q += d[i] * w[i] * h[i];
+            }
+            square += p;
+            dot += q;
+        }
+        square = join.sum(square);
+        dot = join.sum(dot);
+        if (threadIdx.x == 0) {
+            const float r = 1.f / sqrtf(square / (float)a.n + a.eps);
+            a.of_row[2 * row] = r;
+            a.of_row[2 * row + 1] = r * (dot / (float)a.n) * r;
+        }
+    }
+}
+
+template <typename T, bool WHOLE>
+__global__ __launch_bounds__(64) void k_norm_backward_columns(NormBackArgs a, int units) {
+    const int64_t pieces = (a.n + 511) / 512;
+    for (int64_t b = blockIdx.x; b < pieces * units; b += gridDim.x) {
+        const int64_t u = b / pieces, c = (b - u * pieces) * 512 + threadIdx.x * 8;
+        const int valid = columns_left(a.n, c);
+        float w[8], share[8] = {};
+        load_weight<WHOLE, T>(a.w, a.w32, c, valid, w);
+        for (int64_t row = u; row < a.n_rows; row += units) {
+            const float r = a.of_row[2 * row], cr = a.of_row[2 * row + 1];
+            float h[8], d[8], o[8] = {};
+            load<WHOLE>(static_cast<const T *>(a.h) + row * a.hs + c, valid, h);
+            load<WHOLE>(static_cast<const T *>(a.d_y) + row * a.ds + c, valid, d);
+            if (a.d_total) load<WHOLE>(static_cast<const T *>(a.d_total) + row * a.ts + c, valid, o);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                share[i] += d[i] * (h[i] * r);
+                o[i] += r * (d[i] * w[i] - h[i] * cr);
+            }
+            store<WHOLE>(static_cast<T *>(a.d_h) + row * a.os + c, valid, o);
+        }
+        if (a.share) store<WHOLE>(a.share + u * a.n + c, valid, share);
+    }
+}
+
+// ------------------------------------------------------------- gate's gradient
+// With s = sigma(g): d_g = d_a u s (1 + g (1 - s)), d_u = d_a g s. Eight columns a
+// lane, no row is needed as a whole.
+struct GateBackArgs {
+    const void *h, *d_a;
+    void *d_h;
+    int64_t n_rows, n, hs, ds, os;
+};
+
+template <typename T, bool WHOLE>
+__global__ __launch_bounds__(256) void k_gate_backward(GateBackArgs a) {
+    const uint32_t pieces = (uint32_t)((a.n + 7) / 8);
+    const int64_t total = a.n_rows * pieces;
+    for (int64_t b = blockIdx.x * 256ll + threadIdx.x; b < total; b += gridDim.x * 256ll) {
+        const int64_t row = total < INT32_MAX ? (uint32_t)b / pieces : b / pieces, c = (b - row * pieces) * 8;
+        const int valid = columns_left(a.n, c);
+        const T *h = static_cast<const T *>(a.h) + row * a.hs + c;
+        T *o = static_cast<T *>(a.d_h) + row * a.os + c;
+        float g[8], u[8], d[8];
+        load<WHOLE>(h, valid, g);
+        load<WHOLE>(h + a.n, valid, u);
+        load<WHOLE>(static_cast<const T *>(a.d_a) + row * a.ds + c, valid, d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float s, rest;
+            sigmoid(g[i], s, rest);
+            u[i] = d[i] * u[i] * (s * (1.f + g[i] * rest));
+            d[i] = d[i] * (g[i] * s);
+        }
+        store<WHOLE>(o, valid, u);
+        store<WHOLE>(o + a.n, valid, d);
+    }
+}
+
+// ------------------------------------------------------------------- host side
+constexpr int64_t ROWS_GRID = 2048;   // work groups of the norm: each holds the weight for its rows
+constexpr int64_t BACK_UNITS = 512;   // shares of d_w
+
+int64_t back_units(int64_t t, int64_t n) {
+    const int64_t per = n <= 1024 ? 4 : 1, units = (t + per - 1) / per;
+    return units < BACK_UNITS ? units : BACK_UNITS;
+}
+// The longest rows that registers hold; the gradients hold four things of a row for the norm's two, which 16
+// waves have no room for.
+constexpr int64_t HELD = 64 * LONG_W * 2 * 8, HELD_BACK = HELD / 2;
+
+struct BackLayout {
+    int64_t share, of_row, bytes;
+    BackLayout(int64_t t, int64_t n) {
+        share = 0;
+        of_row = (back_units(t, n) * n * 4 + 255) / 256 * 256;
+        bytes = of_row + (n > HELD_BACK ? t * 8 : 0);
+    }
+};
+
+bool back_sizes_ok(int64_t t, int64_t n) { return t >= 0 && t < INT32_MAX && n >= 1 && n <= MAX_SIDE; }
+
+// f(W{}, CH{}, WHOLE{}): waves of a row of n columns and its pieces a lane (W 0: any length), and whether its
+// pieces are whole.
+template <class F>
+void with_row(int64_t n, F &&f) {
+    auto whole = [&](auto w, auto ch) {
+        if (n % 8 == 0)
+            f(w, ch, std::true_type{});
+        else
+            f(w, ch, std::false_type{});
+    };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    using I2 = std::integral_constant<int, 2>;
+    using I4 = std::integral_constant<int, 4>;
+    using I8 = std::integral_constant<int, 8>;
+    using I16 = std::integral_constant<int, 16>;
+    if (n <= 512)
+        whole(I1{}, I1{});
+    else if (n <= 1024)
+        whole(I1{}, I2{});
+    else if (n <= 2048)
+        whole(I4{}, I1{});
+    else if (n <= 4096)
+        whole(I4{}, I2{});
+    else if (n <= 8192)
+        whole(I8{}, I2{});
+    else if (n <= HELD)
+        whole(I16{}, I2{});
+    else
+        whole(I0{}, I0{});
+}
+
+template <Op OP>
+void launch_rows(const RowArgs &a, int32_t type, hipStream_t s) {
+    with_float(type, [&](auto v) {
+        using T = decltype(v);
+        with_row(a.n, [&](auto waves, auto pieces, auto whole) {
+            constexpr int W = decltype(waves)::value, CH = decltype(pieces)::value;
+            constexpr bool WHOLE = decltype(whole)::value;
+            if constexpr (W == 0) {
+                hipLaunchKernelGGL((k_rows_long<OP, T, WHOLE>), dim3(grid_for(a.n_rows, 1, 1 << 16)), dim3(64 * LONG_W), 0, s, a);
+            } else {
+                const int64_t most = OP == Op::NORM ? ROWS_GRID : MAX_GRID;
+                hipLaunchKernelGGL((k_rows<OP, T, W, CH, WHOLE>), dim3(grid_for(a.n_rows, W == 1 ? 4 : 1, most)),
+                                   dim3(W > 4 ? 64 * W : 256), 0, s, a);
+            }
+        });
+    });
+    GM_CHECK_LAUNCH();
+}
+
+void check_rows_n(int64_t t, int64_t n, const char *name) {
+    GM_REQUIRE(t >= 0, GMAGNUS_ERROR_INVALID_VALUE, std::string("negative rows of ") + name);
+    GM_REQUIRE(t < INT32_MAX, GMAGNUS_ERROR_UNSUPPORTED, std::string("rows of ") + name + " beyond 2^31 - 2");
+    check_side(n, "columns");
+}
+
+// A result or operand of the shape and type of the rows.
+void check_like(const gmagnus_dense_t *m, const char *name, int64_t t, int64_t n, int32_t type) {
+    check_dense(m, name, t, n);
+    GM_REQUIRE(m->data_type == type, GMAGNUS_ERROR_INVALID_VALUE, std::string(name) + " has another type than the rows");
+}
+
+void check_weight(const gmagnus_dense_t *w, int64_t n, int32_t type) {
+    if (!w) return;
+    check_dense(w, "weight", 1, n);
+    GM_REQUIRE(w->data_type == type || w->data_type == GMAGNUS_DATA_FP32, GMAGNUS_ERROR_INVALID_VALUE,
+               "weight must have the type of the rows, or fp32");
+}
+
+void check_eps(double eps) {
+    GM_REQUIRE(eps >= 0 && eps <= 1e30, GMAGNUS_ERROR_INVALID_VALUE, "eps must be a number from 0 to 1e30");
+}
+
+// The results of n_stack matrices of t rows of n columns; fills their part of the kernel's arguments.
+void check_results(RowArgs &a, const gmagnus_dense_t *Y, const gmagnus_dense_t *Q, const gmagnus_dense_t *scale, int64_t t,
+                   int64_t n, int64_t n_stack, int32_t type) {
+    GM_REQUIRE(Y || Q, GMAGNUS_ERROR_INVALID_VALUE, "neither a result in the rows' type nor one in 8 bits is wanted");
+    GM_REQUIRE(!Q == !scale, GMAGNUS_ERROR_INVALID_VALUE, "an 8-bit result has its scale, and none has none");
+    a.n_rows = n_stack * t;
+    a.stack_rows = t;
+    a.n = n;
+    a.format = IN_TYPE;
+    if (Y) {
+        check_like(Y, "Y", t, n, type);
+        a.y = Y->data;
+        a.ys = Y->row_stride;
+    }
+    if (!Q) return;
+    check_dense(Q, "Q", t, n, n_stack, GMAGNUS_DATA_INT8);
+    GM_REQUIRE(Q->data_type == GMAGNUS_DATA_FP8_E4M3 || Q->data_type == GMAGNUS_DATA_INT8, GMAGNUS_ERROR_INVALID_VALUE,
+               "Q must be E4M3 or int8");
+    a.format = Q->data_type == GMAGNUS_DATA_INT8 ? INTEGER : E4M3;
+    if (a.format == INTEGER) {
+        check_dense(scale, "scale", n_stack, t);
+        a.sg = scale->row_stride;
+    } else {
+        check_dense(scale, "scale", t, (n + SB - 1) / SB);
+        a.ss = scale->row_stride;
+    }
+    GM_REQUIRE(scale->data_type == GMAGNUS_DATA_FP32, GMAGNUS_ERROR_INVALID_VALUE, "scale must be fp32");
+    GM_REQUIRE(n_stack <= 1 || t == 0 || Q->stack_stride >= (t - 1) * Q->row_stride + n, GMAGNUS_ERROR_INVALID_VALUE,
+               "matrices of Q overlap");
+    a.q = (uint8_t *)Q->data;
+    a.qs = Q->row_stride;
+    a.qg = n_stack > 1 ? Q->stack_stride : 0;
+    a.scale = (float *)scale->data;
+}
+
+}  // namespace
+}  // namespace gm
+
+using namespace gm;
+
+extern "C" gmagnus_status_t gmagnus_rms_norm(const gmagnus_dense_t *X, const gmagnus_dense_t *residual,
+                                             const gmagnus_dense_t *weight, double eps, const gmagnus_dense_t *total,
+                                             const gmagnus_dense_t *Y, const gmagnus_dense_t *Q,
+                                             const gmagnus_dense_t *scale, void *hip_stream) {
+    return guarded([&] {
+        GM_REQUIRE(X != nullptr, GMAGNUS_ERROR_INVALID_VALUE, "NULL X");
+        const int64_t t = X->n_rows, n = X->n_cols;
+        check_rows_n(t, n, "X");
+        check_dense(X, "X", t, n);
+        GM_REQUIRE(is_float(X->data_type), GMAGNUS_ERROR_INVALID_VALUE, "X must be fp32, bf16 or fp16");
+        GM_REQUIRE(!residual == !total, GMAGNUS_ERROR_INVALID_VALUE, "a residual has its total, and none has none");
+        if (residual) {
+            check_like(residual, "residual", t, n, X->data_type);
+            check_like(total, "total", t, n, X->data_type);
+        }
+        check_weight(weight, n, X->data_type);
+        check_eps(eps);
+        RowArgs a{};
+        check_results(a, Y, Q, scale, t, n, 1, X->data_type);
+        if (t == 0) return;
+        a.x = X->data;
+        a.xs = X->row_stride;
+        if (residual) {
+            a.r = residual->data;
+            a.rs = residual->row_stride;
+            a.total = total->data;
+            a.ts = total->row_stride;
+        }
+        a.w = weight ? weight->data : nullptr;
+        a.w32 = weight && weight->data_type == GMAGNUS_DATA_FP32;
+        a.eps = (float)eps;
+        launch_rows<Op::NORM>(a, X->data_type, (hipStream_t)hip_stream);
+    });
+}
+
+extern "C" gmagnus_status_t gmagnus_gate(const gmagnus_dense_t *H, const gmagnus_dense_t *Y, const gmagnus_dense_t *Q,
+                                         const gmagnus_dense_t *scale, void *hip_stream) {
+    return guarded([&] {
+        GM_REQUIRE(H != nullptr, GMAGNUS_ERROR_INVALID_VALUE, "NULL H");
+        const int64_t t = H->n_rows;
+        check_rows_n(t, H->n_cols, "H");
+        GM_REQUIRE(H->n_cols % 2 == 0, GMAGNUS_ERROR_INVALID_VALUE, "H must have an even number of columns");
+        check_dense(H, "H", t, H->n_cols);
+        GM_REQUIRE(is_float(H->data_type), GMAGNUS_ERROR_INVALID_VALUE, "H must be fp32, bf16 or fp16");
+        RowArgs a{};
+        check_results(a, Y, Q, scale, t, H->n_cols / 2, 1, H->data_type);
+        if (t == 0) return;
+        a.x = H->data;
+        a.xs = H->row_stride;
+        launch_rows<Op::GATE>(a, H->data_type, (hipStream_t)hip_stream);
+    });
+}
+
+extern "C" gmagnus_status_t gmagnus_quantise_rows(const gmagnus_dense_t *X, int64_t n_stack, const gmagnus_dense_t *Q,
+                                                  const gmagnus_dense_t *scale, void *hip_stream) {
+    return guarded([&] {
+        GM_REQUIRE(X && Q && scale, GMAGNUS_ERROR_INVALID_VALUE, "NULL X, Q or scale");
+        const int64_t t = X->n_rows, n = X->n_cols;
+        check_rows_n(t, n, "X");
+        GM_REQUIRE(n_stack >= 0, GMAGNUS_ERROR_INVALID_VALUE, "negative stack");
+        GM_REQUIRE(n_stack < INT32_MAX, GMAGNUS_ERROR_UNSUPPORTED, "stack beyond 2^31 - 2");
+        check_dense(X, "X", t, n, n_stack);
+        GM_REQUIRE(is_float(X->data_type), GMAGNUS_ERROR_INVALID_VALUE, "X must be fp32, bf16 or fp16");
+        GM_REQUIRE(Q->data_type == GMAGNUS_DATA_INT8, GMAGNUS_ERROR_INVALID_VALUE, "Q must be int8");
+        RowArgs a{};
+        check_results(a, nullptr, Q, scale, t, n, n_stack, X->data_type);
+        if (t == 0 || n_stack == 0) return;
+        a.x = X->data;
+        a.xs = X->row_stride;
+        a.xg = n_stack > 1 ? X->stack_stride : 0;
+        launch_rows<Op::COPY>(a, X->data_type, (hipStream_t)hip_stream);
+    });
+}
+
+extern "C" int64_t gmagnus_rms_norm_backward_workspace_bytes(int64_t n_rows, int64_t n_cols) {
+    return back_sizes_ok(n_rows, n_cols) ? BackLayout(n_rows, n_cols).bytes : 0;
+}
+
+extern "C" gmagnus_status_t gmagnus_rms_norm_backward(const gmagnus_dense_t *TOTAL, const gmagnus_dense_t *weight,
+                                                      double eps, const gmagnus_dense_t *D_Y,
+                                                      const gmagnus_dense_t *D_TOTAL, const gmagnus_dense_t *D_X,
+                                                      float *d_weight, void *workspace, int64_t workspace_bytes,
+                                                      void *hip_stream) {
+    return guarded([&] {
+        GM_REQUIRE(TOTAL != nullptr, GMAGNUS_ERROR_INVALID_VALUE, "NULL TOTAL");
+        const int64_t t = TOTAL->n_rows, n = TOTAL->n_cols;
+        check_rows_n(t, n, "TOTAL");
+        check_dense(TOTAL, "TOTAL", t, n);
+        GM_REQUIRE(is_float(TOTAL->data_type), GMAGNUS_ERROR_INVALID_VALUE, "TOTAL must be fp32, bf16 or fp16");
+        check_like(D_Y, "D_Y", t, n, TOTAL->data_type);
+        check_like(D_X, "D_X", t, n, TOTAL->data_type);
+        if (D_TOTAL) check_like(D_TOTAL, "D_TOTAL", t, n, TOTAL->data_type);
+        check_weight(weight, n, TOTAL->data_type);
+        check_eps(eps);
+        GM_REQUIRE((uintptr_t)d_weight % 4 == 0, GMAGNUS_ERROR_INVALID_VALUE, "d_weight is not aligned to its type");
+        hipStream_t s = (hipStream_t)hip_stream;
+        if (t == 0) {
+            if (d_weight) fill<float>(d_weight, 0.f, n, s);
+            return;
+        }
+        const BackLayout l(t, n);
+        GM_REQUIRE(workspace && workspace_bytes >= l.bytes, GMAGNUS_ERROR_INVALID_VALUE,
+                   "workspace below gmagnus_rms_norm_backward_workspace_bytes");
+        GM_REQUIRE((uintptr_t)workspace % 16 == 0, GMAGNUS_ERROR_INVALID_VALUE, "workspace is not 16-byte aligned");
+        char *ws = static_cast<char *>(workspace);
+        const int units = (int)back_units(t, n);
+        const NormBackArgs a{TOTAL->data, weight ? weight->data : nullptr, D_Y->data, D_TOTAL ? D_TOTAL->data : nullptr,
+                             D_X->data, d_weight ? (float *)(ws + l.share) : nullptr, (float *)(ws + l.of_row), t, n,
+                             TOTAL->row_stride, D_Y->row_stride, D_TOTAL ? D_TOTAL->row_stride : 0, D_X->row_stride,
+                             (float)eps, weight && weight->data_type == GMAGNUS_DATA_FP32};
+        with_float(TOTAL->data_type, [&](auto v) {
+            using T = decltype(v);
+            with_row(n, [&](auto waves, auto pieces, auto whole) {
+                constexpr int W = decltype(waves)::value, CH = decltype(pieces)::value;
+            constexpr bool WHOLE = decltype(whole)::value;
+                if constexpr (W == 0 || W == 16) {
+                    hipLaunchKernelGGL((k_norm_backward_rows<T, WHOLE>), dim3(grid_for(t, 1, 1 << 16)), dim3(64 * LONG_W), 0, s, a);
+                    hipLaunchKernelGGL((k_norm_backward_columns<T, WHOLE>), dim3(grid_for((n + 511) / 512 * units, 1, MAX_GRID)),
+                                       dim3(64), 0, s, a, units);
+                } else {
+                    hipLaunchKernelGGL((k_norm_backward<T, W, CH, WHOLE>), dim3(units), dim3(W > 4 ? 64 * W : 256), 0, s, a);
+                }
+            });
+        });
+        if (d_weight)
+            hipLaunchKernelGGL(k_add_shares, dim3(grid_for(n, 64, MAX_GRID)), dim3(1024), 0, s, a.share, n, units, d_weight);
+        GM_CHECK_LAUNCH();
+    });
+}
+
+extern "C" gmagnus_status_t gmagnus_gate_backward(const gmagnus_dense_t *H, const gmagnus_dense_t *D_A,
+                                                  const gmagnus_dense_t *D_H, void *hip_stream) {
+    return guarded([&] {
+        GM_REQUIRE(H != nullptr, GMAGNUS_ERROR_INVALID_VALUE, "NULL H");
+        const int64_t t = H->n_rows, n = H->n_cols / 2;
+        check_rows_n(t, H->n_cols, "H");
+        GM_REQUIRE(H->n_cols % 2 == 0, GMAGNUS_ERROR_INVALID_VALUE, "H must have an even number of columns");
+        check_dense(H, "H", t, 2 * n);
+        GM_REQUIRE(is_float(H->data_type), GMAGNUS_ERROR_INVALID_VALUE, "H must be fp32, bf16 or fp16");
+        check_like(D_A, "D_A", t, n, H->data_type);
+        check_like(D_H, "D_H", t, 2 * n, H->data_type);
+        if (t == 0) return;
+        const GateBackArgs a{H->data, D_A->data, D_H->data, t, n, H->row_stride, D_A->row_stride, D_H->row_stride};
+        with_float(H->data_type, [&](auto v) {
+            const dim3 grid(grid_for(t * ((n + 7) / 8), 256, MAX_GRID));
+            if (n % 8 == 0)
+                hipLaunchKernelGGL((k_gate_backward<decltype(v), true>), grid, dim3(256), 0, (hipStream_t)hip_stream, a);
+            else
+                hipLaunchKernelGGL((k_gate_backward<decltype(v), false>), grid, dim3(256), 0, (hipStream_t)hip_stream, a);
+        });
+        GM_CHECK_LAUNCH();
+    });
+}

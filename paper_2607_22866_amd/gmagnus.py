@@ -11,7 +11,7 @@ import functools
 import os
 import struct
 from dataclasses import dataclass
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -58,6 +58,7 @@ class MatrixDesc(ctypes.Structure):
 
 
 DATA_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3}
+DATA_INT8 = 4  # torch.int8, in the calls that take it
 SCALE_BLOCK = 128
 
 
@@ -136,7 +137,8 @@ EXPORTS = ["gmagnus_options_init", "gmagnus_get_params", "gmagnus_plan", "gmagnu
            "gmagnus_update_values_typed", "gmagnus_row_products_typed", "gmagnus_split_panels_typed",
            "gmagnus_route_workspace_bytes", "gmagnus_route", "gmagnus_route_backward", "gmagnus_group_product",
            "gmagnus_group_outer", "gmagnus_quantise_blocks", "gmagnus_group_product_fp8", "gmagnus_combine",
-           "gmagnus_combine_backward"]
+           "gmagnus_combine_backward", "gmagnus_rms_norm", "gmagnus_rms_norm_backward_workspace_bytes",
+           "gmagnus_rms_norm_backward", "gmagnus_gate", "gmagnus_gate_backward", "gmagnus_quantise_rows"]
 
 _lib = None
 
@@ -193,6 +195,13 @@ def load(path: str = LIB_PATH):
     lib.gmagnus_group_product_fp8.argtypes = [G, D, D, D, D, D, P]
     lib.gmagnus_combine.argtypes = [P, P, P, I64, D, D, P]
     lib.gmagnus_combine_backward.argtypes = [P, P, P, I64, D, D, D, P, P]
+    lib.gmagnus_rms_norm.argtypes = [D, D, D, ctypes.c_double, D, D, D, D, P]
+    lib.gmagnus_rms_norm_backward_workspace_bytes.argtypes = [I64, I64]
+    lib.gmagnus_rms_norm_backward_workspace_bytes.restype = ctypes.c_int64
+    lib.gmagnus_rms_norm_backward.argtypes = [D, D, ctypes.c_double, D, D, D, P, P, I64, P]
+    lib.gmagnus_gate.argtypes = [D, D, D, D, P]
+    lib.gmagnus_gate_backward.argtypes = [D, D, D, P]
+    lib.gmagnus_quantise_rows.argtypes = [D, I64, D, D, P]
     lib.gmagnus_release_cache.argtypes = []
     lib.gmagnus_release_cache.restype = None
     lib.gmagnus_last_error.restype = ctypes.c_char_p
@@ -203,7 +212,9 @@ def load(path: str = LIB_PATH):
               "gmagnus_get_params_typed", "gmagnus_plan_typed", "gmagnus_spgemm_numeric_typed",
               "gmagnus_update_values_typed", "gmagnus_row_products_typed", "gmagnus_split_panels_typed",
               "gmagnus_route", "gmagnus_route_backward", "gmagnus_group_product", "gmagnus_group_outer",
-              "gmagnus_quantise_blocks", "gmagnus_group_product_fp8", "gmagnus_combine", "gmagnus_combine_backward"):
+              "gmagnus_quantise_blocks", "gmagnus_group_product_fp8", "gmagnus_combine", "gmagnus_combine_backward",
+              "gmagnus_rms_norm", "gmagnus_rms_norm_backward", "gmagnus_gate", "gmagnus_gate_backward",
+              "gmagnus_quantise_rows"):
         getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -501,8 +512,8 @@ _pack_groups = struct.Struct("@qqPP").pack      # GroupsDesc
 _pack_routing = struct.Struct("@7P").pack       # RoutingDesc
 
 
-def _dense(t: torch.Tensor, dev: int, name: str, dims: int = 2) -> bytes:
-    """Descriptor of a matrix (dims 2) or a stack of them (dims 3) whose columns are contiguous."""
+def _dense(t: torch.Tensor, dev: int, name: str, dims: int = 2, int8: bool = False) -> bytes:
+    """Descriptor of a matrix (dims 2) or a stack of them (dims 3) whose columns are contiguous; int8: may be torch.int8."""
     if not isinstance(t, torch.Tensor) or t.get_device() != dev:
         raise ValueError("%s must be a CUDA tensor on cuda:%d" % (name, dev))
     st, shape = t.stride(), t.shape
@@ -510,7 +521,9 @@ def _dense(t: torch.Tensor, dev: int, name: str, dims: int = 2) -> bytes:
         raise ValueError("%s must have %d dimensions" % (name, dims))
     kind = DATA_TYPES.get(t.dtype)
     if kind is None:
-        raise ValueError("%s has an unsupported type %s" % (name, t.dtype))
+        if not int8 or t.dtype != torch.int8:
+            raise ValueError("%s has an unsupported type %s" % (name, t.dtype))
+        kind = DATA_INT8
     n_rows, n_cols = shape[-2], shape[-1]
     if st[-1] != 1 and n_cols > 1:
         raise ValueError("%s must have contiguous columns" % name)
@@ -779,3 +792,132 @@ def combine_backward(y: Optional[torch.Tensor], row_ptr: torch.Tensor, slot: tor
                                            _dense(d_y, dev, "d_y"),
                                            None if d_w is None else d_w.data_ptr(), _raw_stream(dev)))
     return d_y, d_w
+
+
+# ------------------------------------------------------- rows around the products
+class Rows(NamedTuple):
+    """Results of rms_norm and gate; None where one was not asked for."""
+
+    y: Optional[torch.Tensor]      # in the rows' type
+    q: Optional[torch.Tensor]      # float8_e4m3fn or int8
+    scale: Optional[torch.Tensor]  # its float32 scales: as quantise_blocks gives them, or as quantise_rows does
+    total: Optional[torch.Tensor]  # rms_norm with a residual: x + residual
+
+
+def _vector(t: torch.Tensor, dev: int, name: str, types, n: int) -> bytes:
+    """Descriptor of an array of n entries, as a matrix of one row."""
+    _check_device(t, dev, name)
+    if t.dtype not in types or tuple(t.shape) != (n,) or (t.stride(0) != 1 and n > 1):
+        raise ValueError("%s must be a contiguous array of %d entries of type %s" % (
+            name, n, " or ".join(str(v) for v in dict.fromkeys(types))))
+    return _pack_dense(t.data_ptr(), 1, n, n, 0, DATA_TYPES[t.dtype])
+
+
+def _row_results(like: torch.Tensor, n: int, quantise, plain, dev: int):
+    """The results of like's rows of n columns (y, q, scale), and their descriptors."""
+    if quantise not in (None, torch.float8_e4m3fn, torch.int8):
+        raise ValueError("quantise must be None, torch.float8_e4m3fn or torch.int8")
+    rows, device = like.shape[0], like.device
+    y = q = scale = dy = dq = ds = None
+    if plain or (plain is None and quantise is None):
+        y = torch.empty((rows, n), dtype=like.dtype, device=device)
+        dy = _dense(y, dev, "y")
+    if quantise is not None:
+        q = torch.empty((rows, n), dtype=quantise, device=device)
+        dq = _dense(q, dev, "q", int8=True)
+        if quantise is torch.int8:
+            scale = torch.empty(rows, dtype=torch.float32, device=device)
+            ds = _vector(scale, dev, "scale", (torch.float32,), rows)
+        else:
+            scale = torch.empty((rows, -(-n // SCALE_BLOCK)), dtype=torch.float32, device=device)
+            ds = _dense(scale, dev, "scale")
+    return (y, q, scale), (dy, dq, ds)
+
+
+@_on_stream
+def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+             eps: float = 1e-6, quantise=None, plain: Optional[bool] = None) -> Rows:
+    """total = x + residual and y = total * weight / sqrt(mean(total ** 2) + eps) by rows; without a residual
+    total is x. weight (None: ones) has x's type or float32. quantise: torch.float8_e4m3fn or torch.int8 asks for
+    the result in 8 bits, as group_product_fp8 and group_product_int8 take their rows; plain: whether y is
+    wanted (None: only without quantise)."""
+    dev = _device_of(x, "x")
+    d = _dense(x, dev, "x")
+    n = x.shape[1]
+    dr = dt = total = None
+    if residual is not None:
+        dr = _dense(residual, dev, "residual")
+        total = torch.empty(tuple(x.shape), dtype=x.dtype, device=x.device)
+        dt = _dense(total, dev, "total")
+    dw = None if weight is None else _vector(weight, dev, "weight", (x.dtype, torch.float32), n)
+    (y, q, scale), (dy, dq, ds) = _row_results(x, n, quantise, plain, dev)
+    _check(load().gmagnus_rms_norm(d, dr, dw, eps, dt, dy, dq, ds, _raw_stream(dev)))
+    if x.requires_grad or (weight is not None and weight.requires_grad) or (residual is not None and residual.requires_grad):
+        _no_formula("rms_norm", "its gradients are rms_norm_backward", _floating(y, q, scale, total), x, weight, residual)
+    return Rows(y, q, scale, total)
+
+
+def _floating(*tensors):
+    return [t for t in tensors if t is not None and t.dtype != torch.int8]
+
+
+@_on_stream
+def rms_norm_backward(total: torch.Tensor, weight: Optional[torch.Tensor], d_y: torch.Tensor,
+                      d_total: Optional[torch.Tensor] = None, eps: float = 1e-6):
+    """(gradient of x and of the residual alike, gradient of weight in float32, or None) of rms_norm. total: the
+    sum that the forward gave, or x without a residual; d_total: the gradient that arrives at total by itself."""
+    dev = _device_of(total, "total")
+    d = _dense(total, dev, "total")
+    n = total.shape[1]
+    dw = None if weight is None else _vector(weight, dev, "weight", (total.dtype, torch.float32), n)
+    ddy = _dense(d_y, dev, "d_y")
+    ddt = None if d_total is None else _dense(d_total, dev, "d_total")
+    d_x = torch.empty(tuple(total.shape), dtype=total.dtype, device=total.device)
+    d_weight = None if weight is None else torch.empty(n, dtype=torch.float32, device=total.device)
+    lib = load()
+    nbytes = lib.gmagnus_rms_norm_backward_workspace_bytes(total.shape[0], n)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=total.device)
+    _check(lib.gmagnus_rms_norm_backward(d, dw, eps, ddy, ddt, _dense(d_x, dev, "d_x"),
+                                         None if d_weight is None else d_weight.data_ptr(), ws.data_ptr(), nbytes,
+                                         _raw_stream(dev)))
+    return d_x, d_weight
+
+
+@_on_stream
+def gate(h: torch.Tensor, quantise=None, plain: Optional[bool] = None) -> Rows:
+    """y = silu(g) * u for rows h = [g | u]; quantise and plain as in rms_norm."""
+    dev = _device_of(h, "h")
+    d = _dense(h, dev, "h")
+    if h.shape[1] % 2:
+        raise ValueError("h must have an even number of columns")
+    (y, q, scale), (dy, dq, ds) = _row_results(h, h.shape[1] // 2, quantise, plain, dev)
+    _check(load().gmagnus_gate(d, dy, dq, ds, _raw_stream(dev)))
+    if h.requires_grad:
+        _no_formula("gate", "its gradient is gate_backward", _floating(y, q, scale), h)
+    return Rows(y, q, scale, None)
+
+
+@_on_stream
+def gate_backward(h: torch.Tensor, d_y: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of gate's h from that of its y."""
+    dev = _device_of(h, "h")
+    d, ddy = _dense(h, dev, "h"), _dense(d_y, dev, "d_y")
+    out = _out(out, tuple(h.shape), h.dtype, h, "out")
+    _check(load().gmagnus_gate_backward(d, ddy, _dense(out, dev, "out"), _raw_stream(dev)))
+    return out
+
+
+@_on_stream
+def quantise_rows(x: torch.Tensor):
+    """(q, scale): x / scale as int8 (-127 .. 127), with one float32 scale for each row. x: a matrix or a stack."""
+    dev = _device_of(x, "x")
+    dims = 3 if x.dim() == 3 else 2
+    dx = _dense(x, dev, "x", dims)
+    stack = x.shape[0] if dims == 3 else 1
+    q = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    scale = torch.empty(tuple(x.shape[:-1]), dtype=torch.float32, device=x.device)
+    ds = _dense(scale if dims == 3 else scale[None], dev, "scale")
+    _check(load().gmagnus_quantise_rows(dx, stack, _dense(q, dev, "q", dims, int8=True), ds, _raw_stream(dev)))
+    if x.requires_grad:
+        _no_formula("quantise_rows", "it rounds", (scale,), x)
+    return q, scale
