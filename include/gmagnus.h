@@ -513,6 +513,17 @@ gmagnus_status_t gmagnus_group_product_fp8(const gmagnus_groups_t *groups, const
                                            const gmagnus_dense_t *X_scale, const gmagnus_dense_t *W,
                                            const gmagnus_dense_t *W_scale, const gmagnus_dense_t *Y, void *hip_stream);
 
+/* gmagnus_group_product (W N x K) on 8-bit integers with a scale (fp32) for each row of
+ * X (X_scale: 1 x rows of X) and of W (W_scale: n_groups x N), as
+ * gmagnus_quantise_rows gives them. The products are summed as 32-bit integers,
+ * exactly (any integers from -128 to 127 may be given), and the sum, as fp32, is
+ * multiplied by X's scale, then by W's. Y is bf16, fp16 or fp32. One group is the
+ * plain matrix product.
+ * Errors as gmagnus_group_product; UNSUPPORTED also above 131071 columns of X. */
+gmagnus_status_t gmagnus_group_product_int8(const gmagnus_groups_t *groups, const gmagnus_dense_t *X,
+                                            const gmagnus_dense_t *X_scale, const gmagnus_dense_t *W,
+                                            const gmagnus_dense_t *W_scale, const gmagnus_dense_t *Y, void *hip_stream);
+
 /* OUT[t,:] = sum over the entries j of row t of weight[j] * Y[slot[j],:]
  * (weight NULL: 1). OUT has row_ptr's rows; Y and OUT have one type, fp32,
  * bf16 or fp16. n_entries is the length of slot and weight. A slot outside Y

@@ -127,22 +127,6 @@ GM_DEV int64_t x_row(const Fp8Args &a, const RowTile &t, int r) {
     return i >= a.n_x ? -1 : i;
 }
 
-// 16 bytes, those from `valid` on zero and not read.
-GM_DEV u32x4 load16(const uint8_t *p, int64_t valid) {
-    u32x4 r = {0, 0, 0, 0};
-    if (valid >= 16) {
-        const Bytes16<1> b = *reinterpret_cast<const Bytes16<1> *>(p);
-        r = u32x4{b.v[0], b.v[1], b.v[2], b.v[3]};
-    } else if (valid > 0) {
-        uint32_t e[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) e[i] = p[i < valid ? i : 0];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) r[i >> 2] |= (i < valid ? e[i] : 0u) << (8 * (i & 3));
-    }
-    return r;
-}
-
 // Any alignment: tiles of 128 x 128 staged through registers, four waves of
 // 64 x 64. LDS rows are one block of 128 bytes; chunk c of row r sits at
 // c ^ (r / 2 % 8). A lane's 32 reduction bytes are chunks g and g + 4 of its row,

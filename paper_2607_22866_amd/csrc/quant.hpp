@@ -50,6 +50,22 @@ GM_DEV void store_fp8x8(uint8_t *p, int valid, const float (&v)[8], float scale)
     store_bytes8(p, valid, w);
 }
 
+// 16 bytes, those from `valid` on zero and not read.
+GM_DEV u32x4 load16(const uint8_t *p, int64_t valid) {
+    u32x4 r = {0, 0, 0, 0};
+    if (valid >= 16) {
+        const Bytes16<1> b = *reinterpret_cast<const Bytes16<1> *>(p);
+        r = u32x4{b.v[0], b.v[1], b.v[2], b.v[3]};
+    } else if (valid > 0) {
+        uint32_t e[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) e[i] = p[i < valid ? i : 0];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) r[i >> 2] |= (i < valid ? e[i] : 0u) << (8 * (i & 3));
+    }
+    return r;
+}
+
 // The scale of a row of 8-bit integers.
 GM_DEV float row_scale(uint32_t most) {
     const float s = __uint_as_float(most) / INT8_MAX_F;

@@ -225,6 +225,114 @@ GM_DEV void store_tile(OUT *out, int64_t stride, int rows, int cols, int p0, int
     }
 }
 
+// Products of 16-bit fragments.
+template <typename T>
+struct Mul16 {
+    typedef f32x4 sums;
+    GM_DEV static f32x4 mul(u32x4 a, u32x4 b, f32x4 c) { return mfma_16x16x32(a, b, c, T{}); }
+};
+struct AsTheyAre {
+    GM_DEV AsTheyAre operator()() const { return {}; }
+    GM_DEV f32x4 operator()(int, int, f32x4 v) const { return v; }
+};
+
+// A tile by WP x WQ waves; bound by the matrix units' power and, in small groups,
+// by the weights' bytes. One group of 8192 x 8192 x 8192, bf16: 1265-1440 TFLOP/s from
+// card to card (weights n x k), 1357-1460 (k x n), gradient 1345-1465, on operands of
+// zeros, which draw less power, 1655, 1700 and 1810; 32 groups of 1024 rows, 2048 x
+// 4096, 1090-1130 (with one matrix of weights for all 1360), gradient 845-965. 256 x 256 tiles move the fewest bytes a product
+// that registers hold sums for (128 a lane). A wave's share of a step is four units of (32
+// reduction elements, half of its p rows); a unit's fragments are read from LDS
+// while the one before is multiplied. The barrier stands before a step's last
+// unit, whose fragments are in registers by then, so that the buffer can be
+// filled again and the next step's first fragments read behind it. The loads
+// into LDS are spread over two units: issued together they hold every wave up
+// at the memory pipeline while the matrix units idle.
+//
+// MUL: what two fragments of 16 bytes a lane are multiplied as (a step is 128 bytes
+// of a row, n_k and BK count pairs of them). finish(): called when the sums are whole, gives
+// what makes a lane's four results of (i, j, its sums).
+template <class MUL, typename OUT, bool PK, bool QK, bool PI, bool QI, int BP, int BQ, int WP, int WQ, class F>
+GM_DEV void tile_fast(const Dma &p, const Dma &q, int n_k, OUT *out, int64_t out_stride, char *lds, F &&finish) {
+    typedef typename MUL::sums sums;
+    constexpr int THREADS = 64 * WP * WQ, MP = BP / WP, MQ = BQ / WQ, NP = MP / 32, NQ = MQ / 16;
+    constexpr int PB = BP * BK * 2, QB = BQ * BK * 2;
+    char *lp = lds, *lq = lds + 2 * PB;
+    const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
+    const int p0 = w / WQ * MP, q0 = w % WQ * MQ;
+    Feed<PK, PI, BP, THREADS> fp;
+    Feed<QK, QI, BQ, THREADS> fq;
+    fp.init(p);
+    fq.init(q);
+    const Reader<PK, BP> rp(p0);
+    const Reader<QK, BQ> rq(q0);
+    sums acc[2][NP][NQ] = {};
+    u32x4 a0[NP], a1[NP], b0[NQ], b1[NQ];
+    const int steps = (n_k + BK - 1) / BK;
+    auto feed_p = [&](int s, int i) { fp.issue(p, lp + (s & 1) * PB, s * BK, n_k, i); };
+    auto feed_q = [&](int s, int i) { fq.issue(q, lq + (s & 1) * QB, s * BK, n_k, i); };
+    auto read_p = [&](int s, int kk, int half, int i) { return rp.get(lp + (s & 1) * PB, kk, half * NP + i); };
+    auto read_q = [&](int s, int kk, int j) { return rq.get(lq + (s & 1) * QB, kk, j); };
+    constexpr int LP = decltype(fp)::L, LQ = decltype(fq)::L;
+    // a unit's products, row by row, with a part of what else has to be issued before each
+    auto unit = [&](int half, const u32x4(&a)[NP], const u32x4(&b)[NQ], auto &&before) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            before(i);
+#pragma unroll
+            for (int j = 0; j < NQ; ++j) acc[half][i][j] = MUL::mul(b[j], a[i], acc[half][i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // f(x) for the i-th of NP parts of 0 .. n
+    auto part = [&](int n, int i, auto &&f) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+            if (x < n && x * NP / n == i) f(x);
+    };
+    wait_and_barrier();  // (the last tile's reads of LDS)
+    fp.fetch_ids(p, 0, n_k);
+    fq.fetch_ids(q, 0, n_k);
+#pragma unroll
+    for (int x = 0; x < LP; ++x) feed_p(0, x);
+#pragma unroll
+    for (int x = 0; x < LQ; ++x) feed_q(0, x);
+    fp.fetch_ids(p, BK, n_k);
+    fq.fetch_ids(q, BK, n_k);
+    wait_and_barrier();
+#pragma unroll
+    for (int x = 0; x < LP; ++x) feed_p(1, x);
+    fp.fetch_ids(p, 2 * BK, n_k);
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) b0[j] = read_q(0, 0, j);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) a0[i] = read_p(0, 0, 0, i);
+    // Steps past the last are fed as zeros and their fragments never used: one body for all steps.
+    for (int s = 0; s < steps; ++s) {
+        unit(0, a0, b0, [&](int i) {
+            a1[i] = read_p(s, 0, 1, i);
+            part(LQ, i, [&](int x) { feed_q(s + 1, x); });
+        });
+        fq.fetch_ids(q, (s + 2) * BK, n_k);
+        unit(1, a1, b0, [&](int i) {
+            a0[i] = read_p(s, 1, 0, i);
+            part(NQ, i, [&](int x) { b1[x] = read_q(s, 1, x); });
+        });
+        unit(0, a0, b1, [&](int i) { a1[i] = read_p(s, 1, 1, i); });
+        wait_and_barrier();
+        unit(1, a1, b1, [&](int i) {
+            a0[i] = read_p(s + 1, 0, 0, i);
+            part(NQ, i, [&](int x) { b0[x] = read_q(s + 1, 0, x); });
+            part(LP, i, [&](int x) { feed_p(s + 2, x); });
+        });
+        fp.fetch_ids(p, (s + 3) * BK, n_k);
+    }
+    wait_and_barrier();  // (no load may be on its way to LDS when the work group ends)
+    const auto result = finish();
+    store_tile<OUT, BP, BQ, 2 * NP, NQ, THREADS>(out, out_stride, p.valid, q.valid, p0, q0, lds,
+                                                 [&](int i, int j) { return result(i, j, acc[i / NP][i % NP][j]); });
+}
+
 // Whether an operand's rows can be brought in by 16-byte pieces, with 32-bit
 // offsets over `rows` rows.
 inline bool fast_side(const void *p, int64_t stride, int64_t stack, int64_t axis, int64_t rows, int size = 2) {

@@ -138,7 +138,8 @@ EXPORTS = ["gmagnus_options_init", "gmagnus_get_params", "gmagnus_plan", "gmagnu
            "gmagnus_route_workspace_bytes", "gmagnus_route", "gmagnus_route_backward", "gmagnus_group_product",
            "gmagnus_group_outer", "gmagnus_quantise_blocks", "gmagnus_group_product_fp8", "gmagnus_combine",
            "gmagnus_combine_backward", "gmagnus_rms_norm", "gmagnus_rms_norm_backward_workspace_bytes",
-           "gmagnus_rms_norm_backward", "gmagnus_gate", "gmagnus_gate_backward", "gmagnus_quantise_rows"]
+           "gmagnus_rms_norm_backward", "gmagnus_gate", "gmagnus_gate_backward", "gmagnus_quantise_rows",
+           "gmagnus_group_product_int8"]
 
 _lib = None
 
@@ -202,6 +203,7 @@ def load(path: str = LIB_PATH):
     lib.gmagnus_gate.argtypes = [D, D, D, D, P]
     lib.gmagnus_gate_backward.argtypes = [D, D, D, P]
     lib.gmagnus_quantise_rows.argtypes = [D, I64, D, D, P]
+    lib.gmagnus_group_product_int8.argtypes = [G, D, D, D, D, D, P]
     lib.gmagnus_release_cache.argtypes = []
     lib.gmagnus_release_cache.restype = None
     lib.gmagnus_last_error.restype = ctypes.c_char_p
@@ -214,7 +216,7 @@ def load(path: str = LIB_PATH):
               "gmagnus_route", "gmagnus_route_backward", "gmagnus_group_product", "gmagnus_group_outer",
               "gmagnus_quantise_blocks", "gmagnus_group_product_fp8", "gmagnus_combine", "gmagnus_combine_backward",
               "gmagnus_rms_norm", "gmagnus_rms_norm_backward", "gmagnus_gate", "gmagnus_gate_backward",
-              "gmagnus_quantise_rows"):
+              "gmagnus_quantise_rows", "gmagnus_group_product_int8"):
         getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -921,3 +923,24 @@ def quantise_rows(x: torch.Tensor):
     if x.requires_grad:
         _no_formula("quantise_rows", "it rounds", (scale,), x)
     return q, scale
+
+
+@_on_stream
+def group_product_int8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
+                       group_ptr: torch.Tensor, index: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
+                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """group_product of int8 operands with a scale for each row of x and of w, as quantise_rows gives them (w a stack:
+    w_scale has a row a group). Sums are exact integers. One group is the plain product."""
+    dev = _device_of(x, "x")
+    dx, dw = _dense(x, dev, "x", int8=True), _dense(w, dev, "w", 3, int8=True)
+    dxs, dws = _vector(x_scale, dev, "x_scale", (torch.float32,), x.shape[0]), _dense(w_scale, dev, "w_scale")
+    n_rows = x.shape[0] if index is None else index.numel()
+    gd = _groups(group_ptr, index, n_rows, dev)
+    if not w.shape[0] == w_scale.shape[0] == group_ptr.numel() - 1:
+        raise ValueError("w and w_scale must have one matrix a group")
+    y = _out(out, (n_rows, w.shape[1]), out_dtype, x, "out")
+    dy = _dense(y, dev, "out")
+    _check(load().gmagnus_group_product_int8(gd, dx, dxs, dw, dws, dy, _raw_stream(dev)))
+    if out is None and (x_scale.requires_grad or w_scale.requires_grad):
+        _no_formula("group_product_int8", "it is for serving", (y,), x_scale, w_scale)
+    return y
