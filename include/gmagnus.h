@@ -597,6 +597,28 @@ gmagnus_status_t gmagnus_gate_backward(const gmagnus_dense_t *H, const gmagnus_d
 gmagnus_status_t gmagnus_quantise_rows(const gmagnus_dense_t *X, int64_t n_stack, const gmagnus_dense_t *Q,
                                        const gmagnus_dense_t *scale, void *hip_stream);
 
+/* Device bytes gmagnus_expert_layer needs as workspace, for `inner` columns of W2 and
+ * n_cols of OUT (host-only; 0 for sizes it refuses). */
+int64_t gmagnus_expert_layer_workspace_bytes(int64_t n_tokens, int64_t n_experts, int64_t top_k, int64_t inner,
+                                             int64_t n_cols);
+
+/* A whole layer of gated experts for at most 64 tokens:
+ *   OUT[t,:] = sum over the entries (t, e) of R of R[t,e] * silu(X[t,:] * G_e^T) * (X[t,:] * U_e^T) * W2_e^T
+ * with R as gmagnus_route gives it from the same logits, top_k and normalise (a token
+ * without entries has a row of zeros). W1 is a stack of n_experts matrices 2 inner x K,
+ * G_e above U_e; W2 one of n_cols x inner. X is bf16 or fp16, W1 and W2 have its type
+ * or are both E4M3 with the scales that gmagnus_quantise_blocks gives with block_rows
+ * 128 (scales NULL otherwise); OUT has X's type or fp32. Sums are held in fp32, the
+ * gate's result is rounded to X's type. Of the weights only the chosen experts' are
+ * read. The workspace is the call's until it has run.
+ * Errors: INVALID_VALUE, UNSUPPORTED (more than 64 tokens, 1024 experts or 1024
+ * entries, sides above 2^31 - 1025), HIP. */
+gmagnus_status_t gmagnus_expert_layer(const gmagnus_dense_t *X, const gmagnus_dense_t *logits, int64_t top_k,
+                                      int32_t normalise, const gmagnus_dense_t *W1, const gmagnus_dense_t *W1_scale,
+                                      const gmagnus_dense_t *W2, const gmagnus_dense_t *W2_scale,
+                                      const gmagnus_dense_t *OUT, void *workspace, int64_t workspace_bytes,
+                                      void *hip_stream);
+
 /* Frees device blocks cached by the library's allocator (no plan may be alive). */
 void gmagnus_release_cache(void);
 

@@ -32,7 +32,8 @@ FLAGS = [
 ]
 
 SOURCES = ["prims.hip", "setup.hip", "expand.hip", "rowsplit.hip", "multisplit.hip", "tiles.hip", "accumulate.hip",
-           "plan.hip", "probe.hip", "static_plan.hip", "route.hip", "group.hip", "group_fp8.hip", "group_int8.hip", "rows.hip"]
+           "plan.hip", "probe.hip", "static_plan.hip", "route.hip", "group.hip", "group_fp8.hip", "group_int8.hip", "rows.hip",
+           "layer.hip"]
 
 
 def _compile(src: str) -> str:

@@ -119,6 +119,13 @@ GM_DEV float exp_neg(float x) {
     return __builtin_fmaf(r * LN2, rest, r);
 }
 
+// sigma(g) and 1 - sigma(g), each to a few units however small.
+GM_DEV void sigmoid(float g, float &s, float &rest) {
+    const float z = exp_neg(-fabsf(g)), big = 1.f / (1.f + z), small = z * big;
+    s = g >= 0.f ? big : small;
+    rest = g >= 0.f ? small : big;
+}
+
 GM_DEV uint32_t wave_max(uint32_t x) {
 #define GM_STEP(ctrl, rows) \
     { const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false); x = x > y ? x : y; }

@@ -1,0 +1,561 @@
+// A whole layer of gated experts for a few tokens, from the router's logits to the tokens' sums:
+//   out[t] = sum over the experts e of t of R[t,e] * W2_e (silu(G_e x_t) . (U_e x_t)),   W1_e = [G_e; U_e]
+// R as route gives it. The weights of the experts that are reached are read once and
+// are all there is to it, so they go straight from memory into the matrix units'
+// registers, and all else is kept small: two kernels, the products of W1 with the gate,
+// then those of W2 with the sums. Every work group of the first finds the routing by
+// itself (a few logits) and holds it in LDS; the first one leaves it to the second
+// kernel. Rows are grouped by expert, tokens ascending, as the grouped products have them.
+#include "quant.hpp"
+#include "route.hpp"
+
+namespace gm {
+namespace {
+
+constexpr int MAX_TOKENS = 64;   // one bit each in an expert's mask
+constexpr int MAX_ENTRIES = 1024;
+
+struct LayerArgs {
+    const void *x, *logits;
+    const uint8_t *w1, *w2;
+    const float *s1, *s2;  // of E4M3 weights
+    void *out;
+    int64_t xs, ls, w1s, w1g, s1s, s1g, w2s, w2g, s2s, s2g, os;  // (weights': in bytes)
+    int n_tokens, n_experts, top_k, normalise, logit_type;
+    int d, f, n;  // columns of x, of the gate's result, of out
+    int splits;
+    // workspace
+    int32_t *arrived;  // of each column tile of the second kernel, how many of its splits are there
+    int32_t *table;
+    void *act;         // [entries][act_stride]
+    float *share;      // [column tiles][splits][n_tokens][32]
+    int64_t act_stride;
+};
+
+// The routing: the experts that tokens have chosen, ascending, with their first rows, and the rows' tokens and weights.
+struct Table {
+    int32_t *n, *expert, *first, *token;
+    float *weight;
+    GM_DEV Table(int32_t *p, int entries) {
+        n = p;
+        expert = n + 1;
+        first = expert + entries;
+        token = first + entries + 1;
+        weight = reinterpret_cast<float *>(token + entries);
+    }
+};
+constexpr int table_words(int entries) { return 4 * entries + 2; }
+
+// LDS of the routing: the table and what it is made from.
+__host__ GM_DEV constexpr int route_words(int entries, int experts) { return (table_words(entries) + 1) / 2 * 2 + 2 * experts + 2 * entries + experts; }
+
+template <int V>
+GM_DEV void choose_few(const LayerArgs &a, int t, uint64_t *mask, int32_t *list_e, float *list_w) {
+    const int lane = threadIdx.x & 63;
+    float l[V], p[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int e = j * 64 + lane;
+        const int64_t at = t * a.ls + (e < a.n_experts ? e : 0);
+        l[j] = a.logit_type == GMAGNUS_DATA_FP32   ? static_cast<const float *>(a.logits)[at]
+               : a.logit_type == GMAGNUS_DATA_BF16 ? (float)static_cast<const __bf16 *>(a.logits)[at]
+                                                   : (float)static_cast<const _Float16 *>(a.logits)[at];
+    }
+    uint64_t chosen[V];
+    int n, before = t * a.top_k;
+    const float scale = choose<float, V>(l, a.n_experts, a.top_k, a.normalise, chosen, p, n);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        if (chosen[j] >> lane & 1) {
+            const int at = before + __popcll(chosen[j] & lanemask_lt());
+            list_e[at] = j * 64 + lane;
+            list_w[at] = p[j] * scale;
+            atomicOr(reinterpret_cast<unsigned long long *>(&mask[j * 64 + lane]), 1ull << t);
+        }
+        before += __popcll(chosen[j]);
+    }
+    for (int i = before + lane; i < (t + 1) * a.top_k; i += 64) list_e[i] = -1;
+}
+
+// Fills the table in LDS; all threads of a work group.
+GM_DEV void route_few(const LayerArgs &a, int32_t *lds, int waves) {
+    const int entries = a.n_tokens * a.top_k, lane = threadIdx.x & 63, w = threadIdx.x / 64;
+    const Table t(lds, entries);
+    uint64_t *mask = reinterpret_cast<uint64_t *>(lds + (table_words(entries) + 1) / 2 * 2);
+    int32_t *list_e = reinterpret_cast<int32_t *>(mask + a.n_experts);
+    float *list_w = reinterpret_cast<float *>(list_e + entries);
+    int32_t *row_of = reinterpret_cast<int32_t *>(list_w + entries);
+    for (int e = threadIdx.x; e < a.n_experts; e += 64 * waves) mask[e] = 0;
+    __syncthreads();
+    for (int i = w; i < a.n_tokens; i += waves) {
+        if (a.n_experts <= 64)
+            choose_few<1>(a, i, mask, list_e, list_w);
+        else if (a.n_experts <= 256)
+            choose_few<4>(a, i, mask, list_e, list_w);
+        else
+            choose_few<16>(a, i, mask, list_e, list_w);
+    }
+    __syncthreads();
+    if (w == 0) {
+        int used = 0, rows = 0;
+        for (int e0 = 0; e0 < a.n_experts; e0 += 64) {
+            const int e = e0 + lane, n = e < a.n_experts ? __popcll(mask[e]) : 0;
+            const uint64_t some = ballot(n > 0);
+            const int upto = wave_incl_scan<int32_t>(n);
+            if (n > 0) {
+                const int at = used + __popcll(some & lanemask_lt());
+                t.expert[at] = e;
+                t.first[at] = row_of[e] = rows + upto - n;
+            }
+            used += __popcll(some);
+            rows += __builtin_amdgcn_readlane(upto, 63);
+        }
+        if (lane == 0) {
+            t.first[used] = rows;
+            *t.n = used;
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < entries; i += 64 * waves) {
+        const int e = list_e[i], token = i / a.top_k;
+        if (e < 0) continue;
+        const int row = row_of[e] + __popcll(mask[e] & ((1ull << token) - 1));
+        t.token[row] = token;
+        t.weight[row] = list_w[i];
+    }
+    __syncthreads();
+}
+
+// ------------------------------------------------------------------- fragments
+// A block of the reduction is 128 bytes of a row of weights: 64 values of 16 bits or
+// 128 of E4M3. A lane has 16 bytes at g and 16 at g + 4 of a row's eight pieces, S
+// fragments of 8 values each. E4M3 values are widened, exactly, to the rows' type.
+template <bool FP8, typename T>
+struct Block {
+    static constexpr int S = FP8 ? 2 : 1, VALUES = FP8 ? 128 : 64, BYTES = FP8 ? 1 : 2;
+    static_assert(VALUES * BYTES == 128, "");
+
+    GM_DEV static int first(int h, int g) { return (h * 64 + g * 16) / BYTES; }
+    // 16 bytes of weights, of which `valid` values are there
+    GM_DEV static u32x4 load(const uint8_t *p, int valid) {
+        if constexpr (FP8)
+            return load16(p, valid);
+        else
+            return load8(reinterpret_cast<const T *>(p), valid);
+    }
+    GM_DEV static void widen(u32x4 v, u32x4 (&f)[S]) {
+        if constexpr (!FP8) {
+            f[0] = v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (std::is_same<T, __bf16>::value) {
+                    f[i / 2][i % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)v[i], 1.f, false));
+                    f[i / 2][i % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)v[i], 1.f, true));
+                } else {
+                    f[i / 2][i % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)v[i], 1.f, false));
+                    f[i / 2][i % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)v[i], 1.f, true));
+                }
+            }
+        }
+    }
+    // the rows' fragments of a block at p, of which `valid` values are there
+    GM_DEV static void load_rows(const T *p, int valid, int g, u32x4 (&f)[2 * S]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int s = 0; s < S; ++s) f[h * S + s] = load8(p + first(h, g) + s * 8, valid - first(h, g) - s * 8);
+    }
+    // acc += weights' fragments times the rows', by `scale` where there is one
+    GM_DEV static void multiply(const u32x4 (&w)[2], const u32x4 (&r)[2 * S], f32x4 scale, f32x4 &acc) {
+        if constexpr (!FP8) {
+            acc = mfma_16x16x32(w[1], r[1], mfma_16x16x32(w[0], r[0], acc, T{}), T{});
+        } else {
+            f32x4 sum = {0, 0, 0, 0};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32x4 f[2];
+                widen(w[h], f);
+                sum = mfma_16x16x32(f[1], r[2 * h + 1], mfma_16x16x32(f[0], r[2 * h], sum, T{}), T{});
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] += scale[e] * sum[e];
+        }
+    }
+};
+
+constexpr int LAYER_U = 4;   // blocks whose loads are in flight in a wave
+constexpr int WAVES = 4;
+constexpr int PITCH = 32 + 4;  // of 32 fp32 results in LDS
+
+// ---------------------------------------------------------------- W1 and gate
+// A work group takes 16 columns of an expert's gate, 16 rows of G_e and 16 of U_e; its
+// waves take turns at the blocks of a row, and their sums are joined in LDS in the
+// waves' order. RT: 16 rows each that an expert may have.
+template <bool FP8, typename T, int RT>
+__global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
+    using B = Block<FP8, T>;
+    extern __shared__ int32_t lds_layer[];
+    const int entries = a.n_tokens * a.top_k;
+    const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16;
+    const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
+    float *part = reinterpret_cast<float *>(lds_layer + (route_words(entries, a.n_experts) + 3) / 4 * 4);
+    route_few(a, lds_layer, WAVES);
+    const Table t(lds_layer, entries);
+    const int tiles = (a.f + 15) / 16, n_used = __builtin_amdgcn_readfirstlane(*t.n);
+    if (blockIdx.x == 0) {  // what the second kernel begins with
+        for (int i = threadIdx.x; i < table_words(entries); i += 64 * WAVES) a.table[i] = lds_layer[i];
+        for (int i = threadIdx.x; i < (a.n + 31) / 32; i += 64 * WAVES) a.arrived[i] = 0;
+    }
+    const int full = a.d / B::VALUES;
+    for (int64_t it = blockIdx.x; it < (int64_t)n_used * tiles; it += gridDim.x) {
+        const int u = (int)(it / tiles), f0 = (int)(it - (int64_t)u * tiles) * 16;
+        const int e = __builtin_amdgcn_readfirstlane(t.expert[u]), base = __builtin_amdgcn_readfirstlane(t.first[u]);
+        const int rows = __builtin_amdgcn_readfirstlane(t.first[u + 1]) - base;
+        // (rows and columns that are not there read the last ones: their results are not used)
+        const int c = min(f0 + i16, a.f - 1);
+        const uint8_t *wr[2] = {a.w1 + e * a.w1g + c * a.w1s, a.w1 + e * a.w1g + ((int64_t)a.f + c) * a.w1s};
+        const T *xr[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) xr[r] = static_cast<const T *>(a.x) + t.token[base + min(16 * r + i16, rows - 1)] * a.xs;
+        // a tile of U_e's rows may lie in two blocks of scales
+        const float *sg = nullptr, *su = nullptr, *sv = nullptr;
+        bool second[4] = {};
+        if constexpr (FP8) {
+            const int64_t r0 = (int64_t)a.f + f0, last = min(r0 + 15, 2 * (int64_t)a.f - 1);
+            sg = a.s1 + e * a.s1g + f0 / SB * a.s1s;
+            su = a.s1 + e * a.s1g + r0 / SB * a.s1s;
+            sv = a.s1 + e * a.s1g + last / SB * a.s1s;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) second[i] = (r0 + 4 * g + i) / SB != r0 / SB;
+        }
+        f32x4 acc[RT][2] = {};
+        auto scales = [&](int kb, f32x4(&s)[2]) {
+            if constexpr (FP8) {
+                const float x = sg[kb], y = su[kb], z = sv[kb];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[0][i] = x;
+                    s[1][i] = second[i] ? z : y;
+                }
+            }
+        };
+        for (int k0 = w; k0 < full; k0 += WAVES * LAYER_U) {
+            u32x4 fw[LAYER_U][2][2], fx[LAYER_U][2 * B::S];
+            f32x4 s[LAYER_U][2];
+#pragma unroll
+            for (int i = 0; i < LAYER_U; ++i) {
+                const int kb = min(k0 + i * WAVES, full - 1);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) fw[i][j][h] = B::load(wr[j] + (int64_t)kb * 128 + h * 64 + g * 16, 16);
+                B::load_rows(xr[0] + kb * B::VALUES, B::VALUES, g, fx[i]);
+                scales(kb, s[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < LAYER_U; ++i)
+                if (k0 + i * WAVES < full)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) B::multiply(fw[i][j], fx[i], s[i][j], acc[0][j]);
+#pragma unroll
+            for (int r = 1; r < RT; ++r)
+                if (16 * r < rows) {
+#pragma unroll
+                    for (int i = 0; i < LAYER_U; ++i) B::load_rows(xr[r] + min(k0 + i * WAVES, full - 1) * B::VALUES, B::VALUES, g, fx[i]);
+#pragma unroll
+                    for (int i = 0; i < LAYER_U; ++i)
+                        if (k0 + i * WAVES < full)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) B::multiply(fw[i][j], fx[i], s[i][j], acc[r][j]);
+                }
+        }
+        if (full * B::VALUES < a.d && w == full % WAVES) {  // what is left of the last block
+            const int left = a.d - full * B::VALUES;
+            u32x4 fw[2][2];
+            f32x4 s[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) fw[j][h] = B::load(wr[j] + (int64_t)full * 128 + h * 64 + g * 16, left - B::first(h, g));
+            scales(full, s);
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+                if (16 * r < rows) {
+                    u32x4 fx[2 * B::S];
+                    B::load_rows(xr[r] + full * B::VALUES, left, g, fx);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) B::multiply(fw[j], fx, s[j], acc[r][j]);
+                }
+        }
+        __syncthreads();  // (the last item's sums)
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+            if (16 * r < rows)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    *reinterpret_cast<f32x4 *>(&part[((w * RT + r) * 16 + i16) * PITCH + 16 * j + 4 * g]) = acc[r][j];
+        __syncthreads();
+        for (int i = threadIdx.x; i < rows * 16; i += 64 * WAVES) {
+            const int r = i / 16, col = i % 16;
+            float x = 0.f, y = 0.f;
+#pragma unroll
+            for (int v = 0; v < WAVES; ++v) {
+                x += part[(v * RT * 16 + r) * PITCH + col];
+                y += part[(v * RT * 16 + r) * PITCH + 16 + col];
+            }
+            float s, rest;
+            sigmoid(x, s, rest);
+            // (rounded to the rows' type, as between two products)
+            if (f0 + col < a.f) static_cast<T *>(a.act)[(base + r) * a.act_stride + f0 + col] = (T)(x * s * y);
+        }
+    }
+}
+
+// ----------------------------------------------------------------- W2 and sums
+// A work group takes 32 columns of the result and every splits-th run of units; a
+// wave's unit is LAYER_U blocks of one expert's rows of W2, whose products go, times
+// the tokens' weights, into the wave's own sums in LDS. The waves' sums are added in
+// their order, and the splits' by the last of them to arrive, in theirs.
+template <bool FP8, typename T, typename OUT>
+__global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
+    using B = Block<FP8, T>;
+    extern __shared__ int32_t lds_layer[];
+    const int entries = a.n_tokens * a.top_k;
+    const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16;
+    const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
+    const int tile = blockIdx.x / a.splits, split = blockIdx.x - tile * a.splits, q0 = tile * 32;
+    float *sums = reinterpret_cast<float *>(lds_layer + (table_words(entries) + 4) / 4 * 4), *mine = sums + w * a.n_tokens * PITCH;
+    for (int i = threadIdx.x; i < table_words(entries); i += 64 * WAVES) lds_layer[i] = a.table[i];
+    for (int i = threadIdx.x; i < WAVES * a.n_tokens * PITCH; i += 64 * WAVES) sums[i] = 0.f;
+    __syncthreads();
+    const Table t(lds_layer, entries);
+    const int n_used = __builtin_amdgcn_readfirstlane(*t.n);
+    constexpr int CHUNK = LAYER_U * B::VALUES;
+    const int per = (a.f + CHUNK - 1) / CHUNK;
+    for (int unit = split * WAVES + w; unit < n_used * per; unit += a.splits * WAVES) {
+        const int u = unit / per, k0 = (unit - u * per) * CHUNK;
+        const int e = __builtin_amdgcn_readfirstlane(t.expert[u]), base = __builtin_amdgcn_readfirstlane(t.first[u]);
+        const int rows = __builtin_amdgcn_readfirstlane(t.first[u + 1]) - base;
+        const uint8_t *wr[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) wr[j] = a.w2 + e * a.w2g + min(q0 + 16 * j + i16, a.n - 1) * a.w2s + k0 * B::BYTES;
+        const float *sc = FP8 ? a.s2 + e * a.s2g + q0 / SB * a.s2s + k0 / B::VALUES : nullptr;
+        auto row_at = [&](int r) { return static_cast<const T *>(a.act) + (base + min(r + i16, rows - 1)) * a.act_stride + k0; };
+        auto scale = [&](int i) {
+            const float s = FP8 ? sc[i] : 1.f;
+            return f32x4{s, s, s, s};
+        };
+        auto add = [&](int r, const f32x4(&acc)[2]) {
+            if (r + i16 < rows) {
+                const int token = t.token[base + r + i16];
+                const float weight = t.weight[base + r + i16];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    f32x4 *p = reinterpret_cast<f32x4 *>(&mine[token * PITCH + 16 * j + 4 * g]);
+                    f32x4 v = *p;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] += weight * acc[j][i];
+                    *p = v;
+                }
+            }
+        };
+        const int left = a.f - k0;
+        if (left >= CHUNK) {
+            u32x4 fw[LAYER_U][2][2], fr[LAYER_U][2 * B::S];
+            f32x4 s[LAYER_U];
+            const T *row = row_at(0);
+#pragma unroll
+            for (int i = 0; i < LAYER_U; ++i) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) fw[i][j][h] = B::load(wr[j] + i * 128 + h * 64 + g * 16, 16);
+                B::load_rows(row + i * B::VALUES, B::VALUES, g, fr[i]);
+                s[i] = scale(i);
+            }
+            for (int r = 0;;) {
+                f32x4 acc[2] = {};
+#pragma unroll
+                for (int i = 0; i < LAYER_U; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) B::multiply(fw[i][j], fr[i], s[i], acc[j]);
+                add(r, acc);
+                r += 16;
+                if (r >= rows) break;
+                row = row_at(r);
+#pragma unroll
+                for (int i = 0; i < LAYER_U; ++i) B::load_rows(row + i * B::VALUES, B::VALUES, g, fr[i]);
+            }
+        } else {
+            for (int r = 0; r < rows; r += 16) {
+                f32x4 acc[2] = {};
+                const T *row = row_at(r);
+                for (int i = 0; i * B::VALUES < left; ++i) {
+                    const int there = left - i * B::VALUES;
+                    u32x4 fw[2][2], fr[2 * B::S];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) fw[j][h] = B::load(wr[j] + i * 128 + h * 64 + g * 16, there - B::first(h, g));
+                    B::load_rows(row + i * B::VALUES, there, g, fr);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) B::multiply(fw[j], fr, scale(i), acc[j]);
+                }
+                add(r, acc);
+            }
+        }
+    }
+    __syncthreads();
+    const int cols = a.n - q0;
+    auto joined = [&](int i) {
+        const int at = i / 8 * PITCH + i % 8 * 4;
+        f32x4 v = *reinterpret_cast<const f32x4 *>(&sums[at]);
+#pragma unroll
+        for (int x = 1; x < WAVES; ++x) v += *reinterpret_cast<const f32x4 *>(&sums[x * a.n_tokens * PITCH + at]);
+        return v;
+    };
+    auto result = [&](int i, f32x4 v) { store4(static_cast<OUT *>(a.out) + i / 8 * a.os + q0 + i % 8 * 4, v, cols - i % 8 * 4); };
+    if (a.splits == 1) {
+        for (int i = threadIdx.x; i < a.n_tokens * 8; i += 64 * WAVES) result(i, joined(i));
+        return;
+    }
+    f32x4 *share = reinterpret_cast<f32x4 *>(a.share) + (int64_t)tile * a.splits * a.n_tokens * 8;
+    for (int i = threadIdx.x; i < a.n_tokens * 8; i += 64 * WAVES) share[split * a.n_tokens * 8 + i] = joined(i);
+    __shared__ int arrived;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(&a.arrived[tile], 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (arrived != a.splits - 1) return;
+    __threadfence();
+    for (int i = threadIdx.x; i < a.n_tokens * 8; i += 64 * WAVES) {
+        f32x4 v = share[i];
+        for (int s = 1; s < a.splits; ++s) v += share[s * a.n_tokens * 8 + i];
+        result(i, v);
+    }
+}
+
+// ------------------------------------------------------------------- host side
+struct LayerLayout {
+    int64_t arrived, table, act, share, bytes, act_stride;
+    int splits;
+    LayerLayout(int64_t t, int64_t e, int64_t k, int64_t f, int64_t n) {
+        int64_t at = 0;
+        auto take = [&](int64_t bytes) {
+            const int64_t here = at;
+            at += (bytes + 255) / 256 * 256;
+            return here;
+        };
+        // enough splits for four work groups a CU, as many at most as there can be waves' units
+        const int64_t tiles = (n + 31) / 32, used = e < t * k ? e : t * k, units = used * ((f + 255) / 256);
+        int64_t s = (1024 + tiles - 1) / tiles;
+        if (s > (units + WAVES - 1) / WAVES) s = (units + WAVES - 1) / WAVES;
+        splits = (int)s;
+        act_stride = (f + 7) / 8 * 8;
+        arrived = take(tiles * 4);
+        table = take(table_words((int)(t * k)) * 4);
+        act = take(t * k * act_stride * 2);
+        share = take(s > 1 ? tiles * s * t * 32 * 4 : 0);
+        bytes = at;
+    }
+};
+
+bool layer_sizes_ok(int64_t t, int64_t e, int64_t k, int64_t f, int64_t n) {
+    return t >= 0 && t <= MAX_TOKENS && e >= 1 && e <= MAX_EXPERTS && k >= 1 && k <= e && t * k <= MAX_ENTRIES && f >= 1 &&
+           2 * f <= MAX_SIDE && n >= 1 && n <= MAX_SIDE;
+}
+
+}  // namespace
+}  // namespace gm
+
+using namespace gm;
+
+extern "C" int64_t gmagnus_expert_layer_workspace_bytes(int64_t n_tokens, int64_t n_experts, int64_t top_k, int64_t inner,
+                                                        int64_t n_cols) {
+    return layer_sizes_ok(n_tokens, n_experts, top_k, inner, n_cols) ? LayerLayout(n_tokens, n_experts, top_k, inner, n_cols).bytes : 0;
+}
+
+extern "C" gmagnus_status_t gmagnus_expert_layer(const gmagnus_dense_t *X, const gmagnus_dense_t *logits, int64_t top_k,
+                                                 int32_t normalise, const gmagnus_dense_t *W1, const gmagnus_dense_t *W1_scale,
+                                                 const gmagnus_dense_t *W2, const gmagnus_dense_t *W2_scale,
+                                                 const gmagnus_dense_t *OUT, void *workspace, int64_t workspace_bytes,
+                                                 void *hip_stream) {
+    return guarded([&] {
+        GM_REQUIRE(X && logits && W1 && W2 && OUT, GMAGNUS_ERROR_INVALID_VALUE, "NULL X, logits, W1, W2 or OUT");
+        const int64_t t = X->n_rows, d = X->n_cols, e = logits->n_cols, f = W2->n_cols, n = OUT->n_cols;
+        GM_REQUIRE(t >= 0 && e >= 1 && top_k >= 1 && top_k <= e, GMAGNUS_ERROR_INVALID_VALUE,
+                   "top_k must lie in 1 .. number of experts");
+        GM_REQUIRE(normalise == 0 || normalise == 1, GMAGNUS_ERROR_INVALID_VALUE, "normalise must be 0 or 1");
+        check_side(d, "columns of X");
+        check_side(n, "columns of OUT");
+        check_side(f, "columns of W2");
+        check_side(2 * f, "rows of W1");
+        GM_REQUIRE(t <= MAX_TOKENS, GMAGNUS_ERROR_UNSUPPORTED, "more than 64 tokens: call the routing and the grouped products");
+        GM_REQUIRE(e <= MAX_EXPERTS && t * top_k <= MAX_ENTRIES, GMAGNUS_ERROR_UNSUPPORTED, "more than 1024 experts or entries");
+        check_dense(X, "X", t, d);
+        check_dense(logits, "logits", t, e);
+        check_dense(W1, "W1", 2 * f, d, e);
+        check_dense(W2, "W2", n, f, e);
+        check_dense(OUT, "OUT", t, n);
+        GM_REQUIRE(X->data_type == GMAGNUS_DATA_BF16 || X->data_type == GMAGNUS_DATA_FP16, GMAGNUS_ERROR_INVALID_VALUE,
+                   "X must be bf16 or fp16");
+        GM_REQUIRE(is_float(logits->data_type), GMAGNUS_ERROR_INVALID_VALUE, "logits must be fp32, bf16 or fp16");
+        GM_REQUIRE(OUT->data_type == X->data_type || OUT->data_type == GMAGNUS_DATA_FP32, GMAGNUS_ERROR_INVALID_VALUE,
+                   "OUT must have the type of X, or fp32");
+        const bool fp8 = W1->data_type == GMAGNUS_DATA_FP8_E4M3;
+        GM_REQUIRE(W1->data_type == W2->data_type && (fp8 || W1->data_type == X->data_type), GMAGNUS_ERROR_INVALID_VALUE,
+                   "W1 and W2 must both have the type of X, or both be E4M3");
+        GM_REQUIRE(!W1_scale == !fp8 && !W2_scale == !fp8, GMAGNUS_ERROR_INVALID_VALUE, "E4M3 weights have scales, others none");
+        if (fp8) {
+            check_dense(W1_scale, "W1_scale", (2 * f + SB - 1) / SB, (d + SB - 1) / SB, e);
+            check_dense(W2_scale, "W2_scale", (n + SB - 1) / SB, (f + SB - 1) / SB, e);
+            GM_REQUIRE(W1_scale->data_type == GMAGNUS_DATA_FP32 && W2_scale->data_type == GMAGNUS_DATA_FP32,
+                       GMAGNUS_ERROR_INVALID_VALUE, "scales must be fp32");
+        }
+        if (t == 0) return;
+        const LayerLayout l(t, e, top_k, f, n);
+        GM_REQUIRE(workspace && workspace_bytes >= l.bytes, GMAGNUS_ERROR_INVALID_VALUE,
+                   "workspace below gmagnus_expert_layer_workspace_bytes");
+        GM_REQUIRE((uintptr_t)workspace % 16 == 0, GMAGNUS_ERROR_INVALID_VALUE, "workspace is not 16-byte aligned");
+        const int64_t tiles = (n + 31) / 32, entries = t * top_k, used = e < entries ? e : entries;
+        GM_REQUIRE(tiles * l.splits < INT32_MAX && used * ((f + 255) / 256) < INT32_MAX / 2, GMAGNUS_ERROR_UNSUPPORTED,
+                   "2^31 tiles or 2^30 units of the reduction or more");
+        char *ws = static_cast<char *>(workspace);
+        const int size = fp8 ? 1 : 2;
+        const LayerArgs a{X->data, logits->data, (const uint8_t *)W1->data, (const uint8_t *)W2->data,
+                          fp8 ? (const float *)W1_scale->data : nullptr, fp8 ? (const float *)W2_scale->data : nullptr, OUT->data,
+                          X->row_stride, logits->row_stride, W1->row_stride * size, W1->stack_stride * size,
+                          fp8 ? W1_scale->row_stride : 0, fp8 ? W1_scale->stack_stride : 0, W2->row_stride * size,
+                          W2->stack_stride * size, fp8 ? W2_scale->row_stride : 0, fp8 ? W2_scale->stack_stride : 0,
+                          OUT->row_stride, (int)t, (int)e, (int)top_k, normalise, logits->data_type, (int)d, (int)f, (int)n,
+                          l.splits, (int32_t *)(ws + l.arrived), (int32_t *)(ws + l.table), ws + l.act, (float *)(ws + l.share),
+                          l.act_stride};
+        hipStream_t s = (hipStream_t)hip_stream;
+        const int64_t items = used * ((f + 15) / 16);
+        auto go = [&](auto kernel, int64_t grid, int words) {
+            if (words * 4 > 64 << 10) allow_dynamic_lds(reinterpret_cast<const void *>(kernel), words * 4);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * WAVES), words * 4, s, a);
+            GM_CHECK_LAUNCH();
+        };
+        const int up = (route_words((int)entries, (int)e) + 3) / 4 * 4, down = (table_words((int)entries) + 4) / 4 * 4;
+        auto both = [&](auto v, auto w) {
+            using T = decltype(v);
+            constexpr bool FP8 = decltype(w)::value;
+            const int64_t grid = items < 1024 ? items : 1024;
+            if (t <= 16)
+                go(k_layer_up<FP8, T, 1>, grid, up + WAVES * 16 * PITCH);
+            else
+                go(k_layer_up<FP8, T, 4>, grid, up + WAVES * 64 * PITCH);
+            if (OUT->data_type == GMAGNUS_DATA_FP32)
+                go(k_layer_down<FP8, T, float>, tiles * l.splits, down + WAVES * (int)t * PITCH);
+            else
+                go(k_layer_down<FP8, T, T>, tiles * l.splits, down + WAVES * (int)t * PITCH);
+        };
+        if (X->data_type == GMAGNUS_DATA_BF16) {
+            if (fp8) both(__bf16{}, std::true_type{}); else both(__bf16{}, std::false_type{});
+        } else {
+            if (fp8) both(_Float16{}, std::true_type{}); else both(_Float16{}, std::false_type{});
+        }
+    });
+}

@@ -4,40 +4,14 @@
 // its results) with theirs.
 #include <type_traits>
 
-#include "dense.hpp"
+#include "route.hpp"
 
 namespace gm {
 namespace {
 
-constexpr int MAX_EXPERTS = 1024;
 constexpr int TOK = 32;            // tokens a work group of the routing takes: one bit each in an expert's mask
 constexpr int ROUTE_T = 1024;      // its threads
 constexpr int ROUTE_W = ROUTE_T / GM_WAVE;
-
-// ---------------------------------------------------------------- selection
-// A logit as an unsigned number of the same order, in as many bits as its type
-// has (KEY_BITS); 0 for what is masked (-inf, NaN). -0 counts as +0.
-template <typename T>
-constexpr int KEY_BITS = 8 * (int)sizeof(T);
-
-template <typename T>
-GM_DEV uint32_t order_key(T v) {
-    const float x = to_f32(v);
-    if constexpr (sizeof(T) == 4) {
-        const uint32_t u = __float_as_uint(x + 0.0f);
-        return x > -INFINITY ? (u >> 31 ? ~u : u | 0x80000000u) : 0u;
-    } else {
-        const uint32_t u = x == 0.f ? 0u : __builtin_bit_cast(uint16_t, v);
-        return x > -INFINITY ? (u >> 15 ? ~u & 0xffffu : u | 0x8000u) : 0u;
-    }
-}
-template <typename T>
-GM_DEV float key_value(uint32_t k) {
-    if constexpr (sizeof(T) == 4)
-        return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k);
-    else
-        return to_f32(__builtin_bit_cast(T, (uint16_t)(k >> 15 ? k & 0x7fffu : ~k)));
-}
 
 struct RouteArgs {
     const void *logits;
@@ -56,66 +30,14 @@ struct RouteArgs {
     float *list_w;      // their weights
 };
 
-// One token by one wave: marks its bit in the chosen experts' masks (LDS) and
-// writes its list. Lane l holds experts l, l + 64, ... (V of them). The top_k-th
-// largest key is found bit by bit from the top: a bit stays if at least top_k
-// keys reach it, and once just top_k do, those are the choice (16384 tokens, 256
-// experts, top_k 8: 20 us; taking the maximum over the wave top_k times: 37).
-// Keys equal to the last one are taken from the lowest expert on.
+// One token by one wave: marks its bit in the chosen experts' masks (LDS) and writes its list.
 template <typename T, int V>
 GM_DEV int select_token(const RouteArgs &a, int64_t t, int bit, const T (&l)[V], uint32_t *mask) {
     const int lane = threadIdx.x & 63;
-    uint32_t key[V], best = 0;
     uint64_t chosen[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        key[j] = j * 64 + lane < a.n_experts ? order_key(l[j]) : 0u;
-        best = best > key[j] ? best : key[j];
-    }
-    best = wave_max(best);
-    const float top = key_value<T>(best);
-    auto reach = [&](uint32_t least) {  // keys of at least `least` (above 0)
-        int n = 0;
-#pragma unroll
-        for (int j = 0; j < V; ++j) n += __popcll(ballot(key[j] >= least));
-        return n;
-    };
-    int n = reach(1);
-    uint32_t least = 1;
-    if (n > a.top_k) {
-        least = 0;
-        for (uint32_t b = 1u << (KEY_BITS<T> - 1); b; b >>= 1) {
-            const int m = reach(least | b);
-            if (m >= a.top_k) {
-                least |= b;
-                n = m;
-                if (m == a.top_k) break;
-            }
-        }
-    }
-    // n keys reach `least`; more than top_k only where several equal it
-    int spare = n > a.top_k ? n - a.top_k : 0;
-#pragma unroll
-    for (int j = V - 1; j >= 0; --j) {
-        chosen[j] = ballot(key[j] >= least);
-        if (spare > 0) {
-            uint64_t last = ballot(key[j] == least);
-            while (spare > 0 && last) {
-                const uint64_t high = uint64_t(1) << (63 - __clzll((long long)last));
-                last ^= high;
-                chosen[j] ^= high;
-                --spare;
-            }
-        }
-    }
-    n = n < a.top_k ? n : a.top_k;
-    float p[V], sum = 0.f;
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        p[j] = key[j] ? exp_neg(key_value<T>(key[j]) - top) : 0.f;
-        if (!a.normalise || (chosen[j] >> lane & 1)) sum += p[j];
-    }
-    const float scale = 1.f / wave_sum(sum);
+    float p[V];
+    int n;
+    const float scale = choose<T, V>(l, a.n_experts, a.top_k, a.normalise, chosen, p, n);
     int before = 0;
 #pragma unroll
     for (int j = 0; j < V; ++j) {

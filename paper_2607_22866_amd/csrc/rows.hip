@@ -106,13 +106,6 @@ GM_DEV void load_weight(const void *w, bool w32, int64_t c, int valid, float (&v
     }
 }
 
-// sigma(g) and 1 - sigma(g), each to a few units however small.
-GM_DEV void sigmoid(float g, float &s, float &rest) {
-    const float z = exp_neg(-fabsf(g)), big = 1.f / (1.f + z), small = z * big;
-    s = g >= 0.f ? big : small;
-    rest = g >= 0.f ? small : big;
-}
-
 // Where row number `row` of a stack lies.
 struct Place {
     int64_t g, r;

@@ -139,7 +139,7 @@ EXPORTS = ["gmagnus_options_init", "gmagnus_get_params", "gmagnus_plan", "gmagnu
            "gmagnus_group_outer", "gmagnus_quantise_blocks", "gmagnus_group_product_fp8", "gmagnus_combine",
            "gmagnus_combine_backward", "gmagnus_rms_norm", "gmagnus_rms_norm_backward_workspace_bytes",
            "gmagnus_rms_norm_backward", "gmagnus_gate", "gmagnus_gate_backward", "gmagnus_quantise_rows",
-           "gmagnus_group_product_int8"]
+           "gmagnus_group_product_int8", "gmagnus_expert_layer_workspace_bytes", "gmagnus_expert_layer"]
 
 _lib = None
 
@@ -204,6 +204,9 @@ def load(path: str = LIB_PATH):
     lib.gmagnus_gate_backward.argtypes = [D, D, D, P]
     lib.gmagnus_quantise_rows.argtypes = [D, I64, D, D, P]
     lib.gmagnus_group_product_int8.argtypes = [G, D, D, D, D, D, P]
+    lib.gmagnus_expert_layer_workspace_bytes.argtypes = [I64, I64, I64, I64, I64]
+    lib.gmagnus_expert_layer_workspace_bytes.restype = ctypes.c_int64
+    lib.gmagnus_expert_layer.argtypes = [D, D, I64, I32, D, D, D, D, D, P, I64, P]
     lib.gmagnus_release_cache.argtypes = []
     lib.gmagnus_release_cache.restype = None
     lib.gmagnus_last_error.restype = ctypes.c_char_p
@@ -216,7 +219,7 @@ def load(path: str = LIB_PATH):
               "gmagnus_route", "gmagnus_route_backward", "gmagnus_group_product", "gmagnus_group_outer",
               "gmagnus_quantise_blocks", "gmagnus_group_product_fp8", "gmagnus_combine", "gmagnus_combine_backward",
               "gmagnus_rms_norm", "gmagnus_rms_norm_backward", "gmagnus_gate", "gmagnus_gate_backward",
-              "gmagnus_quantise_rows", "gmagnus_group_product_int8"):
+              "gmagnus_quantise_rows", "gmagnus_group_product_int8", "gmagnus_expert_layer"):
         getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -943,4 +946,34 @@ def group_product_int8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, 
     _check(load().gmagnus_group_product_int8(gd, dx, dxs, dw, dws, dy, _raw_stream(dev)))
     if out is None and (x_scale.requires_grad or w_scale.requires_grad):
         _no_formula("group_product_int8", "it is for serving", (y,), x_scale, w_scale)
+    return y
+
+
+LAYER_TOKENS = 64  # at most, in a call of expert_layer
+
+
+@_on_stream
+def expert_layer(x: torch.Tensor, logits: torch.Tensor, top_k: int, w1: torch.Tensor, w2: torch.Tensor,
+                 normalise: bool = True, w1_scale: Optional[torch.Tensor] = None, w2_scale: Optional[torch.Tensor] = None,
+                 out_dtype=None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """A whole layer of gated experts for at most LAYER_TOKENS tokens: with the entries (t, e) that route gives for the
+    logits, out[t] = sum of weight * (silu(g) * u) @ w2[e].T where [g | u] = x[t] @ w1[e].T. bfloat16 or float16; w1 and
+    w2 may both be float8_e4m3fn with the scales of quantise_blocks(w, 128). out_dtype: x's type or float32."""
+    dev = _device_of(x, "x")
+    dx, dl, d1, d2 = _dense(x, dev, "x"), _dense(logits, dev, "logits"), _dense(w1, dev, "w1", 3), _dense(w2, dev, "w2", 3)
+    s1 = None if w1_scale is None else _dense(w1_scale, dev, "w1_scale", 3)
+    s2 = None if w2_scale is None else _dense(w2_scale, dev, "w2_scale", 3)
+    t, e = logits.shape
+    if any(w is not None and w.shape[0] != e for w in (w1, w2, w1_scale, w2_scale)):
+        raise ValueError("w1, w2 and their scales must have one matrix an expert")
+    y = _out(out, (x.shape[0], w2.shape[1]), out_dtype or x.dtype, x, "out")
+    dy = _dense(y, dev, "out")
+    lib = load()
+    nbytes = lib.gmagnus_expert_layer_workspace_bytes(t, e, top_k, w2.shape[2], w2.shape[1])
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    _check(lib.gmagnus_expert_layer(dx, dl, top_k, int(normalise), d1, s1, d2, s2, dy, ws.data_ptr(), nbytes, _raw_stream(dev)))
+    if out is None:
+        inputs = [v for v in (x, logits, w1, w2, w1_scale, w2_scale) if v is not None and v.requires_grad]
+        if inputs:
+            _no_formula("expert_layer", "it is for serving", (y,), *inputs)
     return y
