@@ -5,7 +5,8 @@
 // registers, and all else is kept small: two kernels, the products of W1 with the gate,
 // then those of W2 with the sums. Every work group of the first finds the routing by
 // itself (a few logits) and holds it in LDS; the first one leaves it to the second
-// kernel. Rows are grouped by expert, tokens ascending, as the grouped products have them.
+// kernel. (Above 16 tokens that costs more than a kernel of its own for it.) Rows are
+// grouped by expert, tokens ascending, as the grouped products have them.
 #include "quant.hpp"
 #include "route.hpp"
 
@@ -126,7 +127,51 @@ GM_DEV void route_few(const LayerArgs &a, int32_t *lds, int waves) {
     __syncthreads();
 }
 
+__host__ GM_DEV constexpr int up_words(bool route, int entries, int experts) { return route ? route_words(entries, experts) : table_words(entries); }
+
+// What the second kernel begins with: the routing, and no split counted.
+GM_DEV void begin_second(const LayerArgs &a, const int32_t *table) {
+    for (int i = threadIdx.x; i < table_words(a.n_tokens * a.top_k); i += blockDim.x) a.table[i] = table[i];
+    for (int i = threadIdx.x; i < (a.n + 31) / 32; i += blockDim.x) a.arrived[i] = 0;
+}
+
+// More than 16 tokens: the routing by one work group, four tokens a wave. (In every work group of the next
+// kernel it would take up to 16 a wave.)
+constexpr int ROUTE_WAVES = 16;
+__global__ __launch_bounds__(64 * ROUTE_WAVES) void k_layer_route(LayerArgs a) {
+    extern __shared__ int32_t lds_layer[];
+    route_few(a, lds_layer, ROUTE_WAVES);
+    begin_second(a, lds_layer);
+}
+
 // ------------------------------------------------------------------- fragments
+// The 16 bytes at `at` of a row of n bytes, zeros past its end, where nothing is read: the row's last 16 bytes,
+// moved down. (Element by element they would take more registers than all else in these kernels.)
+GM_DEV u32x4 cut_piece(const uint8_t *row, int64_t at, int64_t n) {
+    u32x4 r = {0, 0, 0, 0};
+    const int64_t there = n - at;
+    if (there <= 0) return r;
+    if (n >= 16) {
+        const int move = there < 16 ? 16 - (int)there : 0;
+        const Bytes16<1> b = *reinterpret_cast<const Bytes16<1> *>(row + at - move);
+        const bool two = move & 8, one = move & 4;
+        const uint32_t c[4] = {two ? b.v[2] : b.v[0], two ? b.v[3] : b.v[1], two ? 0 : b.v[2], two ? 0 : b.v[3]};
+        const uint32_t d[5] = {one ? c[1] : c[0], one ? c[2] : c[1], one ? c[3] : c[2], one ? 0 : c[3], 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_alignbyte(d[i + 1], d[i], move & 3);
+    } else {  // (a row of less than a piece)
+        uint64_t v[2] = {0, 0};
+#pragma unroll 1
+        for (int i = 0; i < (int)there; ++i) {
+            const uint64_t x = (uint64_t)row[at + i] << (8 * (i & 7));
+            v[0] |= i < 8 ? x : 0;
+            v[1] |= i < 8 ? 0 : x;
+        }
+        r = u32x4{(uint32_t)v[0], (uint32_t)(v[0] >> 32), (uint32_t)v[1], (uint32_t)(v[1] >> 32)};
+    }
+    return r;
+}
+
 // A block of the reduction is 128 bytes of a row of weights: 64 values of 16 bits or
 // 128 of E4M3. A lane has 16 bytes at g and 16 at g + 4 of a row's eight pieces, S
 // fragments of 8 values each. E4M3 values are widened, exactly, to the rows' type.
@@ -136,12 +181,11 @@ struct Block {
     static_assert(VALUES * BYTES == 128, "");
 
     GM_DEV static int first(int h, int g) { return (h * 64 + g * 16) / BYTES; }
-    // 16 bytes of weights, of which `valid` values are there
-    GM_DEV static u32x4 load(const uint8_t *p, int valid) {
+    GM_DEV static u32x4 load(const uint8_t *p) {
         if constexpr (FP8)
-            return load16(p, valid);
+            return load16(p, 16);
         else
-            return load8(reinterpret_cast<const T *>(p), valid);
+            return load8(reinterpret_cast<const T *>(p), 8);
     }
     GM_DEV static void widen(u32x4 v, u32x4 (&f)[S]) {
         if constexpr (!FP8) {
@@ -159,12 +203,24 @@ struct Block {
             }
         }
     }
-    // the rows' fragments of a block at p, of which `valid` values are there
-    GM_DEV static void load_rows(const T *p, int valid, int g, u32x4 (&f)[2 * S]) {
+    // the rows' fragments of a block at p
+    GM_DEV static void load_rows(const T *p, int g, u32x4 (&f)[2 * S]) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int s = 0; s < S; ++s) f[h * S + s] = load8(p + first(h, g) + s * 8, valid - first(h, g) - s * 8);
+            for (int s = 0; s < S; ++s) f[h * S + s] = load8(p + first(h, g) + s * 8, 8);
+    }
+    // a row of weights' and the rows' fragments of the block at value k of n, which may end inside it
+    GM_DEV static void load_cut(const uint8_t *row, int k, int n, int g, u32x4 (&f)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) f[h] = cut_piece(row, (int64_t)(k + first(h, g)) * BYTES, (int64_t)n * BYTES);
+    }
+    GM_DEV static void load_rows_cut(const T *row, int k, int n, int g, u32x4 (&f)[2 * S]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+                f[h * S + s] = cut_piece(reinterpret_cast<const uint8_t *>(row), (int64_t)(k + first(h, g) + s * 8) * 2, (int64_t)n * 2);
     }
     // acc += weights' fragments times the rows', by `scale` where there is one
     GM_DEV static void multiply(const u32x4 (&w)[2], const u32x4 (&r)[2 * S], f32x4 scale, f32x4 &acc) {
@@ -184,29 +240,33 @@ struct Block {
     }
 };
 
-constexpr int LAYER_U = 4;   // blocks whose loads are in flight in a wave
 constexpr int WAVES = 4;
 constexpr int PITCH = 32 + 4;  // of 32 fp32 results in LDS
 
 // ---------------------------------------------------------------- W1 and gate
-// A work group takes 16 columns of an expert's gate, 16 rows of G_e and 16 of U_e; its
-// waves take turns at the blocks of a row, and their sums are joined in LDS in the
-// waves' order. RT: 16 rows each that an expert may have.
-template <bool FP8, typename T, int RT>
+// An item is 16 columns of an expert's gate: 16 rows of G_e and 16 of U_e. The waves of a
+// work group take turns at the blocks of the rows, U blocks' loads in flight each, and
+// their sums are joined in LDS in the waves' order. RT: how many times 16 rows of an
+// expert are multiplied while the weights are in registers; more than those read them
+// again. ROUTE: the work group finds the routing (up to 16 tokens, four a wave).
+template <bool FP8, typename T, int RT, bool ROUTE>
 __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
     using B = Block<FP8, T>;
+    constexpr int U = RT > 1 || FP8 ? 2 : 4;
     extern __shared__ int32_t lds_layer[];
     const int entries = a.n_tokens * a.top_k;
     const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16;
     const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
-    float *part = reinterpret_cast<float *>(lds_layer + (route_words(entries, a.n_experts) + 3) / 4 * 4);
-    route_few(a, lds_layer, WAVES);
+    float *part = reinterpret_cast<float *>(lds_layer + (up_words(ROUTE, entries, a.n_experts) + 3) / 4 * 4);
+    if constexpr (ROUTE) {
+        route_few(a, lds_layer, WAVES);
+        if (blockIdx.x == 0) begin_second(a, lds_layer);
+    } else {
+        for (int i = threadIdx.x; i < table_words(entries); i += 64 * WAVES) lds_layer[i] = a.table[i];
+        __syncthreads();
+    }
     const Table t(lds_layer, entries);
     const int tiles = (a.f + 15) / 16, n_used = __builtin_amdgcn_readfirstlane(*t.n);
-    if (blockIdx.x == 0) {  // what the second kernel begins with
-        for (int i = threadIdx.x; i < table_words(entries); i += 64 * WAVES) a.table[i] = lds_layer[i];
-        for (int i = threadIdx.x; i < (a.n + 31) / 32; i += 64 * WAVES) a.arrived[i] = 0;
-    }
     const int full = a.d / B::VALUES;
     for (int64_t it = blockIdx.x; it < (int64_t)n_used * tiles; it += gridDim.x) {
         const int u = (int)(it / tiles), f0 = (int)(it - (int64_t)u * tiles) * 16;
@@ -215,9 +275,6 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
         // (rows and columns that are not there read the last ones: their results are not used)
         const int c = min(f0 + i16, a.f - 1);
         const uint8_t *wr[2] = {a.w1 + e * a.w1g + c * a.w1s, a.w1 + e * a.w1g + ((int64_t)a.f + c) * a.w1s};
-        const T *xr[RT];
-#pragma unroll
-        for (int r = 0; r < RT; ++r) xr[r] = static_cast<const T *>(a.x) + t.token[base + min(16 * r + i16, rows - 1)] * a.xs;
         // a tile of U_e's rows may lie in two blocks of scales
         const float *sg = nullptr, *su = nullptr, *sv = nullptr;
         bool second[4] = {};
@@ -229,7 +286,6 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) second[i] = (r0 + 4 * g + i) / SB != r0 / SB;
         }
-        f32x4 acc[RT][2] = {};
         auto scales = [&](int kb, f32x4(&s)[2]) {
             if constexpr (FP8) {
                 const float x = sg[kb], y = su[kb], z = sv[kb];
@@ -240,98 +296,107 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
                 }
             }
         };
-        for (int k0 = w; k0 < full; k0 += WAVES * LAYER_U) {
-            u32x4 fw[LAYER_U][2][2], fx[LAYER_U][2 * B::S];
-            f32x4 s[LAYER_U][2];
+        // (at most 16 tokens: one pass)
+        for (int r0 = 0; RT == 1 ? r0 == 0 : r0 < rows; r0 += 16 * RT) {
+            const T *xr[RT];
 #pragma unroll
-            for (int i = 0; i < LAYER_U; ++i) {
-                const int kb = min(k0 + i * WAVES, full - 1);
+            for (int r = 0; r < RT; ++r) xr[r] = static_cast<const T *>(a.x) + t.token[base + min(r0 + 16 * r + i16, rows - 1)] * a.xs;
+            f32x4 acc[RT][2] = {};
+            for (int k0 = w; k0 < full; k0 += WAVES * U) {
+                u32x4 fw[U][2][2], fx[U][2 * B::S];
+                f32x4 s[U][2];
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                for (int i = 0; i < U; ++i) {
+                    const int kb = min(k0 + i * WAVES, full - 1);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) fw[i][j][h] = B::load(wr[j] + (int64_t)kb * 128 + h * 64 + g * 16, 16);
-                B::load_rows(xr[0] + kb * B::VALUES, B::VALUES, g, fx[i]);
-                scales(kb, s[i]);
-            }
+                    for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int i = 0; i < LAYER_U; ++i)
-                if (k0 + i * WAVES < full)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) B::multiply(fw[i][j], fx[i], s[i][j], acc[0][j]);
-#pragma unroll
-            for (int r = 1; r < RT; ++r)
-                if (16 * r < rows) {
-#pragma unroll
-                    for (int i = 0; i < LAYER_U; ++i) B::load_rows(xr[r] + min(k0 + i * WAVES, full - 1) * B::VALUES, B::VALUES, g, fx[i]);
-#pragma unroll
-                    for (int i = 0; i < LAYER_U; ++i)
-                        if (k0 + i * WAVES < full)
-#pragma unroll
-                            for (int j = 0; j < 2; ++j) B::multiply(fw[i][j], fx[i], s[i][j], acc[r][j]);
+                        for (int h = 0; h < 2; ++h) fw[i][j][h] = B::load(wr[j] + (int64_t)kb * 128 + h * 64 + g * 16);
+                    B::load_rows(xr[0] + kb * B::VALUES, g, fx[i]);
+                    scales(kb, s[i]);
                 }
-        }
-        if (full * B::VALUES < a.d && w == full % WAVES) {  // what is left of the last block
-            const int left = a.d - full * B::VALUES;
-            u32x4 fw[2][2];
-            f32x4 s[2];
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+                for (int i = 0; i < U; ++i)
+                    if (k0 + i * WAVES < full)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) fw[j][h] = B::load(wr[j] + (int64_t)full * 128 + h * 64 + g * 16, left - B::first(h, g));
-            scales(full, s);
+                        for (int j = 0; j < 2; ++j) B::multiply(fw[i][j], fx[i], s[i][j], acc[0][j]);
+#pragma unroll
+                for (int r = 1; r < RT; ++r)
+                    if (r0 + 16 * r < rows) {
+#pragma unroll
+                        for (int i = 0; i < U; ++i) B::load_rows(xr[r] + min(k0 + i * WAVES, full - 1) * B::VALUES, g, fx[i]);
+#pragma unroll
+                        for (int i = 0; i < U; ++i)
+                            if (k0 + i * WAVES < full)
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) B::multiply(fw[i][j], fx[i], s[i][j], acc[r][j]);
+                    }
+            }
+            if (full * B::VALUES < a.d && w == full % WAVES) {  // what is left of the last block
+                u32x4 fw[2][2];
+                f32x4 s[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) B::load_cut(wr[j], full * B::VALUES, a.d, g, fw[j]);
+                scales(full, s);
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+                    if (r0 + 16 * r < rows) {
+                        u32x4 fx[2 * B::S];
+                        B::load_rows_cut(xr[r], full * B::VALUES, a.d, g, fx);
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) B::multiply(fw[j], fx, s[j], acc[r][j]);
+                    }
+            }
+            // (the result is rounded to the rows' type, as between two products)
+            auto gated = [](float x, float y) {
+                float s, rest;
+                sigmoid(x, s, rest);
+                return x * s * y;
+            };
+            T *out = static_cast<T *>(a.act) + (base + r0) * a.act_stride + f0;
+            __syncthreads();  // (the last item's sums)
 #pragma unroll
             for (int r = 0; r < RT; ++r)
-                if (16 * r < rows) {
-                    u32x4 fx[2 * B::S];
-                    B::load_rows(xr[r] + full * B::VALUES, left, g, fx);
+                if (r0 + 16 * r < rows)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) B::multiply(fw[j], fx, s[j], acc[r][j]);
+                    for (int j = 0; j < 2; ++j)
+                        *reinterpret_cast<f32x4 *>(&part[((w * RT + r) * 16 + i16) * PITCH + 16 * j + 4 * g]) = acc[r][j];
+            __syncthreads();
+            for (int i = threadIdx.x; i < min(rows - r0, RT * 16) * 16; i += 64 * WAVES) {
+                const int r = i / 16, col = i % 16;
+                float x = 0.f, y = 0.f;
+#pragma unroll
+                for (int v = 0; v < WAVES; ++v) {
+                    x += part[(v * RT * 16 + r) * PITCH + col];
+                    y += part[(v * RT * 16 + r) * PITCH + 16 + col];
                 }
-        }
-        __syncthreads();  // (the last item's sums)
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-            if (16 * r < rows)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    *reinterpret_cast<f32x4 *>(&part[((w * RT + r) * 16 + i16) * PITCH + 16 * j + 4 * g]) = acc[r][j];
-        __syncthreads();
-        for (int i = threadIdx.x; i < rows * 16; i += 64 * WAVES) {
-            const int r = i / 16, col = i % 16;
-            float x = 0.f, y = 0.f;
-#pragma unroll
-            for (int v = 0; v < WAVES; ++v) {
-                x += part[(v * RT * 16 + r) * PITCH + col];
-                y += part[(v * RT * 16 + r) * PITCH + 16 + col];
+                if (f0 + col < a.f) out[r * a.act_stride + col] = (T)gated(x, y);
             }
-            float s, rest;
-            sigmoid(x, s, rest);
-            // (rounded to the rows' type, as between two products)
-            if (f0 + col < a.f) static_cast<T *>(a.act)[(base + r) * a.act_stride + f0 + col] = (T)(x * s * y);
         }
     }
 }
 
 // ----------------------------------------------------------------- W2 and sums
 // A work group takes 32 columns of the result and every splits-th run of units; a
-// wave's unit is LAYER_U blocks of one expert's rows of W2, whose products go, times
+// wave's unit is U blocks of one expert's rows of W2, whose products go, times
 // the tokens' weights, into the wave's own sums in LDS. The waves' sums are added in
 // their order, and the splits' by the last of them to arrive, in theirs.
 template <bool FP8, typename T, typename OUT>
 __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
     using B = Block<FP8, T>;
+    constexpr int U = FP8 ? 1 : 2;
     extern __shared__ int32_t lds_layer[];
     const int entries = a.n_tokens * a.top_k;
     const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16;
     const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
     const int tile = blockIdx.x / a.splits, split = blockIdx.x - tile * a.splits, q0 = tile * 32;
-    float *sums = reinterpret_cast<float *>(lds_layer + (table_words(entries) + 4) / 4 * 4), *mine = sums + w * a.n_tokens * PITCH;
+    float *sums = reinterpret_cast<float *>(lds_layer + (table_words(entries) + 3) / 4 * 4), *mine = sums + w * a.n_tokens * PITCH;
     for (int i = threadIdx.x; i < table_words(entries); i += 64 * WAVES) lds_layer[i] = a.table[i];
     for (int i = threadIdx.x; i < WAVES * a.n_tokens * PITCH; i += 64 * WAVES) sums[i] = 0.f;
     __syncthreads();
     const Table t(lds_layer, entries);
     const int n_used = __builtin_amdgcn_readfirstlane(*t.n);
-    constexpr int CHUNK = LAYER_U * B::VALUES;
+    constexpr int CHUNK = U * B::VALUES;
     const int per = (a.f + CHUNK - 1) / CHUNK;
     for (int unit = split * WAVES + w; unit < n_used * per; unit += a.splits * WAVES) {
         const int u = unit / per, k0 = (unit - u * per) * CHUNK;
@@ -339,13 +404,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
         const int rows = __builtin_amdgcn_readfirstlane(t.first[u + 1]) - base;
         const uint8_t *wr[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) wr[j] = a.w2 + e * a.w2g + min(q0 + 16 * j + i16, a.n - 1) * a.w2s + k0 * B::BYTES;
-        const float *sc = FP8 ? a.s2 + e * a.s2g + q0 / SB * a.s2s + k0 / B::VALUES : nullptr;
-        auto row_at = [&](int r) { return static_cast<const T *>(a.act) + (base + min(r + i16, rows - 1)) * a.act_stride + k0; };
-        auto scale = [&](int i) {
-            const float s = FP8 ? sc[i] : 1.f;
-            return f32x4{s, s, s, s};
-        };
+        for (int j = 0; j < 2; ++j) wr[j] = a.w2 + e * a.w2g + min(q0 + 16 * j + i16, a.n - 1) * a.w2s;
+        const float *sc = FP8 ? a.s2 + e * a.s2g + q0 / SB * a.s2s : nullptr;
+        auto row_at = [&](int r) { return static_cast<const T *>(a.act) + (base + min(r + i16, rows - 1)) * a.act_stride; };
         auto add = [&](int r, const f32x4(&acc)[2]) {
             if (r + i16 < rows) {
                 const int token = t.token[base + r + i16];
@@ -360,24 +421,27 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
                 }
             }
         };
-        const int left = a.f - k0;
-        if (left >= CHUNK) {
-            u32x4 fw[LAYER_U][2][2], fr[LAYER_U][2 * B::S];
-            f32x4 s[LAYER_U];
+        auto scale = [&](int i) {
+            const float x = FP8 ? sc[k0 / B::VALUES + i] : 0.f;
+            return f32x4{x, x, x, x};
+        };
+        if (a.f - k0 >= CHUNK) {
+            u32x4 fw[U][2][2], fr[U][2 * B::S];
+            f32x4 s[U];
             const T *row = row_at(0);
 #pragma unroll
-            for (int i = 0; i < LAYER_U; ++i) {
+            for (int i = 0; i < U; ++i) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) fw[i][j][h] = B::load(wr[j] + i * 128 + h * 64 + g * 16, 16);
-                B::load_rows(row + i * B::VALUES, B::VALUES, g, fr[i]);
+                    for (int h = 0; h < 2; ++h) fw[i][j][h] = B::load(wr[j] + k0 * B::BYTES + i * 128 + h * 64 + g * 16);
+                B::load_rows(row + k0 + i * B::VALUES, g, fr[i]);
                 s[i] = scale(i);
             }
             for (int r = 0;;) {
                 f32x4 acc[2] = {};
 #pragma unroll
-                for (int i = 0; i < LAYER_U; ++i)
+                for (int i = 0; i < U; ++i)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) B::multiply(fw[i][j], fr[i], s[i], acc[j]);
                 add(r, acc);
@@ -385,20 +449,17 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
                 if (r >= rows) break;
                 row = row_at(r);
 #pragma unroll
-                for (int i = 0; i < LAYER_U; ++i) B::load_rows(row + i * B::VALUES, B::VALUES, g, fr[i]);
+                for (int i = 0; i < U; ++i) B::load_rows(row + k0 + i * B::VALUES, g, fr[i]);
             }
         } else {
             for (int r = 0; r < rows; r += 16) {
                 f32x4 acc[2] = {};
                 const T *row = row_at(r);
-                for (int i = 0; i * B::VALUES < left; ++i) {
-                    const int there = left - i * B::VALUES;
+                for (int i = 0; k0 + i * B::VALUES < a.f; ++i) {
                     u32x4 fw[2][2], fr[2 * B::S];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) fw[j][h] = B::load(wr[j] + i * 128 + h * 64 + g * 16, there - B::first(h, g));
-                    B::load_rows(row + i * B::VALUES, there, g, fr);
+                    for (int j = 0; j < 2; ++j) B::load_cut(wr[j], k0 + i * B::VALUES, a.f, g, fw[j]);
+                    B::load_rows_cut(row, k0 + i * B::VALUES, a.f, g, fr);
 #pragma unroll
                     for (int j = 0; j < 2; ++j) B::multiply(fw[j], fr, scale(i), acc[j]);
                 }
@@ -425,13 +486,16 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
     // work group (16 tokens to 4 of 64 experts of 1024 x 2048: this kernel 300 us with fences).
     // What orders them is the wait for the stores' end before the barrier and the count.
     uint64_t *share = reinterpret_cast<uint64_t *>(a.share) + (int64_t)tile * a.splits * a.n_tokens * 16;
-    for (int i = threadIdx.x; i < a.n_tokens * 8; i += 64 * WAVES) {
-        const f32x4 v = joined(i);
+    for (int i = threadIdx.x; i < a.n_tokens * 16; i += 64 * WAVES) {
+        const int at = i / 16 * PITCH + i % 16 * 2;
+        float x = sums[at], y = sums[at + 1];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            __hip_atomic_store(&share[(split * a.n_tokens * 8 + i) * 2 + h],
-                               __builtin_bit_cast(uint64_t, u32x2{__float_as_uint(v[2 * h]), __float_as_uint(v[2 * h + 1])}),
-                               __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (int v = 1; v < WAVES; ++v) {
+            x += sums[v * a.n_tokens * PITCH + at];
+            y += sums[v * a.n_tokens * PITCH + at + 1];
+        }
+        __hip_atomic_store(&share[split * a.n_tokens * 16 + i], __builtin_bit_cast(uint64_t, u32x2{__float_as_uint(x), __float_as_uint(y)}),
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __shared__ int arrived;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -439,18 +503,24 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
     if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(&a.arrived[tile], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     if (arrived != a.splits - 1) return;
-    for (int i = threadIdx.x; i < a.n_tokens * 8; i += 64 * WAVES) {
-        f32x4 v = {0, 0, 0, 0};
-#pragma unroll 4
-        for (int s = 0; s < a.splits; ++s)
+    for (int i = threadIdx.x; i < a.n_tokens * 16; i += 64 * WAVES) {
+        float x = 0.f, y = 0.f;
+        for (int s0 = 0; s0 < a.splits; s0 += 16) {  // (16 loads in flight)
+            uint64_t v[16];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const u32x2 x = __builtin_bit_cast(u32x2, __hip_atomic_load(&share[(s * a.n_tokens * 8 + i) * 2 + h], __ATOMIC_RELAXED,
-                                                                            __HIP_MEMORY_SCOPE_AGENT));
-                v[2 * h] += __uint_as_float(x[0]);
-                v[2 * h + 1] += __uint_as_float(x[1]);
-            }
-        result(i, v);
+            for (int s = 0; s < 16; ++s)
+                v[s] = __hip_atomic_load(&share[min(s0 + s, a.splits - 1) * a.n_tokens * 16 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+            for (int s = 0; s < 16; ++s)
+                if (s0 + s < a.splits) {
+                    const u32x2 p = __builtin_bit_cast(u32x2, v[s]);
+                    x += __uint_as_float(p[0]);
+                    y += __uint_as_float(p[1]);
+                }
+        }
+        OUT *p = static_cast<OUT *>(a.out) + i / 16 * a.os + q0 + i % 16 * 2;
+        if (i % 16 * 2 < cols) p[0] = (OUT)x;
+        if (i % 16 * 2 + 1 < cols) p[1] = (OUT)y;
     }
 }
 
@@ -551,24 +621,26 @@ extern "C" gmagnus_status_t gmagnus_expert_layer(const gmagnus_dense_t *X, const
                           l.act_stride};
         hipStream_t s = (hipStream_t)hip_stream;
         const int64_t items = used * ((f + 15) / 16);
-        auto go = [&](auto kernel, int64_t grid, int words) {
+        auto go = [&](auto kernel, int64_t grid, int threads, int words) {
             if (words * 4 > 64 << 10) allow_dynamic_lds(reinterpret_cast<const void *>(kernel), words * 4);
-            hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * WAVES), words * 4, s, a);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), words * 4, s, a);
             GM_CHECK_LAUNCH();
         };
-        const int up = (route_words((int)entries, (int)e) + 3) / 4 * 4, down = (table_words((int)entries) + 4) / 4 * 4;
+        const int route = (route_words((int)entries, (int)e) + 3) / 4 * 4, table = (table_words((int)entries) + 3) / 4 * 4;
         auto both = [&](auto v, auto w) {
             using T = decltype(v);
             constexpr bool FP8 = decltype(w)::value;
             const int64_t grid = items < 1024 ? items : 1024;
-            if (t <= 16)
-                go(k_layer_up<FP8, T, 1>, grid, up + WAVES * 16 * PITCH);
-            else
-                go(k_layer_up<FP8, T, 4>, grid, up + WAVES * 64 * PITCH);
+            if (t <= 16) {
+                go(k_layer_up<FP8, T, 1, true>, grid, 64 * WAVES, route + WAVES * 16 * PITCH);
+            } else {
+                go(k_layer_route, 1, 64 * ROUTE_WAVES, route);
+                go(k_layer_up<FP8, T, 2, false>, grid, 64 * WAVES, table + WAVES * 32 * PITCH);
+            }
             if (OUT->data_type == GMAGNUS_DATA_FP32)
-                go(k_layer_down<FP8, T, float>, tiles * l.splits, down + WAVES * (int)t * PITCH);
+                go(k_layer_down<FP8, T, float>, tiles * l.splits, 64 * WAVES, table + WAVES * (int)t * PITCH);
             else
-                go(k_layer_down<FP8, T, T>, tiles * l.splits, down + WAVES * (int)t * PITCH);
+                go(k_layer_down<FP8, T, T>, tiles * l.splits, 64 * WAVES, table + WAVES * (int)t * PITCH);
         };
         if (X->data_type == GMAGNUS_DATA_BF16) {
             if (fp8) both(__bf16{}, std::true_type{}); else both(__bf16{}, std::false_type{});
