@@ -50,32 +50,40 @@ constexpr int table_words(int entries) { return 4 * entries + 2; }
 // LDS of the routing: the table and what it is made from.
 __host__ GM_DEV constexpr int route_words(int entries, int experts) { return (table_words(entries) + 1) / 2 * 2 + 2 * experts + 2 * entries + experts; }
 
+// The choice of tokens first, first + step, ..., the next one's logits on their way while one is chosen from.
 template <int V>
-GM_DEV void choose_few(const LayerArgs &a, int t, uint64_t *mask, int32_t *list_e, float *list_w) {
+GM_DEV void choose_few(const LayerArgs &a, int first, int step, uint64_t *mask, int32_t *list_e, float *list_w) {
     const int lane = threadIdx.x & 63;
-    float l[V], p[V];
+    float l[V], next[V], p[V];
+    auto fetch = [&](int t, float(&v)[V]) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int e = j * 64 + lane;
-        const int64_t at = t * a.ls + (e < a.n_experts ? e : 0);
-        l[j] = a.logit_type == GMAGNUS_DATA_FP32   ? static_cast<const float *>(a.logits)[at]
-               : a.logit_type == GMAGNUS_DATA_BF16 ? (float)static_cast<const __bf16 *>(a.logits)[at]
-                                                   : (float)static_cast<const _Float16 *>(a.logits)[at];
-    }
-    uint64_t chosen[V];
-    int n, before = t * a.top_k;
-    const float scale = choose<float, V>(l, a.n_experts, a.top_k, a.normalise, chosen, p, n);
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        if (chosen[j] >> lane & 1) {
-            const int at = before + __popcll(chosen[j] & lanemask_lt());
-            list_e[at] = j * 64 + lane;
-            list_w[at] = p[j] * scale;
-            atomicOr(reinterpret_cast<unsigned long long *>(&mask[j * 64 + lane]), 1ull << t);
+        for (int j = 0; j < V; ++j) {
+            const int e = j * 64 + lane;
+            const int64_t at = t * a.ls + (e < a.n_experts ? e : 0);
+            v[j] = a.logit_type == GMAGNUS_DATA_FP32   ? static_cast<const float *>(a.logits)[at]
+                   : a.logit_type == GMAGNUS_DATA_BF16 ? (float)static_cast<const __bf16 *>(a.logits)[at]
+                                                       : (float)static_cast<const _Float16 *>(a.logits)[at];
         }
-        before += __popcll(chosen[j]);
+    };
+    if (first < a.n_tokens) fetch(first, l);
+    for (int t = first; t < a.n_tokens; t += step) {
+        if (t + step < a.n_tokens) fetch(t + step, next);
+        uint64_t chosen[V];
+        int n, before = t * a.top_k;
+        const float scale = choose<float, V>(l, a.n_experts, a.top_k, a.normalise, chosen, p, n);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if (chosen[j] >> lane & 1) {
+                const int at = before + __popcll(chosen[j] & lanemask_lt());
+                list_e[at] = j * 64 + lane;
+                list_w[at] = p[j] * scale;
+                atomicOr(reinterpret_cast<unsigned long long *>(&mask[j * 64 + lane]), 1ull << t);
+            }
+            before += __popcll(chosen[j]);
+            l[j] = next[j];
+        }
+        for (int i = before + lane; i < (t + 1) * a.top_k; i += 64) list_e[i] = -1;
     }
-    for (int i = before + lane; i < (t + 1) * a.top_k; i += 64) list_e[i] = -1;
 }
 
 // Fills the table in LDS; all threads of a work group.
@@ -88,14 +96,12 @@ GM_DEV void route_few(const LayerArgs &a, int32_t *lds, int waves) {
     int32_t *row_of = reinterpret_cast<int32_t *>(list_w + entries);
     for (int e = threadIdx.x; e < a.n_experts; e += 64 * waves) mask[e] = 0;
     __syncthreads();
-    for (int i = w; i < a.n_tokens; i += waves) {
-        if (a.n_experts <= 64)
-            choose_few<1>(a, i, mask, list_e, list_w);
-        else if (a.n_experts <= 256)
-            choose_few<4>(a, i, mask, list_e, list_w);
-        else
-            choose_few<16>(a, i, mask, list_e, list_w);
-    }
+    if (a.n_experts <= 64)
+        choose_few<1>(a, w, waves, mask, list_e, list_w);
+    else if (a.n_experts <= 256)
+        choose_few<4>(a, w, waves, mask, list_e, list_w);
+    else
+        choose_few<16>(a, w, waves, mask, list_e, list_w);
     __syncthreads();
     if (w == 0) {
         int used = 0, rows = 0;
@@ -528,16 +534,19 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
 struct LayerLayout {
     int64_t arrived, table, act, share, bytes, act_stride;
     int splits;
-    LayerLayout(int64_t t, int64_t e, int64_t k, int64_t f, int64_t n) {
+    LayerLayout(int64_t t, int64_t e, int64_t k, int64_t f, int64_t n, bool fp8) {
         int64_t at = 0;
         auto take = [&](int64_t bytes) {
             const int64_t here = at;
             at += (bytes + 255) / 256 * 256;
             return here;
         };
-        // enough splits for four work groups a CU, as many at most as there can be waves' units
-        const int64_t tiles = (n + 31) / 32, used = e < t * k ? e : t * k, units = used * ((f + 255) / 256);
-        int64_t s = (1024 + tiles - 1) / tiles;
+        // Splits for two work groups a CU, of E4M3 weights for three, as many at most as there can be waves' units. The
+        // second kernel, 2048 x 1024 (outputs x inner), 16 tokens to 4 of 64 experts: 256 work groups 31 us, 512 30, 768 31,
+        // 1024 35, 2048 48; 64 tokens to 6 of 64 53, 52, 55, 72, 92; E4M3, 16 tokens 23, 17, 17, 20, 30, 48 tokens to 6 of 64,
+        // 2048 x 1000, 94, 58, 50, 50, 71.
+        const int64_t tiles = (n + 31) / 32, used = e < t * k ? e : t * k, units = used * ((f + 127) / 128);
+        int64_t s = ((fp8 ? 768 : 512) + tiles - 1) / tiles;
         if (s > (units + WAVES - 1) / WAVES) s = (units + WAVES - 1) / WAVES;
         splits = (int)s;
         act_stride = (f + 7) / 8 * 8;
@@ -561,7 +570,8 @@ using namespace gm;
 
 extern "C" int64_t gmagnus_expert_layer_workspace_bytes(int64_t n_tokens, int64_t n_experts, int64_t top_k, int64_t inner,
                                                         int64_t n_cols) {
-    return layer_sizes_ok(n_tokens, n_experts, top_k, inner, n_cols) ? LayerLayout(n_tokens, n_experts, top_k, inner, n_cols).bytes : 0;
+    // (E4M3 weights have as many splits or more)
+    return layer_sizes_ok(n_tokens, n_experts, top_k, inner, n_cols) ? LayerLayout(n_tokens, n_experts, top_k, inner, n_cols, true).bytes : 0;
 }
 
 extern "C" gmagnus_status_t gmagnus_expert_layer(const gmagnus_dense_t *X, const gmagnus_dense_t *logits, int64_t top_k,
@@ -602,12 +612,12 @@ extern "C" gmagnus_status_t gmagnus_expert_layer(const gmagnus_dense_t *X, const
                        GMAGNUS_ERROR_INVALID_VALUE, "scales must be fp32");
         }
         if (t == 0) return;
-        const LayerLayout l(t, e, top_k, f, n);
+        const LayerLayout l(t, e, top_k, f, n, fp8);
         GM_REQUIRE(workspace && workspace_bytes >= l.bytes, GMAGNUS_ERROR_INVALID_VALUE,
                    "workspace below gmagnus_expert_layer_workspace_bytes");
         GM_REQUIRE((uintptr_t)workspace % 16 == 0, GMAGNUS_ERROR_INVALID_VALUE, "workspace is not 16-byte aligned");
         const int64_t tiles = (n + 31) / 32, entries = t * top_k, used = e < entries ? e : entries;
-        GM_REQUIRE(tiles * l.splits < INT32_MAX && used * ((f + 255) / 256) < INT32_MAX / 2, GMAGNUS_ERROR_UNSUPPORTED,
+        GM_REQUIRE(tiles * l.splits < INT32_MAX && used * ((f + 127) / 128) < INT32_MAX / 2, GMAGNUS_ERROR_UNSUPPORTED,
                    "2^31 tiles or 2^30 units of the reduction or more");
         char *ws = static_cast<char *>(workspace);
         const int size = fp8 ? 1 : 2;
