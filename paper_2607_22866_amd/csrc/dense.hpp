@@ -121,7 +121,7 @@ GM_DEV float exp_neg(float x) {
 
 // sigma(g) and 1 - sigma(g), each to a few units however small.
 GM_DEV void sigmoid(float g, float &s, float &rest) {
-    const float z = exp_neg(-fabsf(g)), big = 1.f / (1.f + z), small = z * big;
+    const float z = exp_neg(-fabsf(g)), big = __builtin_amdgcn_rcpf(1.f + z), small = z * big;
     s = g >= 0.f ? big : small;
     rest = g >= 0.f ? small : big;
 }

@@ -72,17 +72,29 @@ GM_DEV float row_scale(uint32_t most) {
     return s < SCALE_MIN ? SCALE_MIN : s;  // (a NaN stays)
 }
 
-// x / scale to the nearest integer, ties to even, at most 127 in magnitude; a NaN as 0.
-GM_DEV uint32_t to_int8(float x, float scale) {
-    const float v = __builtin_rintf(x / scale);
-    const float c = v > INT8_MAX_F ? INT8_MAX_F : v < -INT8_MAX_F ? -INT8_MAX_F : v == v ? v : 0.f;
-    return (uint32_t)(int)c & 0xffu;
+// The same roundings by 1 / scale, which costs a division for eight values rather than for each: the quotient is off by
+// two units of 2^-24 and may fall on the other side of a tie that it is that near to. (Infinite scales give 0
+// and NaN as the division does.)
+GM_DEV void store_fp8x8_by(uint8_t *p, int valid, const float (&v)[8], float inverse) {
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float x = v[i] * inverse;
+        r[i] = x > FP8_MAX ? FP8_MAX : x < -FP8_MAX ? -FP8_MAX : x;
+    }
+    const uint32_t w[2] = {pack_fp8(r[0], r[1], r[2], r[3]), pack_fp8(r[4], r[5], r[6], r[7])};
+    store_bytes8(p, valid, w);
 }
 
-GM_DEV void store_int8x8(uint8_t *p, int valid, const float (&v)[8], float scale) {
+// To the nearest integers, ties to even, at most 127 in magnitude; a NaN as 0.
+GM_DEV void store_int8x8_by(uint8_t *p, int valid, const float (&v)[8], float inverse) {
     uint32_t w[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i >> 2] |= to_int8(v[i], scale) << (8 * (i & 3));
+    for (int i = 0; i < 8; ++i) {
+        const float x = __builtin_rintf(v[i] * inverse);
+        const float c = x > INT8_MAX_F ? INT8_MAX_F : x < -INT8_MAX_F ? -INT8_MAX_F : x == x ? x : 0.f;
+        w[i >> 2] |= ((uint32_t)(int)c & 0xffu) << (8 * (i & 3));
+    }
     store_bytes8(p, valid, w);
 }
 

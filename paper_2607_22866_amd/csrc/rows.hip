@@ -36,8 +36,8 @@ GM_DEV uint32_t max_with_ror(uint32_t x) {
 // The largest of 16 neighbouring lanes', in all of them.
 GM_DEV uint32_t max16(uint32_t x) { return max_with_ror<1>(max_with_ror<2>(max_with_ror<4>(max_with_ror<8>(x)))); }
 
-// Sums and maxima over the W waves of a row. Two sets of places: a set is written again
-// behind the barrier of the next one, when all have read it.
+// Sums and maxima over the W waves of a row. Two sets of places (for pairs of sums two
+// each): a set is written again behind the barrier of the next one, when all have read it.
 template <int W>
 struct Join {
     float (*part)[W];
@@ -54,6 +54,26 @@ struct Join {
             for (int i = 1; i < W; ++i) x += p[i];
         }
         return x;
+    }
+    GM_DEV void sums(float &x, float &y) {
+        x = wave_sum(x);
+        y = wave_sum(y);
+        if constexpr (W > 1) {
+            float *p = part[turn], *q = part[turn + 2];
+            turn ^= 1;
+            if ((threadIdx.x & 63) == 0) {
+                p[threadIdx.x / 64] = x;
+                q[threadIdx.x / 64] = y;
+            }
+            __syncthreads();
+            x = p[0];
+            y = q[0];
+#pragma unroll
+            for (int i = 1; i < W; ++i) {
+                x += p[i];
+                y += q[i];
+            }
+        }
     }
     GM_DEV uint32_t most(uint32_t x) {
         x = wave_max(x);
@@ -92,6 +112,33 @@ GM_DEV void store(T *p, int valid, const float (&v)[8]) {
         store_f32(p, valid, v);
     }
 }
+
+// Eight columns as they lie in memory, for what is on its way while another row is worked on.
+template <bool WHOLE, typename T>
+struct Piece {
+    u32x4 v[sizeof(T) / 2];
+    GM_DEV void fetch(const T *p, int valid) {
+        if constexpr (sizeof(T) == 2) {
+            v[0] = load8(p, WHOLE ? (valid > 0 ? 8 : 0) : valid);
+        } else {
+            float x[8];
+            load<WHOLE>(p, valid, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i / 4][i % 4] = __float_as_uint(x[i]);
+        }
+    }
+    GM_DEV void get(float (&x)[8]) const {
+        if constexpr (sizeof(T) == 2) {
+            typedef T vec __attribute__((ext_vector_type(8)));
+            const vec t = __builtin_bit_cast(vec, v[0]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = (float)t[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[i / 4][i % 4]);
+        }
+    }
+};
 
 // Of a weight of type T, or float32 (w32); null: ones.
 template <bool WHOLE, typename T>
@@ -143,7 +190,7 @@ GM_DEV void load_piece(const RowArgs &a, const T *x, int64_t row, int64_t c, int
 
 // Eight columns of the results; E4M3: 16 lanes hold a block of 128.
 template <bool WHOLE, typename T>
-GM_DEV void store_piece(const RowArgs &a, const Place &at, int64_t row, int64_t c, int valid, const float (&v)[8], float scale) {
+GM_DEV void store_piece(const RowArgs &a, const Place &at, int64_t row, int64_t c, int valid, const float (&v)[8], float inverse) {
     if (a.y) store<WHOLE>(static_cast<T *>(a.y) + row * a.ys + c, valid, v);
     uint8_t *q = a.q + at.g * a.qg + at.r * a.qs + c;
     if (a.format == E4M3) {
@@ -152,11 +199,11 @@ GM_DEV void store_piece(const RowArgs &a, const Place &at, int64_t row, int64_t 
         for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
         const float s = block_scale(max16(m));
         if (valid > 0) {
-            store_fp8x8(q, WHOLE ? 8 : valid, v, s);
+            store_fp8x8_by(q, WHOLE ? 8 : valid, v, 1.f / s);
             if (threadIdx.x % 16 == 0) a.scale[row * a.ss + c / SB] = s;
         }
     } else if (a.format == INTEGER) {
-        if (valid > 0) store_int8x8(q, WHOLE ? 8 : valid, v, scale);
+        if (valid > 0) store_int8x8_by(q, WHOLE ? 8 : valid, v, inverse);
     }
 }
 
@@ -192,18 +239,19 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void k_rows(RowArgs a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[j][i] = i < valid[j] ? v[j][i] * r * w[j][i] : 0.f;
         }
-        float scale = 0.f;
+        float inverse = 0.f;
         if (a.format == INTEGER) {
             uint32_t m = 0;
 #pragma unroll
             for (int j = 0; j < CH; ++j)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[j][i]));
-            scale = row_scale(join.most(m));
+            const float scale = row_scale(join.most(m));
+            inverse = 1.f / scale;
             if (t == 0) a.scale[at.g * a.sg + at.r] = scale;
         }
 #pragma unroll
-        for (int j = 0; j < CH; ++j) store_piece<WHOLE, T>(a, at, row, (j * W * 64 + t) * 8, valid[j], v[j], scale);
+        for (int j = 0; j < CH; ++j) store_piece<WHOLE, T>(a, at, row, (j * W * 64 + t) * 8, valid[j], v[j], inverse);
     }
 }
 
@@ -218,7 +266,7 @@ __global__ __launch_bounds__(64 * LONG_W) void k_rows_long(RowArgs a) {
     for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
         const Place at(a, row);
         const T *x = static_cast<const T *>(a.x) + at.g * a.xg + at.r * a.xs;
-        float v[8], w[8], r = 0.f, scale = 0.f;
+        float v[8], w[8], r = 0.f, inverse = 0.f;
         if constexpr (OP == Op::NORM) {
             float s = 0.f;
             for (int64_t c0 = 0; c0 < a.n; c0 += STEP) {
@@ -247,14 +295,15 @@ __global__ __launch_bounds__(64 * LONG_W) void k_rows_long(RowArgs a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
             }
-            scale = row_scale(join.most(m));
+            const float scale = row_scale(join.most(m));
+            inverse = 1.f / scale;
             if (threadIdx.x == 0) a.scale[at.g * a.sg + at.r] = scale;
         }
         for (int64_t c0 = 0; c0 < a.n; c0 += STEP) {
             const int64_t c = c0 + threadIdx.x * 8;
             const int valid = columns_left(a.n, c);
             piece(c, valid);
-            store_piece<WHOLE, T>(a, at, row, c, valid, v, scale);
+            store_piece<WHOLE, T>(a, at, row, c, valid, v, inverse);
         }
     }
 }
@@ -278,26 +327,40 @@ struct NormBackArgs {
 template <typename T, int W, int CH, bool WHOLE>
 __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void k_norm_backward(NormBackArgs a) {
     constexpr int PER = W == 1 ? 4 : 1;
-    __shared__ float part[2][W];
+    __shared__ float part[4][W];
     __shared__ float whole[W == 1 ? CH * 512 : 1];
     Join<W> join{part};
     const int t = W == 1 ? threadIdx.x % 64 : threadIdx.x;
+    const int64_t step = (int64_t)gridDim.x * PER;
     int valid[CH];
     float w[CH][8], share[CH][8] = {};
+    Piece<WHOLE, T> nh[CH], nd[CH], nt[CH];  // of the next row
+    auto fetch = [&](int64_t row) {
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int64_t c = (j * W * 64 + t) * 8;
+            nh[j].fetch(static_cast<const T *>(a.h) + row * a.hs + c, valid[j]);
+            nd[j].fetch(static_cast<const T *>(a.d_y) + row * a.ds + c, valid[j]);
+            if (a.d_total) nt[j].fetch(static_cast<const T *>(a.d_total) + row * a.ts + c, valid[j]);
+        }
+    };
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
         const int64_t c = (j * W * 64 + t) * 8;
         valid[j] = columns_left(a.n, c);
         load_weight<WHOLE, T>(a.w, a.w32, c, valid[j], w[j]);
     }
-    for (int64_t row = (int64_t)blockIdx.x * PER + (W == 1 ? threadIdx.x / 64 : 0); row < a.n_rows; row += (int64_t)gridDim.x * PER) {
-        float h[CH][8], d[CH][8], square = 0.f, dot = 0.f;
+    int64_t row = (int64_t)blockIdx.x * PER + (W == 1 ? threadIdx.x / 64 : 0);
+    if (row < a.n_rows) fetch(row);
+    for (; row < a.n_rows; row += step) {
+        float h[CH][8], d[CH][8], o[CH][8], square = 0.f, dot = 0.f;
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            const int64_t c = (j * W * 64 + t) * 8;
-            load<WHOLE>(static_cast<const T *>(a.h) + row * a.hs + c, valid[j], h[j]);
-            load<WHOLE>(static_cast<const T *>(a.d_y) + row * a.ds + c, valid[j], d[j]);
+            nh[j].get(h[j]);
+            nd[j].get(d[j]);
+            nt[j].get(o[j]);
         }
+        if (row + step < a.n_rows) fetch(row + step);
 #pragma unroll
         for (int j = 0; j < CH; ++j)
 #pragma unroll
@@ -305,20 +368,17 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void k_norm_backward(NormBack
                 square += h[j][i] * h[j][i];
                 dot += d[j][i] * w[j][i] * h[j][i];
             }
-        square = join.sum(square);
-        dot = join.sum(dot);
+        join.sums(square, dot);
         const float r = 1.f / sqrtf(square / (float)a.n + a.eps), c = r * (dot / (float)a.n) * r;
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            const int64_t col = (j * W * 64 + t) * 8;
-            float o[8] = {};
-            if (a.d_total) load<WHOLE>(static_cast<const T *>(a.d_total) + row * a.ts + col, valid[j], o);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 share[j][i] += d[j][i] * (h[j][i] * r);
-                o[i] += r * (d[j][i] * w[j][i] - h[j][i] * c);
+                const float x = r * (d[j][i] * w[j][i] - h[j][i] * c);
+                o[j][i] = a.d_total ? x + o[j][i] : x;
             }
-            store<WHOLE>(static_cast<T *>(a.d_h) + row * a.os + col, valid[j], o);
+            store<WHOLE>(static_cast<T *>(a.d_h) + row * a.os + (j * W * 64 + t) * 8, valid[j], o[j]);
         }
     }
     if (!a.share) return;
@@ -366,7 +426,7 @@ __global__ __launch_bounds__(1024) void k_add_shares(const float *share, int64_t
 // Rows of any length: r and c of each row, then the columns 512 at a time.
 template <typename T, bool WHOLE>
 __global__ __launch_bounds__(64 * LONG_W) void k_norm_backward_rows(NormBackArgs a) {
-    __shared__ float part[2][LONG_W];
+    __shared__ float part[4][LONG_W];
     Join<LONG_W> join{part};
     for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
         float square = 0.f, dot = 0.f;
@@ -385,8 +445,7 @@ __global__ __launch_bounds__(64 * LONG_W) void k_norm_backward_rows(NormBackArgs
             square += p;
             dot += q;
         }
-        square = join.sum(square);
-        dot = join.sum(dot);
+        join.sums(square, dot);
         if (threadIdx.x == 0) {
             const float r = 1.f / sqrtf(square / (float)a.n + a.eps);
             a.of_row[2 * row] = r;
