@@ -221,12 +221,41 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void k_rows(RowArgs a) {
         valid[j] = columns_left(a.n, c);
         if constexpr (OP == Op::NORM) load_weight<WHOLE, T>(a.w, a.w32, c, valid[j], w[j]);
     }
-    for (int64_t row = (int64_t)blockIdx.x * PER + (W == 1 ? threadIdx.x / 64 : 0); row < a.n_rows; row += (int64_t)gridDim.x * PER) {
+    const int64_t step = (int64_t)gridDim.x * PER;
+    Piece<WHOLE, T> nx[CH], nr[CH];  // the next row (the gate's are long enough, and rows enough)
+    auto fetch = [&](int64_t row) {
         const Place at(a, row);
-        const T *x = static_cast<const T *>(a.x) + at.g * a.xg + at.r * a.xs;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int64_t c = (j * W * 64 + t) * 8;
+            nx[j].fetch(static_cast<const T *>(a.x) + at.g * a.xg + at.r * a.xs + c, valid[j]);
+            if (OP == Op::NORM && a.r) nr[j].fetch(static_cast<const T *>(a.r) + row * a.rs + c, valid[j]);
+        }
+    };
+    int64_t row = (int64_t)blockIdx.x * PER + (W == 1 ? threadIdx.x / 64 : 0);
+    if constexpr (OP != Op::GATE)
+        if (row < a.n_rows) fetch(row);
+    for (; row < a.n_rows; row += step) {
+        const Place at(a, row);
         float v[CH][8];
 #pragma unroll
-        for (int j = 0; j < CH; ++j) load_piece<OP, WHOLE>(a, x, row, (j * W * 64 + t) * 8, valid[j], true, v[j]);
+        for (int j = 0; j < CH; ++j) {
+            const int64_t c = (j * W * 64 + t) * 8;
+            if constexpr (OP != Op::GATE) {
+                nx[j].get(v[j]);
+                if (OP == Op::NORM && a.r) {
+                    float u[8];
+                    nr[j].get(u);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[j][i] = to_f32((T)(v[j][i] + u[i]));
+                    store<WHOLE>(static_cast<T *>(a.total) + row * a.ts + c, valid[j], v[j]);
+                }
+            } else {
+                load_piece<OP, WHOLE>(a, static_cast<const T *>(a.x) + row * a.xs, row, c, valid[j], true, v[j]);
+            }
+        }
+        if constexpr (OP != Op::GATE)
+            if (row + step < a.n_rows) fetch(row + step);
         if constexpr (OP == Op::NORM) {
             float s = 0.f;
 #pragma unroll
@@ -514,7 +543,10 @@ __global__ __launch_bounds__(256) void k_gate_backward(GateBackArgs a) {
 }
 
 // ------------------------------------------------------------------- host side
-constexpr int64_t ROWS_GRID = 2048;   // work groups of the norm: each holds the weight for its rows
+// Work groups, each of which takes rows in turns with the next one's loads on its way (and the norm's weight in
+// registers): two a CU, short rows eight. Norm with residual and E4M3 result, 16384 x 4096: 512 work groups 114 us, 1024
+// 117, 2048 118; 131072 x 256: 512 93, 2048 70.
+int64_t rows_grid(int64_t n) { return n <= 512 ? 2048 : 512; }
 constexpr int64_t BACK_UNITS = 512;   // shares of d_w
 
 int64_t back_units(int64_t t, int64_t n) {
@@ -578,7 +610,7 @@ void launch_rows(const RowArgs &a, int32_t type, hipStream_t s) {
             if constexpr (W == 0) {
                 hipLaunchKernelGGL((k_rows_long<OP, T, WHOLE>), dim3(grid_for(a.n_rows, 1, 1 << 16)), dim3(64 * LONG_W), 0, s, a);
             } else {
-                const int64_t most = OP == Op::NORM ? ROWS_GRID : MAX_GRID;
+                const int64_t most = OP == Op::GATE ? MAX_GRID : rows_grid(a.n);
                 hipLaunchKernelGGL((k_rows<OP, T, W, CH, WHOLE>), dim3(grid_for(a.n_rows, W == 1 ? 4 : 1, most)),
                                    dim3(W > 4 ? 64 * W : 256), 0, s, a);
             }
