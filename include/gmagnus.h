@@ -609,7 +609,8 @@ int64_t gmagnus_expert_layer_workspace_bytes(int64_t n_tokens, int64_t n_experts
  * G_e above U_e; W2 one of n_cols x inner. X is bf16 or fp16, W1 and W2 have its type
  * or are both E4M3 with the scales that gmagnus_quantise_blocks gives with block_rows
  * 128 (scales NULL otherwise); OUT has X's type or fp32. Sums are held in fp32, the
- * gate's result is rounded to X's type. Of the weights only the chosen experts' are
+ * gate's result as the sum of two values of X's type (so it has X's range, and an
+ * infinity past that). Of the weights only the chosen experts' are
  * read. The workspace is the call's until it has run.
  * Errors: INVALID_VALUE, UNSUPPORTED (more than 64 tokens, 1024 experts or 1024
  * entries, sides above 2^31 - 1025), HIP. */

@@ -119,7 +119,7 @@ GM_DEV float exp_neg(float x) {
     return __builtin_fmaf(r * LN2, rest, r);
 }
 
-// sigma(g) and 1 - sigma(g), each to a few units however small.
+// sigma(g) and 1 - sigma(g), each to a few units however small. (The hardware's reciprocal of 1 + e^-|g| is off by one.)
 GM_DEV void sigmoid(float g, float &s, float &rest) {
     const float z = exp_neg(-fabsf(g)), big = __builtin_amdgcn_rcpf(1.f + z), small = z * big;
     s = g >= 0.f ? big : small;

@@ -77,7 +77,9 @@ struct Scales {
 };
 
 // Any alignment: tiles of 128 x 128 staged through registers, four waves of 64 x 64,
-// LDS rows of 128 bytes as the E4M3 tiles have them.
+// LDS rows of 128 bytes as the E4M3 tiles have them. One buffer, one step's loads in
+// flight: bound by loads that cross lines (4001 x 4001 x 4001 127-137 us, 0.93-1.01
+// POP/s; two buffers 143, two steps' loads in flight as well 152, with spills).
 constexpr int GEN_B = 128, GEN_T = 256;
 
 template <typename OUT>
@@ -290,13 +292,26 @@ Shape int8_shape(const Int8Args &a) {
     const int64_t mean = (a.n_rows + a.n_groups - 1) / a.n_groups, groups = a.n_groups < a.n_rows ? a.n_groups : a.n_rows;
     const bool fast = fast_side(a.x, a.xs, 0, a.k, a.index ? a.n_x : 256, 1) &&
                       fast_side(a.w, a.ws, a.n_groups > 1 ? a.wg : 0, a.k, 256, 1);
-    if (mean <= 8) {
+    // 64 groups, 2048 x 4096, sizes as chance deals them: of 1, 4, 8, 12, 16 and 24 rows 64
+    // columns a work group 78, 111, 117, 124, 144 and 178 us, tiles of 32 x 128 79, 157,
+    // 161, 160, 159 and 173 (all rows in one of the groups, mean 8: 44 / 23, 16: 80 / 25);
+    // one row, 4096 x 4096: 11.7 with 16 columns, 13.6 with 64, 4 groups 19.6 / 18.5; not
+    // aligned, 2047 x 2047, 4 groups of 1 row 19.4 with 16 columns, staged tiles 25.5, 16
+    // groups 73 / 27
+    if (mean <= 16) {
         if (groups * ((a.n + 63) / 64) < 256) return Shape::FEW16;
         if (fast) return Shape::FEW64;
     }
     if (!fast) return Shape::ANY;
-    if (mean <= 32) return Shape::T32;
-    return big_product_tiles(mean, a.n, groups) ? Shape::T256 : Shape::T64;
+    // 256 x 256 tiles where they do not leave CUs without one and the columns' padding does not
+    // grow by more than a third: of 32, 48, 64, 96, 128, 192 and 512 rows 137, 139, 139, 144, 157,
+    // 163 and 356 us, tiles of 32 rows 152, 148, 146, 175, 202, 264 and 606, of 64 177, 172, 150,
+    // 155, 180, 209 and 437 (of 40 rows 139, 133, 178; mean 128, all rows in one of the groups, 60
+    // against 88); 8 groups of 512 rows, 1024 x 1024 (64 tiles) 19.1 against 12.2 with 64 rows, of
+    // 1024 (128 tiles) 21.8 / 19.3
+    const int64_t cols = (a.n + 255) / 256;
+    if (mean >= 48 && (mean + 255) / 256 * cols * groups >= 128 && 3 * 2 * cols <= 4 * ((a.n + 127) / 128)) return Shape::T256;
+    return mean <= 64 ? Shape::T32 : Shape::T64;
 }
 
 }  // namespace

@@ -28,9 +28,9 @@ struct LayerArgs {
     // workspace
     int32_t *arrived;  // of each column tile of the second kernel, how many of its splits are there
     int32_t *table;
-    void *act;         // [entries][act_stride]
+    void *act;         // [2][entries][act_stride], act_part elements between the two
     float *share;      // [column tiles][splits][n_tokens][32]
-    int64_t act_stride;
+    int64_t act_stride, act_part;
 };
 
 // The routing: the experts that tokens have chosen, ascending, with their first rows, and the rows' tokens and weights.
@@ -151,33 +151,6 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void k_layer_route(LayerArgs a) {
 }
 
 // ------------------------------------------------------------------- fragments
-// The 16 bytes at `at` of a row of n bytes, zeros past its end, where nothing is read: the row's last 16 bytes,
-// moved down. (Element by element they would take more registers than all else in these kernels.)
-GM_DEV u32x4 cut_piece(const uint8_t *row, int64_t at, int64_t n) {
-    u32x4 r = {0, 0, 0, 0};
-    const int64_t there = n - at;
-    if (there <= 0) return r;
-    if (n >= 16) {
-        const int move = there < 16 ? 16 - (int)there : 0;
-        const Bytes16<1> b = *reinterpret_cast<const Bytes16<1> *>(row + at - move);
-        const bool two = move & 8, one = move & 4;
-        const uint32_t c[4] = {two ? b.v[2] : b.v[0], two ? b.v[3] : b.v[1], two ? 0 : b.v[2], two ? 0 : b.v[3]};
-        const uint32_t d[5] = {one ? c[1] : c[0], one ? c[2] : c[1], one ? c[3] : c[2], one ? 0 : c[3], 0};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_alignbyte(d[i + 1], d[i], move & 3);
-    } else {  // (a row of less than a piece)
-        uint64_t v[2] = {0, 0};
-#pragma unroll 1
-        for (int i = 0; i < (int)there; ++i) {
-            const uint64_t x = (uint64_t)row[at + i] << (8 * (i & 7));
-            v[0] |= i < 8 ? x : 0;
-            v[1] |= i < 8 ? 0 : x;
-        }
-        r = u32x4{(uint32_t)v[0], (uint32_t)(v[0] >> 32), (uint32_t)v[1], (uint32_t)(v[1] >> 32)};
-    }
-    return r;
-}
-
 // A block of the reduction is 128 bytes of a row of weights: 64 values of 16 bits or
 // 128 of E4M3. A lane has 16 bytes at g and 16 at g + 4 of a row's eight pieces, S
 // fragments of 8 values each. E4M3 values are widened, exactly, to the rows' type.
@@ -228,21 +201,24 @@ struct Block {
             for (int s = 0; s < S; ++s)
                 f[h * S + s] = cut_piece(reinterpret_cast<const uint8_t *>(row), (int64_t)(k + first(h, g) + s * 8) * 2, (int64_t)n * 2);
     }
-    // acc += weights' fragments times the rows', by `scale` where there is one
-    GM_DEV static void multiply(const u32x4 (&w)[2], const u32x4 (&r)[2 * S], f32x4 scale, f32x4 &acc) {
-        if constexpr (!FP8) {
-            acc = mfma_16x16x32(w[1], r[1], mfma_16x16x32(w[0], r[0], acc, T{}), T{});
-        } else {
-            f32x4 sum = {0, 0, 0, 0};
+    // acc += weights' fragments times the rows' (of P parts), by `scale` where there is one
+    template <int P>
+    GM_DEV static void multiply(const u32x4 (&w)[2], const u32x4 (&r)[P][2 * S], f32x4 scale, f32x4 &acc) {
+        f32x4 sum = FP8 ? f32x4{0, 0, 0, 0} : acc;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                u32x4 f[2];
-                widen(w[h], f);
-                sum = mfma_16x16x32(f[1], r[2 * h + 1], mfma_16x16x32(f[0], r[2 * h], sum, T{}), T{});
-            }
+        for (int h = 0; h < 2; ++h) {
+            u32x4 f[S];
+            widen(w[h], f);
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+#pragma unroll
+                for (int p = 0; p < P; ++p) sum = mfma_16x16x32(f[s], r[p][h * S + s], sum, T{});
+        }
+        if constexpr (!FP8)
+            acc = sum;
+        else
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] += scale[e] * sum[e];
-        }
     }
 };
 
@@ -309,7 +285,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
             for (int r = 0; r < RT; ++r) xr[r] = static_cast<const T *>(a.x) + t.token[base + min(r0 + 16 * r + i16, rows - 1)] * a.xs;
             f32x4 acc[RT][2] = {};
             for (int k0 = w; k0 < full; k0 += WAVES * U) {
-                u32x4 fw[U][2][2], fx[U][2 * B::S];
+                u32x4 fw[U][2][2], fx[U][1][2 * B::S];
                 f32x4 s[U][2];
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
@@ -318,7 +294,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
                     for (int j = 0; j < 2; ++j)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) fw[i][j][h] = B::load(wr[j] + (int64_t)kb * 128 + h * 64 + g * 16);
-                    B::load_rows(xr[0] + kb * B::VALUES, g, fx[i]);
+                    B::load_rows(xr[0] + kb * B::VALUES, g, fx[i][0]);
                     scales(kb, s[i]);
                 }
 #pragma unroll
@@ -330,7 +306,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
                 for (int r = 1; r < RT; ++r)
                     if (r0 + 16 * r < rows) {
 #pragma unroll
-                        for (int i = 0; i < U; ++i) B::load_rows(xr[r] + min(k0 + i * WAVES, full - 1) * B::VALUES, g, fx[i]);
+                        for (int i = 0; i < U; ++i) B::load_rows(xr[r] + min(k0 + i * WAVES, full - 1) * B::VALUES, g, fx[i][0]);
 #pragma unroll
                         for (int i = 0; i < U; ++i)
                             if (k0 + i * WAVES < full)
@@ -347,13 +323,14 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
 #pragma unroll
                 for (int r = 0; r < RT; ++r)
                     if (r0 + 16 * r < rows) {
-                        u32x4 fx[2 * B::S];
-                        B::load_rows_cut(xr[r], full * B::VALUES, a.d, g, fx);
+                        u32x4 fx[1][2 * B::S];
+                        B::load_rows_cut(xr[r], full * B::VALUES, a.d, g, fx[0]);
 #pragma unroll
                         for (int j = 0; j < 2; ++j) B::multiply(fw[j], fx, s[j], acc[r][j]);
                     }
             }
-            // (the result is rounded to the rows' type, as between two products)
+            // Two values of the rows' type are kept of a result, itself and what its rounding left (an infinite one leaves
+            // nothing): rounded once it would add as much error to the layer's result as that has from its own rounding.
             auto gated = [](float x, float y) {
                 float s, rest;
                 sigmoid(x, s, rest);
@@ -376,7 +353,12 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
                     x += part[(v * RT * 16 + r) * PITCH + col];
                     y += part[(v * RT * 16 + r) * PITCH + 16 + col];
                 }
-                if (f0 + col < a.f) out[r * a.act_stride + col] = (T)gated(x, y);
+                if (f0 + col < a.f) {
+                    const float v = gated(x, y);
+                    const T top = (T)v;
+                    out[r * a.act_stride + col] = top;
+                    out[a.act_part + r * a.act_stride + col] = fabsf((float)top) < INFINITY ? (T)(v - (float)top) : (T)0.f;
+                }
             }
         }
     }
@@ -432,7 +414,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
             return f32x4{x, x, x, x};
         };
         if (a.f - k0 >= CHUNK) {
-            u32x4 fw[U][2][2], fr[U][2 * B::S];
+            u32x4 fw[U][2][2], fr[U][2][2 * B::S];
             f32x4 s[U];
             const T *row = row_at(0);
 #pragma unroll
@@ -441,7 +423,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) fw[i][j][h] = B::load(wr[j] + k0 * B::BYTES + i * 128 + h * 64 + g * 16);
-                B::load_rows(row + k0 + i * B::VALUES, g, fr[i]);
+#pragma unroll
+                for (int p = 0; p < 2; ++p) B::load_rows(row + p * a.act_part + k0 + i * B::VALUES, g, fr[i][p]);
                 s[i] = scale(i);
             }
             for (int r = 0;;) {
@@ -455,17 +438,20 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
                 if (r >= rows) break;
                 row = row_at(r);
 #pragma unroll
-                for (int i = 0; i < U; ++i) B::load_rows(row + k0 + i * B::VALUES, g, fr[i]);
+                for (int i = 0; i < U; ++i)
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) B::load_rows(row + p * a.act_part + k0 + i * B::VALUES, g, fr[i][p]);
             }
         } else {
             for (int r = 0; r < rows; r += 16) {
                 f32x4 acc[2] = {};
                 const T *row = row_at(r);
                 for (int i = 0; k0 + i * B::VALUES < a.f; ++i) {
-                    u32x4 fw[2][2], fr[2 * B::S];
+                    u32x4 fw[2][2], fr[2][2 * B::S];
 #pragma unroll
                     for (int j = 0; j < 2; ++j) B::load_cut(wr[j], k0 + i * B::VALUES, a.f, g, fw[j]);
-                    B::load_rows_cut(row, k0 + i * B::VALUES, a.f, g, fr);
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) B::load_rows_cut(row + p * a.act_part, k0 + i * B::VALUES, a.f, g, fr[p]);
 #pragma unroll
                     for (int j = 0; j < 2; ++j) B::multiply(fw[j], fr, scale(i), acc[j]);
                 }
@@ -552,7 +538,7 @@ struct LayerLayout {
         act_stride = (f + 7) / 8 * 8;
         arrived = take(tiles * 4);
         table = take(table_words((int)(t * k)) * 4);
-        act = take(t * k * act_stride * 2);
+        act = take(2 * t * k * act_stride * 2);
         share = take(s > 1 ? tiles * s * t * 32 * 4 : 0);
         bytes = at;
     }
@@ -628,7 +614,7 @@ extern "C" gmagnus_status_t gmagnus_expert_layer(const gmagnus_dense_t *X, const
                           W2->stack_stride * size, fp8 ? W2_scale->row_stride : 0, fp8 ? W2_scale->stack_stride : 0,
                           OUT->row_stride, (int)t, (int)e, (int)top_k, normalise, logits->data_type, (int)d, (int)f, (int)n,
                           l.splits, (int32_t *)(ws + l.arrived), (int32_t *)(ws + l.table), ws + l.act, (float *)(ws + l.share),
-                          l.act_stride};
+                          l.act_stride, entries * l.act_stride};
         hipStream_t s = (hipStream_t)hip_stream;
         const int64_t items = used * ((f + 15) / 16);
         auto go = [&](auto kernel, int64_t grid, int threads, int words) {

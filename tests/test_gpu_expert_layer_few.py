@@ -1,7 +1,8 @@
 """A whole layer of gated experts for a few tokens in one call, against its 64-bit form.
 
 Errors are followed through: fp32 sums of K products are off by at most 2^-23 K times the sum of magnitudes, silu's
-slope is below 1.1, the gate's result is rounded to the rows' type once and the layer's result to its type."""
+slope is below 1.1, the gate's result is held as two values of the rows' type (half a step of it, squared, is off; below
+the normal range half a subnormal's step) and the layer's result is rounded to its type."""
 import numpy as np
 import pytest
 
@@ -58,7 +59,7 @@ def reference(x, logits, top_k, normalise, w1, w2):
         s = gg * torch.sigmoid(gg)
         a = s * u
         da = (1.1 * dg + 12 * rr.U32 * s.abs()) * (u.abs() + du) + s.abs() * du + 2.0 ** -125 * (1 + (gg * u).abs())
-        da = da + rr.half_step(x.dtype) * (a.abs() + da) + rr.TINY[x.dtype]
+        da = da + rr.half_step(x.dtype) ** 2 * (a.abs() + da) + rr.TINY[x.dtype]
         y, mag = a @ m2.t(), (a.abs() + da) @ m2.abs().t()
         out[ids] += wt * y
         off[ids] += wt * (da @ m2.abs().t() + ((terms + 40) * 2.0 ** -23 + weight_rel) * mag)
