@@ -818,24 +818,30 @@ def _vector(t: torch.Tensor, dev: int, name: str, types, n: int) -> bytes:
     return _pack_dense(t.data_ptr(), 1, n, n, 0, DATA_TYPES[t.dtype])
 
 
+def _made(t: torch.Tensor, n_rows: int, n_cols: int, kind: int) -> bytes:
+    """Descriptor of a contiguous matrix that a call has made itself."""
+    return _pack_dense(t.data_ptr(), n_rows, n_cols, n_cols, 0, kind)
+
+
 def _row_results(like: torch.Tensor, n: int, quantise, plain, dev: int):
     """The results of like's rows of n columns (y, q, scale), and their descriptors."""
-    if quantise not in (None, torch.float8_e4m3fn, torch.int8):
-        raise ValueError("quantise must be None, torch.float8_e4m3fn or torch.int8")
     rows, device = like.shape[0], like.device
     y = q = scale = dy = dq = ds = None
     if plain or (plain is None and quantise is None):
         y = torch.empty((rows, n), dtype=like.dtype, device=device)
-        dy = _dense(y, dev, "y")
+        dy = _made(y, rows, n, DATA_TYPES[like.dtype])
     if quantise is not None:
-        q = torch.empty((rows, n), dtype=quantise, device=device)
-        dq = _dense(q, dev, "q", int8=True)
         if quantise is torch.int8:
+            q = torch.empty((rows, n), dtype=torch.int8, device=device)
             scale = torch.empty(rows, dtype=torch.float32, device=device)
-            ds = _vector(scale, dev, "scale", (torch.float32,), rows)
+            dq, ds = _made(q, rows, n, DATA_INT8), _made(scale, 1, rows, 0)
+        elif quantise is torch.float8_e4m3fn:
+            blocks = -(-n // SCALE_BLOCK)
+            q = torch.empty((rows, n), dtype=torch.float8_e4m3fn, device=device)
+            scale = torch.empty((rows, blocks), dtype=torch.float32, device=device)
+            dq, ds = _made(q, rows, n, 3), _made(scale, rows, blocks, 0)
         else:
-            scale = torch.empty((rows, -(-n // SCALE_BLOCK)), dtype=torch.float32, device=device)
-            ds = _dense(scale, dev, "scale")
+            raise ValueError("quantise must be None, torch.float8_e4m3fn or torch.int8")
     return (y, q, scale), (dy, dq, ds)
 
 
@@ -852,8 +858,8 @@ def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: O
     dr = dt = total = None
     if residual is not None:
         dr = _dense(residual, dev, "residual")
-        total = torch.empty(tuple(x.shape), dtype=x.dtype, device=x.device)
-        dt = _dense(total, dev, "total")
+        total = torch.empty((x.shape[0], n), dtype=x.dtype, device=x.device)
+        dt = _made(total, x.shape[0], n, DATA_TYPES[x.dtype])
     dw = None if weight is None else _vector(weight, dev, "weight", (x.dtype, torch.float32), n)
     (y, q, scale), (dy, dq, ds) = _row_results(x, n, quantise, plain, dev)
     _check(load().gmagnus_rms_norm(d, dr, dw, eps, dt, dy, dq, ds, _raw_stream(dev)))
