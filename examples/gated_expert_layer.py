@@ -1,0 +1,138 @@
+"""A layer of gated experts with its norm and its residual, from the library's calls.
+
+    h = x + residual,  y = norm(h) * w
+    out[t] = sum over the experts e of token t of R[t, e] * (silu(G_e y[t]) * (U_e y[t])) W2_e^T
+
+R is the routing matrix of the logits y @ router, and [G_e; U_e] are the two halves of
+W1_e. h is handed on as the next layer's residual, out as its x. The layer is trained for a
+few steps (gradients from the library's kernels) and served: in 16 bits, in E4M3, in 8-bit
+integers, and a few tokens at a time in one call.
+
+Usage: python examples/gated_expert_layer.py [--tokens T] [--experts E] [--top-k K]
+[--hidden D] [--inner F] [--steps S]
+"""
+from __future__ import annotations
+
+import argparse
+import os
+import sys
+
+import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+if ROOT not in sys.path:
+    sys.path.insert(0, ROOT)
+
+from paper_2607_22866_amd import gmagnus as g  # noqa: E402
+
+EPS = 1e-6
+
+
+class GatedExpertLayer:
+    """Weights in bfloat16 (norm: hidden, w1: experts x 2 inner x hidden, w2: experts x hidden x inner), the router in float32."""
+
+    def __init__(self, hidden: int, inner: int, experts: int, top_k: int, gen: torch.Generator):
+        def rand(*shape, scale):
+            return torch.randn(shape, device="cuda", generator=gen) * scale
+
+        self.top_k = top_k
+        self.norm = (1 + rand(hidden, scale=0.1)).bfloat16()
+        self.router = rand(hidden, experts, scale=hidden ** -0.5)
+        self.w1 = rand(experts, 2 * inner, hidden, scale=hidden ** -0.5).bfloat16()
+        self.w2 = rand(experts, hidden, inner, scale=inner ** -0.5).bfloat16()
+
+    def forward(self, x: torch.Tensor, residual: torch.Tensor):
+        """(out, the sum of x and residual, what backward() needs)."""
+        n = g.rms_norm(x, self.norm, residual=residual, eps=EPS)
+        logits = n.y.float() @ self.router
+        r = g.route(logits, self.top_k)
+        h = g.group_product(n.y, self.w1, r.group_ptr, index=r.token)
+        a = g.gate(h).y
+        y = g.group_product(a, self.w2, r.group_ptr)
+        return g.combine(y, r.row_ptr, r.slot, r.weight), n.total, (n, logits, r, h, a, y)
+
+    def backward(self, d_out: torch.Tensor, d_total: torch.Tensor, saved):
+        """Gradients of (x and residual alike, norm, router, w1, w2)."""
+        n, logits, r, h, a, y = saved
+        d_y, d_weight = g.combine_backward(y, r.row_ptr, r.slot, r.weight, d_out)
+        d_a = g.group_product(d_y, self.w2, r.group_ptr, transposed=True)
+        d_w2 = g.group_outer(d_y, a, r.group_ptr, out_dtype=torch.float32)
+        d_h = g.gate_backward(h, d_a)
+        d_w1 = g.group_outer(d_h, n.y, r.group_ptr, index=r.token, out_dtype=torch.float32)
+        d_rows = g.group_product(d_h, self.w1, r.group_ptr, transposed=True)
+        d_logits = g.route_backward(logits, r, d_weight)
+        d_n = g.combine(d_rows, r.row_ptr, r.slot).float() + d_logits @ self.router.t()
+        d_x, d_norm = g.rms_norm_backward(n.total, self.norm, d_n.to(n.y.dtype), d_total=d_total, eps=EPS)
+        return d_x, d_norm, n.y.float().t() @ d_logits, d_w1, d_w2
+
+    def quantised(self, form: torch.dtype):
+        """The weights in 8 bits, made once for serving: float8_e4m3fn or int8."""
+        make = g.quantise_rows if form is torch.int8 else lambda w: g.quantise_blocks(w, 128)
+        return form, make(self.w1), make(self.w2)
+
+    def serve(self, x: torch.Tensor, residual: torch.Tensor, weights=None):
+        """(out, the sum) without what training keeps; in 8 bits with the weights of quantised()."""
+        if weights is None:
+            return self.forward(x, residual)[:2]
+        form, (q1, s1), (q2, s2) = weights
+        product = g.group_product_int8 if form is torch.int8 else g.group_product_fp8
+        n = g.rms_norm(x, self.norm, residual=residual, eps=EPS, quantise=form, plain=True)
+        r = g.route(n.y.float() @ self.router, self.top_k)
+        a = g.gate(product(n.q, n.scale, q1, s1, r.group_ptr, index=r.token), quantise=form)
+        y = product(a.q, a.scale, q2, s2, r.group_ptr)
+        return g.combine(y, r.row_ptr, r.slot, r.weight), n.total
+
+    def serve_few(self, x: torch.Tensor, residual: torch.Tensor, weights=None):
+        """serve() for at most g.LAYER_TOKENS tokens, the experts in one call (16 bits or E4M3 weights)."""
+        n = g.rms_norm(x, self.norm, residual=residual, eps=EPS)
+        logits = n.y.float() @ self.router
+        if weights is None:
+            return g.expert_layer(n.y, logits, self.top_k, self.w1, self.w2), n.total
+        _, (q1, s1), (q2, s2) = weights
+        return g.expert_layer(n.y, logits, self.top_k, q1, q2, w1_scale=s1, w2_scale=s2), n.total
+
+
+def main(argv=None) -> dict:
+    ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    ap.add_argument("--tokens", type=int, default=4096)
+    ap.add_argument("--experts", type=int, default=16)
+    ap.add_argument("--top-k", type=int, default=2)
+    ap.add_argument("--hidden", type=int, default=512)
+    ap.add_argument("--inner", type=int, default=512)
+    ap.add_argument("--steps", type=int, default=20)
+    ap.add_argument("--rate", type=float, default=0.5)
+    a = ap.parse_args(argv)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    layer = GatedExpertLayer(a.hidden, a.inner, a.experts, a.top_k, gen)
+    x, residual = (torch.randn(a.tokens, a.hidden, device="cuda", generator=gen).bfloat16() for _ in range(2))
+    target = torch.tanh(x.float() @ torch.randn(a.hidden, a.hidden, device="cuda", generator=gen) * a.hidden ** -0.5)
+    w1, w2, norm = layer.w1.float(), layer.w2.float(), layer.norm.float()
+    losses = []
+    for step in range(a.steps):
+        out, total, saved = layer.forward(x, residual)
+        diff = out.float() - target
+        losses.append(float(diff.square().mean()))
+        _, d_norm, d_router, d_w1, d_w2 = layer.backward((diff * (2.0 / a.hidden)).bfloat16(), torch.zeros_like(total), saved)
+        scale = a.rate * a.experts / a.tokens
+        layer.router -= scale * d_router
+        w1 -= scale * d_w1
+        w2 -= scale * d_w2
+        norm -= scale * d_norm
+        layer.w1, layer.w2, layer.norm = w1.bfloat16(), w2.bfloat16(), norm.bfloat16()
+        if step % 10 == 0 or step == a.steps - 1:
+            print("step %d  loss %.4f" % (step, losses[-1]), flush=True)
+    whole = layer.serve(x[:8], residual[:8])[0].float()
+
+    def off(y):
+        return float((y.float() - whole).norm() / whole.norm())
+
+    fp8 = layer.quantised(torch.float8_e4m3fn)
+    result = {"losses": losses, "few": off(layer.serve_few(x[:8], residual[:8])[0]),
+              "few_fp8": off(layer.serve_few(x[:8], residual[:8], fp8)[0]), "fp8": off(layer.serve(x[:8], residual[:8], fp8)[0]),
+              "int8": off(layer.serve(x[:8], residual[:8], layer.quantised(torch.int8))[0])}
+    print("a few tokens in one call: %(few).1e off; with E4M3 weights %(few_fp8).1e; all in E4M3 %(fp8).1e, in integers %(int8).1e" % result)
+    return result
+
+
+if __name__ == "__main__":
+    main()

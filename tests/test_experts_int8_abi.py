@@ -1,9 +1,7 @@
-"""Argument checks of the products of 8-bit integers, and which kernel a call takes (no GPU here)."""
-import ctypes
-
+"""Argument checks of the products of 8-bit integers: every refusal is a status code with a message and happens before
+a device is touched (no GPU here)."""
 import pytest
 
-from tests import experts_cases as ec
 from tests.test_experts_abi import BF16, F16, F32, FP8, INVALID, PTR, UNSUPPORTED, dense, gm, groups, lib, ref  # noqa: F401
 
 INT8 = 4

@@ -3,8 +3,8 @@
 import numpy as np
 import pytest
 
-from tests import experts_cases as ec
 from tests import experts_ref as er
+from tests import int8_cases as ic
 
 pytestmark = pytest.mark.gpu
 
@@ -60,7 +60,7 @@ def check(g, x, xs, w, ws, sizes, index=None, extra=0, out_dtype=torch.bfloat16,
     return y
 
 
-@pytest.mark.parametrize("kernel,sizes,n,k", ec.FP8_PRODUCTS)
+@pytest.mark.parametrize("kernel,sizes,n,k", ic.PRODUCTS)
 def test_every_kernel(g, kernel, sizes, n, k):
     rows = sum(sizes)
     x, w = integers((rows, k), 1), integers((len(sizes), n, k), 2)
