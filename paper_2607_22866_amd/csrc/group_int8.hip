@@ -77,15 +77,16 @@ struct Scales {
 };
 
 // Any alignment: tiles of 128 x 128 staged through registers, four waves of 64 x 64,
-// LDS rows of 128 bytes as the E4M3 tiles have them. One buffer, one step's loads in
-// flight: bound by loads that cross lines (4001 x 4001 x 4001 127-137 us, 0.93-1.01
-// POP/s; two buffers 143, two steps' loads in flight as well 152, with spills).
+// LDS rows of 128 bytes as the E4M3 tiles have them. One step's loads are in flight while
+// the step before it is multiplied from one of two buffers; bound by loads at odd
+// addresses: 4001 x 4001 x 4001 138-146 us, 0.9 POP/s, with rows of 4004 117 (with two steps'
+// loads in flight, whose registers spill, 157); 20 groups of 35 rows, 1000 x 3000, 29 us.
 constexpr int GEN_B = 128, GEN_T = 256;
 
 template <typename OUT>
 __global__ __launch_bounds__(GEN_T, 2) void k_group_product_int8_any(Int8Args a) {
-    __shared__ u32x4 lds[2 * GEN_B * 8];
-    u32x4 *lp = lds, *lq = lds + GEN_B * 8;
+    __shared__ u32x4 lds[4 * GEN_B * 8];
+    const int n_k = (int)a.k;
     const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16, wv = threadIdx.x / 64;
     const int p0 = wv / 2 * 64, q0 = wv % 2 * 64;
     const uint32_t n_row = count_row_tiles<GEN_B>(a.gp, a.n_groups, a.n_rows, a.max_row_tiles).full;
@@ -105,23 +106,33 @@ __global__ __launch_bounds__(GEN_T, 2) void k_group_product_int8_any(Int8Args a)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = (threadIdx.x + i * GEN_T) / 8;
+            // (columns that are not there read the last one, rows a row of W: the former's results are not stored, the
+            // latter's are not or have the scale 0. Whole steps then have no branch, which would wait for each load)
+            qr[i] = a.w + t.group * a.wg + (n0 + (r < cols ? r : cols - 1)) * a.ws;
             const int64_t xr = x_row(a, t, r);
-            pr[i] = xr < 0 ? nullptr : a.x + xr * a.xs;
-            qr[i] = r < cols ? a.w + t.group * a.wg + (n0 + r) * a.ws : nullptr;
+            pr[i] = xr < 0 ? qr[i] : a.x + xr * a.xs;
         }
         i32x4 acc[4][4] = {};
         u32x4 vp[4], vq[4];
-        auto load = [&](int64_t k0) {
-            const int64_t k = k0 + threadIdx.x % 8 * 16;
+        auto load = [&](int k0) {
+            if (k0 >= n_k) return;
+            const int k = k0 + threadIdx.x % 8 * 16;
+            if (n_k - k0 >= SB) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                vp[i] = pr[i] ? load16(pr[i] + k, a.k - k) : u32x4{0, 0, 0, 0};
-                vq[i] = qr[i] ? load16(qr[i] + k, a.k - k) : u32x4{0, 0, 0, 0};
+                for (int i = 0; i < 4; ++i) {
+                    vp[i] = load16(pr[i] + k, 16);
+                    vq[i] = load16(qr[i] + k, 16);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    vp[i] = cut_piece(pr[i], k, n_k);
+                    vq[i] = cut_piece(qr[i], k, n_k);
+                }
             }
         };
-        load(0);
-        for (int64_t k0 = 0; k0 < a.k; k0 += SB) {
-            __syncthreads();
+        auto step = [&](int k0, int buffer) {
+            u32x4 *lp = lds + buffer * 2 * GEN_B * 8, *lq = lp + GEN_B * 8;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = (threadIdx.x + i * GEN_T) / 8, at = r * 8 + ((threadIdx.x % 8) ^ (r / 2 % 8));
@@ -129,7 +140,7 @@ __global__ __launch_bounds__(GEN_T, 2) void k_group_product_int8_any(Int8Args a)
                 lq[at] = vq[i];
             }
             __syncthreads();
-            if (k0 + SB < a.k) load(k0 + SB);
+            load(k0 + SB);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 u32x4 fp[4], fq[4];
@@ -144,6 +155,12 @@ __global__ __launch_bounds__(GEN_T, 2) void k_group_product_int8_any(Int8Args a)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) acc[i][j] = MulInt8::mul(fq[j], fp[i], acc[i][j]);
             }
+        };
+        load(0);
+        __syncthreads();  // (the last tile's reads of LDS)
+        for (int k0 = 0; k0 < n_k; k0 += 2 * SB) {
+            step(k0, 0);
+            if (k0 + SB < n_k) step(k0 + SB, 1);
         }
         const Scales<4, 4> s(a, t, n0, cols, p0, q0);
         __syncthreads();
