@@ -107,23 +107,24 @@ GM_DEV float row_scale(uint32_t most) {
 GM_DEV void store_fp8x8_by(uint8_t *p, int valid, const float (&v)[8], float inverse) {
     float r[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float x = v[i] * inverse;
-        r[i] = x > FP8_MAX ? FP8_MAX : x < -FP8_MAX ? -FP8_MAX : x;
-    }
+    for (int i = 0; i < 8; ++i) r[i] = v[i] * inverse;  // (448 and two units at most, which is 448 in E4M3)
     const uint32_t w[2] = {pack_fp8(r[0], r[1], r[2], r[3]), pack_fp8(r[4], r[5], r[6], r[7])};
     store_bytes8(p, valid, w);
 }
 
-// To the nearest integers, ties to even, at most 127 in magnitude; a NaN as 0.
+// To the nearest integers, ties to even (127 in magnitude and two units at most before that); a NaN as 0.
 GM_DEV void store_int8x8_by(uint8_t *p, int valid, const float (&v)[8], float inverse) {
-    uint32_t w[2] = {0, 0};
+    uint32_t b[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float x = __builtin_rintf(v[i] * inverse);
-        const float c = x > INT8_MAX_F ? INT8_MAX_F : x < -INT8_MAX_F ? -INT8_MAX_F : x == x ? x : 0.f;
-        w[i >> 2] |= ((uint32_t)(int)c & 0xffu) << (8 * (i & 3));
+        b[i] = (uint32_t)(int)(x == x ? x : 0.f);
     }
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)  // (the low bytes of four)
+        w[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[4 * i + 3], b[4 * i + 2], 0x0c0c0400u),
+                                     __builtin_amdgcn_perm(b[4 * i + 1], b[4 * i], 0x0c0c0400u), 0x05040100u);
     store_bytes8(p, valid, w);
 }
 

@@ -544,9 +544,10 @@ __global__ __launch_bounds__(256) void k_gate_backward(GateBackArgs a) {
 
 // ------------------------------------------------------------------- host side
 // Work groups, each of which takes rows in turns with the next one's loads on its way (and the norm's weight in
-// registers): two a CU, short rows eight. Norm with residual and E4M3 result, 16384 x 4096: 512 work groups 114 us, 1024
-// 117, 2048 118; 131072 x 256: 512 93, 2048 70.
-int64_t rows_grid(int64_t n) { return n <= 512 ? 2048 : 512; }
+// registers). Norm of 16384 x 4096: 512 work groups 51 us, 1024 44, 2048 44, with residual and E4M3 result 88, 92, 90, of
+// 8192 x 4096 30, 25, 25 and 45, 42, 42; with residual, 131072 x 256: 512 93, 2048 70. Integers, 8192 x 4096: 512 34,
+// 1024 28, 2048 23, one for each row 23, 8192 x 8192 46, 42, 41, 48.
+int64_t rows_grid(int64_t n, bool norm) { return norm && n > 512 ? 1024 : 2048; }
 constexpr int64_t BACK_UNITS = 512;   // shares of d_w
 
 int64_t back_units(int64_t t, int64_t n) {
@@ -610,7 +611,7 @@ void launch_rows(const RowArgs &a, int32_t type, hipStream_t s) {
             if constexpr (W == 0) {
                 hipLaunchKernelGGL((k_rows_long<OP, T, WHOLE>), dim3(grid_for(a.n_rows, 1, 1 << 16)), dim3(64 * LONG_W), 0, s, a);
             } else {
-                const int64_t most = OP == Op::GATE ? MAX_GRID : rows_grid(a.n);
+                const int64_t most = OP == Op::GATE ? MAX_GRID : rows_grid(a.n, OP == Op::NORM);
                 hipLaunchKernelGGL((k_rows<OP, T, W, CH, WHOLE>), dim3(grid_for(a.n_rows, W == 1 ? 4 : 1, most)),
                                    dim3(W > 4 ? 64 * W : 256), 0, s, a);
             }
