@@ -83,7 +83,7 @@ class GatedExpertLayer:
         return g.combine(y, r.row_ptr, r.slot, r.weight), n.total
 
     def serve_few(self, x: torch.Tensor, residual: torch.Tensor, weights=None):
-        """serve() for at most g.LAYER_TOKENS tokens, the experts in one call (16 bits or E4M3 weights)."""
+        """serve() for at most g.LAYER_TOKENS tokens, the experts in one call."""
         n = g.rms_norm(x, self.norm, residual=residual, eps=EPS)
         logits = n.y.float() @ self.router
         if weights is None:
@@ -126,11 +126,12 @@ def main(argv=None) -> dict:
     def off(y):
         return float((y.float() - whole).norm() / whole.norm())
 
-    fp8 = layer.quantised(torch.float8_e4m3fn)
+    fp8, int8 = layer.quantised(torch.float8_e4m3fn), layer.quantised(torch.int8)
     result = {"losses": losses, "few": off(layer.serve_few(x[:8], residual[:8])[0]),
               "few_fp8": off(layer.serve_few(x[:8], residual[:8], fp8)[0]), "fp8": off(layer.serve(x[:8], residual[:8], fp8)[0]),
-              "int8": off(layer.serve(x[:8], residual[:8], layer.quantised(torch.int8))[0])}
-    print("a few tokens in one call: %(few).1e off; with E4M3 weights %(few_fp8).1e; all in E4M3 %(fp8).1e, in integers %(int8).1e" % result)
+              "few_int8": off(layer.serve_few(x[:8], residual[:8], int8)[0]), "int8": off(layer.serve(x[:8], residual[:8], int8)[0])}
+    print("a few tokens in one call: %(few).1e off; with E4M3 weights %(few_fp8).1e, integers %(few_int8).1e; all in E4M3 "
+          "%(fp8).1e, in integers %(int8).1e" % result)
     return result
 
 

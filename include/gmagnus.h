@@ -606,12 +606,13 @@ int64_t gmagnus_expert_layer_workspace_bytes(int64_t n_tokens, int64_t n_experts
  *   OUT[t,:] = sum over the entries (t, e) of R of R[t,e] * silu(X[t,:] * G_e^T) * (X[t,:] * U_e^T) * W2_e^T
  * with R as gmagnus_route gives it from the same logits, top_k and normalise (a token
  * without entries has a row of zeros). W1 is a stack of n_experts matrices 2 inner x K,
- * G_e above U_e; W2 one of n_cols x inner. X is bf16 or fp16, W1 and W2 have its type
- * or are both E4M3 with the scales that gmagnus_quantise_blocks gives with block_rows
- * 128 (scales NULL otherwise); OUT has X's type or fp32. Sums are held in fp32, the
- * gate's result as the sum of two values of X's type (so it has X's range, and an
- * infinity past that). Of the weights only the chosen experts' are
- * read. The workspace is the call's until it has run.
+ * G_e above U_e; W2 one of n_cols x inner. X is bf16 or fp16; W1 and W2 have its type
+ * (scales NULL), or are both E4M3 with the scales that gmagnus_quantise_blocks gives
+ * with block_rows 128, or both int8 with those of gmagnus_quantise_rows. OUT has X's
+ * type or fp32. Sums are held in fp32, a gate's result as the sum of two values of
+ * X's type: it has X's range and is infinite past that, and an infinite weight of W2
+ * gives infinities or NaN. Of the weights only the chosen experts' are read. The
+ * workspace is the call's until it has run.
  * Errors: INVALID_VALUE, UNSUPPORTED (more than 64 tokens, 1024 experts or 1024
  * entries, sides above 2^31 - 1025), HIP. */
 gmagnus_status_t gmagnus_expert_layer(const gmagnus_dense_t *X, const gmagnus_dense_t *logits, int64_t top_k,

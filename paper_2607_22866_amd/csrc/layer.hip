@@ -19,7 +19,7 @@ constexpr int MAX_ENTRIES = 1024;
 struct LayerArgs {
     const void *x, *logits;
     const uint8_t *w1, *w2;
-    const float *s1, *s2;  // of E4M3 weights
+    const float *s1, *s2;  // of 8-bit weights
     void *out;
     int64_t xs, ls, w1s, w1g, s1s, s1g, w2s, w2g, s2s, s2g, os;  // (weights': in bytes)
     int n_tokens, n_experts, top_k, normalise, logit_type;
@@ -152,23 +152,42 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void k_layer_route(LayerArgs a) {
 
 // ------------------------------------------------------------------- fragments
 // A block of the reduction is 128 bytes of a row of weights: 64 values of 16 bits or
-// 128 of E4M3. A lane has 16 bytes at g and 16 at g + 4 of a row's eight pieces, S
-// fragments of 8 values each. E4M3 values are widened, exactly, to the rows' type.
-template <bool FP8, typename T>
+// 128 of 8. A lane has 16 bytes at g and 16 at g + 4 of a row's eight pieces, S
+// fragments of 8 values each. Values of 8 bits are widened, exactly, to the rows' type.
+enum Kind { SAME, FP8, INT8 };  // weights: of the rows' type, E4M3 with block scales, integers with a scale a row
+
+template <Kind KIND, typename T>
 struct Block {
-    static constexpr int S = FP8 ? 2 : 1, VALUES = FP8 ? 128 : 64, BYTES = FP8 ? 1 : 2;
+    static constexpr bool EIGHT = KIND != SAME;
+    static constexpr int S = EIGHT ? 2 : 1, VALUES = EIGHT ? 128 : 64, BYTES = EIGHT ? 1 : 2;
     static_assert(VALUES * BYTES == 128, "");
 
     GM_DEV static int first(int h, int g) { return (h * 64 + g * 16) / BYTES; }
     GM_DEV static u32x4 load(const uint8_t *p) {
-        if constexpr (FP8)
+        if constexpr (EIGHT)
             return load16(p, 16);
         else
             return load8(reinterpret_cast<const T *>(p), 8);
     }
     GM_DEV static void widen(u32x4 v, u32x4 (&f)[S]) {
-        if constexpr (!FP8) {
+        if constexpr (!EIGHT) {
             f[0] = v;
+        } else if constexpr (KIND == INT8) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t u = v[i] ^ 0x80808080u;  // value + 128
+                if constexpr (std::is_same<T, __bf16>::value) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        f[i / 2][i % 2 * 2 + k] = pack2<T>((float)(u >> (16 * k) & 0xff) - 128.f, (float)(u >> (16 * k + 8) & 0xff) - 128.f);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {  // 1024 + u as fp16 has u in its low byte
+                        const f16x2 h = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(u, 0x64006400u, k ? 0x01070106u : 0x01050104u));
+                        f[i / 2][i % 2 * 2 + k] = __builtin_bit_cast(uint32_t, h - f16x2{(_Float16)1152.f, (_Float16)1152.f});
+                    }
+                }
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -201,10 +220,10 @@ struct Block {
             for (int s = 0; s < S; ++s)
                 f[h * S + s] = cut_piece(reinterpret_cast<const uint8_t *>(row), (int64_t)(k + first(h, g) + s * 8) * 2, (int64_t)n * 2);
     }
-    // acc += weights' fragments times the rows' (of P parts), by `scale` where there is one
+    // acc += weights' fragments times the rows' (of P parts), by `scale` where blocks have one
     template <int P>
     GM_DEV static void multiply(const u32x4 (&w)[2], const u32x4 (&r)[P][2 * S], f32x4 scale, f32x4 &acc) {
-        f32x4 sum = FP8 ? f32x4{0, 0, 0, 0} : acc;
+        f32x4 sum = KIND == FP8 ? f32x4{0, 0, 0, 0} : acc;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             u32x4 f[S];
@@ -214,7 +233,7 @@ struct Block {
 #pragma unroll
                 for (int p = 0; p < P; ++p) sum = mfma_16x16x32(f[s], r[p][h * S + s], sum, T{});
         }
-        if constexpr (!FP8)
+        if constexpr (KIND != FP8)
             acc = sum;
         else
 #pragma unroll
@@ -231,10 +250,10 @@ constexpr int PITCH = 32 + 4;  // of 32 fp32 results in LDS
 // their sums are joined in LDS in the waves' order. RT: how many times 16 rows of an
 // expert are multiplied while the weights are in registers; more than those read them
 // again. ROUTE: the work group finds the routing (up to 16 tokens, four a wave).
-template <bool FP8, typename T, int RT, bool ROUTE>
+template <Kind KIND, typename T, int RT, bool ROUTE>
 __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
-    using B = Block<FP8, T>;
-    constexpr int U = RT > 1 || FP8 ? 2 : 4;
+    using B = Block<KIND, T>;
+    constexpr int U = RT > 1 || B::EIGHT ? 2 : 4;
     extern __shared__ int32_t lds_layer[];
     const int entries = a.n_tokens * a.top_k;
     const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16;
@@ -260,7 +279,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
         // a tile of U_e's rows may lie in two blocks of scales
         const float *sg = nullptr, *su = nullptr, *sv = nullptr;
         bool second[4] = {};
-        if constexpr (FP8) {
+        if constexpr (KIND == FP8) {
             const int64_t r0 = (int64_t)a.f + f0, last = min(r0 + 15, 2 * (int64_t)a.f - 1);
             sg = a.s1 + e * a.s1g + f0 / SB * a.s1s;
             su = a.s1 + e * a.s1g + r0 / SB * a.s1s;
@@ -269,7 +288,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
             for (int i = 0; i < 4; ++i) second[i] = (r0 + 4 * g + i) / SB != r0 / SB;
         }
         auto scales = [&](int kb, f32x4(&s)[2]) {
-            if constexpr (FP8) {
+            if constexpr (KIND == FP8) {
                 const float x = sg[kb], y = su[kb], z = sv[kb];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -354,6 +373,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
                     y += part[(v * RT * 16 + r) * PITCH + 16 + col];
                 }
                 if (f0 + col < a.f) {
+                    if constexpr (KIND == INT8) {
+                        x *= a.s1[e * a.s1g + f0 + col];
+                        y *= a.s1[e * a.s1g + a.f + f0 + col];
+                    }
                     const float v = gated(x, y);
                     const T top = (T)v;
                     out[r * a.act_stride + col] = top;
@@ -369,10 +392,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
 // wave's unit is U blocks of one expert's rows of W2, whose products go, times
 // the tokens' weights, into the wave's own sums in LDS. The waves' sums are added in
 // their order, and the splits' by the last of them to arrive, in theirs.
-template <bool FP8, typename T, typename OUT>
+template <Kind KIND, typename T, typename OUT>
 __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
-    using B = Block<FP8, T>;
-    constexpr int U = FP8 ? 1 : 2;
+    using B = Block<KIND, T>;
+    constexpr int U = B::EIGHT ? 1 : 2;
     extern __shared__ int32_t lds_layer[];
     const int entries = a.n_tokens * a.top_k;
     const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16;
@@ -393,7 +416,13 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
         const uint8_t *wr[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) wr[j] = a.w2 + e * a.w2g + min(q0 + 16 * j + i16, a.n - 1) * a.w2s;
-        const float *sc = FP8 ? a.s2 + e * a.s2g + q0 / SB * a.s2s : nullptr;
+        const float *sc = KIND == FP8 ? a.s2 + e * a.s2g + q0 / SB * a.s2s : nullptr;
+        f32x4 sr[2];  // of the rows of W2 that a lane has results of
+        if constexpr (KIND == INT8)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sr[j][i] = a.s2[e * a.s2g + min(q0 + 16 * j + 4 * g + i, a.n - 1)];
         auto row_at = [&](int r) { return static_cast<const T *>(a.act) + (base + min(r + i16, rows - 1)) * a.act_stride; };
         auto add = [&](int r, const f32x4(&acc)[2]) {
             if (r + i16 < rows) {
@@ -404,13 +433,13 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
                     f32x4 *p = reinterpret_cast<f32x4 *>(&mine[token * PITCH + 16 * j + 4 * g]);
                     f32x4 v = *p;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] += weight * acc[j][i];
+                    for (int i = 0; i < 4; ++i) v[i] += weight * (KIND == INT8 ? acc[j][i] * sr[j][i] : acc[j][i]);
                     *p = v;
                 }
             }
         };
         auto scale = [&](int i) {
-            const float x = FP8 ? sc[k0 / B::VALUES + i] : 0.f;
+            const float x = KIND == FP8 ? sc[k0 / B::VALUES + i] : 0.f;
             return f32x4{x, x, x, x};
         };
         if (a.f - k0 >= CHUNK) {
@@ -520,19 +549,19 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
 struct LayerLayout {
     int64_t arrived, table, act, share, bytes, act_stride;
     int splits;
-    LayerLayout(int64_t t, int64_t e, int64_t k, int64_t f, int64_t n, bool fp8) {
+    LayerLayout(int64_t t, int64_t e, int64_t k, int64_t f, int64_t n, bool eight) {
         int64_t at = 0;
         auto take = [&](int64_t bytes) {
             const int64_t here = at;
             at += (bytes + 255) / 256 * 256;
             return here;
         };
-        // Splits for two work groups a CU, of E4M3 weights for three, as many at most as there can be waves' units. The
+        // Splits for two work groups a CU, of 8-bit weights for three, as many at most as there can be waves' units. The
         // second kernel, 2048 x 1024 (outputs x inner), 16 tokens to 4 of 64 experts: 256 work groups 31 us, 512 30, 768 31,
         // 1024 35, 2048 48; 64 tokens to 6 of 64 53, 52, 55, 72, 92; E4M3, 16 tokens 23, 17, 17, 20, 30, 48 tokens to 6 of 64,
         // 2048 x 1000, 94, 58, 50, 50, 71.
         const int64_t tiles = (n + 31) / 32, used = e < t * k ? e : t * k, units = used * ((f + 127) / 128);
-        int64_t s = ((fp8 ? 768 : 512) + tiles - 1) / tiles;
+        int64_t s = ((eight ? 768 : 512) + tiles - 1) / tiles;
         if (s > (units + WAVES - 1) / WAVES) s = (units + WAVES - 1) / WAVES;
         splits = (int)s;
         act_stride = (f + 7) / 8 * 8;
@@ -556,7 +585,7 @@ using namespace gm;
 
 extern "C" int64_t gmagnus_expert_layer_workspace_bytes(int64_t n_tokens, int64_t n_experts, int64_t top_k, int64_t inner,
                                                         int64_t n_cols) {
-    // (E4M3 weights have as many splits or more)
+    // (8-bit weights have as many splits or more)
     return layer_sizes_ok(n_tokens, n_experts, top_k, inner, n_cols) ? LayerLayout(n_tokens, n_experts, top_k, inner, n_cols, true).bytes : 0;
 }
 
@@ -579,26 +608,30 @@ extern "C" gmagnus_status_t gmagnus_expert_layer(const gmagnus_dense_t *X, const
         GM_REQUIRE(e <= MAX_EXPERTS && t * top_k <= MAX_ENTRIES, GMAGNUS_ERROR_UNSUPPORTED, "more than 1024 experts or entries");
         check_dense(X, "X", t, d);
         check_dense(logits, "logits", t, e);
-        check_dense(W1, "W1", 2 * f, d, e);
-        check_dense(W2, "W2", n, f, e);
+        check_dense(W1, "W1", 2 * f, d, e, GMAGNUS_DATA_INT8);
+        check_dense(W2, "W2", n, f, e, GMAGNUS_DATA_INT8);
         check_dense(OUT, "OUT", t, n);
         GM_REQUIRE(X->data_type == GMAGNUS_DATA_BF16 || X->data_type == GMAGNUS_DATA_FP16, GMAGNUS_ERROR_INVALID_VALUE,
                    "X must be bf16 or fp16");
         GM_REQUIRE(is_float(logits->data_type), GMAGNUS_ERROR_INVALID_VALUE, "logits must be fp32, bf16 or fp16");
         GM_REQUIRE(OUT->data_type == X->data_type || OUT->data_type == GMAGNUS_DATA_FP32, GMAGNUS_ERROR_INVALID_VALUE,
                    "OUT must have the type of X, or fp32");
-        const bool fp8 = W1->data_type == GMAGNUS_DATA_FP8_E4M3;
-        GM_REQUIRE(W1->data_type == W2->data_type && (fp8 || W1->data_type == X->data_type), GMAGNUS_ERROR_INVALID_VALUE,
-                   "W1 and W2 must both have the type of X, or both be E4M3");
-        GM_REQUIRE(!W1_scale == !fp8 && !W2_scale == !fp8, GMAGNUS_ERROR_INVALID_VALUE, "E4M3 weights have scales, others none");
-        if (fp8) {
+        const Kind kind = W1->data_type == GMAGNUS_DATA_FP8_E4M3 ? FP8 : W1->data_type == GMAGNUS_DATA_INT8 ? INT8 : SAME;
+        GM_REQUIRE(W1->data_type == W2->data_type && (kind != SAME || W1->data_type == X->data_type), GMAGNUS_ERROR_INVALID_VALUE,
+                   "W1 and W2 must both have the type of X, both be E4M3 or both int8");
+        GM_REQUIRE(!W1_scale == (kind == SAME) && !W2_scale == (kind == SAME), GMAGNUS_ERROR_INVALID_VALUE,
+                   "8-bit weights have scales, others none");
+        if (kind == FP8) {
             check_dense(W1_scale, "W1_scale", (2 * f + SB - 1) / SB, (d + SB - 1) / SB, e);
             check_dense(W2_scale, "W2_scale", (n + SB - 1) / SB, (f + SB - 1) / SB, e);
-            GM_REQUIRE(W1_scale->data_type == GMAGNUS_DATA_FP32 && W2_scale->data_type == GMAGNUS_DATA_FP32,
-                       GMAGNUS_ERROR_INVALID_VALUE, "scales must be fp32");
+        } else if (kind == INT8) {
+            check_dense(W1_scale, "W1_scale", e, 2 * f);
+            check_dense(W2_scale, "W2_scale", e, n);
         }
+        GM_REQUIRE(kind == SAME || (W1_scale->data_type == GMAGNUS_DATA_FP32 && W2_scale->data_type == GMAGNUS_DATA_FP32),
+                   GMAGNUS_ERROR_INVALID_VALUE, "scales must be fp32");
         if (t == 0) return;
-        const LayerLayout l(t, e, top_k, f, n, fp8);
+        const LayerLayout l(t, e, top_k, f, n, kind != SAME);
         GM_REQUIRE(workspace && workspace_bytes >= l.bytes, GMAGNUS_ERROR_INVALID_VALUE,
                    "workspace below gmagnus_expert_layer_workspace_bytes");
         GM_REQUIRE((uintptr_t)workspace % 16 == 0, GMAGNUS_ERROR_INVALID_VALUE, "workspace is not 16-byte aligned");
@@ -606,15 +639,17 @@ extern "C" gmagnus_status_t gmagnus_expert_layer(const gmagnus_dense_t *X, const
         GM_REQUIRE(tiles * l.splits < INT32_MAX && used * ((f + 127) / 128) < INT32_MAX / 2, GMAGNUS_ERROR_UNSUPPORTED,
                    "2^31 tiles or 2^30 units of the reduction or more");
         char *ws = static_cast<char *>(workspace);
-        const int size = fp8 ? 1 : 2;
+        const int size = kind == SAME ? 2 : 1;
+        // (integers' scales: a row an expert)
+        auto rows_of = [&](const gmagnus_dense_t *m) { return kind == FP8 ? m->row_stride : 0; };
+        auto stack_of = [&](const gmagnus_dense_t *m) { return kind == FP8 ? m->stack_stride : kind == INT8 ? m->row_stride : 0; };
         const LayerArgs a{X->data, logits->data, (const uint8_t *)W1->data, (const uint8_t *)W2->data,
-                          fp8 ? (const float *)W1_scale->data : nullptr, fp8 ? (const float *)W2_scale->data : nullptr, OUT->data,
-                          X->row_stride, logits->row_stride, W1->row_stride * size, W1->stack_stride * size,
-                          fp8 ? W1_scale->row_stride : 0, fp8 ? W1_scale->stack_stride : 0, W2->row_stride * size,
-                          W2->stack_stride * size, fp8 ? W2_scale->row_stride : 0, fp8 ? W2_scale->stack_stride : 0,
-                          OUT->row_stride, (int)t, (int)e, (int)top_k, normalise, logits->data_type, (int)d, (int)f, (int)n,
-                          l.splits, (int32_t *)(ws + l.arrived), (int32_t *)(ws + l.table), ws + l.act, (float *)(ws + l.share),
-                          l.act_stride, entries * l.act_stride};
+                          kind == SAME ? nullptr : (const float *)W1_scale->data, kind == SAME ? nullptr : (const float *)W2_scale->data,
+                          OUT->data, X->row_stride, logits->row_stride, W1->row_stride * size, W1->stack_stride * size,
+                          rows_of(W1_scale), stack_of(W1_scale), W2->row_stride * size, W2->stack_stride * size, rows_of(W2_scale),
+                          stack_of(W2_scale), OUT->row_stride, (int)t, (int)e, (int)top_k, normalise, logits->data_type, (int)d,
+                          (int)f, (int)n, l.splits, (int32_t *)(ws + l.arrived), (int32_t *)(ws + l.table), ws + l.act,
+                          (float *)(ws + l.share), l.act_stride, entries * l.act_stride};
         hipStream_t s = (hipStream_t)hip_stream;
         const int64_t items = used * ((f + 15) / 16);
         auto go = [&](auto kernel, int64_t grid, int threads, int words) {
@@ -625,23 +660,30 @@ extern "C" gmagnus_status_t gmagnus_expert_layer(const gmagnus_dense_t *X, const
         const int route = (route_words((int)entries, (int)e) + 3) / 4 * 4, table = (table_words((int)entries) + 3) / 4 * 4;
         auto both = [&](auto v, auto w) {
             using T = decltype(v);
-            constexpr bool FP8 = decltype(w)::value;
+            constexpr Kind KIND = decltype(w)::value;
             const int64_t grid = items < 1024 ? items : 1024;
             if (t <= 16) {
-                go(k_layer_up<FP8, T, 1, true>, grid, 64 * WAVES, route + WAVES * 16 * PITCH);
+                go(k_layer_up<KIND, T, 1, true>, grid, 64 * WAVES, route + WAVES * 16 * PITCH);
             } else {
                 go(k_layer_route, 1, 64 * ROUTE_WAVES, route);
-                go(k_layer_up<FP8, T, 2, false>, grid, 64 * WAVES, table + WAVES * 32 * PITCH);
+                go(k_layer_up<KIND, T, 2, false>, grid, 64 * WAVES, table + WAVES * 32 * PITCH);
             }
             if (OUT->data_type == GMAGNUS_DATA_FP32)
-                go(k_layer_down<FP8, T, float>, tiles * l.splits, 64 * WAVES, table + WAVES * (int)t * PITCH);
+                go(k_layer_down<KIND, T, float>, tiles * l.splits, 64 * WAVES, table + WAVES * (int)t * PITCH);
             else
-                go(k_layer_down<FP8, T, T>, tiles * l.splits, 64 * WAVES, table + WAVES * (int)t * PITCH);
+                go(k_layer_down<KIND, T, T>, tiles * l.splits, 64 * WAVES, table + WAVES * (int)t * PITCH);
         };
-        if (X->data_type == GMAGNUS_DATA_BF16) {
-            if (fp8) both(__bf16{}, std::true_type{}); else both(__bf16{}, std::false_type{});
-        } else {
-            if (fp8) both(_Float16{}, std::true_type{}); else both(_Float16{}, std::false_type{});
-        }
+        auto any = [&](auto v) {
+            if (kind == FP8)
+                both(v, std::integral_constant<Kind, FP8>{});
+            else if (kind == INT8)
+                both(v, std::integral_constant<Kind, INT8>{});
+            else
+                both(v, std::integral_constant<Kind, SAME>{});
+        };
+        if (X->data_type == GMAGNUS_DATA_BF16)
+            any(__bf16{});
+        else
+            any(_Float16{});
     });
 }

@@ -964,11 +964,14 @@ def expert_layer(x: torch.Tensor, logits: torch.Tensor, top_k: int, w1: torch.Te
                  out_dtype=None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """A whole layer of gated experts for at most LAYER_TOKENS tokens: with the entries (t, e) that route gives for the
     logits, out[t] = sum of weight * (silu(g) * u) @ w2[e].T where [g | u] = x[t] @ w1[e].T. bfloat16 or float16; w1 and
-    w2 may both be float8_e4m3fn with the scales of quantise_blocks(w, 128). out_dtype: x's type or float32."""
+    w2 may both be float8_e4m3fn with the scales of quantise_blocks(w, 128), or int8 with those of quantise_rows(w).
+    out_dtype: x's type or float32."""
     dev = _device_of(x, "x")
-    dx, dl, d1, d2 = _dense(x, dev, "x"), _dense(logits, dev, "logits"), _dense(w1, dev, "w1", 3), _dense(w2, dev, "w2", 3)
-    s1 = None if w1_scale is None else _dense(w1_scale, dev, "w1_scale", 3)
-    s2 = None if w2_scale is None else _dense(w2_scale, dev, "w2_scale", 3)
+    dx, dl = _dense(x, dev, "x"), _dense(logits, dev, "logits")
+    d1, d2 = _dense(w1, dev, "w1", 3, int8=True), _dense(w2, dev, "w2", 3, int8=True)
+    dims = 2 if w1.dtype == torch.int8 else 3
+    s1 = None if w1_scale is None else _dense(w1_scale, dev, "w1_scale", dims)
+    s2 = None if w2_scale is None else _dense(w2_scale, dev, "w2_scale", dims)
     t, e = logits.shape
     if any(w is not None and w.shape[0] != e for w in (w1, w2, w1_scale, w2_scale)):
         raise ValueError("w1, w2 and their scales must have one matrix an expert")

@@ -13,8 +13,14 @@ def fp8(**kw):
     return dict(dict(w1=dense(300, 200, FP8), s1=dense(3, 2, F32), w2=dense(96, 150, FP8), s2=dense(1, 2, F32)), **kw)
 
 
+def int8(**kw):
+    return dict(dict(w1=dense(300, 200, INT8), s1=dense(8, 300, F32), w2=dense(96, 150, INT8), s2=dense(8, 96, F32)), **kw)
+
+
 @pytest.mark.parametrize("status,kw", [
-    (INVALID, dict(x=None)), (INVALID, dict(logits=None)), (INVALID, dict(w1=None)), (INVALID, dict(w2=None)), (INVALID, dict(out=None)),
+    (INVALID, int8(s1=None)), (INVALID, int8(s2=None)), (INVALID, int8(s1=dense(3, 2, F32))), (INVALID, int8(s1=dense(7, 300, F32))),
+    (INVALID, int8(s2=dense(8, 96, BF16))), (INVALID, int8(w2=dense(96, 150, FP8))), (INVALID, int8(w1=dense(300, 200))),
+    (INVALID, int8(ws=None)), (INVALID, dict(x=None)), (INVALID, dict(logits=None)), (INVALID, dict(w1=None)), (INVALID, dict(w2=None)), (INVALID, dict(out=None)),
     (INVALID, dict(top_k=0)), (INVALID, dict(top_k=9)), (INVALID, dict(normalise=2)), (INVALID, dict(logits=dense(4, 8, F32))),
     (INVALID, dict(logits=dense(5, 8, FP8))), (INVALID, dict(x=dense(5, 200, F32))), (INVALID, dict(x=dense(5, 200, F16))),
     (INVALID, dict(w1=dense(299, 200))), (INVALID, dict(w1=dense(300, 199))), (INVALID, dict(w1=dense(300, 200, INT8))),

@@ -29,9 +29,11 @@ def rand(shape, dtype, seed, scale=1.0):
     return (torch.randn(shape, generator=gen) * scale).to(dtype).cuda()
 
 
-def values(w, scale):
+def dequantised(w, scale):
     if scale is None:
         return w.double()
+    if w.dtype == torch.int8:
+        return w.double() * scale.double()[..., None]
     n, k = w.shape[-2:]
     return w.double() * scale.double().repeat_interleave(128, -2).repeat_interleave(128, -1)[..., :n, :k]
 
@@ -75,7 +77,7 @@ class Stack:
         self.w, self.scale, self.shape = w, scale, w.shape
 
     def __call__(self, e):
-        return values(self.w[e], None if self.scale is None else self.scale[e])
+        return dequantised(self.w[e], None if self.scale is None else self.scale[e])
 
 
 def check(g, x, logits, top_k, w1, w2, normalise=True, s1=None, s2=None, out_dtype=None, **kw):
@@ -119,6 +121,41 @@ def test_e4m3_weights(g, t, e, k, d, f, n, dtype):
     (q1, s1), (q2, s2) = g.quantise_blocks(w1, 128), g.quantise_blocks(w2, 128)
     check(g, x, logits, k, q1, q2, s1=s1, s2=s2)
     check(g, x, logits, k, q1, q2, s1=s1, s2=s2, normalise=False, out_dtype=torch.float32)
+
+
+@pytest.mark.parametrize("t,e,k,d,f,n", SIZES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_integer_weights(g, t, e, k, d, f, n, dtype):
+    x, logits, w1, w2 = case(t, e, d, f, n, dtype, fp8=True)
+    (q1, s1), (q2, s2) = g.quantise_rows(w1), g.quantise_rows(w2)
+    check(g, x, logits, k, q1, q2, s1=s1, s2=s2)
+    check(g, x, logits, k, q1, q2, s1=s1, s2=s2, normalise=False, out_dtype=torch.float32)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_every_integer_and_every_e4m3_value_is_widened_exactly(g, dtype):
+    # one expert, a gate of one (silu(g) is g to a unit at g = 24): each result is a weight of W2 times what the gate gives
+    x = torch.ones((1, 16), dtype=dtype, device="cuda")
+    values = torch.arange(256, dtype=torch.uint8, device="cuda")
+    gate = torch.zeros((2 * 256, 16), device="cuda")
+    gate[:256, 0], gate[256:, 0] = 24.0, 1.0 / 24.0
+    one = torch.zeros((1, 1), device="cuda")
+    # W2 has row i with value i at place i
+    for kind in (torch.int8, torch.float8_e4m3fn):
+        w2 = torch.zeros((1, 256, 256), dtype=torch.uint8, device="cuda")
+        w2[0].diagonal().copy_(values)
+        w2 = w2.view(kind)
+        if kind is torch.int8:
+            (q1, s1), s2 = g.quantise_rows(gate[None]), torch.ones((1, 256), device="cuda")
+        else:
+            (q1, s1), s2 = g.quantise_blocks(gate[None], 128), torch.ones((1, 2, 2), device="cuda")
+        want = w2[0].double().diagonal()
+        h = dequantised(q1, s1)[0] @ x[0].double()
+        unit = (h[:256] * torch.sigmoid(h[:256]) * h[256:])
+        y = g.expert_layer(x, one, 1, q1, w2, w1_scale=s1, w2_scale=s2, out_dtype=torch.float32)[0].double()
+        nan = torch.isnan(want)  # (a NaN of E4M3 makes its own result NaN)
+        assert torch.equal(torch.isnan(y), nan)
+        assert bool(((y - want * unit).abs() <= 40 * 2.0 ** -24 * (want * unit).abs() + rr.half_step(dtype) ** 2 * want.abs())[~nan].all())
 
 
 @pytest.mark.parametrize("fp8", [False, True])
@@ -258,7 +295,9 @@ def test_no_tokens_and_refusals(g):
                  lambda: g.expert_layer(x, logits, 2, w1, w2, w1_scale=s1, w2_scale=s2),
                  lambda: g.expert_layer(x, logits, 2, q1, q2, w1_scale=s1, w2_scale=s2.half()),
                  lambda: g.expert_layer(x.float(), logits, 2, w1.float(), w2.float()),
-                 lambda: g.expert_layer(x, logits, 2, w1, w2, out_dtype=torch.float16)):
+                 lambda: g.expert_layer(x, logits, 2, w1, w2, out_dtype=torch.float16),
+                 lambda: g.expert_layer(x, logits, 2, *(g.quantise_rows(w)[0] for w in (w1, w2))),
+                 lambda: g.expert_layer(x, logits, 2, g.quantise_rows(w1)[0], q2, w1_scale=g.quantise_rows(w1)[1], w2_scale=g.quantise_rows(w2)[1])):
         with pytest.raises(g.GmagnusError) as err:
             call()
         assert err.value.status == 1

@@ -84,6 +84,7 @@ def test_serving_forms(ex, tokens, experts, k, hidden, inner):
     # values of E4M3 are off by 2^-4 at most, 2^-4 / sqrt(3) a value as they come: rows, W1, gate, W2 and the two halves of a product
     assert off(layer.serve_few(x, residual, fp8)[0], want) <= 4 * 2.0 ** -4
     assert off(layer.serve(x, residual, fp8)[0], want) <= 6 * 2.0 ** -4
+    assert off(layer.serve_few(x, residual, int8)[0], want) <= 3 * 4 / 254 + 4 * 2.0 ** -8  # (weights: W1 twice, W2)
     # integers: half a step is 1 / 254 of a row's largest, four times its mean square root at most here
     assert off(layer.serve(x, residual, int8)[0], want) <= 6 * 4 / 254 + 7 * 2.0 ** -8
 
