@@ -409,8 +409,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
     const int n_used = __builtin_amdgcn_readfirstlane(*t.n);
     constexpr int CHUNK = U * B::VALUES;
     const int per = (a.f + CHUNK - 1) / CHUNK;
+    // (an expert's units begin elsewhere with each turn: the last ones of rows that end inside a unit take longer)
+    const int turns = max(1, a.splits * WAVES / per);
     for (int unit = split * WAVES + w; unit < n_used * per; unit += a.splits * WAVES) {
-        const int u = unit / per, k0 = (unit - u * per) * CHUNK;
+        const int u = unit / per, k0 = (unit - u * per + u / turns) % per * CHUNK;
         const int e = __builtin_amdgcn_readfirstlane(t.expert[u]), base = __builtin_amdgcn_readfirstlane(t.first[u]);
         const int rows = __builtin_amdgcn_readfirstlane(t.first[u + 1]) - base;
         const uint8_t *wr[2];

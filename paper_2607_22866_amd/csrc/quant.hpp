@@ -66,32 +66,30 @@ GM_DEV u32x4 load16(const uint8_t *p, int64_t valid) {
     return r;
 }
 
-// The 16 bytes at `at` of a row of n bytes, zeros past its end, where nothing is read: the row's last 16 bytes,
-// moved down. (Element by element they would take more registers than all else in the kernels
-// that use this.)
+// The 16 bytes at `at` of a row of n bytes, zeros past its end, where nothing is read: the row's last 16 bytes where
+// these would pass it, moved down. (Element by element they would take more registers than all else in the kernels
+// that use this; a branch on what is there would wait for each load.)
 GM_DEV u32x4 cut_piece(const uint8_t *row, int64_t at, int64_t n) {
-    u32x4 r = {0, 0, 0, 0};
-    const int64_t there = n - at;
-    if (there <= 0) return r;
     if (n >= 16) {
-        const int move = there < 16 ? 16 - (int)there : 0;
-        const Bytes16<1> b = *reinterpret_cast<const Bytes16<1> *>(row + at - move);
-        const bool two = move & 8, one = move & 4;
+        const int64_t from = at < n - 16 ? at : n - 16, past = at - from;
+        const int move = past < 16 ? (int)past : 16;
+        const Bytes16<1> b = *reinterpret_cast<const Bytes16<1> *>(row + from);
+        const bool all = move & 16, two = move & 8, one = move & 4;
         const uint32_t c[4] = {two ? b.v[2] : b.v[0], two ? b.v[3] : b.v[1], two ? 0 : b.v[2], two ? 0 : b.v[3]};
         const uint32_t d[5] = {one ? c[1] : c[0], one ? c[2] : c[1], one ? c[3] : c[2], one ? 0 : c[3], 0};
+        u32x4 r;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_alignbyte(d[i + 1], d[i], move & 3);
-    } else {  // (a row of less than a piece)
-        uint64_t v[2] = {0, 0};
-#pragma unroll 1
-        for (int i = 0; i < (int)there; ++i) {
-            const uint64_t x = (uint64_t)row[at + i] << (8 * (i & 7));
-            v[0] |= i < 8 ? x : 0;
-            v[1] |= i < 8 ? 0 : x;
-        }
-        r = u32x4{(uint32_t)v[0], (uint32_t)(v[0] >> 32), (uint32_t)v[1], (uint32_t)(v[1] >> 32)};
+        for (int i = 0; i < 4; ++i) r[i] = all ? 0u : __builtin_amdgcn_alignbyte(d[i + 1], d[i], move & 3);
+        return r;
     }
-    return r;
+    uint64_t v[2] = {0, 0};  // (a row of less than a piece)
+#pragma unroll 1
+    for (int i = 0; i < (int)(n - at); ++i) {
+        const uint64_t x = (uint64_t)row[at + i] << (8 * (i & 7));
+        v[0] |= i < 8 ? x : 0;
+        v[1] |= i < 8 ? 0 : x;
+    }
+    return u32x4{(uint32_t)v[0], (uint32_t)(v[0] >> 32), (uint32_t)v[1], (uint32_t)(v[1] >> 32)};
 }
 
 // The scale of a row of 8-bit integers.
