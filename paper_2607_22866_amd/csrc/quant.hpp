@@ -110,12 +110,15 @@ GM_DEV void store_fp8x8_by(uint8_t *p, int valid, const float (&v)[8], float inv
     store_bytes8(p, valid, w);
 }
 
-// To the nearest integers, ties to even (127 in magnitude and two units at most before that); a NaN as 0.
-GM_DEV void store_int8x8_by(uint8_t *p, int valid, const float (&v)[8], float inverse) {
+// To the nearest integers, ties to even; a NaN as 0. Steps are as wide as values are near a tie here, so the quotient is
+// corrected by what it leaves of x, which makes it x / scale rounded. (127 in magnitude and a unit at most before that.
+// An infinite scale, whose inverse is 0, corrects nothing: 0 and NaN, as the division gives.)
+GM_DEV void store_int8x8_by(uint8_t *p, int valid, const float (&v)[8], float scale, float inverse) {
     uint32_t b[8];
+    if (inverse == 0.f) scale = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float x = __builtin_rintf(v[i] * inverse);
+        const float q = v[i] * inverse, x = __builtin_rintf(__builtin_fmaf(__builtin_fmaf(-q, scale, v[i]), inverse, q));
         b[i] = (uint32_t)(int)(x == x ? x : 0.f);
     }
     uint32_t w[2];

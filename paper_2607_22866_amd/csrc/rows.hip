@@ -190,7 +190,7 @@ GM_DEV void load_piece(const RowArgs &a, const T *x, int64_t row, int64_t c, int
 
 // Eight columns of the results; E4M3: 16 lanes hold a block of 128.
 template <bool WHOLE, typename T>
-GM_DEV void store_piece(const RowArgs &a, const Place &at, int64_t row, int64_t c, int valid, const float (&v)[8], float inverse) {
+GM_DEV void store_piece(const RowArgs &a, const Place &at, int64_t row, int64_t c, int valid, const float (&v)[8], float scale, float inverse) {
     if (a.y) store<WHOLE>(static_cast<T *>(a.y) + row * a.ys + c, valid, v);
     uint8_t *q = a.q + at.g * a.qg + at.r * a.qs + c;
     if (a.format == E4M3) {
@@ -203,7 +203,7 @@ GM_DEV void store_piece(const RowArgs &a, const Place &at, int64_t row, int64_t 
             if (threadIdx.x % 16 == 0) a.scale[row * a.ss + c / SB] = s;
         }
     } else if (a.format == INTEGER) {
-        if (valid > 0) store_int8x8_by(q, WHOLE ? 8 : valid, v, inverse);
+        if (valid > 0) store_int8x8_by(q, WHOLE ? 8 : valid, v, scale, inverse);
     }
 }
 
@@ -268,19 +268,19 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void k_rows(RowArgs a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[j][i] = i < valid[j] ? v[j][i] * r * w[j][i] : 0.f;
         }
-        float inverse = 0.f;
+        float scale = 0.f, inverse = 0.f;
         if (a.format == INTEGER) {
             uint32_t m = 0;
 #pragma unroll
             for (int j = 0; j < CH; ++j)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[j][i]));
-            const float scale = row_scale(join.most(m));
+            scale = row_scale(join.most(m));
             inverse = 1.f / scale;
             if (t == 0) a.scale[at.g * a.sg + at.r] = scale;
         }
 #pragma unroll
-        for (int j = 0; j < CH; ++j) store_piece<WHOLE, T>(a, at, row, (j * W * 64 + t) * 8, valid[j], v[j], inverse);
+        for (int j = 0; j < CH; ++j) store_piece<WHOLE, T>(a, at, row, (j * W * 64 + t) * 8, valid[j], v[j], scale, inverse);
     }
 }
 
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(64 * LONG_W) void k_rows_long(RowArgs a) {
     for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
         const Place at(a, row);
         const T *x = static_cast<const T *>(a.x) + at.g * a.xg + at.r * a.xs;
-        float v[8], w[8], r = 0.f, inverse = 0.f;
+        float v[8], w[8], r = 0.f, scale = 0.f, inverse = 0.f;
         if constexpr (OP == Op::NORM) {
             float s = 0.f;
             for (int64_t c0 = 0; c0 < a.n; c0 += STEP) {
@@ -324,7 +324,7 @@ __global__ __launch_bounds__(64 * LONG_W) void k_rows_long(RowArgs a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
             }
-            const float scale = row_scale(join.most(m));
+            scale = row_scale(join.most(m));
             inverse = 1.f / scale;
             if (threadIdx.x == 0) a.scale[at.g * a.sg + at.r] = scale;
         }
@@ -332,7 +332,7 @@ __global__ __launch_bounds__(64 * LONG_W) void k_rows_long(RowArgs a) {
             const int64_t c = c0 + threadIdx.x * 8;
             const int valid = columns_left(a.n, c);
             piece(c, valid);
-            store_piece<WHOLE, T>(a, at, row, c, valid, v, inverse);
+            store_piece<WHOLE, T>(a, at, row, c, valid, v, scale, inverse);
         }
     }
 }
