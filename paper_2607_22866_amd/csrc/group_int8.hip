@@ -170,9 +170,9 @@ __global__ __launch_bounds__(GEN_T, 2) void k_group_product_int8_any(Int8Args a)
 }
 
 // Tiles brought straight from memory into LDS, as the 16-bit products have them (tile.hpp). One group of 8192 x 8192 x
-// 8192 480 us, 2290 TOP/s (of zeros, which draw less power, 3120); 16 groups of 1024 rows, 4096 x 4096, 258-269 us, 2040-2130,
+// 8192 480 us, 2290 TOP/s (of zeros 3120); 16 groups of 1024 rows, 4096 x 4096, 258-269 us, 2040-2130,
 // cut by chance 297-312: the matrix units are busy 53 % of the cycles in which a CU has work, and CUs have none in 15 %
-// of the time, at the end.
+// of the time.
 template <typename OUT, int BP, int BQ, int WP, int WQ>
 GM_DEV void tile_int8_fast(const Int8Args &a, const RowTile &t, int64_t n0, int cols, char *lds) {
     const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));

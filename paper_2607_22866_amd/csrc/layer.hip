@@ -142,7 +142,7 @@ GM_DEV void begin_second(const LayerArgs &a, const int32_t *table) {
 }
 
 // More than 16 tokens: the routing by one work group, four tokens a wave. (In every work group of the next
-// kernel it would take up to 16 a wave: 48 tokens 85 us instead of 6 and 56.)
+// kernel it would take up to 16 a wave.)
 constexpr int ROUTE_WAVES = 16;
 __global__ __launch_bounds__(64 * ROUTE_WAVES) void k_layer_route(LayerArgs a) {
     extern __shared__ int32_t lds_layer[];
@@ -251,10 +251,9 @@ constexpr int PITCH = 32 + 4;  // of 32 fp32 results in LDS
 // expert are multiplied while the weights are in registers; more than those read them
 // again. ROUTE: the work group finds the routing (up to 16 tokens, four a wave).
 // Bound by the weights' bytes: 16 tokens to 4 of 64 experts, 2048 to 1024 (344 MB), 60 us,
-// 5.7 TB/s; 64 tokens to 6 of 64 (537 MB) 99; 48 tokens, E4M3, 2048 to 1000 (262 MB) 54.
+// 5.7 TB/s; 64 tokens to 6 of 64 (537 MB) 99; 48 tokens to 6 of 55, E4M3, 2048 to 1000 (224 MB) 54.
 // One token to 2 of 16, 1024 to 2048 (17 MB), 7.8 us: latency of the routing and of one
-// round of loads. (A wave with whole rows to itself: 82 us for 60, its 16 rows' lines come
-// one after the other; four blocks in flight above 16 tokens 147 for 99, registers.)
+// round of loads. (A wave with whole rows to itself, when the kernel took 65: 82 us.)
 template <Kind KIND, typename T, int RT, bool ROUTE>
 __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
     using B = Block<KIND, T>;
@@ -397,7 +396,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
 // wave's unit is U blocks of one expert's rows of W2, whose products go, times
 // the tokens' weights, into the wave's own sums in LDS. The waves' sums are added in
 // their order, and the splits' by the last of them to arrive, in theirs. The sizes above:
-// 31 us (5.5 TB/s), 52, 44 (2.9: rows of 1000 bytes lie across lines, and end inside a block),
+// 31 us (5.5 TB/s), 52-55, 44 (2.5: rows of 1000 bytes lie across lines, 135 MB come for 112),
 // one token 6.4.
 template <Kind KIND, typename T, typename OUT>
 __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
