@@ -99,9 +99,9 @@ GM_DEV float row_scale(uint32_t most) {
 }
 
 // The same roundings by 1 / scale, which costs a division for eight values rather than for each: the quotient is off by
-// two units of 2^-24 and may fall on the other side of a tie that it is that near to, which 1.4 of a million
-// values of a gate's result do, as many as by exact quotients (those come out of fp32 themselves); the kernel takes 64 us
-// for 32768 x 2048, 67 with a correction of the quotient. (Infinite scales give 0 and NaN as the division does.)
+// two units of 2^-24 and may fall on the other side of a tie that it is that near to, which 1.1 to 1.5 of a
+// million values of a gate's result do, as many as by exact quotients (those come out of fp32 themselves); the kernel took
+// 64 us for 32768 x 2048, 66 with a correction of the quotient. (Infinite scales give 0 and NaN as the division does.)
 GM_DEV void store_fp8x8_by(uint8_t *p, int valid, const float (&v)[8], float inverse) {
     float r[8];
 #pragma unroll

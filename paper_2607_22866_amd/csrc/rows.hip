@@ -207,8 +207,10 @@ GM_DEV void store_piece(const RowArgs &a, const Place &at, int64_t row, int64_t 
     }
 }
 
-// Bound by its bytes. Norm of 16384 x 4096 bf16 with residual, its sum and its results in bf16 and E4M3 114-118 us (5.1-5.3
-// TB/s; without the next row on its way 120), without residual to bf16 44 us (6.1), to E4M3 alone 47 (4.3); gate of 32768 x 2048 to E4M3 61 us (5.5), 9001 x 1365 fp16 21 us (3.5); integers of 8192 x 4096 22 us (4.6), of 65536 x 777 50 (3.0). One row of 4096 with all results 3.5 us.
+// Bound by its bytes. Norm of 16384 x 4096 bf16 with residual, its sum and its results in bf16 and E4M3 114-118 us
+// (5.1-5.3 TB/s; without the next row on its way 120), without residual to bf16 44 us (6.1), to E4M3 alone 47
+// (4.3); gate of 32768 x 2048 to E4M3 61 us (5.5), 9001 x 1365 fp16 21 us (3.5); integers of 8192 x 4096 22 us
+// (4.6), of 65536 x 777 50 (3.0). One row of 4096 with all results 3.5 us.
 template <Op OP, typename T, int W, int CH, bool WHOLE>
 __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void k_rows(RowArgs a) {
     constexpr int PER = W == 1 ? 4 : 1;  // rows of a work group

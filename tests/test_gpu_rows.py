@@ -188,6 +188,31 @@ def test_ties_go_to_even(g):
     assert float(s[0]) == 1.0 and q[0].tolist() == [127, 0, 2, 2, 0, -2, -2, 126]
 
 
+@pytest.mark.parametrize("n", [8, 300, 4097, 20001])
+def test_integers_at_the_ends_of_fp32(g, n):
+    x = rand((6, n), torch.float32, n)
+    x /= x.abs().amax(1, keepdim=True)
+    top = torch.tensor([torch.finfo(torch.float32).max, 2.0 ** -118, 2.0 ** -120, 2.0 ** -126, 2.0 ** -130, 2.0 ** -149], device="cuda")
+    x *= top[:, None]
+    q, s = g.quantise_rows(x)
+    want = x.double().cpu()
+    rr.check_int8(q.cpu(), s.cpu(), want, torch.zeros_like(want))
+    assert bool((s[2:] == 2.0 ** -126).all())
+
+
+@pytest.mark.parametrize("n", [8, 300, 4097, 20001])
+@pytest.mark.parametrize("top", [3e37, 1e-35, 1e-38, 1e-41])
+def test_8_bit_results_at_the_ends_of_fp32(g, n, top):
+    """Values stay below 10 times the weight. Among subnormals a rounding takes 2^-150, here two: 2^-149, and 2^-148 counted."""
+    x = rand((5, n), torch.float32, n)
+    w = torch.full((n,), top, device="cuda")
+    want = rr.rms_norm(x.cpu(), w.cpu(), EPS)
+    assert float(want.abs().max()) < 10 * top
+    error = rr.rms_norm_error(want, n) + 2.0 ** -148
+    for quantise in (torch.int8, torch.float8_e4m3fn):
+        check_results(g.rms_norm(x, w, eps=EPS, quantise=quantise, plain=True), want, error, torch.float32, quantise, True)
+
+
 @pytest.mark.parametrize("off", [1, 3, 8])
 @pytest.mark.parametrize("n", [200, 777, 4099])
 def test_strided_and_unaligned_rows(g, n, off):
