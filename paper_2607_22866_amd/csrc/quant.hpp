@@ -98,14 +98,30 @@ GM_DEV float row_scale(uint32_t most) {
     return s < SCALE_MIN ? SCALE_MIN : s;  // (a NaN stays)
 }
 
-// The same roundings by 1 / scale, which costs a division for eight values rather than for each: the quotient is off by
-// two units of 2^-24 and may fall on the other side of a tie that it is that near to, which 1.1 to 1.5 of a
-// million values of a gate's result do, as many as by exact quotients (those come out of fp32 themselves); the kernel took
-// 64 us for 32768 x 2048, 66 with a correction of the quotient. (Infinite scales give 0 and NaN as the division does.)
-GM_DEV void store_fp8x8_by(uint8_t *p, int valid, const float (&v)[8], float inverse) {
-    float r[8];
+// v / scale as the division rounds it, by 1 / scale, which costs a division for eight values rather than for each: the
+// quotient is corrected by what it leaves of v. (That makes it the division's at all quotients near an odd multiple of
+// 2^-7 times a power of two, where 8-bit roundings have their borders: computed for every scale's mantissa and the
+// seven values around each. Uncorrected it lies on the other side of the border at one in twelve of these. Of a
+// scale below 2^-90 what is left of v may pass the end of fp32. An infinite scale, whose inverse is 0, corrects nothing:
+// 0 and NaN, as the division gives.)
+GM_DEV void quotients(const float (&v)[8], float scale, float inverse, float (&r)[8]) {
+    if (scale < 0x1p-90f) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = v[i] * inverse;  // (448 and two units at most, which is 448 in E4M3)
+        for (int i = 0; i < 8; ++i) r[i] = v[i] / scale;
+    } else {
+        const float s = inverse == 0.f ? 0.f : scale;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float q = v[i] * inverse;
+            r[i] = __builtin_fmaf(__builtin_fmaf(-q, s, v[i]), inverse, q);
+        }
+    }
+}
+
+// The bytes of store_fp8x8 by 1 / scale. (No clamp: 448 and a unit at most, which is 448 in E4M3.)
+GM_DEV void store_fp8x8_by(uint8_t *p, int valid, const float (&v)[8], float scale, float inverse) {
+    float r[8];
+    quotients(v, scale, inverse, r);
     const uint32_t w[2] = {pack_fp8(r[0], r[1], r[2], r[3]), pack_fp8(r[4], r[5], r[6], r[7])};
     store_bytes8(p, valid, w);
 }

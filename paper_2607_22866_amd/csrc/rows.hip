@@ -199,7 +199,7 @@ GM_DEV void store_piece(const RowArgs &a, const Place &at, int64_t row, int64_t 
         for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
         const float s = block_scale(max16(m));
         if (valid > 0) {
-            store_fp8x8_by(q, WHOLE ? 8 : valid, v, 1.f / s);
+            store_fp8x8_by(q, WHOLE ? 8 : valid, v, s, 1.f / s);
             if (threadIdx.x % 16 == 0) a.scale[row * a.ss + c / SB] = s;
         }
     } else if (a.format == INTEGER) {
