@@ -103,7 +103,7 @@ GM_DEV float row_scale(uint32_t most) {
 // 2^-7 times a power of two, where 8-bit roundings have their borders: computed for every scale's mantissa and the
 // seven values around each. Uncorrected it lies on the other side of the border at one in twelve of these. Of a
 // scale below 2^-90 what is left of v may pass the end of fp32. An infinite scale, whose inverse is 0, corrects nothing:
-// 0 and NaN, as the division gives.)
+// 0 and NaN, as the division gives. Zeros keep their sign, of v and q s subtracted in this order.)
 GM_DEV void quotients(const float (&v)[8], float scale, float inverse, float (&r)[8]) {
     if (scale < 0x1p-90f) {
 #pragma unroll
@@ -113,7 +113,7 @@ GM_DEV void quotients(const float (&v)[8], float scale, float inverse, float (&r
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float q = v[i] * inverse;
-            r[i] = __builtin_fmaf(__builtin_fmaf(-q, s, v[i]), inverse, q);
+            r[i] = __builtin_fmaf(-__builtin_fmaf(q, s, -v[i]), inverse, q);
         }
     }
 }
