@@ -101,20 +101,24 @@ GM_DEV float row_scale(uint32_t most) {
 // v / scale as the division rounds it, by 1 / scale, which costs a division for eight values rather than for each: the
 // quotient is corrected by what it leaves of v. (That makes it the division's at all quotients near an odd multiple of
 // 2^-7 times a power of two, where 8-bit roundings have their borders: computed for every scale's mantissa and the
-// seven values around each. Uncorrected it lies on the other side of the border at one in twelve of these. Of a
-// scale below 2^-90 what is left of v may pass the end of fp32. An infinite scale, whose inverse is 0, corrects nothing:
-// 0 and NaN, as the division gives. Zeros keep their sign, of v and q s subtracted in this order.)
+// seven values around each. Uncorrected it lies on the other side of the border at one in twelve of these. What is
+// left of v may pass the end of fp32 where the scale is below 2^-90: both are taken 2^60 times there. An infinite scale,
+// whose inverse is 0, corrects nothing: 0 and NaN, as the division gives. Zeros keep their sign, of v and q s
+// subtracted in this order.)
 GM_DEV void quotients(const float (&v)[8], float scale, float inverse, float (&r)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = v[i];
     if (scale < 0x1p-90f) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r[i] = v[i] / scale;
-    } else {
-        const float s = inverse == 0.f ? 0.f : scale;
+        for (int i = 0; i < 8; ++i) r[i] *= 0x1p60f;
+        scale *= 0x1p60f;
+        inverse *= 0x1p-60f;
+    }
+    if (inverse == 0.f) scale = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float q = v[i] * inverse;
-            r[i] = __builtin_fmaf(-__builtin_fmaf(q, s, -v[i]), inverse, q);
-        }
+    for (int i = 0; i < 8; ++i) {
+        const float q = r[i] * inverse;
+        r[i] = __builtin_fmaf(-__builtin_fmaf(q, scale, -r[i]), inverse, q);
     }
 }
 
@@ -126,15 +130,14 @@ GM_DEV void store_fp8x8_by(uint8_t *p, int valid, const float (&v)[8], float sca
     store_bytes8(p, valid, w);
 }
 
-// To the nearest integers, ties to even; a NaN as 0. Steps are as wide as values are near a tie here, so the quotient is
-// corrected by what it leaves of x, which makes it x / scale rounded. (127 in magnitude and a unit at most before that.
-// An infinite scale, whose inverse is 0, corrects nothing: 0 and NaN, as the division gives.)
+// To the nearest integers, ties to even; a NaN as 0. (127 in magnitude and a unit at most before that.)
 GM_DEV void store_int8x8_by(uint8_t *p, int valid, const float (&v)[8], float scale, float inverse) {
+    float r[8];
+    quotients(v, scale, inverse, r);
     uint32_t b[8];
-    if (inverse == 0.f) scale = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float q = v[i] * inverse, x = __builtin_rintf(__builtin_fmaf(__builtin_fmaf(-q, scale, v[i]), inverse, q));
+        const float x = __builtin_rintf(r[i]);
         b[i] = (uint32_t)(int)(x == x ? x : 0.f);
     }
     uint32_t w[2];

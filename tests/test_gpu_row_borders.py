@@ -62,3 +62,14 @@ def test_e4m3_as_quantise_blocks(g, n, exponent):
     r = g.rms_norm(x, v[0].cuda(), quantise=torch.float8_e4m3fn, plain=True)
     q, s = g.quantise_blocks(r.y)
     assert torch.equal(r.scale, s) and torch.equal(r.q.view(torch.uint8), q.view(torch.uint8))
+
+
+@pytest.mark.parametrize("n", [128, 777, 2056, 20001])
+@pytest.mark.parametrize("exponent", [-126, -125, -110, -92, -89, 0, 100])
+def test_integers_are_the_quotient_rounded(g, n, exponent):
+    v = near_borders(64 if n < 20000 else 8, n, torch.arange(127) + 0.5, 127.0, exponent, n + exponent, block=n)
+    q, s = g.quantise_rows(v.cuda())
+    top = v.abs().amax(1) / 127.0
+    assert torch.equal(s.cpu(), top) and bool((top >= 2.0 ** -126).all())
+    # (ties, and quotients that are nearer to one than fp32 tells, go to even, as the division's do)
+    assert torch.equal(q.cpu().float(), torch.round(v / top[:, None]))
