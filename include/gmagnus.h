@@ -579,14 +579,17 @@ gmagnus_status_t gmagnus_rms_norm_backward(const gmagnus_dense_t *TOTAL, const g
                                            int64_t workspace_bytes, void *hip_stream);
 
 /* Y = silu(G) * U for rows H = [G | U] of twice Y's columns, silu(g) = g / (1 + e^-g): the
- * gate between the two products of an expert. (An infinite G gives what that formula
- * gives in IEEE arithmetic as g * sigma(g): infinities, NaN for -inf and for 0 * inf.)
+ * gate between the two products of an expert. The product is good to a few units of fp32
+ * also where e^g is below fp32's range and silu(g) * u is not. (An infinite G gives what
+ * that formula gives in IEEE arithmetic as g * sigma(g): infinities, NaN for -inf and for
+ * 0 * inf.)
  * Errors as gmagnus_rms_norm. */
 gmagnus_status_t gmagnus_gate(const gmagnus_dense_t *H, const gmagnus_dense_t *Y, const gmagnus_dense_t *Q,
                               const gmagnus_dense_t *scale, void *hip_stream);
 
-/* Gradient D_H = [d_G | d_U] of gmagnus_gate from Y's gradient D_A. H, D_A and D_H have
- * one type. Errors as gmagnus_rms_norm. */
+/* Gradient D_H = [d_G | d_U] of gmagnus_gate from Y's gradient D_A, as exact (products
+ * on the way may pass fp32's range at either end). H, D_A and D_H have one type.
+ * Errors as gmagnus_rms_norm. */
 gmagnus_status_t gmagnus_gate_backward(const gmagnus_dense_t *H, const gmagnus_dense_t *D_A, const gmagnus_dense_t *D_H,
                                        void *hip_stream);
 

@@ -119,11 +119,60 @@ GM_DEV float exp_neg(float x) {
     return __builtin_fmaf(r * LN2, rest, r);
 }
 
-// sigma(g) and 1 - sigma(g), each to a few units however small. (The hardware's reciprocal of 1 + e^-|g| is off by one.)
+// sigma(g) and 1 - sigma(g), each to a few units where it is a normal number (|g| up to FAR; zero soon after).
+// (The hardware's reciprocal of 1 + e^-|g| is off by one.)
 GM_DEV void sigmoid(float g, float &s, float &rest) {
     const float z = exp_neg(-fabsf(g)), big = __builtin_amdgcn_rcpf(1.f + z), small = z * big;
     s = g >= 0.f ? big : small;
     rest = g >= 0.f ? small : big;
+}
+
+// From -FAR on down sigma(g) is e^g to fp32's last place and may be below fp32's normal numbers where its product with g and
+// u is not, so it is taken apart: e^g = m 2^k. (Below -300 m is zero: 2^-432 times g, u and a gradient is.)
+constexpr float FAR = 86.f;
+GM_DEV float exp_apart(float g, int &k) {
+    constexpr float L = 0x1.715476p+0f, L_REST = 0x1.4ae0cp-26f;
+    const float y = __builtin_amdgcn_fmed3f(g, -300.f, 0.f), whole = __builtin_rintf(y * L);
+    k = (int)whole;
+    const float m = __builtin_amdgcn_exp2f(__builtin_fmaf(y, L_REST, __builtin_fmaf(y, L, -whole)));
+    return g > -300.f ? m : 0.f;
+}
+// a b c m 2^k, rounded to fp32's range once, at the end.
+GM_DEV float product_apart(float a, float b, float c, float m, int k) {
+    const float p = __builtin_amdgcn_frexp_mantf(a) * __builtin_amdgcn_frexp_mantf(b) * __builtin_amdgcn_frexp_mantf(c) * m;
+    return __builtin_amdgcn_ldexpf(p, __builtin_amdgcn_frexp_expf(a) + __builtin_amdgcn_frexp_expf(b) + __builtin_amdgcn_frexp_expf(c) + k);
+}
+
+// g sigma(g) u
+GM_DEV float gated_near(float g, float u) {
+    float s, rest;
+    sigmoid(g, s, rest);
+    return g * s * u;
+}
+GM_DEV float gated(float g, float u) {
+    if (g >= -FAR) return gated_near(g, u);
+    int k;
+    const float m = exp_apart(g, k);
+    return product_apart(g, u, 1.f, m, k);  // (of a NaN too)
+}
+// Whether any of eight is below -FAR. (Negative numbers' bits are ordered as their magnitudes, above all others'.)
+GM_DEV bool any_far(const float (&g)[8]) {
+    uint32_t most = __float_as_uint(g[0]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) most = max(most, __float_as_uint(g[i]));
+    return __builtin_expect(most > __float_as_uint(-FAR), 0);
+}
+GM_DEV void gated8(const float (&g)[8], const float (&u)[8], float (&a)[8]) {
+    if (any_far(g)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            a[i] = gated(g[i], u[i]);
+            __builtin_amdgcn_sched_barrier(0);  // (one by one: what is common shall hold no registers for all of them)
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = gated_near(g[i], u[i]);
+    }
 }
 
 GM_DEV uint32_t wave_max(uint32_t x) {

@@ -354,11 +354,6 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
             }
             // Two values of the rows' type are kept of a result, itself and what its rounding left (an infinite one leaves
             // nothing): rounded once it would add as much error to the layer's result as that has from its own rounding.
-            auto gated = [](float x, float y) {
-                float s, rest;
-                sigmoid(x, s, rest);
-                return x * s * y;
-            };
             T *out = static_cast<T *>(a.act) + (base + r0) * a.act_stride + f0;
             __syncthreads();  // (the last item's sums)
 #pragma unroll
