@@ -614,8 +614,9 @@ int64_t gmagnus_expert_layer_workspace_bytes(int64_t n_tokens, int64_t n_experts
  * (scales NULL), or are both E4M3 with the scales that gmagnus_quantise_blocks gives
  * with block_rows 128, or both int8 with those of gmagnus_quantise_rows. OUT has X's
  * type or fp32. Sums are held in fp32, a gate's result as the sum of two values of
- * X's type: it has X's range and is infinite past that, and an infinite weight of W2
- * gives infinities or NaN. Of the weights only the chosen experts' are read. The
+ * X's type (of fp16: the second times 2^-11), to 2^-16 of it in bf16, 2^-22 in fp16 or
+ * 2^-36, whichever is more: it has X's range and is infinite past that, and an infinite
+ * weight of W2 gives infinities or NaN. Of the weights only the chosen experts' are read. The
  * workspace is the call's until it has run.
  * Errors: INVALID_VALUE, UNSUPPORTED (more than 64 tokens, 1024 experts or 1024
  * entries, sides above 2^31 - 1025), HIP. */

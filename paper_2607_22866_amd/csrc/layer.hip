@@ -28,7 +28,7 @@ struct LayerArgs {
     // workspace
     int32_t *arrived;  // of each column tile of the second kernel, how many of its splits are there
     int32_t *table;
-    void *act;         // [2][entries][act_stride], act_part elements between the two
+    void *act;         // [2][entries][act_stride]: results and what is left of them, act_part elements between the two
     float *share;      // [column tiles][splits][n_tokens][32]
     int64_t act_stride, act_part;
 };
@@ -154,6 +154,13 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void k_layer_route(LayerArgs a) {
 // A block of the reduction is 128 bytes of a row of weights: 64 values of 16 bits or
 // 128 of 8. A lane has 16 bytes at g and 16 at g + 4 of a row's eight pieces, S
 // fragments of 8 values each. Values of 8 bits are widened, exactly, to the rows' type.
+
+// A gate's result is kept as two values of the rows' type, itself and what its rounding left: rounded once it would add
+// as much error to the layer's result as that has from its own rounding. What is left is taken REST times, as many as fit:
+// fp16 has 2^-25 for its least half step, and small results would be no better for their second value (of 1e-6, 3 %).
+template <typename T>
+constexpr float REST = std::is_same<T, _Float16>::value ? 2048.f : 1.f;
+
 enum Kind { SAME, FP8, INT8 };  // weights: of the rows' type, E4M3 with block scales, integers with a scale a row
 
 template <Kind KIND, typename T>
@@ -220,10 +227,11 @@ struct Block {
             for (int s = 0; s < S; ++s)
                 f[h * S + s] = cut_piece(reinterpret_cast<const uint8_t *>(row), (int64_t)(k + first(h, g) + s * 8) * 2, (int64_t)n * 2);
     }
-    // acc += weights' fragments times the rows' (of P parts), by `scale` where blocks have one
+    // acc += weights' fragments times the rows' (of P parts, the second REST times), by `scale` where blocks have one
     template <int P>
     GM_DEV static void multiply(const u32x4 (&w)[2], const u32x4 (&r)[P][2 * S], f32x4 scale, f32x4 &acc) {
-        f32x4 sum = KIND == FP8 ? f32x4{0, 0, 0, 0} : acc;
+        constexpr bool APART = P == 2 && REST<T> != 1.f;
+        f32x4 sum = KIND == FP8 ? f32x4{0, 0, 0, 0} : acc, rest = {0, 0, 0, 0};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             u32x4 f[S];
@@ -231,8 +239,14 @@ struct Block {
 #pragma unroll
             for (int s = 0; s < S; ++s)
 #pragma unroll
-                for (int p = 0; p < P; ++p) sum = mfma_16x16x32(f[s], r[p][h * S + s], sum, T{});
+                for (int p = 0; p < P; ++p) {
+                    f32x4 &to = APART && p == 1 ? rest : sum;
+                    to = mfma_16x16x32(f[s], r[p][h * S + s], to, T{});
+                }
         }
+        if constexpr (APART)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += rest[e] * (1.f / REST<T>);
         if constexpr (KIND != FP8)
             acc = sum;
         else
@@ -352,8 +366,6 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
                         for (int j = 0; j < 2; ++j) B::multiply(fw[j], fx, s[j], acc[r][j]);
                     }
             }
-            // Two values of the rows' type are kept of a result, itself and what its rounding left (an infinite one leaves
-            // nothing): rounded once it would add as much error to the layer's result as that has from its own rounding.
             T *out = static_cast<T *>(a.act) + (base + r0) * a.act_stride + f0;
             __syncthreads();  // (the last item's sums)
 #pragma unroll
@@ -379,7 +391,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
                     const float v = gated(x, y);
                     const T top = (T)v;
                     out[r * a.act_stride + col] = top;
-                    out[a.act_part + r * a.act_stride + col] = fabsf((float)top) < INFINITY ? (T)(v - (float)top) : (T)0.f;
+                    // (an infinite one leaves nothing)
+                    out[a.act_part + r * a.act_stride + col] = fabsf((float)top) < INFINITY ? (T)((v - (float)top) * REST<T>) : (T)0.f;
                 }
             }
         }
