@@ -145,7 +145,7 @@ GM_DEV void begin_second(const LayerArgs &a, const int32_t *table) {
 // kernel it would take up to 16 a wave.)
 constexpr int ROUTE_WAVES = 16;
 __global__ __launch_bounds__(64 * ROUTE_WAVES) void k_layer_route(LayerArgs a) {
-    extern __shared__ int32_t lds_layer[];
+    extern __shared__ __align__(16) int32_t lds_layer[];
     route_few(a, lds_layer, ROUTE_WAVES);
     begin_second(a, lds_layer);
 }
@@ -272,7 +272,7 @@ template <Kind KIND, typename T, int RT, bool ROUTE>
 __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
     using B = Block<KIND, T>;
     constexpr int U = RT > 1 || B::EIGHT ? 2 : 4;
-    extern __shared__ int32_t lds_layer[];
+    extern __shared__ __align__(16) int32_t lds_layer[];
     const int entries = a.n_tokens * a.top_k;
     const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16;
     const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
@@ -410,7 +410,7 @@ template <Kind KIND, typename T, typename OUT>
 __global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
     using B = Block<KIND, T>;
     constexpr int U = B::EIGHT ? 1 : 2;
-    extern __shared__ int32_t lds_layer[];
+    extern __shared__ __align__(16) int32_t lds_layer[];
     const int entries = a.n_tokens * a.top_k;
     const int lane = threadIdx.x & 63, i16 = lane % 16, g = lane / 16;
     const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64));
