@@ -406,8 +406,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_layer_up(LayerArgs a) {
 // their order, and the splits' by the last of them to arrive, in theirs. The sizes above:
 // 31 us (5.5 TB/s), 52-55, 44 (2.5: rows of 1000 bytes lie across lines, 135 MB come for 112),
 // one token 6.4.
+// (Waves a SIMD: integers in fp16, left alone, took registers for two: 48 tokens, 2048 x 1000, 145 us a layer, here 123.)
 template <Kind KIND, typename T, typename OUT>
-__global__ __launch_bounds__(64 * WAVES) void k_layer_down(LayerArgs a) {
+__global__ __launch_bounds__(64 * WAVES, KIND == SAME ? 4 : 3) void k_layer_down(LayerArgs a) {
     using B = Block<KIND, T>;
     constexpr int U = B::EIGHT ? 1 : 2;
     extern __shared__ __align__(16) int32_t lds_layer[];
