@@ -550,8 +550,11 @@ gmagnus_status_t gmagnus_combine_backward(const int64_t *row_ptr, const int32_t 
  * (fp32) beside it: E4M3 as gmagnus_quantise_blocks with block_rows 1 gives them
  * (scale n_rows x ceil(n_cols / 128)), int8 as gmagnus_quantise_rows does (scale 1 x
  * n_rows); it is rounded from the fp32 result, not from the one in the rows' type.
- * Q and scale, or Y, may be NULL where that result is not wanted. Outputs (total among
- * them) may not overlap inputs: long rows are read again after a part of them is written. */
+ * Q and scale, or Y, may be NULL where that result is not wanted. An output may be an
+ * input itself (the same data, type, shape and row stride: total the residual, Y or a
+ * gradient's result the rows). Outputs may not share memory with inputs otherwise, nor
+ * with each other: gmagnus_rms_norm refuses that (INVALID_VALUE), the gradients for the
+ * matrices they read and write. */
 
 /* TOTAL = X + residual, rounded to their type, and Y = TOTAL * weight / sqrt(mean of a
  * row's squares + eps), of TOTAL as its type holds it; without a residual (NULL, as
