@@ -472,9 +472,11 @@ def release_cache():
 
 
 # ------------------------------------------------------------ routed expert products
-# Gradients are calls (route_backward, group_product, group_outer, combine_backward).
-# Autograd does not make them: differentiating a result with respect to an input
-# raises. Results written to a given `out` are not part of any graph.
+# Gradients are calls (route_backward, group_product, group_outer, combine_backward,
+# rms_norm_backward, gate_backward). Autograd does not make them: differentiating a
+# result with respect to an input raises, of the norm's and the gate's gradients too.
+# Results written to a given `out`, and those of route_backward, group_outer and
+# combine_backward, are not part of any graph.
 # the current stream's handle, in a tenth of current_stream()'s time (a torch without GPU support does not have it)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -891,6 +893,9 @@ def rms_norm_backward(total: torch.Tensor, weight: Optional[torch.Tensor], d_y: 
     _check(lib.gmagnus_rms_norm_backward(d, dw, eps, ddy, ddt, _dense(d_x, dev, "d_x"),
                                          None if d_weight is None else d_weight.data_ptr(), ws.data_ptr(), nbytes,
                                          _raw_stream(dev)))
+    inputs = [t for t in (total, weight, d_y, d_total) if t is not None and t.requires_grad]
+    if inputs:
+        _no_formula("rms_norm_backward", "second derivatives are not made", [t for t in (d_x, d_weight) if t is not None], *inputs)
     return d_x, d_weight
 
 
@@ -913,9 +918,11 @@ def gate_backward(h: torch.Tensor, d_y: torch.Tensor, out: Optional[torch.Tensor
     """Gradient of gate's h from that of its y."""
     dev = _device_of(h, "h")
     d, ddy = _dense(h, dev, "h"), _dense(d_y, dev, "d_y")
-    out = _out(out, tuple(h.shape), h.dtype, h, "out")
-    _check(load().gmagnus_gate_backward(d, ddy, _dense(out, dev, "out"), _raw_stream(dev)))
-    return out
+    d_h = _out(out, tuple(h.shape), h.dtype, h, "out")
+    _check(load().gmagnus_gate_backward(d, ddy, _dense(d_h, dev, "out"), _raw_stream(dev)))
+    if out is None and (h.requires_grad or d_y.requires_grad):
+        _no_formula("gate_backward", "second derivatives are not made", (d_h,), h, d_y)
+    return d_h
 
 
 @_on_stream
