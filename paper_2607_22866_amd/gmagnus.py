@@ -14,6 +14,7 @@ from dataclasses import dataclass
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd import forward_ad
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libgmagnus.so")
@@ -474,11 +475,21 @@ def release_cache():
 # ------------------------------------------------------------ routed expert products
 # Gradients are calls (route_backward, group_product, group_outer, combine_backward,
 # rms_norm_backward, gate_backward). Autograd does not make them: differentiating a
-# result with respect to an input raises, of the norm's and the gate's gradients too.
+# result with respect to an input raises, of the norm's and the gate's gradients too, and
+# so does an operand with a tangent (forward mode).
 # Results written to a given `out`, and those of route_backward, group_outer and
 # combine_backward, are not part of any graph.
 # the current stream's handle, in a tenth of current_stream()'s time (a torch without GPU support does not have it)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _no_tangents(call: str, operands):
+    """Within a level of forward-mode differentiation (the only time this is called): no result has a tangent, so an
+    operand that has one raises."""
+    for x in operands:
+        for t in x.arrays() if isinstance(x, Routing) else (x,):
+            if isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None:
+                raise RuntimeError("gmagnus.%s has no formula for forward-mode differentiation" % call)
 
 
 def _on_stream(f):
@@ -487,6 +498,8 @@ def _on_stream(f):
 
     @functools.wraps(f)
     def call(*args, stream=None, **kw):
+        if getattr(forward_ad, "_current_level", 0) >= 0:
+            _no_tangents(f.__name__, args + tuple(kw.values()))
         if stream is None:
             return f(*args, **kw)
         for x in args + tuple(kw.values()):
