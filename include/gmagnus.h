@@ -559,8 +559,10 @@ gmagnus_status_t gmagnus_combine_backward(const int64_t *row_ptr, const int32_t 
 /* TOTAL = X + residual, rounded to their type, and Y = TOTAL * weight / sqrt(mean of a
  * row's squares + eps), of TOTAL as its type holds it; without a residual (NULL, as
  * total then) TOTAL is X. X, residual, total and Y have one type, fp32, bf16 or fp16;
- * weight is 1 x n_cols of that type or fp32, NULL: ones. Squares are summed in fp32:
- * rows with values beyond 1e18 overflow there, and are zeros.
+ * weight is 1 x n_cols of that type or fp32, NULL: ones. Squares are summed in fp32: a
+ * row whose squares add up to more than 3.4e38 (the root of their mean above 2.9e17 in
+ * 4096 columns, 1.4e17 in 16384) gives zeros, and squares below 1e-38 lose places, which
+ * shows where eps is not well above them.
  * Errors: INVALID_VALUE, UNSUPPORTED (2^31 - 1 rows or more, columns above 2^31 -
  * 1025), HIP. */
 gmagnus_status_t gmagnus_rms_norm(const gmagnus_dense_t *X, const gmagnus_dense_t *residual,
