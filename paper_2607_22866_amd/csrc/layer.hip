@@ -590,6 +590,11 @@ struct LayerLayout {
     }
 };
 
+// A launch's LDS stays below the 64 KB that need no leave.
+static_assert(4 * (route_words(MAX_ENTRIES, MAX_EXPERTS) + 4 + WAVES * 16 * PITCH) < 64 << 10 &&
+                  4 * (table_words(MAX_ENTRIES) + 4 + WAVES * MAX_TOKENS * PITCH) + 16 < 64 << 10,
+              "");
+
 bool layer_sizes_ok(int64_t t, int64_t e, int64_t k, int64_t f, int64_t n) {
     return t >= 0 && t <= MAX_TOKENS && e >= 1 && e <= MAX_EXPERTS && k >= 1 && k <= e && t * k <= MAX_ENTRIES && f >= 1 &&
            2 * f <= MAX_SIDE && n >= 1 && n <= MAX_SIDE;
@@ -670,7 +675,6 @@ extern "C" gmagnus_status_t gmagnus_expert_layer(const gmagnus_dense_t *X, const
         hipStream_t s = (hipStream_t)hip_stream;
         const int64_t items = used * ((f + 15) / 16);
         auto go = [&](auto kernel, int64_t grid, int threads, int words) {
-            if (words * 4 > 64 << 10) allow_dynamic_lds(reinterpret_cast<const void *>(kernel), words * 4);
             hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), words * 4, s, a);
             GM_CHECK_LAUNCH();
         };
