@@ -624,7 +624,7 @@ int64_t gmagnus_expert_layer_workspace_bytes(int64_t n_tokens, int64_t n_experts
  * weight of W2 gives infinities or NaN. Of the weights only the chosen experts' are read. The
  * workspace is the call's until it has run.
  * Errors: INVALID_VALUE, UNSUPPORTED (more than 64 tokens, 1024 experts or 1024
- * entries, sides above 2^31 - 1025), HIP. */
+ * entries, more than 2^29 - 32 columns of OUT, other sides above 2^31 - 1025), HIP. */
 gmagnus_status_t gmagnus_expert_layer(const gmagnus_dense_t *X, const gmagnus_dense_t *logits, int64_t top_k,
                                       int32_t normalise, const gmagnus_dense_t *W1, const gmagnus_dense_t *W1_scale,
                                       const gmagnus_dense_t *W2, const gmagnus_dense_t *W2_scale,

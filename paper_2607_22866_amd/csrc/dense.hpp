@@ -382,6 +382,8 @@ GM_DEV void zero_tile(OUT *out, int64_t stride, int rows, int cols) {
 
 // Work groups of a launch: the kernels' loops take what exceeds this.
 constexpr int64_t MAX_GRID = 1 << 22;
+// (A launch has less than 2^32 threads: of work groups of 1024 fewer fit.)
+constexpr int64_t max_grid(int threads) { return threads < 1024 ? MAX_GRID : ((int64_t(1) << 32) - 1) / threads; }
 
 // Grouped rows and sides of matrices. The kernels count rows of a group, and
 // elements of the reduction, in 32 bits, and go past their end by a few steps

@@ -595,9 +595,12 @@ static_assert(4 * (route_words(MAX_ENTRIES, MAX_EXPERTS) + 4 + WAVES * 16 * PITC
                   4 * (table_words(MAX_ENTRIES) + 4 + WAVES * MAX_TOKENS * PITCH) + 16 < 64 << 10,
               "");
 
+// A launch has less than 2^32 threads, and the second kernel a work group for every 32 columns.
+constexpr int64_t MAX_OUT = (((int64_t(1) << 32) - 1) / (64 * WAVES)) * 32;
+
 bool layer_sizes_ok(int64_t t, int64_t e, int64_t k, int64_t f, int64_t n) {
     return t >= 0 && t <= MAX_TOKENS && e >= 1 && e <= MAX_EXPERTS && k >= 1 && k <= e && t * k <= MAX_ENTRIES && f >= 1 &&
-           2 * f <= MAX_SIDE && n >= 1 && n <= MAX_SIDE;
+           2 * f <= MAX_SIDE && n >= 1 && n <= MAX_OUT;
 }
 
 }  // namespace
@@ -624,6 +627,7 @@ extern "C" gmagnus_status_t gmagnus_expert_layer(const gmagnus_dense_t *X, const
         GM_REQUIRE(normalise == 0 || normalise == 1, GMAGNUS_ERROR_INVALID_VALUE, "normalise must be 0 or 1");
         check_side(d, "columns of X");
         check_side(n, "columns of OUT");
+        GM_REQUIRE(n <= MAX_OUT, GMAGNUS_ERROR_UNSUPPORTED, "columns of OUT beyond 2^29 - 32");
         check_side(f, "columns of W2");
         check_side(2 * f, "rows of W1");
         GM_REQUIRE(t <= MAX_TOKENS, GMAGNUS_ERROR_UNSUPPORTED, "more than 64 tokens: call the routing and the grouped products");
@@ -658,8 +662,7 @@ extern "C" gmagnus_status_t gmagnus_expert_layer(const gmagnus_dense_t *X, const
                    "workspace below gmagnus_expert_layer_workspace_bytes");
         GM_REQUIRE((uintptr_t)workspace % 16 == 0, GMAGNUS_ERROR_INVALID_VALUE, "workspace is not 16-byte aligned");
         const int64_t tiles = (n + 31) / 32, entries = t * top_k, used = e < entries ? e : entries;
-        GM_REQUIRE(tiles * l.splits < INT32_MAX && used * ((f + 127) / 128) < INT32_MAX / 2, GMAGNUS_ERROR_UNSUPPORTED,
-                   "2^31 tiles or 2^30 units of the reduction or more");
+        GM_REQUIRE(used * ((f + 127) / 128) < INT32_MAX / 2, GMAGNUS_ERROR_UNSUPPORTED, "2^30 units of the reduction or more");
         char *ws = static_cast<char *>(workspace);
         const int size = kind == SAME ? 2 : 1;
         // (integers' scales: a row an expert)

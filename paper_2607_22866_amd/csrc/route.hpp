@@ -38,7 +38,9 @@ GM_DEV float key_value(uint32_t k) {
 // bit from the top: a bit stays if at least top_k keys reach it, and once just top_k
 // do, those are the choice (16384 tokens, 256 experts, top_k 8: 20 us; taking the
 // maximum over the wave top_k times: 37). Keys equal to the last one are taken from
-// the lowest expert on.
+// the lowest expert on. (The whole call for 16384 tokens, bf16, top_k 8, of 256, 512 and
+// 1024 experts 29, 42 and 68 us; with the taken experts written in here rather than by the
+// caller, which changes how registers are given out, 31.5, 42 and 66.)
 template <typename T, int V>
 GM_DEV float choose(const T (&l)[V], int n_experts, int top_k, bool normalise, uint64_t (&chosen)[V], float (&p)[V], int &n) {
     const int lane = threadIdx.x & 63;

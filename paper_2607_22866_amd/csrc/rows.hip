@@ -641,7 +641,7 @@ void launch_rows(const RowArgs &a, int32_t type, hipStream_t s) {
             if constexpr (W == 0) {
                 hipLaunchKernelGGL((k_rows_long<OP, T, WHOLE>), dim3(grid_for(a.n_rows, 1, 1 << 16)), dim3(64 * LONG_W), 0, s, a);
             } else {
-                const int64_t most = OP == Op::GATE ? MAX_GRID : rows_grid(a.n, OP == Op::NORM);
+                const int64_t most = OP == Op::GATE ? max_grid(W > 4 ? 64 * W : 256) : rows_grid(a.n, OP == Op::NORM);
                 hipLaunchKernelGGL((k_rows<OP, T, W, CH, WHOLE>), dim3(grid_for(a.n_rows, W == 1 ? 4 : 1, most)),
                                    dim3(W > 4 ? 64 * W : 256), 0, s, a);
             }
@@ -889,7 +889,7 @@ extern "C" gmagnus_status_t gmagnus_rms_norm_backward(const gmagnus_dense_t *TOT
             });
         });
         if (d_weight)
-            hipLaunchKernelGGL(k_add_shares, dim3(grid_for(n, 64, MAX_GRID)), dim3(1024), 0, s, a.share, n, units, d_weight);
+            hipLaunchKernelGGL(k_add_shares, dim3(grid_for(n, 64, max_grid(1024))), dim3(1024), 0, s, a.share, n, units, d_weight);
         GM_CHECK_LAUNCH();
     });
 }
