@@ -107,29 +107,31 @@ GM_DEV void store_f32(T *p, int valid, const float (&v)[8]) {
     }
 }
 
-// e^x for x <= 0, by the hardware's power of two: what x log2(e) loses when it is
+// e^x for x up to MOST, by the hardware's power of two: what x log2(e) loses when it is
 // rounded (|x| units of 2^-24 of the result) is multiplied in afterwards, so that a few
 // units are off at any x. (From -200 on down the result is zero, for NaN too: an
 // infinite logit, whose difference to itself that is, has a sum of zero and NaN weights.)
-GM_DEV float exp_neg(float x) {
+template <int MOST>
+GM_DEV float exp_upto(float x) {
     constexpr float L = 0x1.715476p+0f, L_REST = 0x1.4ae0cp-26f, LN2 = 0x1.62e43p-1f;
-    const float y = __builtin_amdgcn_fmed3f(x, -200.f, 0.f), t = y * L;
+    const float y = __builtin_amdgcn_fmed3f(x, -200.f, (float)MOST), t = y * L;
     const float rest = __builtin_fmaf(y, L_REST, __builtin_fmaf(y, L, -t));
     const float r = __builtin_amdgcn_exp2f(t);
     return __builtin_fmaf(r * LN2, rest, r);
 }
+GM_DEV float exp_neg(float x) { return exp_upto<0>(x); }
 
-// sigma(g) and 1 - sigma(g), each to a few units where it is a normal number (|g| up to FAR; zero soon after).
-// (The hardware's reciprocal of 1 + e^-|g| is off by one.)
+// sigma(g) and 1 - sigma(g) for g from -FAR on up, each to a few units (the latter zero soon after FAR). (The
+// hardware's reciprocal is off by one.)
+constexpr float FAR = 86.f;
 GM_DEV void sigmoid(float g, float &s, float &rest) {
-    const float z = exp_neg(-fabsf(g)), big = __builtin_amdgcn_rcpf(1.f + z), small = z * big;
-    s = g >= 0.f ? big : small;
-    rest = g >= 0.f ? small : big;
+    const float z = exp_upto<(int)FAR + 1>(-g);
+    s = __builtin_amdgcn_rcpf(1.f + z);
+    rest = z * s;
 }
 
 // From -FAR on down sigma(g) is e^g to fp32's last place and may be below fp32's normal numbers where its product with g and
 // u is not, so it is taken apart: e^g = m 2^k. (Below -300 m is zero: 2^-432 times g, u and a gradient is.)
-constexpr float FAR = 86.f;
 GM_DEV float exp_apart(float g, int &k) {
     constexpr float L = 0x1.715476p+0f, L_REST = 0x1.4ae0cp-26f;
     const float y = __builtin_amdgcn_fmed3f(g, -300.f, 0.f), whole = __builtin_rintf(y * L);
@@ -155,12 +157,13 @@ GM_DEV float gated(float g, float u) {
     const float m = exp_apart(g, k);
     return product_apart(g, u, 1.f, m, k);  // (of a NaN too)
 }
-// Whether any of eight is below -FAR. (Negative numbers' bits are ordered as their magnitudes, above all others'.)
+// Whether any of a wave's lanes has one of eight below -FAR. (Negative numbers' bits are ordered as their magnitudes,
+// above all others'.)
 GM_DEV bool any_far(const float (&g)[8]) {
     uint32_t most = __float_as_uint(g[0]);
 #pragma unroll
     for (int i = 1; i < 8; ++i) most = max(most, __float_as_uint(g[i]));
-    return __builtin_expect(most > __float_as_uint(-FAR), 0);
+    return __builtin_expect(ballot(most > __float_as_uint(-FAR)) != 0, 0);
 }
 GM_DEV void gated8(const float (&g)[8], const float (&u)[8], float (&a)[8]) {
     if (any_far(g)) {

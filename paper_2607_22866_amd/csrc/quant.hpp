@@ -108,11 +108,13 @@ GM_DEV float row_scale(uint32_t most) {
 GM_DEV void quotients(const float (&v)[8], float scale, float inverse, float (&r)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i] = v[i];
-    if (scale < 0x1p-90f) {
+    const bool small = scale < 0x1p-90f;
+    if (__builtin_expect(ballot(small) != 0, 0)) {  // (of any lane)
+        const float up = small ? 0x1p60f : 1.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r[i] *= 0x1p60f;
-        scale *= 0x1p60f;
-        inverse *= 0x1p-60f;
+        for (int i = 0; i < 8; ++i) r[i] *= up;
+        scale *= up;
+        inverse *= small ? 0x1p-60f : 1.f;
     }
     if (inverse == 0.f) scale = 0.f;
 #pragma unroll

@@ -172,12 +172,19 @@ GM_DEV void load_piece(const RowArgs &a, const T *x, int64_t row, int64_t c, int
         load<WHOLE>(static_cast<const T *>(a.total) + row * a.ts + c, valid, v);
         return;
     }
-    load<WHOLE>(x + c, valid, v);
     if constexpr (OP == Op::GATE) {
         float u[8];
-        load<WHOLE>(x + a.n + c, valid, u);
+        if (WHOLE && valid <= 0) {  // (both loads behind one branch, or the second waits for the first)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0.f;
+            return;
+        }
+        load_f32x8(x + c, WHOLE ? 8 : valid, v);
+        load_f32x8(x + a.n + c, WHOLE ? 8 : valid, u);
         gated8(v, u, v);
+        return;
     }
+    load<WHOLE>(x + c, valid, v);
     if constexpr (OP == Op::NORM) {
         if (a.r) {
             float u[8];
@@ -520,6 +527,29 @@ __global__ __launch_bounds__(64) void k_norm_backward_columns(NormBackArgs a, in
 // lane, no row is needed as a whole. Where s is below fp32's normal numbers, or d_a u
 // above its largest, the products are made of fractions and exponents. 9001 x 1365
 // fp16 23 us, 5.4 TB/s.
+GM_DEV void gate_slopes(float g, float u, float d, float &d_g, float &d_u) {
+    float s, rest;
+    sigmoid(g, s, rest);
+    d_g = d * u * (s * (1.f + g * rest));
+    d_u = d * (g * s);
+}
+// (Values that are neither far nor too large: as above, whatever lies beside them.)
+GM_DEV void gate_slopes_apart(float g, float u, float d, float &d_g, float &d_u) {
+    if (g < -FAR) {
+        int k;
+        const float m = exp_apart(g, k);
+        d_g = product_apart(d, u, 1.f + g, m, k);
+        d_u = product_apart(d, g, 1.f, m, k);
+    } else if (fabsf(d * u) == INFINITY) {
+        float s, rest;
+        sigmoid(g, s, rest);
+        d_g = product_apart(d, u, s * (1.f + g * rest), 1.f, 0);
+        d_u = d * (g * s);
+    } else {
+        gate_slopes(g, u, d, d_g, d_u);
+    }
+}
+
 struct GateBackArgs {
     const void *h, *d_a;
     void *d_h;
@@ -532,41 +562,31 @@ __global__ __launch_bounds__(256) void k_gate_backward(GateBackArgs a) {
     const int64_t total = a.n_rows * pieces;
     for (int64_t b = blockIdx.x * 256ll + threadIdx.x; b < total; b += gridDim.x * 256ll) {
         const int64_t row = total < INT32_MAX ? (uint32_t)b / pieces : b / pieces, c = (b - row * pieces) * 8;
-        const int valid = columns_left(a.n, c);
+        // (no lane is without columns: said outright, or each load has a branch and a wait of its own)
+        const int valid = WHOLE ? 8 : columns_left(a.n, c);
         const T *h = static_cast<const T *>(a.h) + row * a.hs + c;
         T *o = static_cast<T *>(a.d_h) + row * a.os + c;
         float g[8], u[8], d[8];
         load<WHOLE>(h, valid, g);
         load<WHOLE>(h + a.n, valid, u);
         load<WHOLE>(static_cast<const T *>(a.d_a) + row * a.ds + c, valid, d);
-        uint32_t most = 0;
+        float most = 0.f;  // (a NaN leaves it as it is, and is one below)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) most = max(most, magnitude(d[i] * u[i]));
-        const bool apart = any_far(g) || __builtin_expect(most >= 0x7f800000u, 0);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float s, rest;
-            sigmoid(g[i], s, rest);
-            u[i] = d[i] * u[i] * (s * (1.f + g[i] * rest));
-            d[i] = d[i] * (g[i] * s);
-        }
-        if (apart) {  // (rare, so from the start: what is common shall hold no registers for it)
-            asm volatile("" ::: "memory");
-            load<WHOLE>(h, valid, g);
-            load<WHOLE>(h + a.n, valid, u);
-            load<WHOLE>(static_cast<const T *>(a.d_a) + row * a.ds + c, valid, d);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const bool far = g[i] < -FAR;
-                int k = 0;
-                float s, rest, m = 1.f;
-                sigmoid(g[i], s, rest);
-                if (far) m = exp_apart(g[i], k);
-                u[i] = product_apart(d[i], u[i], far ? 1.f + g[i] : s * (1.f + g[i] * rest), m, k);
-                d[i] = product_apart(d[i], g[i], far ? 1.f : s, m, k);
-                __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(d[i] * u[i]));
+        if (__builtin_expect(any_far(g) || most == INFINITY, 0)) {  // (rare: one by one from the start, in little code)
+            const T *da = static_cast<const T *>(a.d_a) + row * a.ds + c;
+#pragma unroll 1
+            for (int i = 0; i < valid; ++i) {
+                const float x = to_f32(h[i]), y = to_f32(h[a.n + i]), z = to_f32(da[i]);
+                float d_g, d_u;
+                gate_slopes_apart(x, y, z, d_g, d_u);
+                o[i] = (T)d_g;
+                o[a.n + i] = (T)d_u;
             }
+            continue;
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) gate_slopes(g[i], u[i], d[i], u[i], d[i]);
         store<WHOLE>(o, valid, u);
         store<WHOLE>(o + a.n, valid, d);
     }

@@ -82,3 +82,26 @@ def test_expert_layer(g, tokens):
         # two values of the rows' type (of which the smaller may be below its normal numbers)
         off = (12 * rr.U32 + rr.half_step(torch.bfloat16) ** 2) * want.abs() + rr.TINY[torch.bfloat16]
         assert bool(((y.double().cpu() - want).abs() <= off + rr.U32 * want.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("n", [8, 77, 1032, 20001])
+def test_values_do_not_change_with_what_lies_beside_them(g, dtype, n):
+    gen = torch.Generator().manual_seed(n)
+    rows = 300 if n < 5000 else 5
+    h, d = (torch.randn((rows, k), generator=gen).mul_(3).to(dtype).cuda() for k in (2 * n, n))
+    h[0, :n // 2 + 1] = 1e-30 if dtype != torch.float16 else 1e-7  # (products that may end below normal numbers)
+    d[0] *= 1e-3
+    y, back = g.gate(h).y, g.gate_backward(h, d)
+    other = h.clone()
+    places = torch.rand((rows, n), generator=gen).cuda() < 0.05
+    places[:, 0] = True
+    other[:, :n][places] = -100.0
+    if dtype != torch.float16:
+        d = d.clone()
+        d[:, n - 1], other[:, 2 * n - 1] = 1e30, 1e30
+        places[:, n - 1] = True
+    y2, back2 = g.gate(other).y, g.gate_backward(other, d)
+    keep = ~places
+    assert torch.equal(y[keep], y2[keep])
+    assert torch.equal(back[:, :n][keep], back2[:, :n][keep]) and torch.equal(back[:, n:][keep], back2[:, n:][keep])
