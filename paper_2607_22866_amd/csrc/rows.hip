@@ -216,9 +216,11 @@ GM_DEV void store_piece(const RowArgs &a, const Place &at, int64_t row, int64_t 
 }
 
 // Bound by its bytes. Norm of 16384 x 4096 bf16 with residual, its sum and its results in bf16 and E4M3 114-118 us
-// (5.1-5.3 TB/s; without the next row on its way 120), without residual to bf16 44 us (6.1), to E4M3 alone 47
-// (4.3); gate of 32768 x 2048 to E4M3 61 us (5.5), 9001 x 1365 fp16 21 us (3.5); integers of 8192 x 4096 22 us
-// (4.6), of 65536 x 777 50 (3.0). One row of 4096 with all results 3.5 us.
+// (5.1-5.3 TB/s; without the next row on its way 120), without residual to bf16 44 us (6.1), to E4M3 alone 50
+// (4.0), to integers 52; gate of 32768 x 2048 to E4M3 64 us (5.2), to integers 70, 9001 x 1365 fp16 21-22 us (3.4);
+// integers of 8192 x 4096 22 us (4.6), of 65536 x 777 50 (3.0). One row of 4096 with all results 3.5 us.
+// Rows that end inside a piece have 16 to 96 bytes of scratch a lane, through which the next row passes in the norm of
+// 2049 to 4096 columns: 16384 x 4095 with residual 156 us, 4096 columns 101.
 template <Op OP, typename T, int W, int CH, bool WHOLE>
 __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void k_rows(RowArgs a) {
     constexpr int PER = W == 1 ? 4 : 1;  // rows of a work group
@@ -356,7 +358,8 @@ __global__ __launch_bounds__(64 * LONG_W) void k_rows_long(RowArgs a) {
 // shares are added in their order by a second kernel, so results do not change from
 // run to run. While a row's sums are joined the next row is on its way: 8192 x 4096 bf16
 // with three operands 43-45 us, 6.0-6.2 TB/s (without 83); 1024 work groups 49, and the
-// shares' sum 6 instead of 5.
+// shares' sum 6 instead of 5. 4095 columns, which end inside a piece (176 to 213 registers
+// and scratch), take 115 us with that sum, 4096 48.
 struct NormBackArgs {
     const void *h, *w, *d_y, *d_total;
     void *d_h;
@@ -466,7 +469,8 @@ __global__ __launch_bounds__(1024) void k_add_shares(const float *share, int64_t
     }
 }
 
-// Rows of any length: r and c of each row, then the columns 512 at a time.
+// Rows of any length: r and c of each row, then the columns 512 at a time. 4096 rows of 12288
+// columns 118 us, of 16384 163 (all is read twice).
 template <typename T, bool WHOLE>
 __global__ __launch_bounds__(64 * LONG_W) void k_norm_backward_rows(NormBackArgs a) {
     __shared__ float part[4][LONG_W];
@@ -525,8 +529,8 @@ __global__ __launch_bounds__(64) void k_norm_backward_columns(NormBackArgs a, in
 // ------------------------------------------------------------- gate's gradient
 // With s = sigma(g): d_g = d_a u s (1 + g (1 - s)), d_u = d_a g s. Eight columns a
 // lane, no row is needed as a whole. Where s is below fp32's normal numbers, or d_a u
-// above its largest, the products are made of fractions and exponents. 9001 x 1365
-// fp16 23 us, 5.4 TB/s.
+// above its largest, the products are made of fractions and exponents. 16384 x 2048
+// bf16 60 us, 9001 x 1365 fp16 23 us, 5.4 TB/s.
 GM_DEV void gate_slopes(float g, float u, float d, float &d_g, float &d_u) {
     float s, rest;
     sigmoid(g, s, rest);
