@@ -577,20 +577,16 @@ __global__ __launch_bounds__(256) void k_gate_backward(GateBackArgs a) {
         float most = 0.f;  // (a NaN leaves it as it is, and is one below)
 #pragma unroll
         for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(d[i] * u[i]));
-        if (__builtin_expect(any_far(g) || most == INFINITY, 0)) {  // (rare: one by one from the start, in little code)
-            const T *da = static_cast<const T *>(a.d_a) + row * a.ds + c;
-#pragma unroll 1
-            for (int i = 0; i < valid; ++i) {
-                const float x = to_f32(h[i]), y = to_f32(h[a.n + i]), z = to_f32(da[i]);
-                float d_g, d_u;
-                gate_slopes_apart(x, y, z, d_g, d_u);
-                o[i] = (T)d_g;
-                o[a.n + i] = (T)d_u;
-            }
-            continue;
-        }
+        if (any_far(g) || __builtin_expect(most == INFINITY, 0)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) gate_slopes(g[i], u[i], d[i], u[i], d[i]);
+            for (int i = 0; i < 8; ++i) {
+                gate_slopes_apart(g[i], u[i], d[i], u[i], d[i]);
+                __builtin_amdgcn_sched_barrier(0);  // (as in gated8)
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) gate_slopes(g[i], u[i], d[i], u[i], d[i]);
+        }
         store<WHOLE>(o, valid, u);
         store<WHOLE>(o + a.n, valid, d);
     }
